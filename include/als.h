@@ -412,6 +412,175 @@ als_status als_tensor_gibbs_half_sweep(als_ctx *ctx, als_mode mode, float *U, fl
 als_status als_tensor_sample_alpha(als_ctx *ctx, const float *U, const float *V, const float *T,
                                    double w0, double chi2, double *alpha_out);
 
+/*
+ * Sequence operators: the parts of a next-item model that reads a user's ratings in the order of
+ * time and answers with lists of items. A token is a rating, embedded (for instance by V's row of
+ * its item); its position is its time bin (Sec. 1); the histories of n_rows users are packed one
+ * after the other, row b holding tokens row_ptr[b] .. row_ptr[b + 1] - 1, as in the rating matrix.
+ * The operators are these published layers' formulas; no passage of the paper defines them.
+ *
+ * They need no context: each call takes the stream to enqueue on and the workspace to use (device
+ * memory, 16-byte aligned, of the size that the operator's ..._workspace function returns; it may be
+ * reused as soon as the call's work on the stream is done), allocates nothing and synchronises
+ * nothing. Everything is checked that the host can see; the values of row_ptr, positions, parents and
+ * sources lie on the device, where one out of range is handled as stated and touches no memory
+ * outside the buffers. Messages: als_last_error(NULL). Results are bitwise reproducible.
+ */
+typedef enum {
+  ALS_F32 = 0,
+  ALS_BF16 = 1
+} als_dtype;
+
+/* One value per token, head and feature in device memory: feature d of head h of token t lies at
+ * data[t * token_stride + h * head_stride + d] (strides in values, >= 0). */
+typedef struct {
+  void *data;
+  int64_t token_stride;
+  int64_t head_stride;
+} als_heads;
+
+/*
+ * Norm of queries and keys for each head with the rotation by position:
+ *   y = x / sqrt(mean_d x_d^2 + eps) * weight,
+ * then the first `rotated` features in pairs (a, b), a' = a cos - b sin, b' = b cos + a sin, with
+ * cos and sin of pair p at position s in cos_table[s * rotated / 2 + p], sin_table likewise.
+ *   n_tokens       0 .. 2^31 - 1.
+ *   q_heads, k_heads  1 .. 1024; width 1 .. 256.
+ *   rotated        even, 0 .. width.
+ *   neighbours     0: pair p is features p and p + rotated / 2; 1: features 2 p and 2 p + 1.
+ *   n_positions    rows of the tables, >= 1 (0 allowed with rotated = 0 only if n_tokens = 0).
+ *   positions      device int32[n_tokens]; a token outside [0, n_positions) becomes NaN.
+ *   q_weight, k_weight  device fp32[width].
+ * Sums run in fp32 and outputs are rounded once. als_norm_rotate: q and k to q_out and k_out, which
+ * may be q and k themselves (the same data and strides), and otherwise must not overlap them.
+ * als_norm_rotate_backward: the gradients of q and k (q_out and k_out here) and of the weights
+ * (device fp32[width], overwritten) from those of the outputs (dq, dk); q_out may be dq or q, k_out
+ * likewise.
+ */
+typedef struct {
+  int64_t n_tokens;
+  int64_t n_positions;
+  int32_t q_heads;
+  int32_t k_heads;
+  int32_t width;
+  int32_t rotated;
+  int32_t neighbours;
+  float eps;
+  const int32_t *positions;
+  const float *cos_table;
+  const float *sin_table;
+} als_rotation;
+
+als_status als_norm_rotate(const als_rotation *shape, als_dtype dtype, als_heads q, als_heads k,
+                           const float *q_weight, const float *k_weight, als_heads q_out,
+                           als_heads k_out, void *hip_stream);
+int64_t als_norm_rotate_workspace(const als_rotation *shape);
+als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, als_heads dq,
+                                    als_heads dk, als_heads q, als_heads k, const float *q_weight,
+                                    const float *k_weight, als_heads q_out, als_heads k_out,
+                                    float *dq_weight, float *dk_weight, void *workspace,
+                                    int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Linear attention with a decay for each head: over the tokens t of a row,
+ *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,
+ * S being k_width x v_width; S before the first token is zero or initial_state.
+ *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^31 - 1.
+ *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
+ *                  values out of [0, n_tokens] are taken as the nearest bound.
+ *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
+ *                  head h of k and v. k_width, v_width 1 .. 128.
+ *   log_decay      device fp32[q_heads], <= 0 (-inf forgets at once); a head above 0 or NaN gives NaN.
+ *   initial_state, final_state  device fp32 [n_rows, q_heads, k_width, v_width], nullable.
+ *   out            device [n_tokens, q_heads, v_width], packed.
+ * bf16 inputs: products of bf16 with fp32 sums; the products of q and k with their decay, and the
+ * state as q reads it, are rounded to bf16. The state itself is kept in fp32.
+ */
+typedef struct {
+  int64_t n_tokens;
+  int64_t n_rows;
+  const int64_t *row_ptr;
+  const float *log_decay;
+  int32_t q_heads;
+  int32_t k_heads;
+  int32_t k_width;
+  int32_t v_width;
+  float scale;
+} als_attention;
+
+int64_t als_decay_attention_workspace(const als_attention *shape);
+als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_heads q, als_heads k,
+                               als_heads v, const float *initial_state, void *out,
+                               float *final_state, void *workspace, int64_t workspace_bytes,
+                               void *hip_stream);
+
+/*
+ * Gradients of als_decay_attention: dq [n_tokens, q_heads, k_width], dk [n_tokens, k_heads, k_width]
+ * and dv [n_tokens, k_heads, v_width], packed, from the gradient of its output (d_out) and, nullable,
+ * of its final state. d_initial_state (nullable): the gradient of the initial state.
+ */
+int64_t als_decay_attention_backward_workspace(const als_attention *shape);
+als_status als_decay_attention_backward(const als_attention *shape, als_dtype dtype, als_heads d_out,
+                                        als_heads q, als_heads k, als_heads v,
+                                        const float *initial_state, const float *d_final_state,
+                                        void *dq, void *dk, void *dv, float *d_initial_state,
+                                        void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * One token of each of n_rows rows (n_tokens and row_ptr of shape are not read):
+ *   state_out = exp(log_decay) state[source] + k v^T,   out = scale state_out^T q.
+ *   state        device fp32 [n_sources, q_heads, k_width, v_width].
+ *   source       nullable (row r goes on from state r, n_sources = n_rows): device int32[n_rows], the
+ *                row of state that each row goes on from, as a beam does from its parent; one outside
+ *                [0, n_sources) gives NaN.
+ *   state_out    [n_rows, q_heads, k_width, v_width]; without source it may be state itself, and
+ *                otherwise it must not overlap state.
+ */
+als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype, als_heads q,
+                                    als_heads k, als_heads v, const float *state, int64_t n_sources,
+                                    const int32_t *source, float *state_out, void *out,
+                                    void *hip_stream);
+
+/*
+ * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores
+ *   scores[w] + logits[w, v] - log sum_u exp(logits[w, u]),
+ * and the best `width` of all (w, v) go on, equal scores by the lowest (w, v).
+ *   beams, width   1 .. 32. n_items 1 .. 2^31 - 1. n_lists 0 .. 2^31 - 1.
+ *   logits         device [n_lists * beams, n_items], rows row_stride values apart. -inf and NaN mask
+ *                  an item; +inf counts as the largest finite value.
+ *   scores         device fp32 [n_lists, beams]; -inf or NaN: a dead beam, without candidates.
+ *   finished       nullable, device uint8 [n_lists, beams]: a finished beam's logits are not read; it
+ *                  goes on with end_token alone, at its own score.
+ *   end_token      the item that finishes a beam, or -1 (then finished must be NULL).
+ *   parents, tokens, scores_out, finished_out  device int32, int32, fp32, uint8 [n_lists, width], the
+ *                  chosen beam and item by descending score, its score, and whether it is finished.
+ *                  Where there are fewer candidates: 0, -1, -inf and 0.
+ * Scores are formed and compared in fp64 and rounded to fp32 on the way out.
+ */
+typedef struct {
+  int64_t n_lists;
+  int64_t n_items;
+  int64_t row_stride;
+  int32_t beams;
+  int32_t width;
+  int32_t end_token;
+} als_beams;
+
+int64_t als_beam_select_workspace(const als_beams *shape);
+als_status als_beam_select(const als_beams *shape, als_dtype dtype, const void *logits,
+                           const float *scores, const uint8_t *finished, int32_t *parents,
+                           int32_t *tokens, float *scores_out, uint8_t *finished_out,
+                           void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * The beams' states in their new order: row w of list b of dst [n_lists, width] becomes row
+ * parents[b, w] of list b of src [n_lists, beams], rows of row_bytes bytes. dst may be src where width
+ * equals beams, and otherwise must not overlap it. A parent outside [0, beams) leaves its row of dst
+ * as it is.
+ */
+als_status als_reorder_states(int64_t n_lists, int32_t beams, int32_t width, int64_t row_bytes,
+                              const void *src, void *dst, const int32_t *parents, void *hip_stream);
+
 /* Release the context of als_create (the rating matrix of paper Sec. 2.2, its device
  * layouts, schedules and workspace) after synchronising its stream; NULL is ignored.
  * Caller-owned factor buffers are untouched. */
@@ -421,8 +590,8 @@ void als_destroy(als_ctx *ctx);
  * defines it. The string is static. */
 const char *als_status_str(als_status s);
 
-/* Message of the last failing call on ctx (or of the last failed
- * als_create when ctx is NULL); valid until the next call on ctx. Error reporting of
+/* Message of the last failing call on ctx (when ctx is NULL, of the calling thread's last
+ * failed als_create or sequence operator); valid until the next call on ctx. Error reporting of
  * this interface; no passage of the paper defines it. */
 const char *als_last_error(const als_ctx *ctx);
 

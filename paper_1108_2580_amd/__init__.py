@@ -1,4 +1,5 @@
-"""Python binding of libals, the MI355X ALS half-sweep (C ABI in include/als.h).
+"""Python binding of libals, the MI355X ALS half-sweep (C ABI in include/als.h) and the sequence
+operators that stand beside it (``sequence``).
 
 Argument marshalling only: every step of the half-sweep runs in the HIP
 kernels of ``csrc/``. PyTorch supplies device memory (fp32 tensors on
@@ -36,6 +37,10 @@ EXPORTS = ("als_create", "als_half_sweep", "als_last_rmse_in", "als_rmse", "als_
            "als_set_time_bins", "als_tensor_half_sweep", "als_tensor_rmse",
            "als_set_time_nw_prior", "als_sample_time_hyper", "als_tensor_gibbs_half_sweep",
            "als_tensor_sample_alpha",
+           "als_norm_rotate", "als_norm_rotate_workspace", "als_norm_rotate_backward",
+           "als_decay_attention", "als_decay_attention_workspace", "als_decay_attention_backward",
+           "als_decay_attention_backward_workspace", "als_decay_attention_step",
+           "als_beam_select", "als_beam_select_workspace", "als_reorder_states",
            "als_destroy", "als_status_str", "als_last_error")
 
 PHASES = ("stage", "gather", "solve", "residual", "reduce")
@@ -489,3 +494,9 @@ class ALS:
 
     def __exit__(self, *a):
         self.close()
+
+
+# the sequence operators, which need no rating matrix
+from .sequence import (beam_select, decay_attention, decay_attention_backward,  # noqa: E402
+                       decay_attention_step, norm_rotate, norm_rotate_backward, reorder_states,
+                       rotary_tables)

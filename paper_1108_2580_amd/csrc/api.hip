@@ -21,6 +21,7 @@
 
 #include "als.h"
 #include "internal.h"
+#include "sequence.h"
 
 using als::RowTask;
 using als::WorkItem;
@@ -213,6 +214,27 @@ als_status fail(als_ctx *ctx, als_status st, const char *fmt, ...) {
   if (ctx) ctx->err = buf; else g_create_err = buf;
   return st;
 }
+
+}  // namespace
+
+namespace als {
+
+als_status fail_without_context(als_status st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    g_create_err = buf;
+  } catch (...) {  // no memory for the message: the status alone
+  }
+  return st;
+}
+
+}  // namespace als
+
+namespace {
 
 #define HIP_OR_FAIL(ctx, call)                                                              \
   do {                                                                                      \

@@ -1,0 +1,406 @@
+"""Sequence operators of libals (include/als.h): the parts of a next-item model.
+
+A next-item model reads a user's ratings in the order of time and answers with lists of items:
+``norm_rotate`` prepares queries and keys, ``decay_attention`` runs over the histories
+(``decay_attention_step`` over one new rating), ``beam_select`` extends the lists and
+``reorder_states`` moves the beams' states along. Histories are packed one after the other, with a
+``row_ptr`` like the rating matrix's.
+
+Argument marshalling only: the work runs in the HIP kernels of ``csrc/``. Every call is enqueued on
+the current HIP stream of the current device, on which its tensors have to lie, and nothing is
+synchronised. Inputs are fp32 or bf16 tensors whose features are contiguous; tokens and heads may
+have any strides. Where an input of ``norm_rotate`` or ``decay_attention`` requires a gradient, the
+result carries it.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import ALS_OK, ALSError, lib
+
+ALS_F32, ALS_BF16 = 0, 1
+_DTYPES = {torch.float32: ALS_F32, torch.bfloat16: ALS_BF16}
+MAX_BEAMS = 32
+
+_P, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", _P), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("n_tokens", _i64), ("n_positions", _i64), ("q_heads", _i32), ("k_heads", _i32),
+                ("width", _i32), ("rotated", _i32), ("neighbours", _i32), ("eps", _f32),
+                ("positions", _P), ("cos_table", _P), ("sin_table", _P)]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = [("n_tokens", _i64), ("n_rows", _i64), ("row_ptr", _P), ("log_decay", _P),
+                ("q_heads", _i32), ("k_heads", _i32), ("k_width", _i32), ("v_width", _i32),
+                ("scale", _f32)]
+
+
+class _Beams(ctypes.Structure):
+    _fields_ = [("n_lists", _i64), ("n_items", _i64), ("row_stride", _i64), ("beams", _i32),
+                ("width", _i32), ("end_token", _i32)]
+
+
+def _declare():
+    R, A, B = (ctypes.POINTER(t) for t in (_Rotation, _Attention, _Beams))
+    H, st = _Heads, ctypes.c_int
+    for name, args in (
+            ("als_norm_rotate", [R, st, H, H, _P, _P, H, H, _P]),
+            ("als_norm_rotate_backward",
+             [R, st, H, H, H, H, _P, _P, H, H, _P, _P, _P, _i64, _P]),
+            ("als_decay_attention", [A, st, H, H, H, _P, _P, _P, _P, _i64, _P]),
+            ("als_decay_attention_backward",
+             [A, st, H, H, H, H, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
+            ("als_decay_attention_step", [A, st, H, H, H, _P, _i64, _P, _P, _P, _P]),
+            ("als_beam_select", [B, st, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
+            ("als_reorder_states", [_i64, _i32, _i32, _i64, _P, _P, _P, _P])):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = args, st
+    for name, arg in (("als_norm_rotate_workspace", R), ("als_decay_attention_workspace", A),
+                      ("als_decay_attention_backward_workspace", A),
+                      ("als_beam_select_workspace", B)):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = [arg], _i64
+
+
+_declare()
+
+
+def _check(status):
+    if status != ALS_OK:
+        raise ALSError(status, lib.als_last_error(None).decode())
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _on_device(t, name):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+
+
+def _array(t, name, dtype, shape):
+    """A contiguous tensor of this type and shape, as a pointer."""
+    _on_device(t, name)
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _heads(t, name, dtype, shape=None):
+    """A [tokens, heads, width] tensor with contiguous features."""
+    _on_device(t, name)
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be {dtype or 'float32 or bfloat16'}, not {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have the dimensions tokens, heads, width")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    token, head, feature = t.stride()
+    if feature != 1 and t.shape[2] > 1:
+        raise TypeError(f"the features of {name} must be contiguous")
+    return _Heads(t.data_ptr(), token, head)
+
+
+def _workspace(size, device):
+    return torch.empty(size, dtype=torch.uint8, device=device) if size > 0 else None
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# ---- norm and rotation -------------------------------------------------------------------------
+
+def rotary_tables(n_positions, rotated, base=10_000.0, device="cuda"):
+    """(cos, sin) fp32 tables [n_positions, rotated / 2] of the angles position * base^(-2 p /
+    rotated), formed in fp64."""
+    pair = torch.arange(rotated // 2, dtype=torch.float64)
+    angle = torch.arange(n_positions, dtype=torch.float64)[:, None] * base ** (-2.0 * pair / max(rotated, 1))
+    return angle.cos().float().to(device), angle.sin().float().to(device)
+
+
+def _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
+    hq = _heads(q, "q", None)
+    N, Hq, D = q.shape
+    hk = _heads(k, "k", q.dtype)
+    if k.shape[0] != N or k.shape[2] != D:
+        raise ValueError(f"k has shape {tuple(k.shape)}, expected {N} tokens of width {D}")
+    _on_device(cos, "cos")
+    if cos.dim() != 2:
+        raise ValueError("cos must have the dimensions positions, pairs")
+    P, half = cos.shape
+    shape = _Rotation(N, P, Hq, k.shape[1], D, 2 * half, 1 if neighbours else 0, eps,
+                      _array(positions, "positions", torch.int32, (N,)),
+                      _array(cos, "cos", torch.float32, (P, half)),
+                      _array(sin, "sin", torch.float32, (P, half)))
+    return shape, hq, hk, _array(q_weight, "q_weight", torch.float32, (D,)), \
+        _array(k_weight, "k_weight", torch.float32, (D,))
+
+
+def _norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
+    shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    D = q.shape[2]
+    _check(lib.als_norm_rotate(shape, _DTYPES[q.dtype], hq, hk, wq, wk,
+                               _Heads(q_out.data_ptr(), q.shape[1] * D, D),
+                               _Heads(k_out.data_ptr(), k.shape[1] * D, D), _stream()))
+    return q_out, k_out
+
+
+def norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps=1e-6, neighbours=False):
+    """Norm of queries [tokens, heads, width] and keys [tokens, key heads, width] for each head, and
+    the rotation by position: y = x / sqrt(mean x^2 + eps) * weight, then the first 2 * cos.shape[1]
+    features turned in pairs by the angle of the token's position.
+
+    ``q_weight``, ``k_weight``: fp32 [width]; ``cos``, ``sin``: fp32 [positions, pairs]
+    (``rotary_tables``); ``positions``: int32 [tokens], a row of the tables each (one outside them
+    makes its token NaN). ``neighbours``: pair p is features 2 p and 2 p + 1 instead of p and
+    p + pairs. Returns new (q, k)."""
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, q_weight, k_weight)):
+        return _NormRotate.apply(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
+    return _norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
+
+
+def norm_rotate_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps=1e-6,
+                         neighbours=False):
+    """Gradients of ``norm_rotate``'s inputs (dq, dk, dq_weight, dk_weight) from those of its
+    outputs."""
+    shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
+    hdq, hdk = _heads(dq, "dq", q.dtype, q.shape), _heads(dk, "dk", q.dtype, k.shape)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    dwq, dwk = torch.empty_like(q_weight), torch.empty_like(k_weight)
+    D = q.shape[2]
+    size = lib.als_norm_rotate_workspace(shape)
+    work = _workspace(size, q.device)
+    _check(lib.als_norm_rotate_backward(
+        shape, _DTYPES[q.dtype], hdq, hdk, hq, hk, wq, wk,
+        _Heads(q_out.data_ptr(), q.shape[1] * D, D), _Heads(k_out.data_ptr(), k.shape[1] * D, D),
+        dwq.data_ptr(), dwk.data_ptr(), _ptr(work), size, _stream()))
+    return q_out, k_out, dwq, dwk
+
+
+def _dense(t):
+    """A gradient as the operators take it: contiguous features."""
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
+        ctx.save_for_backward(q, k, q_weight, k_weight, cos, sin, positions)
+        ctx.more = (eps, neighbours)
+        return _norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        return (*norm_rotate_backward(_dense(dq), _dense(dk), *ctx.saved_tensors, *ctx.more),
+                None, None, None, None, None)
+
+
+# ---- attention with a decay for each head --------------------------------------------------------
+
+def _attention(q, k, v, log_decay, row_ptr, scale):
+    hq = _heads(q, "q", None)
+    N, Hq, K = q.shape
+    hk, hv = _heads(k, "k", q.dtype), _heads(v, "v", q.dtype)
+    Hk, V = v.shape[1:]
+    if tuple(k.shape) != (N, Hk, K) or v.shape[0] != N:
+        raise ValueError(f"q, k and v have shapes {tuple(q.shape)}, {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
+    rows = N
+    if row_ptr is not None:
+        _on_device(row_ptr, "row_ptr")
+        if row_ptr.dim() != 1 or row_ptr.numel() < 1:
+            raise ValueError("row_ptr must have one more entry than there are rows")
+        rows = row_ptr.numel() - 1
+        row_ptr = _array(row_ptr, "row_ptr", torch.int64, (rows + 1,))
+    shape = _Attention(N, rows, row_ptr, _array(log_decay, "log_decay", torch.float32, (Hq,)), Hq, Hk,
+                       K, V, K ** -0.5 if scale is None else scale)
+    return shape, hq, hk, hv
+
+
+def _state_ptr(t, name, shape):
+    return None if t is None else \
+        _array(t, name, torch.float32, (shape.n_rows, shape.q_heads, shape.k_width, shape.v_width))
+
+
+def _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state):
+    shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    first = _state_ptr(initial_state, "initial_state", shape)
+    out = torch.empty((q.shape[0], shape.q_heads, shape.v_width), dtype=q.dtype, device=q.device)
+    state = torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width),
+                        device=q.device) if return_state else None
+    size = lib.als_decay_attention_workspace(shape)
+    work = _workspace(size, q.device)
+    _check(lib.als_decay_attention(shape, _DTYPES[q.dtype], hq, hk, hv, first, out.data_ptr(),
+                                   _ptr(state), _ptr(work), size, _stream()))
+    return out, state
+
+
+def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
+                    return_state=False):
+    """Linear attention with a decay for each head over packed rows of tokens: with
+    S_t = exp(log_decay) S_{t-1} + k_t v_t^T, out_t = scale S_t^T q_t.
+
+    ``q``: [tokens, heads, key width]; ``k``, ``v``: [tokens, key heads, width], each key head shared
+    by heads / key heads query heads; widths up to 128. ``log_decay``: fp32 [heads], <= 0.
+    ``row_ptr``: int64 [rows + 1] on the device, row b holding tokens row_ptr[b] .. row_ptr[b + 1].
+    ``scale``: 1 / sqrt(key width) if None. ``initial_state``: fp32 [rows, heads, key width, value
+    width], zero if None. Returns out [tokens, heads, value width], with ``return_state`` (out, the
+    states after the rows' last tokens). ``log_decay`` takes no gradient."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
+        raise ValueError("log_decay takes no gradient")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
+                                       for t in (q, k, v, initial_state)):
+        out, state = _DecayAttention.apply(q, k, v, initial_state, log_decay, row_ptr, scale)
+    else:
+        out, state = _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
+    return (out, state) if return_state else out
+
+
+def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
+                             dstate=None, d_initial=None):
+    """Gradients (dq, dk, dv, d_initial_state) of ``decay_attention`` from that of its output and,
+    if given, of its returned state (``dstate``). The last is None unless there is an
+    ``initial_state`` or ``d_initial`` is true."""
+    shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    hdo = _heads(d_out, "d_out", q.dtype, (q.shape[0], shape.q_heads, shape.v_width))
+    first = _state_ptr(initial_state, "initial_state", shape)
+    last = _state_ptr(dstate, "dstate", shape)
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dfirst = None
+    if d_initial or (d_initial is None and initial_state is not None):
+        dfirst = torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width),
+                             device=q.device)
+    size = lib.als_decay_attention_backward_workspace(shape)
+    work = _workspace(size, q.device)
+    _check(lib.als_decay_attention_backward(shape, _DTYPES[q.dtype], hdo, hq, hk, hv, first, last,
+                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                            _ptr(dfirst), _ptr(work), size, _stream()))
+    return dq, dk, dv, dfirst
+
+
+class _DecayAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, initial_state, log_decay, row_ptr, scale):
+        ctx.save_for_backward(q, k, v, log_decay, row_ptr, initial_state)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, True)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out, dstate):
+        q, k, v, log_decay, row_ptr, initial_state = ctx.saved_tensors
+        if d_out is None:
+            d_out = torch.zeros((q.shape[0], q.shape[1], v.shape[2]), dtype=q.dtype, device=q.device)
+        dstate = None if dstate is None else dstate.contiguous()
+        grads = decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale,
+                                         initial_state, dstate, d_initial=ctx.needs_input_grad[3])
+        return (*grads, None, None, None)
+
+
+def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, state_out=None):
+    """One token of each row: state_out = exp(log_decay) state[source] + k v^T, out = scale
+    state_out^T q, for ``q``: [rows, heads, key width] and ``k``, ``v``: [rows, key heads, width].
+
+    ``state``: fp32 [rows, heads, key width, value width], updated in place unless ``state_out`` is
+    given. ``source``: int32 [rows], the row of ``state`` that each row goes on from (a beam's
+    parent; one outside it gives NaN); ``state`` may then have another number of rows, and
+    ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out)."""
+    shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
+    N, H, K, V = shape.n_rows, shape.q_heads, shape.k_width, shape.v_width
+    _on_device(state, "state")
+    sources = state.shape[0] if source is not None and state.dim() == 4 else N
+    sp = _array(state, "state", torch.float32, (sources, H, K, V))
+    src = None if source is None else _array(source, "source", torch.int32, (N,))
+    if state_out is None:
+        state_out = state if source is None else torch.empty((N, H, K, V), device=q.device)
+    to = _array(state_out, "state_out", torch.float32, (N, H, K, V))
+    out = torch.empty((N, H, V), dtype=q.dtype, device=q.device)
+    _check(lib.als_decay_attention_step(shape, _DTYPES[q.dtype], hq, hk, hv, sp, sources, src, to,
+                                        out.data_ptr(), _stream()))
+    return out, state_out
+
+
+# ---- beams ---------------------------------------------------------------------------------------
+
+def beam_select(logits, scores, finished=None, end_token=-1, width=None):
+    """The best ``width`` (as many as there are beams if None) extensions of each list's beams.
+
+    ``logits``: fp32 or bf16 [lists, beams, items] (-inf and NaN mask an item); ``scores``: fp32
+    [lists, beams], -inf for a beam without candidates; ``finished``: bool or uint8 [lists, beams],
+    beams that go on with ``end_token`` alone at their own score. A candidate scores its beam's score
+    plus the log-softmax of its item; equal scores go by the lowest beam, then the lowest item.
+    Returns (parents int32, tokens int32, scores fp32, finished bool), each [lists, width] by
+    descending score; where candidates run out: 0, -1, -inf and False."""
+    _on_device(logits, "logits")
+    if logits.dtype not in _DTYPES:
+        raise TypeError(f"logits must be float32 or bfloat16, not {logits.dtype}")
+    if logits.dim() != 3:
+        raise ValueError("logits must have the dimensions lists, beams, items")
+    B, W, V = logits.shape
+    stride = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    if (V > 1 and logits.stride(2) != 1) or (B > 1 and W > 1 and logits.stride(0) != W * stride):
+        raise TypeError("logits must have contiguous items and evenly spaced rows")
+    sp = _array(scores, "scores", torch.float32, (B, W))
+    fp = None
+    if finished is not None:
+        if isinstance(finished, torch.Tensor) and finished.dtype == torch.bool:
+            finished = finished.view(torch.uint8)
+        fp = _array(finished, "finished", torch.uint8, (B, W))
+    width = W if width is None else int(width)
+    shape = _Beams(B, V, stride, W, width, end_token)
+    size = lib.als_beam_select_workspace(shape)
+    if size < 0:
+        raise ALSError(1, lib.als_last_error(None).decode())
+    dev = logits.device
+    parents = torch.empty((B, width), dtype=torch.int32, device=dev)
+    tokens = torch.empty((B, width), dtype=torch.int32, device=dev)
+    new = torch.empty((B, width), device=dev)
+    done = torch.empty((B, width), dtype=torch.bool, device=dev)
+    work = _workspace(size, dev)
+    _check(lib.als_beam_select(shape, _DTYPES[logits.dtype], logits.data_ptr(), sp, fp,
+                               parents.data_ptr(), tokens.data_ptr(), new.data_ptr(),
+                               done.data_ptr(), _ptr(work), size, _stream()))
+    return parents, tokens, new, done
+
+
+def reorder_states(states, parents, out=None):
+    """The beams' states in their new order: out[b, w] = states[b, parents[b, w]] for ``states``
+    [lists, beams, ...] of any type, contiguous, and ``parents`` int32 [lists, width]. ``out`` (a new
+    tensor if None) may be ``states`` itself where width equals beams."""
+    _on_device(states, "states")
+    if states.dim() < 2 or not states.is_contiguous():
+        raise TypeError("states must be contiguous with the dimensions lists, beams, ...")
+    _on_device(parents, "parents")
+    if parents.dim() != 2:
+        raise ValueError("parents must have the dimensions lists, width")
+    B, W = states.shape[:2]
+    width = parents.shape[1]
+    pp = _array(parents, "parents", torch.int32, (B, width))
+    shape = (B, width) + tuple(states.shape[2:])
+    if out is None:
+        out = torch.empty(shape, dtype=states.dtype, device=states.device)
+    else:
+        _array(out, "out", states.dtype, shape)
+    size = states[:1, :1].numel() * states.element_size() if B and W else 0
+    _check(lib.als_reorder_states(B, W, width, size, states.data_ptr(), out.data_ptr(), pp,
+                                  _stream()))
+    return out
