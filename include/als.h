@@ -486,6 +486,7 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,
  * S being k_width x v_width; S before the first token is zero or initial_state.
  *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^31 - 1.
+ *   q, k, v        token strides at most 2^22 values.
  *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
  *                  values out of [0, n_tokens] are taken as the nearest bound.
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share

@@ -37,10 +37,13 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinLogDecay = -1e4f;
 
 // ---- fragments: 8 values of a contraction of 32 per lane ---------------------------------------
-// Lane l holds, for row (or column) l & 15, the places 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3
-// with g = l >> 4: the order in which two result tiles of an MFMA hold their rows, so that results
-// are operands of the next product as they are. (A sum's terms may come in any order, provided both
-// operands use the same.)
+// Lane l holds 8 of 32 places for row (or column) m = l & 15, in one of two orders (a sum's terms may
+// come in any, provided both operands use the same). With g = l >> 4:
+//   along a row of LDS, places 8 g .. 8 g + 7, one 16-byte read;
+//   down the tokens, places 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3.
+// Two result tiles of an MFMA hold their rows 4 g .. 4 g + 3 in a lane, which is the second order, so
+// that weights are operands of the next product as they are. The state's tiles take the columns of k
+// in such an order (frag_col's STEP 8) that a pair of them is an operand of the first order.
 template <typename T> struct Frag;
 template <> struct Frag<float> {
   f32x4 lo, hi;
@@ -75,16 +78,19 @@ __device__ __forceinline__ f32x4 mma(const Frag<float> &a, const Frag<float> &b,
   return c;
 }
 
-// Row l & 15 of a 16-row tile at x (row length ld), contraction along the row from column 0.
-template <typename T>
-__device__ __forceinline__ Frag<T> frag_row(const T *x, int ld, int lane) {
-  using V = typename Vec4<T>::type;
-  const T *p = x + (lane & 15) * ld + (lane >> 4) * 4;
-  return joined(*(const V *)p, *(const V *)(p + 16));
+// Row m of a 16-row tile at x (row length ld), contraction along the row from column 0.
+__device__ __forceinline__ Frag<float> frag_row(const float *x, int ld, int lane) {
+  const float *p = x + (lane & 15) * ld + (lane >> 4) * 8;
+  return {*(const f32x4 *)p, *(const f32x4 *)(p + 4)};
 }
-// Column l & 15 of a 16-column tile at x, contraction down 32 rows.
+__device__ __forceinline__ Frag<bf16> frag_row(const bf16 *x, int ld, int lane) {
+  return {*(const bf16x8 *)(x + (lane & 15) * ld + (lane >> 4) * 8)};
+}
+// Column STEP * (m / 4) + m % 4 from x, contraction down 32 rows.
+template <int STEP>
 __device__ __forceinline__ Frag<float> frag_col(const float *x, int ld, int lane) {
-  const float *p = x + (lane >> 4) * 4 * ld + (lane & 15);
+  const int m = lane & 15;
+  const float *p = x + (lane >> 4) * 4 * ld + m / 4 * STEP + m % 4;
   Frag<float> f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -95,11 +101,16 @@ __device__ __forceinline__ Frag<float> frag_col(const float *x, int ld, int lane
 }
 // The transposing LDS read: 16 lanes name the 16 8-byte pieces of a 4 x 16 block, and lane i of
 // them gets column i.
+template <int STEP>
 __device__ __forceinline__ Frag<bf16> frag_col(const bf16 *x, int ld, int lane) {
   using L = __attribute__((address_space(3))) bf16x4 *;
-  const bf16 *p = x + (lane >> 2) * ld + (lane & 3) * 4;
+  const bf16 *p = x + (lane >> 2) * ld + (lane & 3) * STEP;
   return joined(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)p),
                 __builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)(p + 16 * ld)));
+}
+// Row of the state that element e of lane group g holds in tile kt.
+__device__ __forceinline__ constexpr int state_row(int kt, int g, int e) {
+  return kt / 2 * 32 + g * 8 + kt % 2 * 4 + e;
 }
 
 template <typename T> __device__ __forceinline__ typename Vec4<T>::type rounded(f32x4 x) {
@@ -112,95 +123,205 @@ template <typename T> constexpr int padded(int width) { return width + (sizeof(T
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
-// Row and place of a slot. Row b's segments have the slots row_ptr[b] / L + b onwards: at least as
-// many as it has segments, one for an empty row, and never another row's.
+// Rows are cut into segments of L = 2^shift tokens, which run side by side. Row b's segments have the
+// slots row_ptr[b] / L + b onwards: at least as many as it has segments, one for an empty row, and
+// never another row's. The segments that are not their row's last, whose states the later ones need,
+// have the entries row_ptr[b] / L onwards, again never another row's.
 struct Place {
-  int64_t row, first, len;  // the row, its first token and length
-  int64_t segment;          // of the row
+  int64_t first;    // of the row's tokens
+  int32_t len;      // tokens of the row
+  int32_t row;
+  int64_t segment;  // of the row; none where it is not below the number of segments
 };
 
-// One wave searches 64 rows at a time. Values of row_ptr outside [0, n_tokens] are taken as the
-// nearest inside, so that nothing outside the tensors is touched whatever it holds.
+// Values of row_ptr outside [0, n_tokens] are taken as the nearest inside, so that nothing outside
+// the tensors is touched whatever it holds.
 __device__ __forceinline__ int64_t clamped(int64_t x, int64_t lo, int64_t hi) {
   return x < lo ? lo : (x > hi ? hi : x);
 }
+__device__ __forceinline__ int64_t segments_of(int64_t len, int shift) {
+  return (len + (1LL << shift) - 1) >> shift;
+}
+// The last row whose slots (or entries) begin at `index` or before, 64 rows at a time.
+template <bool ENTRY>
 __device__ __forceinline__ Place find_place(const int64_t *__restrict__ row_ptr, int64_t n_rows,
-                                            int64_t n_tokens, int64_t L, int64_t slot, int lane) {
+                                            int64_t n_tokens, int shift, int64_t index, int lane) {
   int64_t lo = 0, hi = n_rows;
   while (hi - lo > 1) {
     const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-    const bool before = at < hi && clamped(row_ptr[at], 0, n_tokens) / L + at <= slot;
+    const bool before =
+        at < hi && (clamped(row_ptr[at], 0, n_tokens) >> shift) + (ENTRY ? 0 : at) <= index;
     const int n = __popcll(__ballot(before));
     lo += (n > 0 ? n - 1 : 0) * step;
     hi = lo + step < hi ? lo + step : hi;
   }
   Place p;
-  p.row = lo;
+  p.row = (int32_t)lo;
   p.first = clamped(row_ptr[lo], 0, n_tokens);
-  p.len = clamped(row_ptr[lo + 1], p.first, n_tokens) - p.first;
-  p.segment = slot - (p.first / L + lo);
+  p.len = (int32_t)(clamped(row_ptr[lo + 1], p.first, n_tokens) - p.first);
+  p.segment = index - ((p.first >> shift) + (ENTRY ? 0 : lo));
   return p;
+}
+
+// The places of all slots and the slots of all entries (-1: none), one wave a row. Where there are
+// more rows than one step of the search covers, a block's search took about 4 us of a few chunks'
+// work (35 000 blocks of 4096 rows: 170 us), and this table one launch of 5 us for all of them.
+constexpr int64_t kSearchedRows = 64;
+__global__ __launch_bounds__(256) void k_places(const int64_t *__restrict__ row_ptr, int64_t n_rows,
+                                                int64_t n_tokens, int shift, int64_t n_slots,
+                                                int64_t n_entries, Place *__restrict__ places,
+                                                int32_t *__restrict__ entries) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (row >= n_rows) return;
+  const int lane = (int)threadIdx.x & 63;
+  Place p;
+  p.row = (int32_t)row;
+  p.first = clamped(row_ptr[row], 0, n_tokens);
+  p.len = (int32_t)(clamped(row_ptr[row + 1], p.first, n_tokens) - p.first);
+  const int64_t e0 = p.first >> shift, s0 = e0 + row, n = segments_of(p.len, shift);
+  const int64_t e1 = row + 1 == n_rows ? n_entries : (p.first + p.len) >> shift;
+  const int64_t s1 = row + 1 == n_rows ? n_slots : e1 + row + 1;
+  for (int64_t s = (row ? s0 : 0) + lane; s < s1 && s < n_slots; s += 64) {
+    p.segment = s - s0;
+    places[s] = p;
+  }
+  for (int64_t e = (row ? e0 : 0) + lane; e < e1 && e < n_entries; e += 64)
+    entries[e] = e >= e0 && e - e0 + 1 < n ? (int32_t)(s0 + e - e0) : -1;
 }
 
 struct Args {
   AttentionPass p;
-  int64_t segment;  // tokens a segment
-  int64_t slot0;    // first slot of this launch
-  int vec;          // bit 0: q, 1: k, 2: v read 16 bytes at a time, 3: out written 4 values at a time
+  int shift;        // log2 of the tokens a segment
+  int64_t slot0;    // first slot (or entry) of this launch
+  int64_t n_slots;
+  const Place *places;     // nullable: searched for
+  const int32_t *entries;
+  bool vec_in;      // q, k and v are read 16 bytes at a time
+  bool vec_out;     // out is written 4 values at a time
 };
 
-// Stages `size` tokens of one head of x, zero past them and past `width`, into rows of LD elements.
-template <typename T, int C, int WP, int THREADS>
-__device__ __forceinline__ void stage(T *lds, const T *__restrict__ x, int64_t token_stride,
-                                      int64_t first, int64_t step, int size, int width, bool vec) {
-  constexpr int LD = padded<T>(WP), E = 16 / sizeof(T), PIECES = C * WP / E;
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A chunk's tokens of one head of x on their way to LDS, in rows of padded(WP) elements, zero past
+// `size` tokens and past `width`. They are fetched into registers while the chunk before is worked
+// on: 16 bytes at a time, or value by value where a width or an alignment does not allow that.
+// Place r of the chunk is row r ^ flip from `base`, the chunk's lowest token: flip is C - 1 in a pass
+// from the last token to the first, and 0 otherwise. Offsets from there are below 2^31
+// (kMaxTokenStride).
+template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
+  static constexpr int LD = padded<T>(WP), E = 16 / sizeof(T), ROW = WP / E;
+  static constexpr int ROWS = THREADS / ROW, N = (C + ROWS - 1) / ROWS;
+  static_assert(THREADS % ROW == 0 && (ROWS >= C || C % ROWS == 0), "whole rows a pass");
+  struct alignas(16) Piece { T v[E]; };
+  Piece held[N];
+
+  __device__ __forceinline__ void fetch(const char *base, uint32_t row_bytes, int flip, int size,
+                                        int width, int tid) {
+    const int r0 = tid / ROW, c = tid % ROW * E;
 #pragma unroll
-  for (int i = 0; i < (PIECES + THREADS - 1) / THREADS; ++i) {
-    const int n = i * THREADS + (int)threadIdx.x;
-    if (PIECES % THREADS != 0 && n >= PIECES) break;
-    const int r = n / (WP / E), c = n % (WP / E) * E;
-    T v[E];
-    if (vec) {
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (r < size && c < width) raw = *(const uint4 *)(x + (first + r * step) * token_stride + c);
-      *(uint4 *)(lds + r * LD + c) = raw;
-    } else {
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + i * ROWS;
+      const uint32_t at = (uint32_t)(r ^ flip) * row_bytes + c * (int)sizeof(T);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        v[e] = r < size && c + e < width ? x[(first + r * step) * token_stride + c + e] : (T)0.f;
+      for (int e = 0; e < E; ++e) held[i].v[e] = (T)0.f;
+      if (VEC) {
+        if (r < size && c < width) held[i] = *(const Piece *)(base + at);
+      } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) lds[r * LD + c + e] = v[e];
+        for (int e = 0; e < E; ++e)
+          if (r < size && c + e < width) held[i].v[e] = ((const T *)(base + at))[e];
+      }
     }
   }
+  __device__ __forceinline__ void put(T *lds, int tid) const {
+    const int r0 = tid / ROW, c = tid % ROW * E;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (ROWS <= C || r0 < C) *(Piece *)(lds + (r0 + i * ROWS) * LD + c) = held[i];
+  }
+};
+
+// Eight values in three bf16 parts whose sum they are: each part is the leading 8 bits of what is
+// left (cut off, so that it is exact), and 3 * 8 bits are all that fp32 has.
+__device__ __forceinline__ void split3(const f32x4 lo, const f32x4 hi, Frag<bf16> *part) {
+  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+  u32x4 out[3];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x = e < 2 ? lo[2 * e] : hi[2 * e - 4], y = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+      out[n][e] = __builtin_amdgcn_perm(b, a, 0x07060302);  // the upper halves of b and a
+      x -= __uint_as_float(a & 0xffff0000u);
+      y -= __uint_as_float(b & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 3; ++n) part[n].x = __builtin_bit_cast(bf16x8, out[n]);
 }
 
-__device__ __forceinline__ void split3(f32x4 x, bf16x4 *part) {
+// Whether a lane's values are all finite.
+__device__ __forceinline__ bool finite(const Frag<float> &f) {
+  float x = 0.f;
 #pragma unroll
-  for (int n = 0; n < 3; ++n) {
-    part[n] = rounded<bf16>(x);
-    x -= __builtin_convertvector(part[n], f32x4);
-  }
+  for (int e = 0; e < 4; ++e) x = fmaf(f.lo[e], 0.f, fmaf(f.hi[e], 0.f, x));
+  return x == 0.f;
+}
+__device__ __forceinline__ bool finite(const Frag<bf16> &f) {
+  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+  const u32x4 bits = __builtin_bit_cast(u32x4, f.x);
+  uint32_t carry = 0;  // into either half's sign: its exponent was all ones
+#pragma unroll
+  for (int e = 0; e < 4; ++e) carry |= (bits[e] & 0x7fff7fffu) + 0x00800080u;
+  return (carry & 0x80008000u) == 0;
+}
+
+// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, two where
+// few threads hold them, or hold them value by value.
+template <typename T> constexpr int waves_for(int VP, bool vec) {
+  return VP == 32 || (!vec && sizeof(T) == 2) ? 2 : 4;
 }
 
 // One block: one head of one segment. STATES: only the state after the segment, for all segments of
 // a row but its last.
-template <typename T, int KP, int VP, bool STATES>
-__global__ __launch_bounds__(VP * 4) void k_attention(Args A) {
+template <typename T, int KP, int VP, bool STATES, bool VEC>
+__global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
   constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<T>(KP), LV = padded<T>(VP);
   constexpr int PT = NT * (NT + 1) / 2;
   using V4 = typename Vec4<T>::type;
+  using TK = Tile<T, C, KP, THREADS, VEC>;
+  using TV = Tile<T, C, VP, THREADS, VEC>;
   __shared__ __align__(16) T lq[STATES ? 1 : C * LK];
   __shared__ __align__(16) T lk[C * LK];
   __shared__ __align__(16) T lv[C * LV];
   __shared__ __align__(16) T lp[STATES ? 1 : PT * 256];
 
   const AttentionPass &P = A.p;
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, m = lane & 15;
-  const int64_t slot = A.slot0 + blockIdx.x / P.heads;
+  const int lane0 = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int lane = lane0, g = lane >> 4, m = lane & 15;
+  int64_t slot = A.slot0 + blockIdx.x / P.heads;
   const int head = (int)(blockIdx.x % P.heads);
-  const Place at = find_place(P.row_ptr, P.n_rows, P.n_tokens, A.segment, slot, lane);
-  const int64_t n_segments = (at.len + A.segment - 1) / A.segment;
+  Place at;
+  if (STATES) {
+    if (A.places) {
+      slot = A.entries[slot];
+      if (slot < 0 || slot >= A.n_slots) return;
+      at = A.places[slot];
+    } else {
+      at = find_place<true>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, slot, lane);
+      slot += at.row;
+    }
+  } else {
+    at = A.places ? A.places[slot]
+                  : find_place<false>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, slot, lane);
+  }
+  // a row_ptr that decreases leaves places unwritten: nothing is taken from them unchecked
+  if (at.row < 0 || at.row >= P.n_rows || at.first < 0 || at.len < 0 ||
+      at.first + at.len > P.n_tokens)
+    return;
+  const int64_t L = 1LL << A.shift, n_segments = segments_of(at.len, A.shift);
   const bool last = at.segment == (n_segments > 0 ? n_segments - 1 : 0);
   if (at.segment < 0 || at.segment >= (n_segments > 0 ? n_segments : 1) || (STATES && last)) return;
 
@@ -209,190 +330,221 @@ __global__ __launch_bounds__(VP * 4) void k_attention(Args A) {
   const float a2 = (raw <= 0.f ? fmaxf(raw, kMinLogDecay) : __builtin_nanf("")) * kLog2e;
   const int read_off = P.reverse ? 0 : 1, add_off = P.reverse ? 1 : 0;
 
-  // the state: tile kt holds rows 16 kt + 4 g + e of its column 16 wave + m
+  const int64_t begin = at.segment << A.shift;
+  const int count = (int)(begin + L < at.len ? L : at.len - begin);  // tokens
+  const int flip = P.reverse ? C - 1 : 0;
+  const int64_t token0 = P.reverse ? at.first + at.len - begin - C : at.first + begin;
+  const int64_t q_row = P.q.token_stride * (int)sizeof(T), k_row = P.k.token_stride * (int)sizeof(T),
+                v_row = P.v.token_stride * (int)sizeof(T),
+                out_row = (int64_t)P.heads * P.v_width * (P.out_f32 ? 4 : (int)sizeof(T));
+  const char *q = (const char *)((const T *)P.q.data + head / P.q_group * P.q.head_stride);
+  const char *k = (const char *)((const T *)P.k.data + head / P.group * P.k.head_stride);
+  const char *v = (const char *)((const T *)P.v.data + head / P.v_group * P.v.head_stride);
+
+  TK hq, hk;
+  TV hv;
+  const auto fetch = [&](int c, int tid) {
+    const int size = count - c < C ? count - c : C;
+    const int64_t low = token0 + (P.reverse ? -c : c);
+    if (!STATES) hq.fetch(q + low * q_row, (uint32_t)q_row, flip, size, P.k_width, tid);
+    hk.fetch(k + low * k_row, (uint32_t)k_row, flip, size, P.k_width, tid);
+    hv.fetch(v + low * v_row, (uint32_t)v_row, flip, size, P.v_width, tid);
+  };
+  if (count > 0) fetch(0, (int)threadIdx.x);
+
+  // the state: tile kt holds rows state_row(kt, g, e) of its column 16 wave + m
   f32x4 S[KT];
-  const int64_t state = (at.row * P.heads + head) * (int64_t)P.k_width * P.v_width;
+  const int64_t state = ((int64_t)at.row * P.heads + head) * (int64_t)P.k_width * P.v_width;
   const int col = wave * 16 + m;
   float *slot_state = P.segments + ((slot * P.heads + head) * (int64_t)(KT * NW) + wave * KT) * 256 +
                       lane * 4;
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt) {
-    S[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (at.segment > 0 && !STATES) {
-      S[kt] = *(const f32x4 *)(slot_state + kt * 256);
-    } else if (at.segment == 0 && P.first_state) {
+  for (int kt = 0; kt < KT; ++kt) S[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (at.segment > 0 && !STATES) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) S[kt] = *(const f32x4 *)(slot_state + kt * 256);
+  } else if (at.segment == 0 && P.first_state) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = kt * 16 + g * 4 + e;
+        const int r = state_row(kt, g, e);
         if (r < P.k_width && col < P.v_width)
           S[kt][e] = P.first_state[state + r * P.first_ld[0] + col * P.first_ld[1]];
       }
-    }
   }
 
-  const int64_t begin = at.segment * A.segment;
-  const int64_t end = begin + A.segment < at.len ? begin + A.segment : at.len;
-  const T *q = (const T *)P.q.data + head / P.q_group * P.q.head_stride;
-  const T *k = (const T *)P.k.data + head / P.group * P.k.head_stride;
-  const T *v = (const T *)P.v.data + head / P.v_group * P.v.head_stride;
-  const int64_t step = P.reverse ? -1 : 1;
-
-  float read[NT];  // of place 16 i + m
+  // Powers of the decay. Exponents are split into parts that are never negative, so that no factor
+  // exceeds one: e^{a n} may be zero while e^{-a n} is infinite.
+  float near[4], diag[4];  // e^{a (3 - e)}; weight_scale e^{a (m - 4 g - e)}
 #pragma unroll
-  for (int i = 0; i < NT; ++i) read[i] = P.read_scale * exp2f(a2 * (float)(16 * i + m + read_off));
+  for (int e = 0; e < 4; ++e) {
+    near[e] = exp2_fast(a2 * (float)(3 - e));
+    diag[e] = P.weight_scale * exp2_fast(a2 * (float)(m >= g * 4 + e ? m - g * 4 - e : 0));
+  }
 
-  for (int64_t c = begin; c < end; c += C) {
-    const int size = (int)(end - c < C ? end - c : C);
-    const int64_t first = P.reverse ? at.first + at.len - 1 - c : at.first + c;
+  for (int c = 0; c < count; c += C) {
+    const int size = count - c < C ? count - c : C;
+    const int64_t low = token0 + (P.reverse ? -c : c);
+    // addresses are formed anew in each chunk: held across chunks, as the compiler would by itself,
+    // they cost a wave its place on the SIMD (53 registers spilled at four waves)
+    int lane = lane0, tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(lane), "+v"(tid));
+    const int g = lane >> 4, m = lane & 15;
     __syncthreads();
-    if (!STATES)
-      stage<T, C, KP, THREADS>(lq, q, P.q.token_stride, first, step, size, P.k_width, A.vec & 1);
-    stage<T, C, KP, THREADS>(lk, k, P.k.token_stride, first, step, size, P.k_width, A.vec & 2);
-    stage<T, C, VP, THREADS>(lv, v, P.v.token_stride, first, step, size, P.v_width, A.vec & 4);
+    if (!STATES) hq.put(lq, tid);
+    hk.put(lk, tid);
+    hv.put(lv, tid);
     __syncthreads();
-
-    Frag<T> vf[SF];  // column `col` of v
-#pragma unroll
-    for (int s = 0; s < SF; ++s) vf[s] = frag_col(lv + s * 32 * LV + wave * 16, LV, lane);
+    if (c + C < count) fetch(c + C, tid);
 
     if (!STATES) {
       // weights of places i (columns) and j (rows) <= i, one 16 x 16 tile at a time
-#pragma unroll
-      for (int n = 0; n < (PT + NW - 1) / NW; ++n) {
-        const int tile = n * NW + wave;
-        if (tile < PT) {
-          int i = 0;
-          while ((i + 1) * (i + 2) / 2 <= tile) ++i;
-          const int j = tile - i * (i + 1) / 2;
+#pragma unroll 1
+      for (int tile = wave; tile < PT; tile += NW) {
+        {
+          const int i = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, j = tile - i * (i + 1) / 2;
           f32x4 w = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int d = 0; d < KF; ++d)
             w = mma(frag_row(lk + j * 16 * LK + d * 32, LK, lane),
                     frag_row(lq + i * 16 * LK + d * 32, LK, lane), w);
+          if (i == j) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int gap = 16 * (i - j) + m - g * 4 - e;
-            w[e] = gap >= 0 ? w[e] * (P.weight_scale * exp2f(a2 * (float)gap)) : 0.f;
+            for (int e = 0; e < 4; ++e) w[e] = m >= g * 4 + e ? w[e] * diag[e] : 0.f;
+          } else {
+            const float far = P.weight_scale * exp2_fast(a2 * (float)(16 * (i - j) + m - g * 4 - 3));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] *= far * near[e];
           }
           *(V4 *)(lp + tile * 256 + lane * 4) = rounded<T>(w);
         }
       }
-      // what the state before the chunk gives: rows 16 wave + 4 g + e of v, column 16 i + m
-      f32x4 o[NT];
+    }
+    if (!STATES) __syncthreads();
+    Frag<T> vf[SF];  // column `col` of v
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int d = 0; d < KF; ++d)
-          o[i] = mma(joined(rounded<T>(S[2 * d]), rounded<T>(S[2 * d + 1])),
-                     frag_row(lq + i * 16 * LK + d * 32, LK, lane), o[i]);
-        o[i] *= read[i];
-      }
-      __syncthreads();
+    for (int s = 0; s < SF; ++s) vf[s] = frag_col<4>(lv + s * 32 * LV + wave * 16, LV, lane);
+    if (!STATES) {
       // 0 * inf and 0 * NaN are NaN: values of v that are neither enter the products as zeros, and
       // are added to their own and later places alone
-      float finite = 0.f;
+      bool mine = true;
 #pragma unroll
-      for (int s = 0; s < SF; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) finite = fmaf((float)vf[s].get(e), 0.f, finite);
-      const bool all_finite = !__any(finite != 0.f);
-      Frag<T> vc[SF];
-#pragma unroll
-      for (int s = 0; s < SF; ++s) vc[s] = vf[s];
+      for (int s = 0; s < SF; ++s) mine = mine && finite(vf[s]);
+      const bool all_finite = !__any(!mine);
       if (!all_finite) {
 #pragma unroll
         for (int s = 0; s < SF; ++s)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if ((float)vf[s].get(e) * 0.f != 0.f) vc[s].set(e, (T)0.f);
+            if ((float)vf[s].get(e) * 0.f != 0.f) vf[s].set(e, (T)0.f);
       }
+      Frag<T> sf[KF];
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+      for (int d = 0; d < KF; ++d) sf[d] = joined(rounded<T>(S[2 * d]), rounded<T>(S[2 * d + 1]));
+      const V4 zero = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+      const int c0 = wave * 16 + g * 4;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        // rows c0 + e of v, column 16 i + m: what the state before the chunk gives, then the weights
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < KF; ++d) o = mma(sf[d], frag_row(lq + i * 16 * LK + d * 32, LK, lane), o);
+        o *= P.read_scale * exp2_fast(a2 * (float)(16 * i + m + read_off));
 #pragma unroll
         for (int s = 0; s <= i / 2; ++s) {
           const T *t = lp + (i * (i + 1) / 2 + 2 * s) * 256 + lane * 4;
-          const V4 zero = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
-          o[i] = mma(vc[s], joined(*(const V4 *)t, 2 * s + 1 <= i ? *(const V4 *)(t + 256) : zero),
-                     o[i]);
+          o = mma(vf[s], joined(*(const V4 *)t, 2 * s + 1 <= i ? *(const V4 *)(t + 256) : zero), o);
         }
-      if (!all_finite) {
-        for (int i = 0; i < NT; ++i) {
-          f32x4 add = {0.f, 0.f, 0.f, 0.f};
-          for (int j = 0; j <= 16 * i + m; ++j) {
+        const int place = 16 * i + m;
+        if (!all_finite) {
+#pragma unroll 1
+          for (int j = 0; j <= place; ++j) {
             const float w = (float)lp[(i * (i + 1) / 2 + j / 16) * 256 + (m + j % 16 / 4 * 16) * 4 + j % 4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float x = (float)lv[j * LV + wave * 16 + g * 4 + e];
-              if (x * 0.f != 0.f) add[e] = fmaf(w, x, add[e]);
+              const float x = (float)lv[j * LV + c0 + e];
+              if (x * 0.f != 0.f) o[e] = fmaf(w, x, o[e]);
             }
           }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            if (n == i) o[n] += add;
         }
-      }
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const int place = 16 * i + m, c0 = wave * 16 + g * 4;
         if (place < size && c0 < P.v_width) {
-          const int64_t to = ((first + place * step) * P.heads + head) * (int64_t)P.v_width + c0;
-          if (P.out_f32) {
-            float *x = (float *)P.out + to;
-            if (A.vec & 8) {
-              *(f32x4 *)x = o[i];
-            } else {
-              for (int e = 0; e < 4; ++e)
-                if (c0 + e < P.v_width) x[e] = o[i][e];
-            }
+          char *to = (char *)P.out + low * out_row + (int64_t)head * P.v_width * (P.out_f32 ? 4 : (int)sizeof(T));
+          to += (uint32_t)(place ^ flip) * (uint32_t)out_row + c0 * (P.out_f32 ? 4 : (int)sizeof(T));
+          if (A.vec_out) {
+            if (P.out_f32) *(f32x4 *)to = o;
+            else *(V4 *)to = rounded<T>(o);
           } else {
-            T *x = (T *)P.out + to;
-            const V4 r = rounded<T>(o[i]);
-            if (A.vec & 8) {
-              *(V4 *)x = r;
-            } else {
-              for (int e = 0; e < 4; ++e)
-                if (c0 + e < P.v_width) x[e] = r[e];
-            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (c0 + e < P.v_width) {
+                if (P.out_f32) ((float *)to)[e] = o[e];
+                else ((T *)to)[e] = (T)o[e];
+              }
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!all_finite) {
+#pragma unroll
+        for (int s = 0; s < SF; ++s) vf[s] = frag_col<4>(lv + s * 32 * LV + wave * 16, LV, lane);
       }
     }
 
     // S <- e^{a size} S + sum_j k_j (e^{a (size - 1 - j + add_off)} update_scale v_j)^T
-    const float whole = exp2f(a2 * (float)size);
+    const float whole = exp2_fast(a2 * (float)size);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) S[kt] *= whole;
 #pragma unroll
     for (int s = 0; s < SF; ++s) {
       f32x4 w[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int left = size - 1 - (s * 32 + h * 16 + g * 4 + e);
-          w[h][e] = left >= 0 ? P.update_scale * exp2f(a2 * (float)(left + add_off)) : 0.f;
-        }
-      if constexpr (sizeof(T) == 2) {
-        bf16x4 part[2][3];
+      if (size == C) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          f32x4 x;
+          const int left = C - 4 - s * 32 - h * 16 - g * 4;
+          const float far = P.update_scale * exp2_fast(a2 * (float)(left + add_off));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = w[h][e] * (float)vf[s].x[h * 4 + e];
-          split3(x, part[h]);
-        }
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const Frag<bf16> kf = frag_col(lk + s * 32 * LK + kt * 16, LK, lane);
-#pragma unroll
-          for (int n = 0; n < 3; ++n) S[kt] = mma(kf, joined(part[0][n], part[1][n]), S[kt]);
+          for (int e = 0; e < 4; ++e) w[h][e] = far * near[e];
         }
       } else {
-        const Frag<float> x = {vf[s].lo * w[0], vf[s].hi * w[1]};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int left = size - 1 - s * 32 - h * 16 - g * 4 - e;  // below 0: no token, v is zero
+            w[h][e] = P.update_scale * exp2_fast(a2 * (float)((left > 0 ? left : 0) + add_off));
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[0][e] *= (float)vf[s].get(e);
+        w[1][e] *= (float)vf[s].get(4 + e);
+      }
+      const T *kc = lk + s * 32 * LK;
+      if constexpr (sizeof(T) == 2) {
+        Frag<bf16> part[3];
+        split3(w[0], w[1], part);
+        if (P.last_state) {
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            const Frag<bf16> kf = frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) S[kt] = mma(kf, part[n], S[kt]);
+          }
+        } else {  // read as bf16 alone: 16 bits are enough
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            const Frag<bf16> kf = frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) S[kt] = mma(kf, part[n], S[kt]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        const Frag<float> x = {w[0], w[1]};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
-          S[kt] = mma(frag_col(lk + s * 32 * LK + kt * 16, LK, lane), x, S[kt]);
+          S[kt] = mma(frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane), x, S[kt]);
       }
     }
   }
@@ -405,37 +557,46 @@ __global__ __launch_bounds__(VP * 4) void k_attention(Args A) {
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = kt * 16 + g * 4 + e;
+        const int r = state_row(kt, g, e);
         if (r < P.k_width && col < P.v_width)
           P.last_state[state + r * P.last_ld[0] + col * P.last_ld[1]] = S[kt][e];
       }
   }
 }
 
-// States after each segment alone -> states before each segment. One thread a value of the state,
-// one block a part of one head of one row.
+// States after each segment alone -> states before each segment: one block (of blockIdx.y parts) a
+// head of a row, one thread four values of the state.
 __global__ __launch_bounds__(256) void k_join_segments(float *segments, const int64_t *row_ptr,
                                                        int64_t row0, int64_t n_tokens,
-                                                       int64_t n_slots, int64_t L, int heads,
+                                                       int64_t n_slots, int shift, int heads,
                                                        const float *log_decay, int64_t floats) {
   const int64_t row = row0 + blockIdx.x / heads;
   const int head = (int)(blockIdx.x % heads);
   const int64_t first = clamped(row_ptr[row], 0, n_tokens);
   const int64_t len = clamped(row_ptr[row + 1], first, n_tokens) - first;
-  const int64_t slot = first / L + row;
-  const int64_t n = (len + L - 1) / L;
-  const int64_t x = (int64_t)blockIdx.y * 256 + threadIdx.x;
-  if (n < 2 || x >= floats || slot + n > n_slots) return;
+  const int64_t slot = (first >> shift) + row;
+  const int64_t n = (len + (1LL << shift) - 1) >> shift;
+  if (n < 2 || slot + n > n_slots) return;
   const float raw = log_decay[head];
   const float a2 = (raw <= 0.f ? fmaxf(raw, kMinLogDecay) : __builtin_nanf("")) * kLog2e;
-  const float whole = exp2f(a2 * (float)L);
-  float *p = segments + (slot * heads + head) * floats + x;
+  const float whole = exp2_fast(a2 * (float)(1 << shift));
   const int64_t stride = heads * floats;
-  float state = p[0];
-  for (int64_t j = 1; j < n; ++j) {
-    const float own = j + 1 < n ? p[j * stride] : 0.f;
-    p[j * stride] = state;
-    state = fmaf(whole, state, own);
+  for (int64_t x = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; x < floats;
+       x += (int64_t)gridDim.y * 1024) {
+    float *p = segments + (slot * heads + head) * floats + x;
+    f32x4 state = *(const f32x4 *)p;
+    for (int64_t j = 1; j < n; j += 4) {
+      f32x4 own[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        own[i] = j + i + 1 < n ? *(const f32x4 *)(p + (j + i) * stride) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j + i < n) {
+          *(f32x4 *)(p + (j + i) * stride) = state;
+          state = state * whole + own[i];
+        }
+    }
   }
 }
 
@@ -472,7 +633,7 @@ __global__ __launch_bounds__(256) void k_step(int64_t row0, int heads, int group
   const int64_t from = source ? source[row] : row;
   const bool ok = from >= 0 && from < n_sources;
   const float raw = log_decay[head];
-  const float decay = raw <= 0.f ? exp2f(fmaxf(raw, kMinLogDecay) * kLog2e) : __builtin_nanf("");
+  const float decay = raw <= 0.f ? exp2_fast(fmaxf(raw, kMinLogDecay) * kLog2e) : __builtin_nanf("");
   const int lanes = (V + VW - 1) / VW, rows = 256 / lanes, c = tid % lanes * VW, r0 = tid / lanes;
   const int64_t size = (int64_t)K * V;
   const float *in = state + ((ok ? from : 0) * heads + head) * size;
@@ -517,73 +678,104 @@ __global__ __launch_bounds__(256) void k_step(int64_t row0, int heads, int group
 
 int padded_width3(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : 128; }
 
-template <typename T, int KP, int VP>
-hipError_t launch_kv(Args A, int64_t slots, bool split, hipStream_t s) {
+template <typename T, int KP, int VP> hipError_t launch_kv(Args A, bool split, hipStream_t s) {
   const AttentionPass &P = A.p;
-  const auto each = [&](auto kernel) {
-    const int64_t per = max_blocks(VP * 4) / P.heads;  // slots a launch
-    for (A.slot0 = 0; A.slot0 < slots; A.slot0 += per) {
-      const int64_t n = slots - A.slot0 < per ? slots - A.slot0 : per;
+  const auto each = [&](auto kernel, int64_t places) {
+    const int64_t per = max_blocks(VP * 4) / P.heads;  // a launch
+    for (A.slot0 = 0; A.slot0 < places; A.slot0 += per) {
+      const int64_t n = places - A.slot0 < per ? places - A.slot0 : per;
       hipLaunchKernelGGL(kernel, dim3((unsigned)(n * P.heads)), dim3(VP * 4), 0, s, A);
     }
   };
   if (split) {
-    each(k_attention<T, KP, VP, true>);
+    each(A.vec_in ? k_attention<T, KP, VP, true, true> : k_attention<T, KP, VP, true, false>,
+         P.n_tokens >> A.shift);
     const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / P.heads;
     for (int64_t r = 0; r < P.n_rows; r += per) {
       const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
-      hipLaunchKernelGGL(k_join_segments, dim3((unsigned)(n * P.heads), (unsigned)(floats / 256)),
-                         dim3(256), 0, s, P.segments, P.row_ptr, r, P.n_tokens, slots, A.segment,
-                         P.heads, P.log_decay, floats);
+      // parts of a state: as many as fill the chip, where rows and heads alone do not
+      const int64_t parts = n * P.heads >= 1024 ? 1 : (floats + 1023) / 1024;
+      hipLaunchKernelGGL(k_join_segments, dim3((unsigned)(n * P.heads), (unsigned)parts), dim3(256),
+                         0, s, P.segments, P.row_ptr, r, P.n_tokens, A.n_slots, A.shift, P.heads,
+                         P.log_decay, floats);
     }
   }
-  each(k_attention<T, KP, VP, false>);
+  each(A.vec_in ? k_attention<T, KP, VP, false, true> : k_attention<T, KP, VP, false, false>,
+       A.n_slots);
   return hipGetLastError();
 }
 
 template <typename T, int KP>
-hipError_t launch_k(const Args &A, int64_t slots, bool split, hipStream_t s) {
+hipError_t launch_k(const Args &A, bool split, hipStream_t s) {
   switch (padded_width3(A.p.v_width)) {
-    case 32: return launch_kv<T, KP, 32>(A, slots, split, s);
-    case 64: return launch_kv<T, KP, 64>(A, slots, split, s);
-    default: return launch_kv<T, KP, 128>(A, slots, split, s);
+    case 32: return launch_kv<T, KP, 32>(A, split, s);
+    case 64: return launch_kv<T, KP, 64>(A, split, s);
+    default: return launch_kv<T, KP, 128>(A, split, s);
   }
 }
 
-template <typename T> hipError_t launch_t(const Args &A, int64_t slots, bool split, hipStream_t s) {
+template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t s) {
   switch (padded_width3(A.p.k_width)) {
-    case 32: return launch_k<T, 32>(A, slots, split, s);
-    case 64: return launch_k<T, 64>(A, slots, split, s);
-    default: return launch_k<T, 128>(A, slots, split, s);
+    case 32: return launch_k<T, 32>(A, split, s);
+    case 64: return launch_k<T, 64>(A, split, s);
+    default: return launch_k<T, 128>(A, split, s);
   }
 }
 
 }  // namespace
 
-int64_t attention_segment(int64_t n_tokens, int32_t heads) {
-  int64_t L = 512;
-  while (L < 4096 && n_tokens / L * heads > 2048) L *= 2;
-  return L;
+// Short segments fill the chip where tokens are few; each costs a pass over its k and v and a state
+// written and read. From four chunks up, as many as leave 512 blocks (bf16) or 2048 (f32, whose chunks
+// are half as long and bound by the products), at most 2048 tokens. Us with segments of 256, 512, 1024
+// and 2048: one row of 62496 bf16 tokens, 8 heads of 64 142, 126, 115, -; forward and backward of 4096
+// rows of 263 -, 5800, 5275, 5213 (4096: 5640); 100 f32 rows of 1000 at 128 wide -, 3860, 4037, -; 8
+// bf16 rows of 250 33, 42, 72, -.
+int attention_shift(als_dtype dtype, int64_t n_tokens, int32_t heads) {
+  int shift = dtype == ALS_F32 ? 7 : 8;
+  while (shift < 11 && (n_tokens >> shift) * heads > (dtype == ALS_F32 ? 2048 : 512)) ++shift;
+  return shift;
 }
 
-int64_t attention_segment_floats(int64_t n_tokens, int64_t n_rows, int32_t heads, int k_width,
-                                 int v_width) {
-  const int64_t L = attention_segment(n_tokens, heads);
-  if (n_tokens <= L) return 0;  // no row is longer than a segment
-  return (n_tokens / L + n_rows) * heads * padded_width3(k_width) * padded_width3(v_width);
+AttentionSpace attention_space(als_dtype dtype, int64_t n_tokens, int64_t n_rows, int32_t heads,
+                               int k_width, int v_width) {
+  const int shift = attention_shift(dtype, n_tokens, heads);
+  const int64_t entries = n_tokens >> shift, slots = entries + n_rows;
+  AttentionSpace x{};
+  if (n_rows > kSearchedRows) {
+    x.places = (slots * (int64_t)sizeof(Place) + 15) / 16 * 16;
+    x.entries = (entries * 4 + 15) / 16 * 16;
+  }
+  if (n_tokens > 1LL << shift)  // else no row is longer than a segment
+    x.states = slots * heads * padded_width3(k_width) * padded_width3(v_width) * 4;
+  return x;
+}
+
+hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s) {
+  if (!p.places) return hipSuccess;
+  const int shift = attention_shift(dtype, p.n_tokens, p.heads);
+  const int64_t entries = p.n_tokens >> shift;
+  hipLaunchKernelGGL(k_places, dim3((unsigned)((p.n_rows + 3) / 4)), dim3(256), 0, s, p.row_ptr,
+                     p.n_rows, p.n_tokens, shift, entries + p.n_rows, entries, (Place *)p.places,
+                     p.entries);
+  return hipGetLastError();
 }
 
 hipError_t launch_attention(als_dtype dtype, const AttentionPass &p, hipStream_t s) {
   if (p.n_rows == 0) return hipSuccess;
-  Args A{p, attention_segment(p.n_tokens, p.heads), 0};
+  Args A{};
+  A.p = p;
+  A.shift = attention_shift(dtype, p.n_tokens, p.heads);
+  A.n_slots = (p.n_tokens >> A.shift) + p.n_rows;
+  A.places = (const Place *)p.places;
+  A.entries = p.entries;
   const int size = dtype == ALS_F32 ? 4 : 2, out = p.out_f32 ? 4 : size;
-  A.vec = (aligned16(p.q.data, p.q.token_stride, p.q.head_stride, p.k_width, size) ? 1 : 0) |
-          (aligned16(p.k.data, p.k.token_stride, p.k.head_stride, p.k_width, size) ? 2 : 0) |
-          (aligned16(p.v.data, p.v.token_stride, p.v.head_stride, p.v_width, size) ? 4 : 0) |
-          (p.v_width % 4 == 0 && (uintptr_t)p.out % (4 * out) == 0 ? 8 : 0);
-  const int64_t slots = p.n_tokens / A.segment + p.n_rows;
-  const bool split = p.n_tokens > A.segment;
-  return dtype == ALS_F32 ? launch_t<float>(A, slots, split, s) : launch_t<bf16>(A, slots, split, s);
+  const auto vec = [&](const als_heads &x, int width) {
+    return aligned16(x.data, x.token_stride, x.head_stride, width, size);
+  };
+  A.vec_in = vec(p.q, p.k_width) && vec(p.k, p.k_width) && vec(p.v, p.v_width);
+  A.vec_out = p.v_width % 4 == 0 && (uintptr_t)p.out % (4 * out) == 0;
+  const bool split = p.n_tokens > 1LL << A.shift;
+  return dtype == ALS_F32 ? launch_t<float>(A, split, s) : launch_t<bf16>(A, split, s);
 }
 
 hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,

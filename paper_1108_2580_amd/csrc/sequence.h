@@ -27,6 +27,9 @@ inline bool aligned16(const void *p, int64_t token_stride, int64_t head_stride, 
           (uint64_t)(width * size)) % 16 == 0;
 }
 
+// The largest stride of attention's tokens (values): a chunk is addressed with 32-bit offsets.
+constexpr int64_t kMaxTokenStride = 1 << 22;
+
 // One pass of decayed attention over packed rows of tokens; the gradients are passes of the same
 // form (attention.hip).
 struct AttentionPass {
@@ -48,14 +51,24 @@ struct AttentionPass {
   int64_t last_ld[2];
   void *out;              // [n_tokens, heads, v_width], packed
   bool out_f32;           // out is fp32 whatever the type of the inputs
-  float *segments;        // states of the segments (attention_segments floats), null without a split
+  // workspace (attention_space), each null where its size is 0
+  void *places;           // of the segments, written by launch_places
+  int32_t *entries;
+  float *segments;        // states of the segments
 };
 
-// Tokens a segment: rows longer than it are cut and their segments run side by side.
-int64_t attention_segment(int64_t n_tokens, int32_t heads);
-// Floats of the segments' states.
-int64_t attention_segment_floats(int64_t n_tokens, int64_t n_rows, int32_t heads, int k_width,
-                                 int v_width);
+// Bytes of a pass's workspace, by part, each a multiple of 16.
+struct AttentionSpace {
+  int64_t places, entries, states;
+  int64_t total() const { return places + entries + states; }
+};
+
+// log2 of the tokens a segment: longer rows are cut and their segments run side by side.
+int attention_shift(als_dtype dtype, int64_t n_tokens, int32_t heads);
+AttentionSpace attention_space(als_dtype dtype, int64_t n_tokens, int64_t n_rows, int32_t heads,
+                               int k_width, int v_width);
+// Fills p.places and p.entries, which all passes over the same rows and heads share.
+hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s);
 hipError_t launch_attention(als_dtype dtype, const AttentionPass &p, hipStream_t s);
 // out[t, k, d] = sum over the head's group of x[t, k * group + i, d], in order.
 hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,

@@ -160,6 +160,7 @@ als_status check_attention(const als_attention *s, als_dtype dtype, bool step) {
 
 als_status check_input(const char *name, const als_heads &x, int64_t n, int size) {
   const char *w = wrong(x, n, size);
+  if (!w && n > 1 && x.token_stride > als::kMaxTokenStride) w = "a token_stride above 2^22";
   return w ? fail_without_context(ALS_ERR_INVALID_ARG, "%s has %s", name, w) : ALS_OK;
 }
 
@@ -169,9 +170,13 @@ bool sane(const als_attention *s) {
          s->k_width <= 128 && s->v_width >= 1 && s->v_width <= 128;
 }
 
-int64_t segment_bytes(const als_attention *s) {
-  return 4 * als::attention_segment_floats(s->n_tokens, s->n_rows, s->q_heads, s->k_width,
-                                           s->v_width);
+als::AttentionSpace space_of(const als_attention *s, als_dtype dtype) {
+  return als::attention_space(dtype, s->n_tokens, s->n_rows, s->q_heads, s->k_width, s->v_width);
+}
+// Of either type.
+int64_t space_bytes(const als_attention *s) {
+  const int64_t a = space_of(s, ALS_F32).total(), b = space_of(s, ALS_BF16).total();
+  return a > b ? a : b;
 }
 // Gradients of shared heads, one per query head, before their sum.
 int64_t shared_bytes(const als_attention *s) {
@@ -180,7 +185,7 @@ int64_t shared_bytes(const als_attention *s) {
   return rounded16(4 * s->n_tokens * s->q_heads * w);
 }
 
-AttentionPass pass_of(const als_attention *s, void *workspace) {
+AttentionPass pass_of(const als_attention *s, als_dtype dtype, void *workspace) {
   AttentionPass p{};
   p.n_tokens = s->n_tokens;
   p.n_rows = s->n_rows;
@@ -190,7 +195,11 @@ AttentionPass pass_of(const als_attention *s, void *workspace) {
   p.row_ptr = s->row_ptr;
   p.weight_scale = s->scale;
   p.update_scale = p.read_scale = 1.f;
-  p.segments = (float *)workspace;
+  const als::AttentionSpace x = space_of(s, dtype);
+  char *w = (char *)workspace;
+  p.places = x.places ? w : nullptr;
+  p.entries = x.places ? (int32_t *)(w + x.places) : nullptr;
+  p.segments = x.states ? (float *)(w + x.places + x.entries) : nullptr;
   return p;
 }
 
@@ -238,7 +247,7 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
 }
 
 int64_t als_decay_attention_workspace(const als_attention *shape) {
-  return sane(shape) ? segment_bytes(shape) : -1;
+  return sane(shape) ? space_bytes(shape) : -1;
 }
 
 als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_heads q, als_heads k,
@@ -262,8 +271,8 @@ als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_
   REQUIRE(!initial_state || !final_state ||
               !overlap(span(initial_state, states), span(final_state, states)),
           "final_state overlaps initial_state");
-  if (als_status st = check_workspace(workspace, workspace_bytes, segment_bytes(s))) return st;
-  AttentionPass p = pass_of(s, workspace);
+  if (als_status st = check_workspace(workspace, workspace_bytes, space_bytes(s))) return st;
+  AttentionPass p = pass_of(s, dtype, workspace);
   p.group = p.v_group = s->q_heads / s->k_heads;
   p.k_width = s->k_width;
   p.v_width = s->v_width;
@@ -276,11 +285,13 @@ als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_
   p.first_ld[0] = p.last_ld[0] = s->v_width;
   p.first_ld[1] = p.last_ld[1] = 1;
   p.out = out;
-  return launched(als::launch_attention(dtype, p, (hipStream_t)hip_stream), "als_decay_attention");
+  hipError_t e = als::launch_places(dtype, p, (hipStream_t)hip_stream);
+  if (e == hipSuccess) e = als::launch_attention(dtype, p, (hipStream_t)hip_stream);
+  return launched(e, "als_decay_attention");
 }
 
 int64_t als_decay_attention_backward_workspace(const als_attention *shape) {
-  return sane(shape) ? segment_bytes(shape) + shared_bytes(shape) : -1;
+  return sane(shape) ? space_bytes(shape) + shared_bytes(shape) : -1;
 }
 
 als_status als_decay_attention_backward(const als_attention *shape, als_dtype dtype, als_heads d_out,
@@ -321,10 +332,10 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
                                       als_decay_attention_backward_workspace(s)))
     return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  float *shared = group > 1 ? (float *)((char *)workspace + segment_bytes(s)) : nullptr;
+  float *shared = group > 1 ? (float *)((char *)workspace + space_bytes(s)) : nullptr;
 
   // dq: the pass over (d_out, v, k), with the state transposed
-  AttentionPass p = pass_of(s, workspace);
+  AttentionPass p = pass_of(s, dtype, workspace);
   p.group = p.v_group = group;
   p.k_width = s->v_width;
   p.v_width = s->k_width;
@@ -336,9 +347,10 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
   p.first_ld[0] = 1;
   p.first_ld[1] = s->v_width;
   p.out = dq;
-  hipError_t e = als::launch_attention(dtype, p, stream);
+  hipError_t e = als::launch_places(dtype, p, stream);
+  if (e == hipSuccess) e = als::launch_attention(dtype, p, stream);
   // dv: the reversed pass over (k, q, d_out); its last state is the initial state's gradient
-  p = pass_of(s, workspace);
+  p = pass_of(s, dtype, workspace);
   p.reverse = true;
   p.update_scale = s->scale;
   p.q_group = group;
