@@ -15,10 +15,11 @@ result carries it.
 from __future__ import annotations
 
 import ctypes
+import math
 
 import torch
 
-from . import ALS_OK, ALSError, lib
+from . import ALS_ERR_INVALID_ARG, ALS_OK, ALSError, lib
 
 ALS_F32, ALS_BF16 = 0, 1
 _DTYPES = {torch.float32: ALS_F32, torch.bfloat16: ALS_BF16}
@@ -78,40 +79,60 @@ def _check(status):
         raise ALSError(status, lib.als_last_error(None).decode())
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+# A token's calls are bound by the host. The current stream's handle by itself takes a fifth of the
+# time of the Stream object around it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _on_device(t, name):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+def _stream(device):
+    return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
+
+
+def _device(t, name):
+    """The current device's index, on which t has to lie."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.device.index != torch.cuda.current_device():
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, not on the current device")
+    return device
 
 
-def _array(t, name, dtype, shape):
+def _array(t, name, dtype, shape, device):
     """A contiguous tensor of this type and shape, as a pointer."""
-    _on_device(t, name)
-    if t.dtype != dtype or not t.is_contiguous():
-        raise TypeError(f"{name} must be contiguous {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype != dtype or \
+            not t.is_contiguous() or t.shape != shape:
+        _device(t, name)
+        if t.dtype != dtype or not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous {dtype}")
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t.data_ptr()
 
 
-def _heads(t, name, dtype, shape=None):
+def _heads(t, name, dtype, device):
     """A [tokens, heads, width] tensor with contiguous features."""
-    _on_device(t, name)
-    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
-        raise TypeError(f"{name} must be {dtype or 'float32 or bfloat16'}, not {t.dtype}")
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _device(t, name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.dim() != 3:
         raise ValueError(f"{name} must have the dimensions tokens, heads, width")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     token, head, feature = t.stride()
     if feature != 1 and t.shape[2] > 1:
         raise TypeError(f"the features of {name} must be contiguous")
     return _Heads(t.data_ptr(), token, head)
+
+
+def _dtype(t, name):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return code
+
+
+def _shaped(t, name, shape):
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _workspace(size, device):
@@ -133,31 +154,36 @@ def rotary_tables(n_positions, rotated, base=10_000.0, device="cuda"):
 
 
 def _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
-    hq = _heads(q, "q", None)
+    dev = _device(q, "q")
+    code = _dtype(q, "q")
+    hq, hk = _heads(q, "q", q.dtype, dev), _heads(k, "k", q.dtype, dev)
     N, Hq, D = q.shape
-    hk = _heads(k, "k", q.dtype)
-    if k.shape[0] != N or k.shape[2] != D:
-        raise ValueError(f"k has shape {tuple(k.shape)}, expected {N} tokens of width {D}")
-    _on_device(cos, "cos")
-    if cos.dim() != 2:
+    Hk = k.shape[1]
+    _shaped(k, "k", (N, Hk, D))
+    if not isinstance(cos, torch.Tensor) or cos.dim() != 2:
         raise ValueError("cos must have the dimensions positions, pairs")
     P, half = cos.shape
-    shape = _Rotation(N, P, Hq, k.shape[1], D, 2 * half, 1 if neighbours else 0, eps,
-                      _array(positions, "positions", torch.int32, (N,)),
-                      _array(cos, "cos", torch.float32, (P, half)),
-                      _array(sin, "sin", torch.float32, (P, half)))
-    return shape, hq, hk, _array(q_weight, "q_weight", torch.float32, (D,)), \
-        _array(k_weight, "k_weight", torch.float32, (D,))
+    f32 = torch.float32
+    shape = _Rotation(N, P, Hq, Hk, D, 2 * half, 1 if neighbours else 0, eps,
+                      _array(positions, "positions", torch.int32, (N,), dev),
+                      _array(cos, "cos", f32, (P, half), dev), _array(sin, "sin", f32, (P, half), dev))
+    return dev, code, shape, hq, hk, _array(q_weight, "q_weight", f32, (D,), dev), \
+        _array(k_weight, "k_weight", f32, (D,), dev)
+
+
+def _packed(t):
+    """A new tensor like t, tokens one after the other, and its strides."""
+    out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    _, H, D = t.shape
+    return out, _Heads(out.data_ptr(), H * D, D)
 
 
 def _norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
-    shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    D = q.shape[2]
-    _check(lib.als_norm_rotate(shape, _DTYPES[q.dtype], hq, hk, wq, wk,
-                               _Heads(q_out.data_ptr(), q.shape[1] * D, D),
-                               _Heads(k_out.data_ptr(), k.shape[1] * D, D), _stream()))
+    dev, code, shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps,
+                                                 neighbours)
+    q_out, ho = _packed(q)
+    k_out, ko = _packed(k)
+    _check(lib.als_norm_rotate(shape, code, hq, hk, wq, wk, ho, ko, _stream(dev)))
     return q_out, k_out
 
 
@@ -170,7 +196,8 @@ def norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps=1e-6, neighbo
     (``rotary_tables``); ``positions``: int32 [tokens], a row of the tables each (one outside them
     makes its token NaN). ``neighbours``: pair p is features 2 p and 2 p + 1 instead of p and
     p + pairs. Returns new (q, k)."""
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, q_weight, k_weight)):
+    if torch.is_grad_enabled() and (
+            q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad):
         return _NormRotate.apply(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
     return _norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
 
@@ -179,18 +206,19 @@ def norm_rotate_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, 
                          neighbours=False):
     """Gradients of ``norm_rotate``'s inputs (dq, dk, dq_weight, dk_weight) from those of its
     outputs."""
-    shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
-    hdq, hdk = _heads(dq, "dq", q.dtype, q.shape), _heads(dk, "dk", q.dtype, k.shape)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    dev, code, shape, hq, hk, wq, wk = _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps,
+                                                 neighbours)
+    hdq, hdk = _heads(dq, "dq", q.dtype, dev), _heads(dk, "dk", q.dtype, dev)
+    _shaped(dq, "dq", q.shape)
+    _shaped(dk, "dk", k.shape)
+    q_out, ho = _packed(q)
+    k_out, ko = _packed(k)
     dwq, dwk = torch.empty_like(q_weight), torch.empty_like(k_weight)
-    D = q.shape[2]
     size = lib.als_norm_rotate_workspace(shape)
     work = _workspace(size, q.device)
-    _check(lib.als_norm_rotate_backward(
-        shape, _DTYPES[q.dtype], hdq, hdk, hq, hk, wq, wk,
-        _Heads(q_out.data_ptr(), q.shape[1] * D, D), _Heads(k_out.data_ptr(), k.shape[1] * D, D),
-        dwq.data_ptr(), dwk.data_ptr(), _ptr(work), size, _stream()))
+    _check(lib.als_norm_rotate_backward(shape, code, hdq, hdk, hq, hk, wq, wk, ho, ko,
+                                        dwq.data_ptr(), dwk.data_ptr(), _ptr(work), size,
+                                        _stream(dev)))
     return q_out, k_out, dwq, dwk
 
 
@@ -216,40 +244,42 @@ class _NormRotate(torch.autograd.Function):
 # ---- attention with a decay for each head --------------------------------------------------------
 
 def _attention(q, k, v, log_decay, row_ptr, scale):
-    hq = _heads(q, "q", None)
+    dev = _device(q, "q")
+    code = _dtype(q, "q")
+    hq, hk, hv = (_heads(t, n, q.dtype, dev) for t, n in ((q, "q"), (k, "k"), (v, "v")))
     N, Hq, K = q.shape
-    hk, hv = _heads(k, "k", q.dtype), _heads(v, "v", q.dtype)
-    Hk, V = v.shape[1:]
-    if tuple(k.shape) != (N, Hk, K) or v.shape[0] != N:
-        raise ValueError(f"q, k and v have shapes {tuple(q.shape)}, {tuple(k.shape)} and "
-                         f"{tuple(v.shape)}")
+    _, Hk, V = v.shape
+    _shaped(k, "k", (N, Hk, K))
+    _shaped(v, "v", (N, Hk, V))
     rows = N
     if row_ptr is not None:
-        _on_device(row_ptr, "row_ptr")
-        if row_ptr.dim() != 1 or row_ptr.numel() < 1:
+        if not isinstance(row_ptr, torch.Tensor) or row_ptr.dim() != 1 or row_ptr.numel() < 1:
             raise ValueError("row_ptr must have one more entry than there are rows")
         rows = row_ptr.numel() - 1
-        row_ptr = _array(row_ptr, "row_ptr", torch.int64, (rows + 1,))
-    shape = _Attention(N, rows, row_ptr, _array(log_decay, "log_decay", torch.float32, (Hq,)), Hq, Hk,
-                       K, V, K ** -0.5 if scale is None else scale)
-    return shape, hq, hk, hv
+        row_ptr = _array(row_ptr, "row_ptr", torch.int64, (rows + 1,), dev)
+    shape = _Attention(N, rows, row_ptr, _array(log_decay, "log_decay", torch.float32, (Hq,), dev), Hq,
+                       Hk, K, V, K ** -0.5 if scale is None else scale)
+    return dev, code, shape, hq, hk, hv
 
 
-def _state_ptr(t, name, shape):
-    return None if t is None else \
-        _array(t, name, torch.float32, (shape.n_rows, shape.q_heads, shape.k_width, shape.v_width))
+def _state_ptr(t, name, shape, dev):
+    return None if t is None else _array(
+        t, name, torch.float32, (shape.n_rows, shape.q_heads, shape.k_width, shape.v_width), dev)
+
+
+def _new_state(shape, device):
+    return torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width), device=device)
 
 
 def _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state):
-    shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
-    first = _state_ptr(initial_state, "initial_state", shape)
+    dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    first = _state_ptr(initial_state, "initial_state", shape, dev)
     out = torch.empty((q.shape[0], shape.q_heads, shape.v_width), dtype=q.dtype, device=q.device)
-    state = torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width),
-                        device=q.device) if return_state else None
+    state = _new_state(shape, q.device) if return_state else None
     size = lib.als_decay_attention_workspace(shape)
     work = _workspace(size, q.device)
-    _check(lib.als_decay_attention(shape, _DTYPES[q.dtype], hq, hk, hv, first, out.data_ptr(),
-                                   _ptr(state), _ptr(work), size, _stream()))
+    _check(lib.als_decay_attention(shape, code, hq, hk, hv, first, out.data_ptr(), _ptr(state),
+                                   _ptr(work), size, _stream(dev)))
     return out, state
 
 
@@ -279,20 +309,19 @@ def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, ini
     """Gradients (dq, dk, dv, d_initial_state) of ``decay_attention`` from that of its output and,
     if given, of its returned state (``dstate``). The last is None unless there is an
     ``initial_state`` or ``d_initial`` is true."""
-    shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
-    hdo = _heads(d_out, "d_out", q.dtype, (q.shape[0], shape.q_heads, shape.v_width))
-    first = _state_ptr(initial_state, "initial_state", shape)
-    last = _state_ptr(dstate, "dstate", shape)
+    dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    hdo = _heads(d_out, "d_out", q.dtype, dev)
+    _shaped(d_out, "d_out", (q.shape[0], shape.q_heads, shape.v_width))
+    first = _state_ptr(initial_state, "initial_state", shape, dev)
+    last = _state_ptr(dstate, "dstate", shape, dev)
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-    dfirst = None
-    if d_initial or (d_initial is None and initial_state is not None):
-        dfirst = torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width),
-                             device=q.device)
+    wanted = initial_state is not None if d_initial is None else d_initial
+    dfirst = _new_state(shape, q.device) if wanted else None
     size = lib.als_decay_attention_backward_workspace(shape)
     work = _workspace(size, q.device)
-    _check(lib.als_decay_attention_backward(shape, _DTYPES[q.dtype], hdo, hq, hk, hv, first, last,
-                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                            _ptr(dfirst), _ptr(work), size, _stream()))
+    _check(lib.als_decay_attention_backward(shape, code, hdo, hq, hk, hv, first, last, dq.data_ptr(),
+                                            dk.data_ptr(), dv.data_ptr(), _ptr(dfirst), _ptr(work),
+                                            size, _stream(dev)))
     return dq, dk, dv, dfirst
 
 
@@ -324,18 +353,22 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
     given. ``source``: int32 [rows], the row of ``state`` that each row goes on from (a beam's
     parent; one outside it gives NaN); ``state`` may then have another number of rows, and
     ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out)."""
-    shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
-    N, H, K, V = shape.n_rows, shape.q_heads, shape.k_width, shape.v_width
-    _on_device(state, "state")
-    sources = state.shape[0] if source is not None and state.dim() == 4 else N
-    sp = _array(state, "state", torch.float32, (sources, H, K, V))
-    src = None if source is None else _array(source, "source", torch.int32, (N,))
+    dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
+    _device(state, "state")
+    if state.dim() != 4:
+        raise ValueError("state must have the dimensions rows, heads, key width, value width")
+    N, one = shape.n_rows, (shape.q_heads, shape.k_width, shape.v_width)
+    sources, src = N, None
+    if source is not None:
+        sources = state.shape[0]
+        src = _array(source, "source", torch.int32, (N,), dev)
+    sp = _array(state, "state", torch.float32, (sources, *one), dev)
     if state_out is None:
-        state_out = state if source is None else torch.empty((N, H, K, V), device=q.device)
-    to = _array(state_out, "state_out", torch.float32, (N, H, K, V))
-    out = torch.empty((N, H, V), dtype=q.dtype, device=q.device)
-    _check(lib.als_decay_attention_step(shape, _DTYPES[q.dtype], hq, hk, hv, sp, sources, src, to,
-                                        out.data_ptr(), _stream()))
+        state_out = state if source is None else _new_state(shape, q.device)
+    to = _array(state_out, "state_out", torch.float32, (N, *one), dev)
+    out = torch.empty((N, one[0], one[2]), dtype=q.dtype, device=q.device)
+    _check(lib.als_decay_attention_step(shape, code, hq, hk, hv, sp, sources, src, to, out.data_ptr(),
+                                        _stream(dev)))
     return out, state_out
 
 
@@ -350,35 +383,37 @@ def beam_select(logits, scores, finished=None, end_token=-1, width=None):
     plus the log-softmax of its item; equal scores go by the lowest beam, then the lowest item.
     Returns (parents int32, tokens int32, scores fp32, finished bool), each [lists, width] by
     descending score; where candidates run out: 0, -1, -inf and False."""
-    _on_device(logits, "logits")
-    if logits.dtype not in _DTYPES:
-        raise TypeError(f"logits must be float32 or bfloat16, not {logits.dtype}")
+    dev = _device(logits, "logits")
+    code = _dtype(logits, "logits")
     if logits.dim() != 3:
         raise ValueError("logits must have the dimensions lists, beams, items")
     B, W, V = logits.shape
-    stride = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-    if (V > 1 and logits.stride(2) != 1) or (B > 1 and W > 1 and logits.stride(0) != W * stride):
+    apart, stride, unit = logits.stride()
+    if W == 1:
+        stride = apart if B > 1 else V
+    if (V > 1 and unit != 1) or (B > 1 and apart != W * stride):
         raise TypeError("logits must have contiguous items and evenly spaced rows")
-    sp = _array(scores, "scores", torch.float32, (B, W))
+    sp = _array(scores, "scores", torch.float32, (B, W), dev)
     fp = None
     if finished is not None:
         if isinstance(finished, torch.Tensor) and finished.dtype == torch.bool:
-            finished = finished.view(torch.uint8)
-        fp = _array(finished, "finished", torch.uint8, (B, W))
+            fp = _array(finished, "finished", torch.bool, (B, W), dev)
+        else:
+            fp = _array(finished, "finished", torch.uint8, (B, W), dev)
     width = W if width is None else int(width)
     shape = _Beams(B, V, stride, W, width, end_token)
     size = lib.als_beam_select_workspace(shape)
     if size < 0:
-        raise ALSError(1, lib.als_last_error(None).decode())
-    dev = logits.device
-    parents = torch.empty((B, width), dtype=torch.int32, device=dev)
-    tokens = torch.empty((B, width), dtype=torch.int32, device=dev)
-    new = torch.empty((B, width), device=dev)
-    done = torch.empty((B, width), dtype=torch.bool, device=dev)
-    work = _workspace(size, dev)
-    _check(lib.als_beam_select(shape, _DTYPES[logits.dtype], logits.data_ptr(), sp, fp,
-                               parents.data_ptr(), tokens.data_ptr(), new.data_ptr(),
-                               done.data_ptr(), _ptr(work), size, _stream()))
+        raise ALSError(ALS_ERR_INVALID_ARG, lib.als_last_error(None).decode())
+    device = logits.device
+    parents = torch.empty((B, width), dtype=torch.int32, device=device)
+    tokens = torch.empty((B, width), dtype=torch.int32, device=device)
+    new = torch.empty((B, width), device=device)
+    done = torch.empty((B, width), dtype=torch.bool, device=device)
+    work = _workspace(size, device)
+    _check(lib.als_beam_select(shape, code, logits.data_ptr(), sp, fp, parents.data_ptr(),
+                               tokens.data_ptr(), new.data_ptr(), done.data_ptr(), _ptr(work), size,
+                               _stream(dev)))
     return parents, tokens, new, done
 
 
@@ -386,21 +421,20 @@ def reorder_states(states, parents, out=None):
     """The beams' states in their new order: out[b, w] = states[b, parents[b, w]] for ``states``
     [lists, beams, ...] of any type, contiguous, and ``parents`` int32 [lists, width]. ``out`` (a new
     tensor if None) may be ``states`` itself where width equals beams."""
-    _on_device(states, "states")
+    dev = _device(states, "states")
     if states.dim() < 2 or not states.is_contiguous():
         raise TypeError("states must be contiguous with the dimensions lists, beams, ...")
-    _on_device(parents, "parents")
-    if parents.dim() != 2:
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2:
         raise ValueError("parents must have the dimensions lists, width")
-    B, W = states.shape[:2]
+    B, W, *rest = states.shape
     width = parents.shape[1]
-    pp = _array(parents, "parents", torch.int32, (B, width))
-    shape = (B, width) + tuple(states.shape[2:])
+    pp = _array(parents, "parents", torch.int32, (B, width), dev)
+    shape = (B, width, *rest)
     if out is None:
         out = torch.empty(shape, dtype=states.dtype, device=states.device)
     else:
-        _array(out, "out", states.dtype, shape)
-    size = states[:1, :1].numel() * states.element_size() if B and W else 0
+        _array(out, "out", states.dtype, shape, dev)
+    size = math.prod(rest) * states.element_size()
     _check(lib.als_reorder_states(B, W, width, size, states.data_ptr(), out.data_ptr(), pp,
-                                  _stream()))
+                                  _stream(dev)))
     return out
