@@ -10,7 +10,7 @@
 // maximum and its sum of exponentials, and writes the slice's best `width` items. Within a row
 // scores order as logits do, so those are all that can be chosen. k_merge takes one list's slices,
 // forms log-sum-exp and scores in fp64 from them (so that two candidates tie only where their
-// logits do) and picks the best `width`, one at a time, from the heads of the sorted slices.
+// logits do) and ranks those that reach the width-th best head of the sorted slices.
 #include <cfloat>
 
 #include "internal.h"
@@ -21,10 +21,12 @@ namespace als {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSlice = 8192;             // items a slice
-constexpr int kHeld = kSlice / kThreads; // of them in one thread's registers
-constexpr int kFound = 256;              // candidates that k_slices ranks at once
-constexpr int kMergeThreads = 256;
+constexpr int kSlice = 4096;             // items a slice
+constexpr int kHeld = kSlice / kThreads; // of them in one thread's registers, one bit of a mask each
+static_assert(kHeld <= 32, "a mask of 32 bits");
+constexpr int kFound = 256;              // candidates that are ranked at once
+constexpr int kMergeThreads = 1024;
+constexpr int kFirst = 4;                // heads that a thread of k_merge fetches at the start
 
 // fp32 as a whole number of the same order. Both zeros give the same one.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -39,8 +41,35 @@ __device__ __forceinline__ uint64_t key_of(float x, uint32_t item) {
   return (uint64_t)ordered(x) << 32 | (0xffffffffu - item);
 }
 
-__device__ __forceinline__ float usable(float x) {
-  return x > -INFINITY ? fminf(x, FLT_MAX) : -INFINITY;  // NaN compares false
+// -inf for NaN (of NaN and a number the maximum is the number), the largest finite value for +inf.
+__device__ __forceinline__ float usable(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); }
+
+// Maximum over the wave: within rows of 16 by lane exchanges of the vector unit, then over the rows.
+template <int CTRL> __device__ __forceinline__ float max_with(float x) {
+  const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false);
+  return fmaxf(x, __int_as_float(y));
+}
+__device__ __forceinline__ float row_lane(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = max_with<0xb1>(x);   // lanes 1 0 3 2
+  x = max_with<0x4e>(x);   // lanes 2 3 0 1
+  x = max_with<0x141>(x);  // mirrored in 8
+  x = max_with<0x140>(x);  // mirrored in 16
+  return fmaxf(fmaxf(row_lane(x, 0), row_lane(x, 16)), fmaxf(row_lane(x, 32), row_lane(x, 48)));
+}
+
+// A value that at least n of the wave's lanes reach, and (to 11 bits) the largest such one, bit by
+// bit: the lanes that reach a value are counted by one comparison.
+__device__ __forceinline__ uint32_t reached_by(uint32_t x, int n) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int b = 31; b >= 12; --b) {
+    const uint32_t next = bound | 1u << b;
+    bound = __popcll(__ballot(x >= next)) >= n ? next : bound;
+  }
+  return bound;
 }
 
 struct SliceStats {
@@ -55,7 +84,8 @@ __global__ __launch_bounds__(kThreads) void k_slices(const T *__restrict__ logit
                                                      SliceStats *__restrict__ stats,
                                                      uint64_t *__restrict__ best) {
   constexpr int E = 16 / sizeof(T);
-  __shared__ float part[kThreads / 64], total[kThreads / 64], bound[kThreads / 64];
+  __shared__ float part[kThreads / 64], total[kThreads / 64];
+  __shared__ uint32_t bound[kThreads / 64];
   __shared__ uint64_t found[kFound];
   __shared__ uint64_t top[kThreads / 64];
   __shared__ int n_found;
@@ -91,32 +121,22 @@ __global__ __launch_bounds__(kThreads) void k_slices(const T *__restrict__ logit
   float mine = -INFINITY;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) mine = fmaxf(mine, v[j]);
-  float m = mine;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  // the width-th largest of the lanes' maxima: at least `width` items of the wave reach it
-  float sorted = mine;
-#pragma unroll
-  for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-    for (int o = size / 2; o > 0; o >>= 1) {
-      const float other = __shfl_xor(sorted, o);
-      const bool larger = ((lane & o) == 0) == ((lane & size) == 0);  // descending at the end
-      sorted = larger ? fmaxf(sorted, other) : fminf(sorted, other);
-    }
-  const float reach = __shfl(sorted, width - 1);
+  // at least `width` items of the wave reach this: one in each of that many lanes
+  const uint32_t reach = reached_by(ordered(mine), width);
+  float m = wave_max(mine);
   if (lane == 0) {
     part[wave] = m;
     bound[wave] = reach;
   }
   __syncthreads();
   m = part[0];
-  float least = bound[0];
+  uint32_t most = bound[0];
 #pragma unroll
   for (int w = 1; w < kThreads / 64; ++w) {
     m = fmaxf(m, part[w]);
-    least = fmaxf(least, bound[w]);
+    most = bound[w] > most ? bound[w] : most;
   }
+  const float least = most <= ordered(-INFINITY) ? -INFINITY : from_ordered(most);
   float sum = 0.f;
   if (m > -INFINITY) {
 #pragma unroll
@@ -125,12 +145,17 @@ __global__ __launch_bounds__(kThreads) void k_slices(const T *__restrict__ logit
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) total[wave] = sum;
+  // few lanes hold any: the places as a mask, and the values read again
+  uint32_t hits = 0;
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (v[j] >= least && v[j] > -INFINITY) {
-      const int n = atomicAdd(&n_found, 1);
-      if (n < kFound) found[n] = key_of(v[j], item(j));
-    }
+  for (int j = 0; j < kHeld; ++j) hits |= v[j] >= least && v[j] > -INFINITY ? 1u << j : 0u;
+  while (hits) {
+    const int j = __ffs(hits) - 1;
+    hits &= hits - 1;
+    const uint32_t at = item(j);
+    const int n = atomicAdd(&n_found, 1);
+    if (n < kFound) found[n] = key_of(usable((float)x[at]), at);
+  }
   __syncthreads();
   uint64_t *out = best + (int64_t)blockIdx.x * width;
   const int n = n_found;
@@ -188,22 +213,32 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
     const uint64_t *__restrict__ best, int32_t *__restrict__ parents, int32_t *__restrict__ tokens,
     float *__restrict__ scores_out, uint8_t *__restrict__ finished_out) {
   __shared__ double base[kMaxBeams], top[kMaxBeams];
-  __shared__ Candidate wave_best[kMergeThreads / 64];
-  __shared__ Candidate chosen;
+  __shared__ int kind[kMaxBeams];  // 0 dead, 1 live, 2 finished
+  __shared__ Candidate found[kFound];
+  __shared__ uint32_t best_heads[kMergeThreads];
+  __shared__ int n_found;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t list = blockIdx.x;
   scores += list * beams;
   if (finished) finished += list * beams;
   stats += list * beams * slices;
   best += list * beams * slices * width;
+  const int lists = beams * slices;
+  // the first heads are on their way while log-sum-exp is formed
+  uint64_t first[kFirst];
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) {
+    const int l = tid + i * kMergeThreads;
+    first[i] = l < lists ? best[(int64_t)l * width] : 0;
+  }
   // score of an item: base + (x - top)
   for (int w = wave; w < beams; w += kMergeThreads / 64) {
     const float c = scores[w];
-    const bool live = c > -INFINITY && !(finished && finished[w]);
+    const bool done = finished && finished[w], live = c > -INFINITY && !done;
     float m = -INFINITY;
     if (live)
       for (int i = lane; i < slices; i += 64) m = fmaxf(m, stats[w * slices + i].max);
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    m = wave_max(m);
     double s = 0.0;
     if (m > -INFINITY)
       for (int i = lane; i < slices; i += 64) {
@@ -214,54 +249,108 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
     if (lane == 0) {
       top[w] = m;
       base[w] = (double)fminf(c, FLT_MAX) - (m > -INFINITY ? log(s) : 0.0);
+      kind[w] = live ? 1 : done && c > -INFINITY ? 2 : 0;
     }
   }
+  if (tid == 0) n_found = 0;
   __syncthreads();
-  // each thread keeps the best unused head of its (beam, slice) lists
-  const int lists = beams * slices;
+  // Every (beam, slice) list is sorted, so that `width` of the lists' heads reach a bound, and no
+  // candidate below it can be chosen: those that reach it are gathered and ranked at once.
+  const Candidate none = {-INFINITY, ~0ull};
+  const auto of_key = [&](int l, int j, uint64_t key) {  // candidate j of list l, whose key this is
+    const int w = l / slices;
+    if (kind[w] == 2)  // finished
+      return l == w * slices && j == 0 ? Candidate{base[w], (uint64_t)w << 32 | (uint32_t)end} : none;
+    if (kind[w] == 0 || !key) return none;
+    return Candidate{base[w] + ((double)from_ordered((uint32_t)(key >> 32)) - top[w]),
+                     (uint64_t)w << 32 | (0xffffffffu - (uint32_t)key)};
+  };
+  const auto head = [&](int l, int j) { return of_key(l, j, best[(int64_t)l * width + j]); };
+  const auto write = [&](int i, const Candidate &c) {
+    const bool any = c.place != ~0ull;
+    const int p = any ? (int)(c.place >> 32) : 0;
+    const int t = any ? (int)(uint32_t)c.place : -1;
+    const int64_t to = list * width + i;
+    parents[to] = p;
+    tokens[to] = t;
+    scores_out[to] = any ? (float)c.score : -INFINITY;
+    finished_out[to] = any && ((finished && finished[p]) || t == end);
+  };
+  float mine = -INFINITY;
+  float heads[kFirst];
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) {
+    const int l = tid + i * kMergeThreads;
+    heads[i] = l < lists ? (float)of_key(l, 0, first[i]).score : -INFINITY;
+    mine = fmaxf(mine, heads[i]);
+  }
+  for (int l = tid + kFirst * kMergeThreads; l < lists; l += kMergeThreads)
+    mine = fmaxf(mine, (float)head(l, 0).score);
+  best_heads[tid] = ordered(mine);
+  __syncthreads();
+  // the bound over 64 groups of threads, formed by every wave
+  uint32_t group = 0;
+#pragma unroll
+  for (int i = 0; i < kMergeThreads / 64; ++i) {
+    const uint32_t x = best_heads[i * 64 + lane];
+    group = x > group ? x : group;
+  }
+  const uint32_t most = reached_by(group, width);
+  const auto gather = [&](int l) {
+    constexpr int kAhead = 4;
+    for (int j = 0; j < width; j += kAhead) {
+      uint64_t keys[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) keys[i] = j + i < width ? best[(int64_t)l * width + j + i] : 0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const Candidate c = of_key(l, j + i, keys[i]);
+        if (c.place == ~0ull || ordered((float)c.score) < most) return;
+        const int n = atomicAdd(&n_found, 1);
+        if (n < kFound) found[n] = c;
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i)
+    if (heads[i] > -INFINITY && ordered(heads[i]) >= most) gather(tid + i * kMergeThreads);
+  for (int l = tid + kFirst * kMergeThreads; l < lists; l += kMergeThreads) gather(l);
+  __syncthreads();
+  const int n = n_found;
+  if (n <= kFound) {
+    for (int i = tid; i < n; i += kMergeThreads) {
+      const Candidate c = found[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += better(found[j], c);
+      if (rank < width) write(rank, c);
+    }
+    if (tid < width && tid >= n) write(tid, none);
+    return;
+  }
+  // many equal scores: one at a time
   Candidate last = {INFINITY, 0};
   for (int i = 0; i < width; ++i) {
-    Candidate mine = {-INFINITY, ~0ull};
-    for (int l = tid; l < lists; l += kMergeThreads) {
-      const int w = l / slices;
-      if (!(scores[w] > -INFINITY)) continue;
-      if (finished && finished[w]) {
-        const Candidate c = {base[w], (uint64_t)w << 32 | (uint32_t)end};
-        if (l == w * slices && (i == 0 || better(last, c)) && better(c, mine)) mine = c;
-        continue;
-      }
+    Candidate mine = none;
+    for (int l = tid; l < lists; l += kMergeThreads)
       for (int j = 0; j < width; ++j) {
-        const uint64_t key = best[(int64_t)l * width + j];
-        if (!key) break;
-        const Candidate c = {base[w] + ((double)from_ordered((uint32_t)(key >> 32)) - top[w]),
-                             (uint64_t)w << 32 | (0xffffffffu - (uint32_t)key)};
+        const Candidate c = head(l, j);
+        if (c.place == ~0ull) break;
         if (i == 0 || better(last, c)) {
           if (better(c, mine)) mine = c;
           break;
         }
       }
-    }
     for (int o = 32; o > 0; o >>= 1) {
       const Candidate c = {__shfl_xor(mine.score, o), __shfl_xor(mine.place, o)};
       if (better(c, mine)) mine = c;
     }
-    if (lane == 0) wave_best[wave] = mine;
+    if (lane == 0) found[wave] = mine;
     __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kMergeThreads / 64; ++w)
-        if (better(wave_best[w], mine)) mine = wave_best[w];
-      chosen = mine;
-      const bool any = mine.place != ~0ull;
-      const int p = any ? (int)(mine.place >> 32) : 0;
-      const int t = any ? (int)(uint32_t)mine.place : -1;
-      const int64_t to = list * width + i;
-      parents[to] = p;
-      tokens[to] = t;
-      scores_out[to] = any ? (float)mine.score : -INFINITY;
-      finished_out[to] = any && ((finished && finished[p]) || t == end);
-    }
+    last = found[0];
+    for (int w = 1; w < kMergeThreads / 64; ++w)
+      if (better(found[w], last)) last = found[w];
+    if (tid == 0) write(i, last);
     __syncthreads();
-    last = chosen;
   }
 }
 
