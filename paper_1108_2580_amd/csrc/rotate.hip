@@ -7,7 +7,7 @@
 //
 // Every byte is read and written once; the arithmetic is small, so memory bounds it. A group of G
 // lanes shares a row (one head of one token), and a lane holds whole pairs: VW values of each half
-// (or 2 VW neighbours), so that the rotation needs no exchange and the norm one sum over the group.
+// (or two runs of VW neighbours), so that the rotation needs no exchange and the norm one sum over the group.
 // Sums and products run in fp32, rounded once on the way out. The weights' gradient is summed per
 // lane over the rows that it meets, then per block, then over the blocks in fp64, always in one
 // order.
@@ -67,53 +67,63 @@ __device__ __forceinline__ void store(T *p, int left, const float *x) {
   }
 }
 
-// Where a lane's unit u lies in a row: two runs of VW values. A rotated unit holds VW pairs.
+// Where unit n of a lane lies in a row: two runs of VW values. A lane group's runs lie side by side, so
+// that each load and store of the group is one piece of memory. Turned pairs lie across the two runs
+// (halves, and neighbours one by one), or within each run (neighbours otherwise).
 struct Unit {
   int a, b;            // first features of the runs
   int left_a, left_b;  // values there, at most VW count
-  bool turned;
+  bool turned_a, turned_b;
 };
-template <int VW, bool NEXT> __device__ __forceinline__ Unit unit_of(int u, int width, int half) {
-  const int pairs = half / VW;
+template <int VW, bool NEXT, int G>
+__device__ __forceinline__ Unit unit_of(int lane, int n, int width, int half) {
   Unit x;
-  x.turned = u < pairs;
-  if (x.turned) {
-    x.a = NEXT ? u * 2 * VW : u * VW;
-    x.b = NEXT ? x.a + VW : half + u * VW;
+  if (NEXT && VW > 1) {
+    x.a = (2 * n * G + lane) * VW;
+    x.b = x.a + G * VW;
+    x.turned_a = x.a < 2 * half;
+    x.turned_b = x.b < 2 * half;
   } else {
-    x.a = 2 * half + (u - pairs) * 2 * VW;
-    x.b = x.a + VW;
+    const int u = n * G + lane, pairs = half / VW;
+    x.turned_a = x.turned_b = u < pairs;
+    if (u < pairs) {
+      x.a = NEXT ? 2 * u : u * VW;
+      x.b = NEXT ? 2 * u + 1 : half + u * VW;
+    } else {
+      x.a = 2 * half + (u - pairs) * 2 * VW;
+      x.b = x.a + VW;
+    }
   }
   x.left_a = width - x.a;
   x.left_b = width - x.b;
   return x;
 }
-
-// A rotated unit's runs as (a, b) of its pairs, and back. Neighbours lie as a0 b0 a1 b1 ...
-template <int VW> __device__ __forceinline__ void apart(float *x, float *y) {
-  float a[VW], b[VW];
-#pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    a[e] = 2 * e < VW ? x[2 * e] : y[2 * e - VW];
-    b[e] = 2 * e + 1 < VW ? x[2 * e + 1] : y[2 * e + 1 - VW];
-  }
-#pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    x[e] = a[e];
-    y[e] = b[e];
-  }
+// Units in a row, for halves and for neighbours.
+template <int VW, bool NEXT> __host__ __device__ inline int units_in(int width, int half) {
+  return NEXT && VW > 1 ? (width + 2 * VW - 1) / (2 * VW)
+                        : half / VW + (width - 2 * half + 2 * VW - 1) / (2 * VW);
 }
-template <int VW> __device__ __forceinline__ void together(float *a, float *b) {
-  float x[2 * VW];
+
+// Turns a unit's pairs by the angles of cs and sn, or back with SIGN -1.
+template <int VW, bool NEXT, int SIGN>
+__device__ __forceinline__ void turn(const Unit &u, float *a, float *b, const float *cs, const float *sn) {
+  const auto pair = [&](float &x, float &y, int p) {
+    const float c = cs[p], s = SIGN * sn[p], was = x;
+    x = was * c - y * s;
+    y = y * c + was * s;
+  };
+  if constexpr (NEXT && VW > 1) {
+    if (u.turned_a) {
 #pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    x[2 * e] = a[e];
-    x[2 * e + 1] = b[e];
-  }
+      for (int e = 0; e < VW; e += 2) pair(a[e], a[e + 1], (u.a + e) / 2);
+    }
+    if (u.turned_b) {
 #pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    a[e] = x[e];
-    b[e] = x[VW + e];
+      for (int e = 0; e < VW; e += 2) pair(b[e], b[e + 1], (u.b + e) / 2);
+    }
+  } else if (u.turned_a) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) pair(a[e], b[e], (NEXT ? u.a / 2 : u.a) + e);
   }
 }
 
@@ -131,22 +141,22 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
   const int64_t t0 = (int64_t)blockIdx.x * R.tokens_per_block;
   const int64_t t1 = t0 + R.tokens_per_block < R.n_tokens ? t0 + R.tokens_per_block : R.n_tokens;
   const int rows = (int)(t1 > t0 ? t1 - t0 : 0) * S.heads;
-  const int units = R.half / VW + (R.width - 2 * R.half + 2 * VW - 1) / (2 * VW);
   float wa[UN][VW], wb[UN][VW], ga[UN][VW], gb[UN][VW];
 #pragma unroll
   for (int n = 0; n < UN; ++n) {
-    const Unit u = unit_of<VW, NEXT>(lane + n * G, R.width, R.half);
-    const bool on = lane + n * G < units;
+    const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
 #pragma unroll
     for (int e = 0; e < VW; ++e) {
-      wa[n][e] = on && e < u.left_a ? S.weight[u.a + e] : 0.f;
-      wb[n][e] = on && e < u.left_b ? S.weight[u.b + e] : 0.f;
+      wa[n][e] = e < u.left_a ? S.weight[u.a + e] : 0.f;
+      wb[n][e] = e < u.left_b ? S.weight[u.b + e] : 0.f;
       ga[n][e] = gb[n][e] = 0.f;
     }
   }
-  for (int row = tid / G; row < rows; row += kBlock / G) {
-    const int64_t token = t0 + row / S.heads;
-    const int head = row % S.heads;
+  constexpr int kStep = kBlock / G;
+  const int token_step = kStep / S.heads, head_step = kStep % S.heads;
+  int head = tid / G % S.heads;
+  int64_t token = t0 + tid / G / S.heads;
+  for (int row = tid / G; row < rows; row += kStep) {
     const T *x = (const T *)S.x.data + token * S.x.token_stride + head * S.x.head_stride;
     T *out = (T *)S.out.data + token * S.out.token_stride + head * S.out.head_stride;
     const T *dy = BACK ? (const T *)S.dy.data + token * S.dy.token_stride + head * S.dy.head_stride
@@ -158,13 +168,12 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     float squares = 0.f, along = 0.f;
 #pragma unroll
     for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT>(lane + n * G, R.width, R.half);
-      const bool on = lane + n * G < units;
-      load<T, VW>(x + u.a, on ? u.left_a : 0, xa[n]);
-      load<T, VW>(x + u.b, on ? u.left_b : 0, xb[n]);
+      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
+      load<T, VW>(x + u.a, u.left_a, xa[n]);
+      load<T, VW>(x + u.b, u.left_b, xb[n]);
       if (BACK) {
-        load<T, VW>(dy + u.a, on ? u.left_a : 0, da[n]);
-        load<T, VW>(dy + u.b, on ? u.left_b : 0, db[n]);
+        load<T, VW>(dy + u.a, u.left_a, da[n]);
+        load<T, VW>(dy + u.b, u.left_b, db[n]);
       }
 #pragma unroll
       for (int e = 0; e < VW; ++e) squares = fmaf(xa[n][e], xa[n][e], fmaf(xb[n][e], xb[n][e], squares));
@@ -174,8 +183,7 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     const float r = ok ? 1.f / sqrtf(squares / (float)R.width + R.eps) : __builtin_nanf("");
 #pragma unroll
     for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT>(lane + n * G, R.width, R.half);
-      if (lane + n * G >= units) continue;
+      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
       float *a = BACK ? da[n] : xa[n], *b = BACK ? db[n] : xb[n];
       if (!BACK) {
 #pragma unroll
@@ -184,17 +192,7 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
           b[e] *= r * wb[n][e];
         }
       }
-      if (u.turned) {
-        if (NEXT) apart<VW>(a, b);
-        const int p = (lane + n * G) * VW;
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float c = cs[p + e], s = BACK ? -sn[p + e] : sn[p + e], was = a[e];
-          a[e] = was * c - b[e] * s;
-          b[e] = b[e] * c + was * s;
-        }
-        if (NEXT) together<VW>(a, b);
-      }
+      turn<VW, NEXT, BACK ? -1 : 1>(u, a, b, cs, sn);
       if (BACK) {
 #pragma unroll
         for (int e = 0; e < VW; ++e) {
@@ -219,10 +217,15 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     }
 #pragma unroll
     for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT>(lane + n * G, R.width, R.half);
-      if (lane + n * G >= units) continue;
+      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
       store<T, VW>(out + u.a, u.left_a, xa[n]);
       store<T, VW>(out + u.b, u.left_b, xb[n]);
+    }
+    token += token_step;
+    head += head_step;
+    if (head >= S.heads) {
+      head -= S.heads;
+      ++token;
     }
   }
   if (BACK) {
@@ -235,8 +238,8 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
         sums[tid / G][((lane + n * G) * 2 + 1) * VW + e] = gb[n][e];
       }
     __syncthreads();
-    for (int i = tid; i < units * 2 * VW; i += kBlock) {
-      const Unit u = unit_of<VW, NEXT>(i / (2 * VW), R.width, R.half);
+    for (int i = tid; i < G * UN * 2 * VW; i += kBlock) {
+      const Unit u = unit_of<VW, NEXT, G>(i / (2 * VW) % G, i / (2 * VW) / G, R.width, R.half);
       const int run = i / VW % 2, d = (run ? u.b : u.a) + i % VW;
       if (d >= R.width) continue;
       float sum = 0.f;
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(256) void k_sum_partials(Rotate R, int blocks) {
 
 template <typename T, int VW, bool NEXT, bool BACK>
 hipError_t launch_vw(const Rotate &R, int blocks, hipStream_t s) {
-  const int units = R.half / VW + (R.width - 2 * R.half + 2 * VW - 1) / (2 * VW);
+  const int units = units_in<VW, NEXT>(R.width, R.half);
   const dim3 grid((unsigned)blocks, 2);
 #define ROTATE(G, UN) \
   hipLaunchKernelGGL((k_rotate<T, VW, NEXT, G, UN, BACK>), grid, dim3(kBlock), 0, s, R)
@@ -282,8 +285,8 @@ hipError_t launch_vw(const Rotate &R, int blocks, hipStream_t s) {
 // Values per load: the widest (16 bytes, two values, one) that every run's alignment allows.
 int run_width(const Rotate &R, bool next, bool back, int size) {
   for (int vw : {16 / size, 2, 1}) {
-    // halves: the second half starts at `half`; the rest starts at 2 half
-    bool fits = R.half % vw == 0 && (2 * R.half) % vw == 0;
+    // halves: the second starts at `half`; neighbours: a run is turned as a whole or not at all
+    bool fits = (next ? 2 * R.half : R.half) % vw == 0;
     for (const Side &S : R.side)
       for (const als_heads *x : {&S.x, &S.out, back ? &S.dy : &S.x})
         fits = fits && ((uintptr_t)x->data % (vw * size) == 0) && x->token_stride % vw == 0 &&
@@ -305,7 +308,7 @@ hipError_t launch_next(const Rotate &R, int blocks, hipStream_t s) {
 
 int64_t rotate_blocks(int64_t n_tokens) {
   const int64_t n = (n_tokens + 7) / 8;
-  return n < 2048 ? (n > 0 ? n : 1) : 2048;
+  return n < 8192 ? (n > 0 ? n : 1) : 8192;
 }
 
 hipError_t launch_rotate(als_dtype dtype, bool back, const als_rotation &shape, const als_heads *x,
