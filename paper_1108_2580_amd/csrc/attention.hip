@@ -21,10 +21,10 @@
 // A reversed pass reads its state one step nearer and adds to it one step further
 // (read e^{a i}, add e^{a (C - j)}).
 //
-// Rounding. Products run in the inputs' type with sums in fp32. bf16: the weights and the state are
-// rounded once more where they enter a product, which is as much again as the output's own rounding.
-// What a token adds to the state is split into three bf16 parts (24 bits), so that the state, an
-// output in fp32, has no bf16 rounding in it.
+// Rounding. Products have sums in fp32. bf16 inputs: the weights and the state are rounded once more
+// where they enter a product, which is as much again as the output's own rounding; what a token adds
+// to the state is split into three bf16 parts (24 bits), so that the state, an output in fp32, has no
+// bf16 rounding in it. fp32 inputs: all operands are split so.
 #include "internal.h"
 #include "sequence.h"
 
@@ -44,77 +44,141 @@ constexpr float kMinLogDecay = -1e4f;
 // Two result tiles of an MFMA hold their rows 4 g .. 4 g + 3 in a lane, which is the second order, so
 // that weights are operands of the next product as they are. The state's tiles take the columns of k
 // in such an order (frag_col's STEP 8) that a pair of them is an operand of the first order.
-template <typename T> struct Frag;
-template <> struct Frag<float> {
-  f32x4 lo, hi;
-  __device__ __forceinline__ float get(int e) const { return e < 4 ? lo[e] : hi[e - 4]; }
-  __device__ __forceinline__ void set(int e, float v) {
-    if (e < 4) lo[e] = v; else hi[e - 4] = v;
-  }
-};
-template <> struct Frag<bf16> {
-  bf16x8 x;
-  __device__ __forceinline__ bf16 get(int e) const { return x[e]; }
-  __device__ __forceinline__ void set(int e, bf16 v) { x[e] = v; }
-};
+//
+// bf16 values are held as they are. fp32 values are held in three bf16 parts, whose sum they are, and
+// a product is the sum of six products of parts, which leaves out 2^-24 of it: six MFMAs of 16 cycles
+// where the fp32 MFMAs of the same tile take 256.
+template <typename T> constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+template <int NP> struct Frag { bf16x8 p[NP]; };
 
 template <typename T> struct Vec4;
 template <> struct Vec4<float> { using type = f32x4; };
 template <> struct Vec4<bf16> { using type = bf16x4; };
 
-__device__ __forceinline__ Frag<float> joined(f32x4 lo, f32x4 hi) { return {lo, hi}; }
-__device__ __forceinline__ Frag<bf16> joined(bf16x4 lo, bf16x4 hi) {
-  return {__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)};
+__device__ __forceinline__ bf16x8 joined(bf16x4 lo, bf16x4 hi) {
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-__device__ __forceinline__ f32x4 mma(const Frag<bf16> &a, const Frag<bf16> &b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x, b.x, c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma(const Frag<float> &a, const Frag<float> &b, f32x4 c) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.lo[e], b.lo[e], c, 0, 0, 0);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.hi[e], b.hi[e], c, 0, 0, 0);
-  return c;
+__device__ __forceinline__ f32x4 mma(const Frag<1> &a, const Frag<1> &b, f32x4 c) {
+  return mma(a.p[0], b.p[0], c);
+}
+__device__ __forceinline__ f32x4 mma(const Frag<3> &a, const Frag<3> &b, f32x4 c) {
+  c = mma(a.p[0], b.p[2], c);
+  c = mma(a.p[2], b.p[0], c);
+  c = mma(a.p[1], b.p[1], c);
+  c = mma(a.p[0], b.p[1], c);
+  c = mma(a.p[1], b.p[0], c);
+  return mma(a.p[0], b.p[0], c);
 }
 
-// Row m of a 16-row tile at x (row length ld), contraction along the row from column 0.
-__device__ __forceinline__ Frag<float> frag_row(const float *x, int ld, int lane) {
-  const float *p = x + (lane & 15) * ld + (lane >> 4) * 8;
-  return {*(const f32x4 *)p, *(const f32x4 *)(p + 4)};
-}
-__device__ __forceinline__ Frag<bf16> frag_row(const bf16 *x, int ld, int lane) {
-  return {*(const bf16x8 *)(x + (lane & 15) * ld + (lane >> 4) * 8)};
-}
-// Column STEP * (m / 4) + m % 4 from x, contraction down 32 rows.
-template <int STEP>
-__device__ __forceinline__ Frag<float> frag_col(const float *x, int ld, int lane) {
-  const int m = lane & 15;
-  const float *p = x + (lane >> 4) * 4 * ld + m / 4 * STEP + m % 4;
-  Frag<float> f;
+// Row m of a 16-row tile at x (row length ld, parts `part` apart), contraction along the row from
+// column 0.
+template <int NP>
+__device__ __forceinline__ Frag<NP> frag_row(const bf16 *x, int ld, int part, int lane) {
+  const bf16 *p = x + (lane & 15) * ld + (lane >> 4) * 8;
+  Frag<NP> f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f.lo[e] = p[e * ld];
-    f.hi[e] = p[(16 + e) * ld];
-  }
+  for (int n = 0; n < NP; ++n) f.p[n] = *(const bf16x8 *)(p + n * part);
   return f;
 }
-// The transposing LDS read: 16 lanes name the 16 8-byte pieces of a 4 x 16 block, and lane i of
-// them gets column i.
-template <int STEP>
-__device__ __forceinline__ Frag<bf16> frag_col(const bf16 *x, int ld, int lane) {
+// Column STEP * (m / 4) + m % 4 from x, contraction down 32 rows. The transposing LDS read: 16 lanes
+// name the 16 8-byte pieces of a 4 x 16 block, and lane i of them gets column i.
+template <int NP, int STEP>
+__device__ __forceinline__ Frag<NP> frag_col(const bf16 *x, int ld, int part, int lane) {
   using L = __attribute__((address_space(3))) bf16x4 *;
   const bf16 *p = x + (lane >> 2) * ld + (lane & 3) * STEP;
-  return joined(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)p),
-                __builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)(p + 16 * ld)));
+  Frag<NP> f;
+#pragma unroll
+  for (int n = 0; n < NP; ++n)
+    f.p[n] = joined(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)(p + n * part)),
+                    __builtin_amdgcn_ds_read_tr16_b64_v4bf16((L)(p + n * part + 16 * ld)));
+  return f;
 }
+
+// Four values in three bf16 parts: each is the leading 8 bits of what is left (cut off, so that it is
+// exact), and 3 * 8 bits are all that fp32 has.
+__device__ __forceinline__ void split3(f32x4 x, bf16x4 *part) {
+  using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int n = 0; n < 3; ++n) {
+    const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]), c = __float_as_uint(x[2]),
+                   d = __float_as_uint(x[3]);
+    // the upper halves of b and a, and of d and c
+    const u32x2 out = {__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
+    part[n] = __builtin_bit_cast(bf16x4, out);
+    if (n < 2) {
+      x[0] -= __uint_as_float(a & 0xffff0000u);
+      x[1] -= __uint_as_float(b & 0xffff0000u);
+      x[2] -= __uint_as_float(c & 0xffff0000u);
+      x[3] -= __uint_as_float(d & 0xffff0000u);
+    }
+  }
+}
+// As an operand: rounded, or in three parts.
+template <int NP> __device__ __forceinline__ void as_parts(f32x4 x, bf16x4 *part) {
+  if constexpr (NP == 1)
+    part[0] = __builtin_convertvector(x, bf16x4);
+  else
+    split3(x, part);
+}
+template <int NP> __device__ __forceinline__ Frag<NP> as_frag(f32x4 lo, f32x4 hi) {
+  bf16x4 a[NP], b[NP];
+  as_parts<NP>(lo, a);
+  as_parts<NP>(hi, b);
+  Frag<NP> f;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) f.p[n] = joined(a[n], b[n]);
+  return f;
+}
+
+// A lane's 8 values down 32 rows of column m from x, as they lie in LDS.
+template <typename T> struct Column;
+template <> struct Column<bf16> {
+  Frag<1> f;
+  __device__ __forceinline__ void read(const bf16 *x, int ld, int lane) {
+    f = frag_col<1, 4>(x, ld, 0, lane);
+  }
+  __device__ __forceinline__ float get(int e) const { return (float)f.p[0][e]; }
+  __device__ __forceinline__ void clear(int e) { f.p[0][e] = (bf16)0.f; }
+  __device__ __forceinline__ Frag<1> frag() const { return f; }
+  __device__ __forceinline__ bool finite() const {
+    using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+    const u32x4 bits = __builtin_bit_cast(u32x4, f.p[0]);
+    uint32_t carry = 0;  // into either half's sign: its exponent was all ones
+#pragma unroll
+    for (int e = 0; e < 4; ++e) carry |= (bits[e] & 0x7fff7fffu) + 0x00800080u;
+    return (carry & 0x80008000u) == 0;
+  }
+};
+template <> struct Column<float> {
+  f32x4 lo, hi;
+  __device__ __forceinline__ void read(const float *x, int ld, int lane) {
+    const float *p = x + (lane >> 4) * 4 * ld + (lane & 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      lo[e] = p[e * ld];
+      hi[e] = p[(16 + e) * ld];
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return e < 4 ? lo[e] : hi[e - 4]; }
+  __device__ __forceinline__ void clear(int e) {
+    if (e < 4) lo[e] = 0.f; else hi[e - 4] = 0.f;
+  }
+  __device__ __forceinline__ Frag<3> frag() const { return as_frag<3>(lo, hi); }
+  __device__ __forceinline__ bool finite() const {
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = fmaf(lo[e], 0.f, fmaf(hi[e], 0.f, x));
+    return x == 0.f;
+  }
+};
+
 // Row of the state that element e of lane group g holds in tile kt.
 __device__ __forceinline__ constexpr int state_row(int kt, int g, int e) {
   return kt / 2 * 32 + g * 8 + kt % 2 * 4 + e;
-}
-
-template <typename T> __device__ __forceinline__ typename Vec4<T>::type rounded(f32x4 x) {
-  return __builtin_convertvector(x, typename Vec4<T>::type);
 }
 
 // Padding of a staged row: with it the four lane groups and the rows of one LDS read fall on
@@ -189,27 +253,26 @@ __global__ __launch_bounds__(256) void k_places(const int64_t *__restrict__ row_
     entries[e] = e >= e0 && e - e0 + 1 < n ? (int32_t)(s0 + e - e0) : -1;
 }
 
+// Passes of one launch, whose blocks alternate: those that read the same tensors run side by side.
 struct Args {
-  AttentionPass p;
+  AttentionPass p[3];
+  int n;
   int shift;        // log2 of the tokens a segment
   int64_t slot0;    // first slot (or entry) of this launch
   int64_t n_slots;
   const Place *places;     // nullable: searched for
   const int32_t *entries;
-  bool vec_in;      // q, k and v are read 16 bytes at a time
-  bool vec_out;     // out is written 4 values at a time
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A chunk's tokens of one head of x on their way to LDS, in rows of padded(WP) elements, zero past
-// `size` tokens and past `width`. They are fetched into registers while the chunk before is worked
+// A chunk's tokens of one head of x on their way to LDS, zero past `size` tokens and past `width`. They are fetched into registers while the chunk before is worked
 // on: 16 bytes at a time, or value by value where a width or an alignment does not allow that.
 // Place r of the chunk is row r ^ flip from `base`, the chunk's lowest token: flip is C - 1 in a pass
 // from the last token to the first, and 0 otherwise. Offsets from there are below 2^31
 // (kMaxTokenStride).
 template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
-  static constexpr int LD = padded<T>(WP), E = 16 / sizeof(T), ROW = WP / E;
+  static constexpr int E = 16 / sizeof(T), ROW = WP / E;
   static constexpr int ROWS = THREADS / ROW, N = (C + ROWS - 1) / ROWS;
   static_assert(THREADS % ROW == 0 && (ROWS >= C || C % ROWS == 0), "whole rows a pass");
   struct alignas(16) Piece { T v[E]; };
@@ -233,54 +296,35 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
       }
     }
   }
-  __device__ __forceinline__ void put(T *lds, int tid) const {
+  __device__ __forceinline__ void put(T *lds, int ld, int tid) const {
     const int r0 = tid / ROW, c = tid % ROW * E;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (ROWS <= C || r0 < C) *(Piece *)(lds + (r0 + i * ROWS) * LD + c) = held[i];
+      if (ROWS <= C || r0 < C) *(Piece *)(lds + (r0 + i * ROWS) * ld + c) = held[i];
+  }
+  // as operands of products: fp32 in parts
+  __device__ __forceinline__ void put_parts(bf16 *lds, int ld, int tid) const {
+    if constexpr (sizeof(T) == 2) {
+      put(lds, ld, tid);
+    } else {
+      const int r0 = tid / ROW, c = tid % ROW * E;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (ROWS <= C || r0 < C) {
+          bf16x4 part[3];
+          split3(f32x4{held[i].v[0], held[i].v[1], held[i].v[2], held[i].v[3]}, part);
+#pragma unroll
+          for (int n = 0; n < 3; ++n)
+            *(bf16x4 *)(lds + n * C * ld + (r0 + i * ROWS) * ld + c) = part[n];
+        }
+    }
   }
 };
 
-// Eight values in three bf16 parts whose sum they are: each part is the leading 8 bits of what is
-// left (cut off, so that it is exact), and 3 * 8 bits are all that fp32 has.
-__device__ __forceinline__ void split3(const f32x4 lo, const f32x4 hi, Frag<bf16> *part) {
-  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
-  u32x4 out[3];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float x = e < 2 ? lo[2 * e] : hi[2 * e - 4], y = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
-#pragma unroll
-    for (int n = 0; n < 3; ++n) {
-      const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-      out[n][e] = __builtin_amdgcn_perm(b, a, 0x07060302);  // the upper halves of b and a
-      x -= __uint_as_float(a & 0xffff0000u);
-      y -= __uint_as_float(b & 0xffff0000u);
-    }
-  }
-#pragma unroll
-  for (int n = 0; n < 3; ++n) part[n].x = __builtin_bit_cast(bf16x8, out[n]);
-}
-
-// Whether a lane's values are all finite.
-__device__ __forceinline__ bool finite(const Frag<float> &f) {
-  float x = 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x = fmaf(f.lo[e], 0.f, fmaf(f.hi[e], 0.f, x));
-  return x == 0.f;
-}
-__device__ __forceinline__ bool finite(const Frag<bf16> &f) {
-  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
-  const u32x4 bits = __builtin_bit_cast(u32x4, f.x);
-  uint32_t carry = 0;  // into either half's sign: its exponent was all ones
-#pragma unroll
-  for (int e = 0; e < 4; ++e) carry |= (bits[e] & 0x7fff7fffu) + 0x00800080u;
-  return (carry & 0x80008000u) == 0;
-}
-
-// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, two where
-// few threads hold them, or hold them value by value.
+// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, three where
+// LDS holds no more, two where few threads hold the pieces, or hold them value by value.
 template <typename T> constexpr int waves_for(int VP, bool vec) {
-  return VP == 32 || (!vec && sizeof(T) == 2) ? 2 : 4;
+  return VP == 32 || (!vec && sizeof(T) == 2) ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
 }
 
 // One block: one head of one segment. STATES: only the state after the segment, for all segments of
@@ -288,21 +332,22 @@ template <typename T> constexpr int waves_for(int VP, bool vec) {
 template <typename T, int KP, int VP, bool STATES, bool VEC>
 __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
-  constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<T>(KP), LV = padded<T>(VP);
-  constexpr int PT = NT * (NT + 1) / 2;
+  constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<bf16>(KP), LV = padded<T>(VP);
+  constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, KPART = C * LK;
   using V4 = typename Vec4<T>::type;
   using TK = Tile<T, C, KP, THREADS, VEC>;
   using TV = Tile<T, C, VP, THREADS, VEC>;
-  __shared__ __align__(16) T lq[STATES ? 1 : C * LK];
-  __shared__ __align__(16) T lk[C * LK];
+  __shared__ __align__(16) bf16 lq[STATES ? 1 : NP * KPART];
+  __shared__ __align__(16) bf16 lk[NP * KPART];
   __shared__ __align__(16) T lv[C * LV];
-  __shared__ __align__(16) T lp[STATES ? 1 : PT * 256];
+  __shared__ __align__(16) bf16 lp[STATES ? 1 : PT * NP * 256];  // by tile, part, lane
 
-  const AttentionPass &P = A.p;
+  const AttentionPass &P = A.p[blockIdx.x % (unsigned)A.n];
+  const unsigned block = blockIdx.x / (unsigned)A.n;
   const int lane0 = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   const int lane = lane0, g = lane >> 4, m = lane & 15;
-  int64_t slot = A.slot0 + blockIdx.x / P.heads;
-  const int head = (int)(blockIdx.x % P.heads);
+  int64_t slot = A.slot0 + block / P.heads;
+  const int head = (int)(block % P.heads);
   Place at;
   if (STATES) {
     if (A.places) {
@@ -356,21 +401,27 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
   f32x4 S[KT];
   const int64_t state = ((int64_t)at.row * P.heads + head) * (int64_t)P.k_width * P.v_width;
   const int col = wave * 16 + m;
-  float *slot_state = P.segments + ((slot * P.heads + head) * (int64_t)(KT * NW) + wave * KT) * 256 +
-                      lane * 4;
+  // a segment's: row r, column c at r * segment_ld[0] + c * segment_ld[1]
+  float *slot_state = P.segments + (slot * P.heads + head) * (int64_t)(KP * VP);
+  const auto in_slot = [&](int kt, int e) {
+    return (unsigned)(state_row(kt, g, e) * P.segment_ld[0] + col * P.segment_ld[1]);
+  };
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) S[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (at.segment > 0 && !STATES) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) S[kt] = *(const f32x4 *)(slot_state + kt * 256);
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[kt][e] = slot_state[in_slot(kt, e)];
   } else if (at.segment == 0 && P.first_state) {
+    const float *from = P.first_state + state;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int r = state_row(kt, g, e);
         if (r < P.k_width && col < P.v_width)
-          S[kt][e] = P.first_state[state + r * P.first_ld[0] + col * P.first_ld[1]];
+          S[kt][e] = from[(unsigned)(r * P.first_ld[0] + col * P.first_ld[1])];
       }
   }
 
@@ -383,6 +434,30 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
     diag[e] = P.weight_scale * exp2_fast(a2 * (float)(m >= g * 4 + e ? m - g * 4 - e : 0));
   }
 
+  // of the tokens 16 n + 4 g + e of a chunk of `size` in the state's update. A full chunk's are held,
+  // where the state leaves the registers for it.
+  constexpr bool HELD = KP < 128 && NP == 1;
+  const auto for_update = [&](int n, int size, int g) {
+    f32x4 w;
+    if (size == C) {
+      const float far = P.update_scale * exp2_fast(a2 * (float)(C - 4 - n * 16 - g * 4 + add_off));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = far * near[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int left = size - 1 - n * 16 - g * 4 - e;  // below 0: no token, v is zero
+        w[e] = P.update_scale * exp2_fast(a2 * (float)((left > 0 ? left : 0) + add_off));
+      }
+    }
+    return w;
+  };
+  f32x4 add[HELD ? 2 * SF : 1];
+  if constexpr (HELD) {
+#pragma unroll
+    for (int n = 0; n < 2 * SF; ++n) add[n] = for_update(n, C, g);
+  }
+
   for (int c = 0; c < count; c += C) {
     const int size = count - c < C ? count - c : C;
     const int64_t low = token0 + (P.reverse ? -c : c);
@@ -392,9 +467,9 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
     asm volatile("" : "+v"(lane), "+v"(tid));
     const int g = lane >> 4, m = lane & 15;
     __syncthreads();
-    if (!STATES) hq.put(lq, tid);
-    hk.put(lk, tid);
-    hv.put(lv, tid);
+    if (!STATES) hq.put_parts(lq, LK, tid);
+    hk.put_parts(lk, LK, tid);
+    hv.put(lv, LV, tid);
     __syncthreads();
     if (c + C < count) fetch(c + C, tid);
 
@@ -402,65 +477,96 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
       // weights of places i (columns) and j (rows) <= i, one 16 x 16 tile at a time
 #pragma unroll 1
       for (int tile = wave; tile < PT; tile += NW) {
-        {
-          const int i = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, j = tile - i * (i + 1) / 2;
-          f32x4 w = {0.f, 0.f, 0.f, 0.f};
+        const int i = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, j = tile - i * (i + 1) / 2;
+        f32x4 w = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int d = 0; d < KF; ++d)
-            w = mma(frag_row(lk + j * 16 * LK + d * 32, LK, lane),
-                    frag_row(lq + i * 16 * LK + d * 32, LK, lane), w);
-          if (i == j) {
+        for (int d = 0; d < KF; ++d)
+          w = mma(frag_row<NP>(lk + j * 16 * LK + d * 32, LK, KPART, lane),
+                  frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane), w);
+        if (i == j) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = m >= g * 4 + e ? w[e] * diag[e] : 0.f;
-          } else {
-            const float far = P.weight_scale * exp2_fast(a2 * (float)(16 * (i - j) + m - g * 4 - 3));
+          for (int e = 0; e < 4; ++e) w[e] = m >= g * 4 + e ? w[e] * diag[e] : 0.f;
+        } else {
+          const float far = P.weight_scale * exp2_fast(a2 * (float)(16 * (i - j) + m - g * 4 - 3));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] *= far * near[e];
-          }
-          *(V4 *)(lp + tile * 256 + lane * 4) = rounded<T>(w);
+          for (int e = 0; e < 4; ++e) w[e] *= far * near[e];
         }
-      }
-    }
-    if (!STATES) __syncthreads();
-    Frag<T> vf[SF];  // column `col` of v
+        bf16x4 part[NP];
+        as_parts<NP>(w, part);
 #pragma unroll
-    for (int s = 0; s < SF; ++s) vf[s] = frag_col<4>(lv + s * 32 * LV + wave * 16, LV, lane);
+        for (int n = 0; n < NP; ++n) *(bf16x4 *)(lp + (tile * NP + n) * 256 + lane * 4) = part[n];
+      }
+      __syncthreads();
+    }
+    Column<T> vc[SF];  // column `col` of v
+#pragma unroll
+    for (int s = 0; s < SF; ++s) vc[s].read(lv + s * 32 * LV + wave * 16, LV, lane);
     if (!STATES) {
       // 0 * inf and 0 * NaN are NaN: values of v that are neither enter the products as zeros, and
       // are added to their own and later places alone
       bool mine = true;
 #pragma unroll
-      for (int s = 0; s < SF; ++s) mine = mine && finite(vf[s]);
+      for (int s = 0; s < SF; ++s) mine = mine && vc[s].finite();
       const bool all_finite = !__any(!mine);
       if (!all_finite) {
 #pragma unroll
         for (int s = 0; s < SF; ++s)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if ((float)vf[s].get(e) * 0.f != 0.f) vf[s].set(e, (T)0.f);
+            if (vc[s].get(e) * 0.f != 0.f) vc[s].clear(e);
       }
-      Frag<T> sf[KF];
-#pragma unroll
-      for (int d = 0; d < KF; ++d) sf[d] = joined(rounded<T>(S[2 * d]), rounded<T>(S[2 * d + 1]));
-      const V4 zero = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+      const bf16x4 zero = {(bf16)0.f, (bf16)0.f, (bf16)0.f, (bf16)0.f};
       const int c0 = wave * 16 + g * 4;
+      // rows c0 + e of v, column 16 i + m: what the state before the chunk gives. In parts the state
+      // is one operand at a time, as bf16 all of it and one column.
+      Frag<NP> sf[NP == 1 ? KF : 1], vf[SF];
+      f32x4 all[NP == 1 ? 1 : NT];
+      if constexpr (NP == 1) {
+#pragma unroll
+        for (int d = 0; d < KF; ++d) sf[d] = as_frag<NP>(S[2 * d], S[2 * d + 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < KF; ++d) {
+          sf[0] = as_frag<NP>(S[2 * d], S[2 * d + 1]);
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            all[i] = mma(sf[0], frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane), all[i]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < SF; ++s) vf[s] = vc[s].frag();
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        // rows c0 + e of v, column 16 i + m: what the state before the chunk gives, then the weights
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (NP == 1) {
 #pragma unroll
-        for (int d = 0; d < KF; ++d) o = mma(sf[d], frag_row(lq + i * 16 * LK + d * 32, LK, lane), o);
+          for (int d = 0; d < KF; ++d)
+            o = mma(sf[d], frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane), o);
+        } else {
+          o = all[i];
+        }
         o *= P.read_scale * exp2_fast(a2 * (float)(16 * i + m + read_off));
 #pragma unroll
         for (int s = 0; s <= i / 2; ++s) {
-          const T *t = lp + (i * (i + 1) / 2 + 2 * s) * 256 + lane * 4;
-          o = mma(vf[s], joined(*(const V4 *)t, 2 * s + 1 <= i ? *(const V4 *)(t + 256) : zero), o);
+          const bf16 *t = lp + (i * (i + 1) / 2 + 2 * s) * NP * 256 + lane * 4;
+          Frag<NP> pf;
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            pf.p[n] = joined(*(const bf16x4 *)(t + n * 256),
+                             2 * s + 1 <= i ? *(const bf16x4 *)(t + (NP + n) * 256) : zero);
+          o = mma(vf[s], pf, o);
         }
         const int place = 16 * i + m;
         if (!all_finite) {
 #pragma unroll 1
           for (int j = 0; j <= place; ++j) {
-            const float w = (float)lp[(i * (i + 1) / 2 + j / 16) * 256 + (m + j % 16 / 4 * 16) * 4 + j % 4];
+            const bf16 *t = lp + (i * (i + 1) / 2 + j / 16) * NP * 256 + (m + j % 16 / 4 * 16) * 4 + j % 4;
+            float w = 0.f;
+#pragma unroll
+            for (int n = NP - 1; n >= 0; --n) w += (float)t[n * 256];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x = (float)lv[j * LV + c0 + e];
@@ -471,9 +577,9 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
         if (place < size && c0 < P.v_width) {
           char *to = (char *)P.out + low * out_row + (int64_t)head * P.v_width * (P.out_f32 ? 4 : (int)sizeof(T));
           to += (uint32_t)(place ^ flip) * (uint32_t)out_row + c0 * (P.out_f32 ? 4 : (int)sizeof(T));
-          if (A.vec_out) {
+          if (P.vec_out) {
             if (P.out_f32) *(f32x4 *)to = o;
-            else *(V4 *)to = rounded<T>(o);
+            else *(V4 *)to = __builtin_convertvector(o, V4);
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -487,79 +593,69 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
       }
       if (!all_finite) {
 #pragma unroll
-        for (int s = 0; s < SF; ++s) vf[s] = frag_col<4>(lv + s * 32 * LV + wave * 16, LV, lane);
+        for (int s = 0; s < SF; ++s) vc[s].read(lv + s * 32 * LV + wave * 16, LV, lane);
       }
     }
 
     // S <- e^{a size} S + sum_j k_j (e^{a (size - 1 - j + add_off)} update_scale v_j)^T
     const float whole = exp2_fast(a2 * (float)size);
+    if constexpr (HELD) {
+      if (size < C) {
+#pragma unroll
+        for (int n = 0; n < 2 * SF; ++n) add[n] = for_update(n, size, g);
+      }
+    }
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) S[kt] *= whole;
 #pragma unroll
     for (int s = 0; s < SF; ++s) {
       f32x4 w[2];
-      if (size == C) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int left = C - 4 - s * 32 - h * 16 - g * 4;
-          const float far = P.update_scale * exp2_fast(a2 * (float)(left + add_off));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[h][e] = far * near[e];
-        }
+      if constexpr (HELD) {
+        w[0] = add[2 * s];
+        w[1] = add[2 * s + 1];
       } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int left = size - 1 - s * 32 - h * 16 - g * 4 - e;  // below 0: no token, v is zero
-            w[h][e] = P.update_scale * exp2_fast(a2 * (float)((left > 0 ? left : 0) + add_off));
-          }
+        w[0] = for_update(2 * s, size, g);
+        w[1] = for_update(2 * s + 1, size, g);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        w[0][e] *= (float)vf[s].get(e);
-        w[1][e] *= (float)vf[s].get(4 + e);
+        w[0][e] *= vc[s].get(e);
+        w[1][e] *= vc[s].get(4 + e);
       }
-      const T *kc = lk + s * 32 * LK;
-      if constexpr (sizeof(T) == 2) {
-        Frag<bf16> part[3];
-        split3(w[0], w[1], part);
-        if (P.last_state) {
+      const Frag<3> x = as_frag<3>(w[0], w[1]);
+      const auto update = [&](int parts) {  // of x, where k has one
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            const Frag<bf16> kf = frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) S[kt] = mma(kf, part[n], S[kt]);
-          }
-        } else {  // read as bf16 alone: 16 bits are enough
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            const Frag<bf16> kf = frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) S[kt] = mma(kf, part[n], S[kt]);
+        for (int kt = 0; kt < KT; ++kt) {
+          const Frag<NP> kf =
+              frag_col<NP, 8>(lk + s * 32 * LK + kt / 2 * 32 + kt % 2 * 4, LK, KPART, lane);
+          if constexpr (NP == 3) {
+            S[kt] = mma(kf, x, S[kt]);
+          } else {
+            for (int n = 0; n < parts; ++n) S[kt] = mma(kf.p[0], x.p[n], S[kt]);
           }
         }
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-        const Frag<float> x = {w[0], w[1]};
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-          S[kt] = mma(frag_col<8>(kc + kt / 2 * 32 + kt % 2 * 4, LK, lane), x, S[kt]);
-      }
+      };
+      // a state that only bf16 products read needs no more than 16 bits of what is added
+      if (NP == 3 || P.last_state) update(3);
+      else update(2);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
   if (STATES) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) *(f32x4 *)(slot_state + kt * 256) = S[kt];
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) slot_state[in_slot(kt, e)] = S[kt][e];
   } else if (last && P.last_state) {
+    float *to = P.last_state + state;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int r = state_row(kt, g, e);
         if (r < P.k_width && col < P.v_width)
-          P.last_state[state + r * P.last_ld[0] + col * P.last_ld[1]] = S[kt][e];
+          to[(unsigned)(r * P.last_ld[0] + col * P.last_ld[1])] = S[kt][e];
       }
   }
 }
@@ -679,35 +775,51 @@ __global__ __launch_bounds__(256) void k_step(int64_t row0, int heads, int group
 int padded_width3(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : 128; }
 
 template <typename T, int KP, int VP> hipError_t launch_kv(Args A, bool split, hipStream_t s) {
-  const AttentionPass &P = A.p;
-  const auto each = [&](auto kernel, int64_t places) {
-    const int64_t per = max_blocks(VP * 4) / P.heads;  // a launch
-    for (A.slot0 = 0; A.slot0 < places; A.slot0 += per) {
-      const int64_t n = places - A.slot0 < per ? places - A.slot0 : per;
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(n * P.heads)), dim3(VP * 4), 0, s, A);
+  const int heads = A.p[0].heads;
+  bool vec = true;
+  for (int i = 0; i < A.n; ++i) vec = vec && A.p[i].vec_in;
+  const auto each = [&](auto kernel, const Args &all, int64_t places) {
+    Args a = all;
+    const int64_t per = max_blocks(VP * 4) / (heads * a.n);  // a launch
+    for (a.slot0 = 0; a.slot0 < places; a.slot0 += per) {
+      const int64_t n = places - a.slot0 < per ? places - a.slot0 : per;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(n * heads * a.n)), dim3(VP * 4), 0, s, a);
     }
   };
-  if (split) {
-    each(A.vec_in ? k_attention<T, KP, VP, true, true> : k_attention<T, KP, VP, true, false>,
-         P.n_tokens >> A.shift);
-    const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / P.heads;
-    for (int64_t r = 0; r < P.n_rows; r += per) {
-      const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
-      // parts of a state: as many as fill the chip, where rows and heads alone do not
-      const int64_t parts = n * P.heads >= 1024 ? 1 : (floats + 1023) / 1024;
-      hipLaunchKernelGGL(k_join_segments, dim3((unsigned)(n * P.heads), (unsigned)parts), dim3(256),
-                         0, s, P.segments, P.row_ptr, r, P.n_tokens, A.n_slots, A.shift, P.heads,
-                         P.log_decay, floats);
+  const auto states = [&](const Args &a) {
+    each(vec ? k_attention<T, KP, VP, true, true> : k_attention<T, KP, VP, true, false>, a,
+         a.p[0].n_tokens >> a.shift);
+  };
+  const auto outputs = [&](const Args &a) {
+    each(vec ? k_attention<T, KP, VP, false, true> : k_attention<T, KP, VP, false, false>, a,
+         a.n_slots);
+  };
+  if (split) {  // the states of those passes that do not take another's
+    Args own = A;
+    own.n = 0;
+    for (int i = 0; i < A.n; ++i)
+      if (!A.p[i].shares_segments) own.p[own.n++] = A.p[i];
+    if (own.n > 0) states(own);
+    for (int i = 0; i < own.n; ++i) {
+      const AttentionPass &P = own.p[i];
+      const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / heads;
+      for (int64_t r = 0; r < P.n_rows; r += per) {
+        const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
+        // parts of a state: as many as fill the chip, where rows and heads alone do not
+        const int64_t parts = n * heads >= 1024 ? 1 : (floats + 1023) / 1024;
+        hipLaunchKernelGGL(k_join_segments, dim3((unsigned)(n * heads), (unsigned)parts), dim3(256), 0,
+                           s, P.segments, P.row_ptr, r, P.n_tokens, A.n_slots, A.shift, heads,
+                           P.log_decay, floats);
+      }
     }
   }
-  each(A.vec_in ? k_attention<T, KP, VP, false, true> : k_attention<T, KP, VP, false, false>,
-       A.n_slots);
+  outputs(A);
   return hipGetLastError();
 }
 
 template <typename T, int KP>
 hipError_t launch_k(const Args &A, bool split, hipStream_t s) {
-  switch (padded_width3(A.p.v_width)) {
+  switch (padded_width3(A.p[0].v_width)) {
     case 32: return launch_kv<T, KP, 32>(A, split, s);
     case 64: return launch_kv<T, KP, 64>(A, split, s);
     default: return launch_kv<T, KP, 128>(A, split, s);
@@ -715,7 +827,7 @@ hipError_t launch_k(const Args &A, bool split, hipStream_t s) {
 }
 
 template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t s) {
-  switch (padded_width3(A.p.k_width)) {
+  switch (padded_width3(A.p[0].k_width)) {
     case 32: return launch_k<T, 32>(A, split, s);
     case 64: return launch_k<T, 64>(A, split, s);
     default: return launch_k<T, 128>(A, split, s);
@@ -760,22 +872,33 @@ hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s)
   return hipGetLastError();
 }
 
-hipError_t launch_attention(als_dtype dtype, const AttentionPass &p, hipStream_t s) {
-  if (p.n_rows == 0) return hipSuccess;
+hipError_t launch_attention(als_dtype dtype, const AttentionPass *p, int n, hipStream_t s) {
+  if (p[0].n_rows == 0) return hipSuccess;
   Args A{};
-  A.p = p;
-  A.shift = attention_shift(dtype, p.n_tokens, p.heads);
-  A.n_slots = (p.n_tokens >> A.shift) + p.n_rows;
-  A.places = (const Place *)p.places;
-  A.entries = p.entries;
-  const int size = dtype == ALS_F32 ? 4 : 2, out = p.out_f32 ? 4 : size;
-  const auto vec = [&](const als_heads &x, int width) {
-    return aligned16(x.data, x.token_stride, x.head_stride, width, size);
-  };
-  A.vec_in = vec(p.q, p.k_width) && vec(p.k, p.k_width) && vec(p.v, p.v_width);
-  A.vec_out = p.v_width % 4 == 0 && (uintptr_t)p.out % (4 * out) == 0;
-  const bool split = p.n_tokens > 1LL << A.shift;
-  return dtype == ALS_F32 ? launch_t<float>(A, split, s) : launch_t<bf16>(A, split, s);
+  A.shift = attention_shift(dtype, p[0].n_tokens, p[0].heads);
+  A.n_slots = (p[0].n_tokens >> A.shift) + p[0].n_rows;
+  A.places = (const Place *)p[0].places;
+  A.entries = p[0].entries;
+  const bool split = p[0].n_tokens > 1LL << A.shift;
+  const int size = dtype == ALS_F32 ? 4 : 2;
+  for (int i = 0; i < n;) {  // neighbours of the same padded widths go in one launch
+    A.n = 0;
+    const int kp = padded_width3(p[i].k_width), vp = padded_width3(p[i].v_width);
+    for (; i < n && padded_width3(p[i].k_width) == kp && padded_width3(p[i].v_width) == vp; ++i) {
+      AttentionPass &x = A.p[A.n++] = p[i];
+      const auto vec = [&](const als_heads &h, int width) {
+        return aligned16(h.data, h.token_stride, h.head_stride, width, size);
+      };
+      x.vec_in = vec(x.q, x.k_width) && vec(x.k, x.k_width) && vec(x.v, x.v_width);
+      x.vec_out = x.v_width % 4 == 0 && (uintptr_t)x.out % (4 * (x.out_f32 ? 4 : size)) == 0;
+      // row-major as the pass that forms them has them, its rows padded to its v_width
+      x.segment_ld[0] = x.shares_segments ? 1 : vp;
+      x.segment_ld[1] = x.shares_segments ? kp : 1;
+    }
+    const hipError_t e = dtype == ALS_F32 ? launch_t<float>(A, split, s) : launch_t<bf16>(A, split, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,

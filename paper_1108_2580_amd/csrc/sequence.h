@@ -55,6 +55,11 @@ struct AttentionPass {
   void *places;           // of the segments, written by launch_places
   int32_t *entries;
   float *segments;        // states of the segments
+  bool shares_segments;   // they are another pass's, whose state is this one's transposed
+  // set by launch_attention
+  int64_t segment_ld[2];
+  bool vec_in;            // q, k and v are read 16 bytes at a time
+  bool vec_out;           // out is written 4 values at a time
 };
 
 // Bytes of a pass's workspace, by part, each a multiple of 16.
@@ -69,7 +74,8 @@ AttentionSpace attention_space(als_dtype dtype, int64_t n_tokens, int64_t n_rows
                                int k_width, int v_width);
 // Fills p.places and p.entries, which all passes over the same rows and heads share.
 hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s);
-hipError_t launch_attention(als_dtype dtype, const AttentionPass &p, hipStream_t s);
+// Up to three passes over the same rows and heads. One that shares segments comes after its owner.
+hipError_t launch_attention(als_dtype dtype, const AttentionPass *p, int n, hipStream_t s);
 // out[t, k, d] = sum over the head's group of x[t, k * group + i, d], in order.
 hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,
                              int32_t group, int32_t width, void *out, hipStream_t s);

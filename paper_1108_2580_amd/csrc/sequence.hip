@@ -178,11 +178,17 @@ int64_t space_bytes(const als_attention *s) {
   const int64_t a = space_of(s, ALS_F32).total(), b = space_of(s, ALS_BF16).total();
   return a > b ? a : b;
 }
-// Gradients of shared heads, one per query head, before their sum.
-int64_t shared_bytes(const als_attention *s) {
-  if (s->q_heads == s->k_heads) return 0;
-  const int64_t w = s->k_width > s->v_width ? s->k_width : s->v_width;
-  return rounded16(4 * s->n_tokens * s->q_heads * w);
+// Gradients of shared heads, one per query head, before their sum: of k, then of v.
+int64_t shared_bytes(const als_attention *s, int width) {
+  return s->q_heads == s->k_heads ? 0 : rounded16(4 * s->n_tokens * s->q_heads * width);
+}
+int64_t backward_bytes(const als_attention *s) {  // the segments of two passes
+  int64_t states = 0;
+  for (als_dtype t : {ALS_F32, ALS_BF16}) {
+    const als::AttentionSpace x = space_of(s, t);
+    states = x.total() + x.states > states ? x.total() + x.states : states;
+  }
+  return states + shared_bytes(s, s->k_width) + shared_bytes(s, s->v_width);
 }
 
 AttentionPass pass_of(const als_attention *s, als_dtype dtype, void *workspace) {
@@ -286,12 +292,12 @@ als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_
   p.first_ld[1] = p.last_ld[1] = 1;
   p.out = out;
   hipError_t e = als::launch_places(dtype, p, (hipStream_t)hip_stream);
-  if (e == hipSuccess) e = als::launch_attention(dtype, p, (hipStream_t)hip_stream);
+  if (e == hipSuccess) e = als::launch_attention(dtype, &p, 1, (hipStream_t)hip_stream);
   return launched(e, "als_decay_attention");
 }
 
 int64_t als_decay_attention_backward_workspace(const als_attention *shape) {
-  return sane(shape) ? space_bytes(shape) + shared_bytes(shape) : -1;
+  return sane(shape) ? backward_bytes(shape) : -1;
 }
 
 als_status als_decay_attention_backward(const als_attention *shape, als_dtype dtype, als_heads d_out,
@@ -332,55 +338,59 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
                                       als_decay_attention_backward_workspace(s)))
     return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  float *shared = group > 1 ? (float *)((char *)workspace + space_bytes(s)) : nullptr;
+  const als::AttentionSpace space = space_of(s, dtype);
+  char *rest = (char *)workspace + space.total() + space.states;
+  float *shared_k = group > 1 ? (float *)rest : nullptr;
+  float *shared_v = group > 1 ? (float *)(rest + shared_bytes(s, s->k_width)) : nullptr;
 
+  AttentionPass p[3] = {pass_of(s, dtype, workspace), pass_of(s, dtype, workspace),
+                        pass_of(s, dtype, workspace)};
   // dq: the pass over (d_out, v, k), with the state transposed
-  AttentionPass p = pass_of(s, dtype, workspace);
-  p.group = p.v_group = group;
-  p.k_width = s->v_width;
-  p.v_width = s->k_width;
-  p.q = d_out;
-  p.k = v;
-  p.v = k;
-  p.read_scale = s->scale;
-  p.first_state = initial_state;
-  p.first_ld[0] = 1;
-  p.first_ld[1] = s->v_width;
-  p.out = dq;
-  hipError_t e = als::launch_places(dtype, p, stream);
-  if (e == hipSuccess) e = als::launch_attention(dtype, p, stream);
+  p[0].group = p[0].v_group = group;
+  p[0].k_width = s->v_width;
+  p[0].v_width = s->k_width;
+  p[0].q = d_out;
+  p[0].k = v;
+  p[0].v = k;
+  p[0].read_scale = s->scale;
+  p[0].first_state = initial_state;
+  p[0].first_ld[0] = 1;
+  p[0].first_ld[1] = s->v_width;
+  p[0].out = dq;
   // dv: the reversed pass over (k, q, d_out); its last state is the initial state's gradient
-  p = pass_of(s, dtype, workspace);
-  p.reverse = true;
-  p.update_scale = s->scale;
-  p.q_group = group;
-  p.k_width = s->k_width;
-  p.v_width = s->v_width;
-  p.q = k;
-  p.k = q;
-  p.v = d_out;
-  p.first_state = d_final_state;
-  p.last_state = d_initial_state;
-  p.first_ld[0] = p.last_ld[0] = s->v_width;
-  p.first_ld[1] = p.last_ld[1] = 1;
-  p.out = shared ? (void *)shared : dv;
-  p.out_f32 = shared || dtype == ALS_F32;
-  if (e == hipSuccess) e = als::launch_attention(dtype, p, stream);
-  if (e == hipSuccess && shared)
-    e = als::launch_sum_groups(dtype, shared, n, s->q_heads, group, s->v_width, dv, stream);
-  // dk: the reversed pass over (v, d_out, q), with the state transposed
-  p.k_width = s->v_width;
-  p.v_width = s->k_width;
-  p.q = v;
-  p.k = d_out;
-  p.v = q;
-  p.last_state = nullptr;
-  p.first_ld[0] = 1;
-  p.first_ld[1] = s->v_width;
-  p.out = shared ? (void *)shared : dk;
-  if (e == hipSuccess) e = als::launch_attention(dtype, p, stream);
-  if (e == hipSuccess && shared)
-    e = als::launch_sum_groups(dtype, shared, n, s->q_heads, group, s->k_width, dk, stream);
+  p[1].reverse = true;
+  p[1].update_scale = s->scale;
+  p[1].q_group = group;
+  p[1].k_width = s->k_width;
+  p[1].v_width = s->v_width;
+  p[1].q = k;
+  p[1].k = q;
+  p[1].v = d_out;
+  p[1].first_state = d_final_state;
+  p[1].last_state = d_initial_state;
+  p[1].first_ld[0] = p[1].last_ld[0] = s->v_width;
+  p[1].first_ld[1] = p[1].last_ld[1] = 1;
+  p[1].out = shared_v ? (void *)shared_v : dv;
+  p[1].out_f32 = shared_v || dtype == ALS_F32;
+  if (space.states) p[1].segments = (float *)((char *)workspace + space.total());
+  // dk: the reversed pass over (v, d_out, q), with dv's state transposed
+  p[2] = p[1];
+  p[2].k_width = s->v_width;
+  p[2].v_width = s->k_width;
+  p[2].q = v;
+  p[2].k = d_out;
+  p[2].v = q;
+  p[2].last_state = nullptr;
+  p[2].first_ld[0] = 1;
+  p[2].first_ld[1] = s->v_width;
+  p[2].shares_segments = true;
+  p[2].out = shared_k ? (void *)shared_k : dk;
+  hipError_t e = als::launch_places(dtype, p[0], stream);
+  if (e == hipSuccess) e = als::launch_attention(dtype, p, 3, stream);
+  if (e == hipSuccess && shared_k)
+    e = als::launch_sum_groups(dtype, shared_k, n, s->q_heads, group, s->k_width, dk, stream);
+  if (e == hipSuccess && shared_v)
+    e = als::launch_sum_groups(dtype, shared_v, n, s->q_heads, group, s->v_width, dv, stream);
   return launched(e, "als_decay_attention_backward");
 }
 
