@@ -681,13 +681,14 @@ __global__ __launch_bounds__(256) void k_join_segments(float *segments, const in
        x += (int64_t)gridDim.y * 1024) {
     float *p = segments + (slot * heads + head) * floats + x;
     f32x4 state = *(const f32x4 *)p;
-    for (int64_t j = 1; j < n; j += 4) {
-      f32x4 own[4];
+    constexpr int kAhead = 16;  // states on their way: the sums wait for each other, the reads need not
+    for (int64_t j = 1; j < n; j += kAhead) {
+      f32x4 own[kAhead];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kAhead; ++i)
         own[i] = j + i + 1 < n ? *(const f32x4 *)(p + (j + i) * stride) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kAhead; ++i)
         if (j + i < n) {
           *(f32x4 *)(p + (j + i) * stride) = state;
           state = state * whole + own[i];
@@ -837,14 +838,14 @@ template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t
 }  // namespace
 
 // Short segments fill the chip where tokens are few; each costs a pass over its k and v and a state
-// written and read. From four chunks up, as many as leave 512 blocks (bf16) or 2048 (f32, whose chunks
-// are half as long and bound by the products), at most 2048 tokens. Us with segments of 256, 512, 1024
+// written and read. From four chunks up, as many as leave 1024 blocks (bf16: what the chip holds at
+// a time) or 2048 (f32, whose chunks are half as long), at most 2048 tokens. Us with segments of 256, 512, 1024
 // and 2048: one row of 62496 bf16 tokens, 8 heads of 64 142, 126, 115, -; forward and backward of 4096
 // rows of 263 -, 5800, 5275, 5213 (4096: 5640); 100 f32 rows of 1000 at 128 wide -, 3860, 4037, -; 8
 // bf16 rows of 250 33, 42, 72, -.
 int attention_shift(als_dtype dtype, int64_t n_tokens, int32_t heads) {
   int shift = dtype == ALS_F32 ? 7 : 8;
-  while (shift < 11 && (n_tokens >> shift) * heads > (dtype == ALS_F32 ? 2048 : 512)) ++shift;
+  while (shift < 11 && (n_tokens >> shift) * heads > (dtype == ALS_F32 ? 2048 : 1024)) ++shift;
   return shift;
 }
 
