@@ -25,6 +25,8 @@
 // where they enter a product, which is as much again as the output's own rounding; what a token adds
 // to the state is split into three bf16 parts (24 bits), so that the state, an output in fp32, has no
 // bf16 rounding in it. fp32 inputs: all operands are split so.
+#include <type_traits>
+
 #include "internal.h"
 #include "sequence.h"
 
@@ -266,8 +268,10 @@ struct Args {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A chunk's tokens of one head of x on their way to LDS, zero past `size` tokens and past `width`. They are fetched into registers while the chunk before is worked
-// on: 16 bytes at a time, or value by value where a width or an alignment does not allow that.
+// A chunk's tokens of one head of x on their way to LDS, zero past `size` tokens and past `width`: 16
+// bytes at a time, fetched into registers while the chunk before is worked on. Without VEC the pieces
+// lie at any alignment of their type, and a row's last one is read so that it ends with the row and is
+// shifted into place on its way out (read value by value, such rows took three times as long).
 // Place r of the chunk is row r ^ flip from `base`, the chunk's lowest token: flip is C - 1 in a pass
 // from the last token to the first, and 0 otherwise. Offsets from there are below 2^31
 // (kMaxTokenStride).
@@ -276,43 +280,74 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   static constexpr int ROWS = THREADS / ROW, N = (C + ROWS - 1) / ROWS;
   static_assert(THREADS % ROW == 0 && (ROWS >= C || C % ROWS == 0), "whole rows a pass");
   struct alignas(16) Piece { T v[E]; };
+  struct Rows {  // of one chunk
+    const char *base;
+    uint32_t bytes;  // from row to row
+    int flip, size, width;
+    __device__ __forceinline__ const char *at(int r, int c) const {
+      return base + ((uint32_t)(r ^ flip) * bytes + c * (int)sizeof(T));
+    }
+  };
   Piece held[N];
 
-  __device__ __forceinline__ void fetch(const char *base, uint32_t row_bytes, int flip, int size,
-                                        int width, int tid) {
+  __device__ __forceinline__ void fetch(const Rows &x, int tid) {
     const int r0 = tid / ROW, c = tid % ROW * E;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = r0 + i * ROWS;
-      const uint32_t at = (uint32_t)(r ^ flip) * row_bytes + c * (int)sizeof(T);
 #pragma unroll
       for (int e = 0; e < E; ++e) held[i].v[e] = (T)0.f;
-      if (VEC) {
-        if (r < size && c < width) held[i] = *(const Piece *)(base + at);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (r < size && c + e < width) held[i].v[e] = ((const T *)(base + at))[e];
+      if (r < x.size && c < x.width) {
+        if (VEC)
+          held[i] = *(const Piece *)x.at(r, c);
+        else if (x.width >= E)
+          __builtin_memcpy(&held[i], x.at(r, c < x.width - E ? c : x.width - E), 16);
       }
     }
   }
-  __device__ __forceinline__ void put(T *lds, int ld, int tid) const {
+  // piece i of this lane, as it goes to column c
+  __device__ __forceinline__ Piece piece(const Rows &x, int i, int r, int c) const {
+    if (VEC) return held[i];
+    if (x.width < E) {  // too narrow for any whole piece
+      Piece p;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        p.v[e] = r < x.size && c + e < x.width ? ((const T *)x.at(r, 0))[e] : (T)0.f;
+      return p;
+    }
+    int bits = (c + E > x.width ? c + E - x.width : 0) * (int)sizeof(T) * 8;
+    uint64_t w[2];
+    __builtin_memcpy(w, &held[i], 16);
+    if (bits >= 64) {
+      w[0] = w[1];
+      w[1] = 0;
+      bits -= 64;
+    }
+    if (bits >= 64) bits = 0;  // past the row: nothing was fetched
+    const uint64_t out[2] = {w[0] >> bits | w[1] << 1 << (63 - bits), w[1] >> bits};
+    Piece p;
+    __builtin_memcpy(&p, out, 16);
+    return p;
+  }
+  __device__ __forceinline__ void put(T *lds, int ld, const Rows &x, int tid) const {
     const int r0 = tid / ROW, c = tid % ROW * E;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (ROWS <= C || r0 < C) *(Piece *)(lds + (r0 + i * ROWS) * ld + c) = held[i];
+      if (ROWS <= C || r0 < C)
+        *(Piece *)(lds + (r0 + i * ROWS) * ld + c) = piece(x, i, r0 + i * ROWS, c);
   }
   // as operands of products: fp32 in parts
-  __device__ __forceinline__ void put_parts(bf16 *lds, int ld, int tid) const {
+  __device__ __forceinline__ void put_parts(bf16 *lds, int ld, const Rows &x, int tid) const {
     if constexpr (sizeof(T) == 2) {
-      put(lds, ld, tid);
+      put(lds, ld, x, tid);
     } else {
       const int r0 = tid / ROW, c = tid % ROW * E;
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (ROWS <= C || r0 < C) {
+          const Piece p = piece(x, i, r0 + i * ROWS, c);
           bf16x4 part[3];
-          split3(f32x4{held[i].v[0], held[i].v[1], held[i].v[2], held[i].v[3]}, part);
+          split3(f32x4{p.v[0], p.v[1], p.v[2], p.v[3]}, part);
 #pragma unroll
           for (int n = 0; n < 3; ++n)
             *(bf16x4 *)(lds + n * C * ld + (r0 + i * ROWS) * ld + c) = part[n];
@@ -322,15 +357,15 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 };
 
 // Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, three where
-// LDS holds no more, two where few threads hold the pieces, or hold them value by value.
-template <typename T> constexpr int waves_for(int VP, bool vec) {
-  return VP == 32 || (!vec && sizeof(T) == 2) ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
+// LDS holds no more, two where few threads hold the pieces.
+template <typename T> constexpr int waves_for(int VP) {
+  return VP == 32 ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
 }
 
 // One block: one head of one segment. STATES: only the state after the segment, for all segments of
 // a row but its last.
 template <typename T, int KP, int VP, bool STATES, bool VEC>
-__global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Args A) {
+__global__ __launch_bounds__(VP * 4, waves_for<T>(VP)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
   constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<bf16>(KP), LV = padded<T>(VP);
   constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, KPART = C * LK;
@@ -388,12 +423,15 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
 
   TK hq, hk;
   TV hv;
+  const auto rows_of = [&](auto &tile, const char *x, int64_t bytes, int width, int c) {
+    using Rows = typename std::remove_reference<decltype(tile)>::type::Rows;
+    return Rows{x + (token0 + (P.reverse ? -c : c)) * bytes, (uint32_t)bytes, flip,
+                count - c < C ? count - c : C, width};
+  };
   const auto fetch = [&](int c, int tid) {
-    const int size = count - c < C ? count - c : C;
-    const int64_t low = token0 + (P.reverse ? -c : c);
-    if (!STATES) hq.fetch(q + low * q_row, (uint32_t)q_row, flip, size, P.k_width, tid);
-    hk.fetch(k + low * k_row, (uint32_t)k_row, flip, size, P.k_width, tid);
-    hv.fetch(v + low * v_row, (uint32_t)v_row, flip, size, P.v_width, tid);
+    if (!STATES) hq.fetch(rows_of(hq, q, q_row, P.k_width, c), tid);
+    hk.fetch(rows_of(hk, k, k_row, P.k_width, c), tid);
+    hv.fetch(rows_of(hv, v, v_row, P.v_width, c), tid);
   };
   if (count > 0) fetch(0, (int)threadIdx.x);
 
@@ -467,9 +505,9 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
     asm volatile("" : "+v"(lane), "+v"(tid));
     const int g = lane >> 4, m = lane & 15;
     __syncthreads();
-    if (!STATES) hq.put_parts(lq, LK, tid);
-    hk.put_parts(lk, LK, tid);
-    hv.put(lv, LV, tid);
+    if (!STATES) hq.put_parts(lq, LK, rows_of(hq, q, q_row, P.k_width, c), tid);
+    hk.put_parts(lk, LK, rows_of(hk, k, k_row, P.k_width, c), tid);
+    hv.put(lv, LV, rows_of(hv, v, v_row, P.v_width, c), tid);
     __syncthreads();
     if (c + C < count) fetch(c + C, tid);
 
@@ -577,12 +615,13 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP, VEC)) void k_attention(Arg
         if (place < size && c0 < P.v_width) {
           char *to = (char *)P.out + low * out_row + (int64_t)head * P.v_width * (P.out_f32 ? 4 : (int)sizeof(T));
           to += (uint32_t)(place ^ flip) * (uint32_t)out_row + c0 * (P.out_f32 ? 4 : (int)sizeof(T));
-          if (P.vec_out) {
-            if (P.out_f32) *(f32x4 *)to = o;
-            else *(V4 *)to = __builtin_convertvector(o, V4);
+          if (c0 + 4 <= P.v_width) {  // at any alignment of the type
+            const V4 r = __builtin_convertvector(o, V4);
+            if (P.out_f32) __builtin_memcpy(to, &o, 16);
+            else __builtin_memcpy(to, &r, sizeof r);
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
               if (c0 + e < P.v_width) {
                 if (P.out_f32) ((float *)to)[e] = o[e];
                 else ((T *)to)[e] = (T)o[e];
@@ -891,7 +930,6 @@ hipError_t launch_attention(als_dtype dtype, const AttentionPass *p, int n, hipS
         return aligned16(h.data, h.token_stride, h.head_stride, width, size);
       };
       x.vec_in = vec(x.q, x.k_width) && vec(x.k, x.k_width) && vec(x.v, x.v_width);
-      x.vec_out = x.v_width % 4 == 0 && (uintptr_t)x.out % (4 * (x.out_f32 ? 4 : size)) == 0;
       // row-major as the pass that forms them has them, its rows padded to its v_width
       x.segment_ld[0] = x.shares_segments ? 1 : vp;
       x.segment_ld[1] = x.shares_segments ? kp : 1;

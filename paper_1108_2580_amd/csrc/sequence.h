@@ -59,7 +59,6 @@ struct AttentionPass {
   // set by launch_attention
   int64_t segment_ld[2];
   bool vec_in;            // q, k and v are read 16 bytes at a time
-  bool vec_out;           // out is written 4 values at a time
 };
 
 // Bytes of a pass's workspace, by part, each a multiple of 16.
