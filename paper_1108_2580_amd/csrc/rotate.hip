@@ -38,92 +38,111 @@ struct Rotate {
   float eps;
 };
 
-template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
-
-// VW values from p, zero past `left` of them; whole where VW of them are left.
-template <typename T, int VW>
-__device__ __forceinline__ void load(const T *p, int left, float *x) {
-  Pack<T, VW> v;
+// VW values in one access at any alignment of their type.
+template <typename T, int VW> struct Run {
+  using V = T __attribute__((ext_vector_type(VW)));
+  using U = V __attribute__((aligned(sizeof(T))));
+};
+// VW values from p, zero past `left` of them.
+template <typename T, int VW> __device__ __forceinline__ void load(const T *p, int left, float (&x)[VW]) {
   if (left >= VW) {
-    v = *(const Pack<T, VW> *)p;
+    const typename Run<T, VW>::V v = *(const typename Run<T, VW>::U *)p;
 #pragma unroll
-    for (int e = 0; e < VW; ++e) x[e] = (float)v.v[e];
+    for (int e = 0; e < VW; ++e) x[e] = (float)v[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < VW; ++e) x[e] = e < left ? (float)p[e] : 0.f;
+    for (int e = 0; e < VW - 1; ++e) x[e] = e < left ? (float)p[e] : 0.f;
+    x[VW - 1] = 0.f;
   }
 }
 template <typename T, int VW>
-__device__ __forceinline__ void store(T *p, int left, const float *x) {
+__device__ __forceinline__ void store(T *p, int left, const float (&x)[VW]) {
   if (left >= VW) {
-    Pack<T, VW> v;
+    typename Run<T, VW>::V v;
 #pragma unroll
-    for (int e = 0; e < VW; ++e) v.v[e] = (T)x[e];
-    *(Pack<T, VW> *)p = v;
+    for (int e = 0; e < VW; ++e) v[e] = (T)x[e];
+    *(typename Run<T, VW>::U *)p = v;
   } else {
 #pragma unroll
-    for (int e = 0; e < VW; ++e)
+    for (int e = 0; e < VW - 1; ++e)
       if (e < left) p[e] = (T)x[e];
   }
 }
 
-// Where unit n of a lane lies in a row: two runs of VW values. A lane group's runs lie side by side, so
-// that each load and store of the group is one piece of memory. Turned pairs lie across the two runs
-// (halves, and neighbours one by one), or within each run (neighbours otherwise).
+// Where a lane's unit lies in a row: two runs of VW values. Of a lane group, runs a lie side by side,
+// and so do runs b, so that each load and store of the group is one piece of memory. Turned pairs lie
+// across the two runs (halves) or within each run (neighbours).
 struct Unit {
   int a, b;            // first features of the runs
   int left_a, left_b;  // values there, at most VW count
-  bool turned_a, turned_b;
+  bool turned;
 };
 template <int VW, bool NEXT, int G>
-__device__ __forceinline__ Unit unit_of(int lane, int n, int width, int half) {
+__device__ __forceinline__ Unit unit_of(int lane, int width, int half) {
   Unit x;
-  if (NEXT && VW > 1) {
-    x.a = (2 * n * G + lane) * VW;
+  if (NEXT) {
+    x.a = lane * VW;
     x.b = x.a + G * VW;
-    x.turned_a = x.a < 2 * half;
-    x.turned_b = x.b < 2 * half;
+    x.left_a = width - x.a;
+    x.left_b = width - x.b;
+    x.turned = true;
   } else {
-    const int u = n * G + lane, pairs = half / VW;
-    x.turned_a = x.turned_b = u < pairs;
-    if (u < pairs) {
-      x.a = NEXT ? 2 * u : u * VW;
-      x.b = NEXT ? 2 * u + 1 : half + u * VW;
+    const int pairs = (half + VW - 1) / VW;
+    x.turned = lane < pairs;
+    if (x.turned) {
+      x.a = lane * VW;
+      x.b = half + lane * VW;
+      x.left_a = x.left_b = half - lane * VW;
     } else {
-      x.a = 2 * half + (u - pairs) * 2 * VW;
+      x.a = 2 * half + (lane - pairs) * 2 * VW;
       x.b = x.a + VW;
+      x.left_a = width - x.a;
+      x.left_b = width - x.b;
     }
   }
-  x.left_a = width - x.a;
-  x.left_b = width - x.b;
   return x;
 }
-// Units in a row, for halves and for neighbours.
-template <int VW, bool NEXT> __host__ __device__ inline int units_in(int width, int half) {
-  return NEXT && VW > 1 ? (width + 2 * VW - 1) / (2 * VW)
-                        : half / VW + (width - 2 * half + 2 * VW - 1) / (2 * VW);
+template <int VW, bool NEXT> inline int units_in(int width, int half) {
+  return NEXT ? (width + 2 * VW - 1) / (2 * VW)
+              : (half + VW - 1) / VW + (width - 2 * half + 2 * VW - 1) / (2 * VW);
 }
 
+// N angles from pair p of a table of `half`, of which those past its end turn nothing.
+template <int N> struct Angles {
+  float c[N], s[N];
+  __device__ __forceinline__ Angles(const float *cs, const float *sn, int p, int half) {
+    if (p + N <= half) {
+      __builtin_memcpy(c, cs + p, sizeof c);
+      __builtin_memcpy(s, sn + p, sizeof s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        c[e] = p + e < half ? cs[p + e] : 1.f;
+        s[e] = p + e < half ? sn[p + e] : 0.f;
+      }
+    }
+  }
+  template <int SIGN> __device__ __forceinline__ void turn(int e, float &x, float &y) const {
+    const float was = x;
+    x = was * c[e] - y * (SIGN * s[e]);
+    y = y * c[e] + was * (SIGN * s[e]);
+  }
+};
 // Turns a unit's pairs by the angles of cs and sn, or back with SIGN -1.
 template <int VW, bool NEXT, int SIGN>
-__device__ __forceinline__ void turn(const Unit &u, float *a, float *b, const float *cs, const float *sn) {
-  const auto pair = [&](float &x, float &y, int p) {
-    const float c = cs[p], s = SIGN * sn[p], was = x;
-    x = was * c - y * s;
-    y = y * c + was * s;
-  };
-  if constexpr (NEXT && VW > 1) {
-    if (u.turned_a) {
+__device__ __forceinline__ void turn(const Unit &u, float (&a)[VW], float (&b)[VW], const float *cs,
+                                     const float *sn, int half) {
+  if constexpr (NEXT) {
+    const Angles<VW / 2> x(cs, sn, u.a / 2, half), y(cs, sn, u.b / 2, half);
 #pragma unroll
-      for (int e = 0; e < VW; e += 2) pair(a[e], a[e + 1], (u.a + e) / 2);
+    for (int e = 0; e < VW / 2; ++e) {
+      x.template turn<SIGN>(e, a[2 * e], a[2 * e + 1]);
+      y.template turn<SIGN>(e, b[2 * e], b[2 * e + 1]);
     }
-    if (u.turned_b) {
+  } else if (u.turned) {
+    const Angles<VW> x(cs, sn, u.a, half);
 #pragma unroll
-      for (int e = 0; e < VW; e += 2) pair(b[e], b[e + 1], (u.b + e) / 2);
-    }
-  } else if (u.turned_a) {
-#pragma unroll
-    for (int e = 0; e < VW; ++e) pair(a[e], b[e], (NEXT ? u.a / 2 : u.a) + e);
+    for (int e = 0; e < VW; ++e) x.template turn<SIGN>(e, a[e], b[e]);
   }
 }
 
@@ -133,24 +152,21 @@ template <int G> __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// blockIdx.y: queries or keys; blockIdx.x: a run of tokens. G lanes a row, UN units a lane.
-template <typename T, int VW, bool NEXT, int G, int UN, bool BACK>
+// blockIdx.y: queries or keys; blockIdx.x: a run of tokens. G lanes a row, a unit a lane.
+template <typename T, int VW, bool NEXT, int G, bool BACK>
 __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
   const Side &S = R.side[blockIdx.y];
   const int tid = (int)threadIdx.x, lane = tid % G;
   const int64_t t0 = (int64_t)blockIdx.x * R.tokens_per_block;
   const int64_t t1 = t0 + R.tokens_per_block < R.n_tokens ? t0 + R.tokens_per_block : R.n_tokens;
   const int rows = (int)(t1 > t0 ? t1 - t0 : 0) * S.heads;
-  float wa[UN][VW], wb[UN][VW], ga[UN][VW], gb[UN][VW];
+  const Unit u = unit_of<VW, NEXT, G>(lane, R.width, R.half);
+  float wa[VW], wb[VW], ga[VW], gb[VW];
 #pragma unroll
-  for (int n = 0; n < UN; ++n) {
-    const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
-#pragma unroll
-    for (int e = 0; e < VW; ++e) {
-      wa[n][e] = e < u.left_a ? S.weight[u.a + e] : 0.f;
-      wb[n][e] = e < u.left_b ? S.weight[u.b + e] : 0.f;
-      ga[n][e] = gb[n][e] = 0.f;
-    }
+  for (int e = 0; e < VW; ++e) {
+    wa[e] = e < u.left_a ? S.weight[u.a + e] : 0.f;
+    wb[e] = e < u.left_b ? S.weight[u.b + e] : 0.f;
+    ga[e] = gb[e] = 0.f;
   }
   constexpr int kStep = kBlock / G;
   const int token_step = kStep / S.heads, head_step = kStep % S.heads;
@@ -164,63 +180,46 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     const int64_t at = R.positions[token];
     const bool ok = at >= 0 && at < R.n_positions;
     const float *cs = R.cos + (ok ? at : 0) * R.half, *sn = R.sin + (ok ? at : 0) * R.half;
-    float xa[UN][VW], xb[UN][VW], da[UN][VW], db[UN][VW];
+    float xa[VW], xb[VW], da[VW], db[VW];
+    load<T, VW>(x + u.a, u.left_a, xa);
+    load<T, VW>(x + u.b, u.left_b, xb);
+    if (BACK) {
+      load<T, VW>(dy + u.a, u.left_a, da);
+      load<T, VW>(dy + u.b, u.left_b, db);
+    }
     float squares = 0.f, along = 0.f;
 #pragma unroll
-    for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
-      load<T, VW>(x + u.a, u.left_a, xa[n]);
-      load<T, VW>(x + u.b, u.left_b, xb[n]);
-      if (BACK) {
-        load<T, VW>(dy + u.a, u.left_a, da[n]);
-        load<T, VW>(dy + u.b, u.left_b, db[n]);
-      }
-#pragma unroll
-      for (int e = 0; e < VW; ++e) squares = fmaf(xa[n][e], xa[n][e], fmaf(xb[n][e], xb[n][e], squares));
-    }
+    for (int e = 0; e < VW; ++e) squares = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], squares));
     squares = group_sum<G>(squares);
     // a position outside the tables makes its rows NaN
     const float r = ok ? 1.f / sqrtf(squares / (float)R.width + R.eps) : __builtin_nanf("");
+    if (!BACK) {
 #pragma unroll
-    for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
-      float *a = BACK ? da[n] : xa[n], *b = BACK ? db[n] : xb[n];
-      if (!BACK) {
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          a[e] *= r * wa[n][e];
-          b[e] *= r * wb[n][e];
-        }
+      for (int e = 0; e < VW; ++e) {
+        xa[e] *= r * wa[e];
+        xb[e] *= r * wb[e];
       }
-      turn<VW, NEXT, BACK ? -1 : 1>(u, a, b, cs, sn);
-      if (BACK) {
+      turn<VW, NEXT, 1>(u, xa, xb, cs, sn, R.half);
+    } else {
+      turn<VW, NEXT, -1>(u, da, db, cs, sn, R.half);
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          ga[n][e] = fmaf(a[e], xa[n][e] * r, ga[n][e]);
-          gb[n][e] = fmaf(b[e], xb[n][e] * r, gb[n][e]);
-          a[e] *= wa[n][e];
-          b[e] *= wb[n][e];
-          along = fmaf(a[e], xa[n][e], fmaf(b[e], xb[n][e], along));
-        }
+      for (int e = 0; e < VW; ++e) {
+        ga[e] = fmaf(da[e], xa[e] * r, ga[e]);
+        gb[e] = fmaf(db[e], xb[e] * r, gb[e]);
+        da[e] *= wa[e];
+        db[e] *= wb[e];
+        along = fmaf(da[e], xa[e], fmaf(db[e], xb[e], along));
       }
-    }
-    if (BACK) {
       along = group_sum<G>(along);
       const float f = r * r * r * (along / (float)R.width);
 #pragma unroll
-      for (int n = 0; n < UN; ++n)
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          xa[n][e] = da[n][e] * r - xa[n][e] * f;
-          xb[n][e] = db[n][e] * r - xb[n][e] * f;
-        }
+      for (int e = 0; e < VW; ++e) {
+        xa[e] = da[e] * r - xa[e] * f;
+        xb[e] = db[e] * r - xb[e] * f;
+      }
     }
-#pragma unroll
-    for (int n = 0; n < UN; ++n) {
-      const Unit u = unit_of<VW, NEXT, G>(lane, n, R.width, R.half);
-      store<T, VW>(out + u.a, u.left_a, xa[n]);
-      store<T, VW>(out + u.b, u.left_b, xb[n]);
-    }
+    store<T, VW>(out + u.a, u.left_a, xa);
+    store<T, VW>(out + u.b, u.left_b, xb);
     token += token_step;
     head += head_step;
     if (head >= S.heads) {
@@ -229,22 +228,20 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     }
   }
   if (BACK) {
-    __shared__ float sums[kBlock / G][G * UN * 2 * VW];
+    __shared__ float sums[kBlock / G][G * 2 * VW];
 #pragma unroll
-    for (int n = 0; n < UN; ++n)
-#pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        sums[tid / G][((lane + n * G) * 2) * VW + e] = ga[n][e];
-        sums[tid / G][((lane + n * G) * 2 + 1) * VW + e] = gb[n][e];
-      }
+    for (int e = 0; e < VW; ++e) {
+      sums[tid / G][lane * 2 * VW + e] = ga[e];
+      sums[tid / G][lane * 2 * VW + VW + e] = gb[e];
+    }
     __syncthreads();
-    for (int i = tid; i < G * UN * 2 * VW; i += kBlock) {
-      const Unit u = unit_of<VW, NEXT, G>(i / (2 * VW) % G, i / (2 * VW) / G, R.width, R.half);
-      const int run = i / VW % 2, d = (run ? u.b : u.a) + i % VW;
-      if (d >= R.width) continue;
+    for (int i = tid; i < G * 2 * VW; i += kBlock) {
+      const Unit v = unit_of<VW, NEXT, G>(i / (2 * VW), R.width, R.half);
+      const int run = i / VW % 2, e = i % VW;
+      if (e >= (run ? v.left_b : v.left_a)) continue;
       float sum = 0.f;
       for (int j = 0; j < kBlock / G; ++j) sum += sums[j][i];
-      S.partial[(int64_t)blockIdx.x * R.width + d] = sum;
+      S.partial[(int64_t)blockIdx.x * R.width + (run ? v.b : v.a) + e] = sum;
     }
   }
 }
@@ -268,39 +265,33 @@ template <typename T, int VW, bool NEXT, bool BACK>
 hipError_t launch_vw(const Rotate &R, int blocks, hipStream_t s) {
   const int units = units_in<VW, NEXT>(R.width, R.half);
   const dim3 grid((unsigned)blocks, 2);
-#define ROTATE(G, UN) \
-  hipLaunchKernelGGL((k_rotate<T, VW, NEXT, G, UN, BACK>), grid, dim3(kBlock), 0, s, R)
-  if (units <= 4) ROTATE(4, 1);
-  else if (units <= 8) ROTATE(8, 1);
-  else if (units <= 16) ROTATE(16, 1);
-  else if (units <= 32) ROTATE(32, 1);
-  else if (units <= 64) ROTATE(64, 1);
-  else ROTATE(64, 2);
+#define ROTATE(G) hipLaunchKernelGGL((k_rotate<T, VW, NEXT, G, BACK>), grid, dim3(kBlock), 0, s, R)
+  if (units <= 4) ROTATE(4);
+  else if (units <= 8) ROTATE(8);
+  else if (units <= 16) ROTATE(16);
+  else if (units <= 32) ROTATE(32);
+  else ROTATE(64);
 #undef ROTATE
   if (BACK)
     hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)R.width, 2), dim3(256), 0, s, R, blocks);
   return hipGetLastError();
 }
 
-// Values per load: the widest (16 bytes, two values, one) that every run's alignment allows.
-int run_width(const Rotate &R, bool next, bool back, int size) {
-  for (int vw : {16 / size, 2, 1}) {
-    // halves: the second starts at `half`; neighbours: a run is turned as a whole or not at all
-    bool fits = (next ? 2 * R.half : R.half) % vw == 0;
-    for (const Side &S : R.side)
-      for (const als_heads *x : {&S.x, &S.out, back ? &S.dy : &S.x})
-        fits = fits && ((uintptr_t)x->data % (vw * size) == 0) && x->token_stride % vw == 0 &&
-               x->head_stride % vw == 0;
-    if (fits) return vw;
-  }
-  return 1;
+// Whether every run is whole and aligned at 16 bytes. Others go four values at a time: with eight
+// bf16, the values past a row's last whole run take up to seven loads of their own.
+bool whole_runs(const Rotate &R, bool next, bool back, int size) {
+  const int vw = 16 / size;
+  bool fits = R.width % vw == 0 && (next || R.half % vw == 0);
+  for (const Side &S : R.side)
+    for (const als_heads *x : {&S.x, &S.out, back ? &S.dy : &S.x})
+      fits = fits && (uintptr_t)x->data % 16 == 0 && x->token_stride % vw == 0 && x->head_stride % vw == 0;
+  return fits;
 }
 
 template <typename T, bool NEXT, bool BACK>
 hipError_t launch_next(const Rotate &R, int blocks, hipStream_t s) {
-  const int vw = run_width(R, NEXT, BACK, sizeof(T));
-  if (vw == 1) return launch_vw<T, 1, NEXT, BACK>(R, blocks, s);
-  if (vw == 2) return launch_vw<T, 2, NEXT, BACK>(R, blocks, s);
+  if (sizeof(T) == 4 || !whole_runs(R, NEXT, BACK, sizeof(T)))
+    return launch_vw<T, 4, NEXT, BACK>(R, blocks, s);
   return launch_vw<T, 16 / sizeof(T), NEXT, BACK>(R, blocks, s);
 }
 
