@@ -259,6 +259,7 @@ __global__ __launch_bounds__(256) void k_places(const int64_t *__restrict__ row_
 struct Args {
   AttentionPass p[3];
   int n;
+  int kp, vp;       // widths of the state that all of them are compiled for
   int shift;        // log2 of the tokens a segment
   int64_t slot0;    // first slot (or entry) of this launch
   int64_t n_slots;
@@ -701,10 +702,12 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP)) void k_attention(Args A) 
 
 // States after each segment alone -> states before each segment: one block (of blockIdx.y parts) a
 // head of a row, one thread four values of the state.
-__global__ __launch_bounds__(256) void k_join_segments(float *segments, const int64_t *row_ptr,
+__global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float *second_pass,
+                                                       const int64_t *row_ptr,
                                                        int64_t row0, int64_t n_tokens,
                                                        int64_t n_slots, int shift, int heads,
                                                        const float *log_decay, int64_t floats) {
+  float *segments = blockIdx.z ? second_pass : first_pass;
   const int64_t row = row0 + blockIdx.x / heads;
   const int head = (int)(blockIdx.x % heads);
   const int64_t first = clamped(row_ptr[row], 0, n_tokens);
@@ -736,9 +739,16 @@ __global__ __launch_bounds__(256) void k_join_segments(float *segments, const in
   }
 }
 
+// The gradients of shared heads: blockIdx.y: of k, of v.
 template <typename T>
-__global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ x, int64_t n, int group,
-                                                    int width, T *__restrict__ out) {
+__global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ of_k,
+                                                    const float *__restrict__ of_v, int64_t n_heads,
+                                                    int group, int k_width, int v_width,
+                                                    T *__restrict__ dk, T *__restrict__ dv) {
+  const float *x = blockIdx.y ? of_v : of_k;
+  T *out = blockIdx.y ? dv : dk;
+  const int width = blockIdx.y ? v_width : k_width;
+  const int64_t n = n_heads * width;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t head = i / width;
     const float *p = x + head * group * width + (i - head * width);
@@ -839,18 +849,17 @@ template <typename T, int KP, int VP> hipError_t launch_kv(Args A, bool split, h
     own.n = 0;
     for (int i = 0; i < A.n; ++i)
       if (!A.p[i].shares_segments) own.p[own.n++] = A.p[i];
-    if (own.n > 0) states(own);
-    for (int i = 0; i < own.n; ++i) {
-      const AttentionPass &P = own.p[i];
-      const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / heads;
-      for (int64_t r = 0; r < P.n_rows; r += per) {
-        const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
-        // parts of a state: as many as fill the chip, where rows and heads alone do not
-        const int64_t parts = n * heads >= 1024 ? 1 : (floats + 1023) / 1024;
-        hipLaunchKernelGGL(k_join_segments, dim3((unsigned)(n * heads), (unsigned)parts), dim3(256), 0,
-                           s, P.segments, P.row_ptr, r, P.n_tokens, A.n_slots, A.shift, heads,
-                           P.log_decay, floats);
-      }
+    states(own);  // of one pass, or two
+    const AttentionPass &P = own.p[0];
+    const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / heads;
+    for (int64_t r = 0; r < P.n_rows; r += per) {
+      const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
+      // parts of a state: as many as fill the chip, where rows and heads alone do not
+      const int64_t parts = n * heads >= 1024 ? 1 : (floats + 1023) / 1024;
+      hipLaunchKernelGGL(k_join_segments,
+                         dim3((unsigned)(n * heads), (unsigned)parts, (unsigned)own.n), dim3(256), 0, s,
+                         P.segments, own.n > 1 ? own.p[1].segments : nullptr, P.row_ptr, r, P.n_tokens,
+                         A.n_slots, A.shift, heads, P.log_decay, floats);
     }
   }
   outputs(A);
@@ -859,7 +868,7 @@ template <typename T, int KP, int VP> hipError_t launch_kv(Args A, bool split, h
 
 template <typename T, int KP>
 hipError_t launch_k(const Args &A, bool split, hipStream_t s) {
-  switch (padded_width3(A.p[0].v_width)) {
+  switch (A.vp) {
     case 32: return launch_kv<T, KP, 32>(A, split, s);
     case 64: return launch_kv<T, KP, 64>(A, split, s);
     default: return launch_kv<T, KP, 128>(A, split, s);
@@ -867,7 +876,7 @@ hipError_t launch_k(const Args &A, bool split, hipStream_t s) {
 }
 
 template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t s) {
-  switch (padded_width3(A.p[0].k_width)) {
+  switch (A.kp) {
     case 32: return launch_k<T, 32>(A, split, s);
     case 64: return launch_k<T, 64>(A, split, s);
     default: return launch_k<T, 128>(A, split, s);
@@ -921,34 +930,41 @@ hipError_t launch_attention(als_dtype dtype, const AttentionPass *p, int n, hipS
   A.entries = p[0].entries;
   const bool split = p[0].n_tokens > 1LL << A.shift;
   const int size = dtype == ALS_F32 ? 4 : 2;
-  for (int i = 0; i < n;) {  // neighbours of the same padded widths go in one launch
-    A.n = 0;
-    const int kp = padded_width3(p[i].k_width), vp = padded_width3(p[i].v_width);
-    for (; i < n && padded_width3(p[i].k_width) == kp && padded_width3(p[i].v_width) == vp; ++i) {
-      AttentionPass &x = A.p[A.n++] = p[i];
-      const auto vec = [&](const als_heads &h, int width) {
-        return aligned16(h.data, h.token_stride, h.head_stride, width, size);
-      };
-      x.vec_in = vec(x.q, x.k_width) && vec(x.k, x.k_width) && vec(x.v, x.v_width);
-      // row-major as the pass that forms them has them, its rows padded to its v_width
-      x.segment_ld[0] = x.shares_segments ? 1 : vp;
-      x.segment_ld[1] = x.shares_segments ? kp : 1;
-    }
-    const hipError_t e = dtype == ALS_F32 ? launch_t<float>(A, split, s) : launch_t<bf16>(A, split, s);
-    if (e != hipSuccess) return e;
+  // passes over a state and over its transpose share launches at the wider of its widths
+  int k = 0, v = 0;
+  for (int i = 0; i < n; ++i) {
+    k = p[i].k_width > k ? p[i].k_width : k;
+    v = p[i].v_width > v ? p[i].v_width : v;
   }
-  return hipSuccess;
+  A.kp = padded_width3(k);
+  A.vp = padded_width3(v);
+  A.n = n;
+  for (int i = 0; i < n; ++i) {
+    AttentionPass &x = A.p[i] = p[i];
+    const auto vec = [&](const als_heads &h, int width) {
+      return aligned16(h.data, h.token_stride, h.head_stride, width, size);
+    };
+    x.vec_in = vec(x.q, x.k_width) && vec(x.k, x.k_width) && vec(x.v, x.v_width);
+    // row-major as the pass that forms them has them, its rows padded
+    x.segment_ld[0] = x.shares_segments ? 1 : A.vp;
+    x.segment_ld[1] = x.shares_segments ? A.kp : 1;
+  }
+  return dtype == ALS_F32 ? launch_t<float>(A, split, s) : launch_t<bf16>(A, split, s);
 }
 
-hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,
-                             int32_t group, int32_t width, void *out, hipStream_t s) {
-  const int64_t n = n_tokens * (heads / group) * width;
-  if (n == 0) return hipSuccess;
-  const dim3 grid((unsigned)((n + 255) / 256 < 8192 ? (n + 255) / 256 : 8192));
+hipError_t launch_sum_groups(als_dtype dtype, const float *of_k, const float *of_v, int64_t n_tokens,
+                             int32_t heads, int32_t group, int32_t k_width, int32_t v_width, void *dk,
+                             void *dv, hipStream_t s) {
+  const int64_t n_heads = n_tokens * (heads / group);
+  if (n_heads == 0) return hipSuccess;
+  const int64_t blocks = (n_heads * (k_width > v_width ? k_width : v_width) + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192), 2);
   if (dtype == ALS_F32)
-    hipLaunchKernelGGL(k_sum_groups<float>, grid, dim3(256), 0, s, x, n, group, width, (float *)out);
+    hipLaunchKernelGGL(k_sum_groups<float>, grid, dim3(256), 0, s, of_k, of_v, n_heads, group, k_width,
+                       v_width, (float *)dk, (float *)dv);
   else
-    hipLaunchKernelGGL(k_sum_groups<bf16>, grid, dim3(256), 0, s, x, n, group, width, (bf16 *)out);
+    hipLaunchKernelGGL(k_sum_groups<bf16>, grid, dim3(256), 0, s, of_k, of_v, n_heads, group, k_width,
+                       v_width, (bf16 *)dk, (bf16 *)dv);
   return hipGetLastError();
 }
 

@@ -75,9 +75,10 @@ AttentionSpace attention_space(als_dtype dtype, int64_t n_tokens, int64_t n_rows
 hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s);
 // Up to three passes over the same rows and heads. One that shares segments comes after its owner.
 hipError_t launch_attention(als_dtype dtype, const AttentionPass *p, int n, hipStream_t s);
-// out[t, k, d] = sum over the head's group of x[t, k * group + i, d], in order.
-hipError_t launch_sum_groups(als_dtype dtype, const float *x, int64_t n_tokens, int32_t heads,
-                             int32_t group, int32_t width, void *out, hipStream_t s);
+// dk[t, h, d] = sum over the head's group of of_k[t, h * group + i, d], in order; dv likewise.
+hipError_t launch_sum_groups(als_dtype dtype, const float *of_k, const float *of_v, int64_t n_tokens,
+                             int32_t heads, int32_t group, int32_t k_width, int32_t v_width, void *dk,
+                             void *dv, hipStream_t s);
 hipError_t launch_attention_step(als_dtype dtype, int64_t n_rows, int32_t heads, int32_t group,
                                  int32_t k_width, int32_t v_width, const als_heads &q,
                                  const als_heads &k, const als_heads &v, const float *log_decay,

@@ -173,6 +173,11 @@ bool sane(const als_attention *s) {
 als::AttentionSpace space_of(const als_attention *s, als_dtype dtype) {
   return als::attention_space(dtype, s->n_tokens, s->n_rows, s->q_heads, s->k_width, s->v_width);
 }
+// Of passes over a state and its transpose.
+als::AttentionSpace backward_space(const als_attention *s, als_dtype dtype) {
+  const int32_t w = s->k_width > s->v_width ? s->k_width : s->v_width;
+  return als::attention_space(dtype, s->n_tokens, s->n_rows, s->q_heads, w, w);
+}
 // Of either type.
 int64_t space_bytes(const als_attention *s) {
   const int64_t a = space_of(s, ALS_F32).total(), b = space_of(s, ALS_BF16).total();
@@ -185,7 +190,7 @@ int64_t shared_bytes(const als_attention *s, int width) {
 int64_t backward_bytes(const als_attention *s) {  // the segments of two passes
   int64_t states = 0;
   for (als_dtype t : {ALS_F32, ALS_BF16}) {
-    const als::AttentionSpace x = space_of(s, t);
+    const als::AttentionSpace x = backward_space(s, t);
     states = x.total() + x.states > states ? x.total() + x.states : states;
   }
   return states + shared_bytes(s, s->k_width) + shared_bytes(s, s->v_width);
@@ -338,7 +343,7 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
                                       als_decay_attention_backward_workspace(s)))
     return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const als::AttentionSpace space = space_of(s, dtype);
+  const als::AttentionSpace space = backward_space(s, dtype);
   char *rest = (char *)workspace + space.total() + space.states;
   float *shared_k = group > 1 ? (float *)rest : nullptr;
   float *shared_v = group > 1 ? (float *)(rest + shared_bytes(s, s->k_width)) : nullptr;
@@ -388,9 +393,8 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
   hipError_t e = als::launch_places(dtype, p[0], stream);
   if (e == hipSuccess) e = als::launch_attention(dtype, p, 3, stream);
   if (e == hipSuccess && shared_k)
-    e = als::launch_sum_groups(dtype, shared_k, n, s->q_heads, group, s->k_width, dk, stream);
-  if (e == hipSuccess && shared_v)
-    e = als::launch_sum_groups(dtype, shared_v, n, s->q_heads, group, s->v_width, dv, stream);
+    e = als::launch_sum_groups(dtype, shared_k, shared_v, n, s->q_heads, group, s->k_width, s->v_width,
+                               dk, dv, stream);
   return launched(e, "als_decay_attention_backward");
 }
 
