@@ -485,7 +485,7 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  * Linear attention with a decay for each head: over the tokens t of a row,
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,
  * S being k_width x v_width; S before the first token is zero or initial_state.
- *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^31 - 1.
+ *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^30.
  *   q, k, v        token strides at most 2^22 values.
  *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
  *                  values out of [0, n_tokens] are taken as the nearest bound.
@@ -546,7 +546,7 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
  * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores
  *   scores[w] + logits[w, v] - log sum_u exp(logits[w, u]),
  * and the best `width` of all (w, v) go on, equal scores by the lowest (w, v).
- *   beams, width   1 .. 32. n_items 1 .. 2^31 - 1. n_lists 0 .. 2^31 - 1.
+ *   beams, width   1 .. 32. n_items 1 .. 2^31 - 1. n_lists 0 .. 2^31 - 1. Outputs overlap no input.
  *   logits         device [n_lists * beams, n_items], rows row_stride values apart. -inf and NaN mask
  *                  an item; +inf counts as the largest finite value.
  *   scores         device fp32 [n_lists, beams]; -inf or NaN: a dead beam, without candidates.

@@ -233,11 +233,11 @@ __device__ __forceinline__ Place find_place(const int64_t *__restrict__ row_ptr,
 // more rows than one step of the search covers, a block's search took about 4 us of a few chunks'
 // work (35 000 blocks of 4096 rows: 170 us), and this table one launch of 5 us for all of them.
 constexpr int64_t kSearchedRows = 64;
-__global__ __launch_bounds__(256) void k_places(const int64_t *__restrict__ row_ptr, int64_t n_rows,
-                                                int64_t n_tokens, int shift, int64_t n_slots,
+__global__ __launch_bounds__(256) void k_places(const int64_t *__restrict__ row_ptr, int64_t row0,
+                                                int64_t n_rows, int64_t n_tokens, int shift, int64_t n_slots,
                                                 int64_t n_entries, Place *__restrict__ places,
                                                 int32_t *__restrict__ entries) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  const int64_t row = row0 + (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (row >= n_rows) return;
   const int lane = (int)threadIdx.x & 63;
   Place p;
@@ -915,9 +915,12 @@ hipError_t launch_places(als_dtype dtype, const AttentionPass &p, hipStream_t s)
   if (!p.places) return hipSuccess;
   const int shift = attention_shift(dtype, p.n_tokens, p.heads);
   const int64_t entries = p.n_tokens >> shift;
-  hipLaunchKernelGGL(k_places, dim3((unsigned)((p.n_rows + 3) / 4)), dim3(256), 0, s, p.row_ptr,
-                     p.n_rows, p.n_tokens, shift, entries + p.n_rows, entries, (Place *)p.places,
-                     p.entries);
+  const int64_t per = max_blocks(256) * 4;  // rows a launch
+  for (int64_t r = 0; r < p.n_rows; r += per) {
+    const int64_t n = p.n_rows - r < per ? p.n_rows - r : per;
+    hipLaunchKernelGGL(k_places, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, p.row_ptr, r, p.n_rows,
+                       p.n_tokens, shift, entries + p.n_rows, entries, (Place *)p.places, p.entries);
+  }
   return hipGetLastError();
 }
 

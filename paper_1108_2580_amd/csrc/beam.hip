@@ -208,7 +208,7 @@ __device__ __forceinline__ bool better(const Candidate &a, const Candidate &b) {
 }
 
 __global__ __launch_bounds__(kMergeThreads) void k_merge(
-    int beams, int width, int slices, const float *__restrict__ scores,
+    int64_t list0, int beams, int width, int slices, const float *__restrict__ scores,
     const uint8_t *__restrict__ finished, int32_t end, const SliceStats *__restrict__ stats,
     const uint64_t *__restrict__ best, int32_t *__restrict__ parents, int32_t *__restrict__ tokens,
     float *__restrict__ scores_out, uint8_t *__restrict__ finished_out) {
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
   __shared__ uint32_t best_heads[kMergeThreads];
   __shared__ int n_found;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t list = blockIdx.x;
+  const int64_t list = list0 + blockIdx.x;
   scores += list * beams;
   if (finished) finished += list * beams;
   stats += list * beams * slices;
@@ -446,8 +446,12 @@ hipError_t launch_beam_select(als_dtype dtype, int64_t lists, int beams, int wid
       SLICES(bf16);
 #undef SLICES
   }
-  hipLaunchKernelGGL(k_merge, dim3((unsigned)lists), dim3(kMergeThreads), 0, s, beams, width, slices,
-                     scores, finished, end, stats, best, parents, tokens, scores_out, finished_out);
+  const int64_t merged = max_blocks(kMergeThreads);
+  for (int64_t l = 0; l < lists; l += merged) {
+    const int64_t n = lists - l < merged ? lists - l : merged;
+    hipLaunchKernelGGL(k_merge, dim3((unsigned)n), dim3(kMergeThreads), 0, s, l, beams, width, slices,
+                       scores, finished, end, stats, best, parents, tokens, scores_out, finished_out);
+  }
   return hipGetLastError();
 }
 

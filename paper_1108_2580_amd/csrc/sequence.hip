@@ -11,6 +11,7 @@ using als::fail_without_context;
 namespace {
 
 constexpr int64_t kMax31 = (1LL << 31) - 1;
+constexpr int64_t kMaxRows = 1LL << 30;  // of attention: with its segments below 2^31
 
 #define REQUIRE(cond, ...) \
   if (!(cond)) return fail_without_context(ALS_ERR_INVALID_ARG, __VA_ARGS__)
@@ -43,7 +44,8 @@ const char *wrong(const als_heads &x, int64_t n, int size) {
   if (n == 0) return nullptr;
   if (!x.data) return "NULL data";
   if (x.token_stride < 0 || x.head_stride < 0) return "a negative stride";
-  if (x.token_stride > (1LL << 40) || x.head_stride > (1LL << 40)) return "a stride out of range";
+  // the last value's offset stays far inside 64 bits
+  if (x.token_stride > (1LL << 56) / n || x.head_stride > (1LL << 40)) return "a stride out of range";
   if ((uintptr_t)x.data % size) return "data not aligned to its type";
   return nullptr;
 }
@@ -142,7 +144,7 @@ als_status check_both(const als_rotation *s, als_dtype dtype, const als_heads *x
 als_status check_attention(const als_attention *s, als_dtype dtype, bool step) {
   REQUIRE(s, "shape is NULL");
   if (als_status st = check_dtype(dtype)) return st;
-  REQUIRE(s->n_rows >= 0 && s->n_rows <= kMax31, "n_rows %lld out of range", (long long)s->n_rows);
+  REQUIRE(s->n_rows >= 0 && s->n_rows <= kMaxRows, "n_rows %lld out of range", (long long)s->n_rows);
   REQUIRE(s->q_heads >= 1 && s->q_heads <= 1024 && s->k_heads >= 1 &&
               s->q_heads % (s->k_heads > 0 ? s->k_heads : 1) == 0,
           "q_heads %d is not in [1, 1024] and a multiple of k_heads %d", s->q_heads, s->k_heads);
@@ -165,7 +167,7 @@ als_status check_input(const char *name, const als_heads &x, int64_t n, int size
 }
 
 bool sane(const als_attention *s) {
-  return s && s->n_tokens >= 0 && s->n_tokens <= kMax31 && s->n_rows >= 0 && s->n_rows <= kMax31 &&
+  return s && s->n_tokens >= 0 && s->n_tokens <= kMax31 && s->n_rows >= 0 && s->n_rows <= kMaxRows &&
          s->q_heads >= 1 && s->q_heads <= 1024 && s->k_heads >= 1 && s->k_width >= 1 &&
          s->k_width <= 128 && s->v_width >= 1 && s->v_width <= 128;
 }
@@ -421,6 +423,8 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
               !overlap(span(state, n_sources * one), span(state_out, s->n_rows * one)),
           "state_out overlaps state");
   const Span o = span(out, s->n_rows * s->q_heads * s->v_width * size);
+  REQUIRE(!overlap(o, span(state, n_sources * one)) && !overlap(o, span(state_out, s->n_rows * one)),
+          "out overlaps a state");
   REQUIRE(!overlap(o, span(q, s->n_rows, s->q_heads, s->k_width, size)) &&
               !overlap(o, span(k, s->n_rows, s->k_heads, s->k_width, size)) &&
               !overlap(o, span(v, s->n_rows, s->k_heads, s->v_width, size)),
@@ -440,7 +444,7 @@ static als_status check_beams(const als_beams *s) {
           "beams %d or width %d outside [1, %d]", s->beams, s->width, als::kMaxBeams);
   REQUIRE(s->n_items >= 1 && s->n_items <= kMax31, "n_items %lld out of range",
           (long long)s->n_items);
-  REQUIRE(s->row_stride >= s->n_items && s->row_stride <= (1LL << 40),
+  REQUIRE(s->row_stride >= s->n_items && s->row_stride <= (1LL << 56) / (s->n_lists * s->beams + 1),
           "row_stride %lld below n_items or out of range", (long long)s->row_stride);
   REQUIRE(s->end_token >= -1 && s->end_token < s->n_items, "end_token %d outside [-1, n_items)",
           s->end_token);
@@ -463,8 +467,19 @@ als_status als_beam_select(const als_beams *shape, als_dtype dtype, const void *
   if (s->n_lists == 0) return ALS_OK;
   REQUIRE(logits && scores && parents && tokens && scores_out && finished_out, "a NULL tensor");
   REQUIRE((uintptr_t)logits % size_of(dtype) == 0, "logits are not aligned to their type");
-  REQUIRE(scores != scores_out && finished != finished_out,
-          "scores_out or finished_out is the input itself");
+  const int64_t before = s->n_lists * s->beams, after = s->n_lists * s->width;
+  REQUIRE((uintptr_t)scores % 4 == 0 && (uintptr_t)scores_out % 4 == 0 && (uintptr_t)parents % 4 == 0 &&
+              (uintptr_t)tokens % 4 == 0,
+          "a tensor is not aligned to its type");
+  const Span ins[3] = {
+      span(logits, ((before - 1) * s->row_stride + s->n_items) * size_of(dtype)),
+      span(scores, 4 * before), span(finished, finished ? before : 0)};
+  const Span outs[4] = {span(parents, 4 * after), span(tokens, 4 * after), span(scores_out, 4 * after),
+                        span(finished_out, after)};
+  for (int i = 0; i < 4; ++i) {
+    for (const Span &x : ins) REQUIRE(!overlap(outs[i], x), "an output overlaps an input");
+    for (int j = 0; j < i; ++j) REQUIRE(!overlap(outs[i], outs[j]), "two outputs overlap");
+  }
   if (als_status st = check_workspace(
           workspace, workspace_bytes,
           als::beam_workspace(s->n_lists, s->beams, s->width, s->n_items)))
@@ -481,7 +496,7 @@ als_status als_reorder_states(int64_t n_lists, int32_t beams, int32_t width, int
   REQUIRE(n_lists >= 0 && n_lists <= kMax31, "n_lists %lld out of range", (long long)n_lists);
   REQUIRE(beams >= 1 && beams <= als::kMaxBeams && width >= 1 && width <= als::kMaxBeams,
           "beams %d or width %d outside [1, %d]", beams, width, als::kMaxBeams);
-  REQUIRE(row_bytes >= 0 && row_bytes <= (1LL << 40), "row_bytes %lld out of range",
+  REQUIRE(row_bytes >= 0 && row_bytes <= (1LL << 56) / (32 * (n_lists + 1)), "row_bytes %lld out of range",
           (long long)row_bytes);
   if (n_lists == 0 || row_bytes == 0) return ALS_OK;
   REQUIRE(src && dst && parents, "a NULL tensor");

@@ -170,6 +170,43 @@ def test_norm_rotate_without_tokens():
     assert (dw == 0).all() and (dv == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nb", [False, True])
+def test_norm_rotate_in_place(nb, dtype):
+    """Through the C entries, outputs that are the inputs themselves (views of one projection)."""
+    import ctypes
+
+    import paper_1108_2580_amd as p
+    from paper_1108_2580_amd import sequence as s
+
+    N, H, Hk, D, R = 50, 3, 2, 37, 30
+    both = torch.randn(N, H + Hk, D, device="cuda:0").to(DTYPES[dtype])
+    w = torch.rand(D, device="cuda:0") + 0.5
+    cos, sin = p.rotary_tables(9, R)
+    pos = torch.arange(N, dtype=torch.int32, device="cuda:0") % 9
+    args = (w, w, cos, sin, pos, 1e-6, nb)
+    want = p.norm_rotate(both[:, :H], both[:, H:], *args)
+    dy = torch.randn_like(both)
+    grads = p.norm_rotate_backward(dy[:, :H], dy[:, H:], both[:, :H], both[:, H:], *args)
+    shape = s._Rotation(N, 9, H, Hk, D, R, int(nb), 1e-6, pos.data_ptr(), cos.data_ptr(), sin.data_ptr())
+    heads = lambda t, h: s._Heads(t.data_ptr() + h * D * t.element_size(), (H + Hk) * D, D)  # noqa: E731
+    x, code = both.clone(), s._DTYPES[both.dtype]
+    assert p.lib.als_norm_rotate(shape, code, heads(x, 0), heads(x, H), w.data_ptr(), w.data_ptr(), heads(x, 0),
+                                 heads(x, H), s._stream(0)) == 0
+    assert torch.equal(x[:, :H], want[0]) and torch.equal(x[:, H:], want[1])
+    dw = torch.empty(2, D, device="cuda:0")
+    size = p.lib.als_norm_rotate_workspace(shape)
+    work = torch.empty(size, dtype=torch.uint8, device="cuda:0")
+    for into in (dy.clone(), both.clone()):  # over the outputs' gradients, and over the inputs
+        a, b = (into, both) if torch.equal(into, dy) else (dy, into)
+        assert p.lib.als_norm_rotate_backward(
+            shape, code, heads(a, 0), heads(a, H), heads(b, 0), heads(b, H), w.data_ptr(), w.data_ptr(),
+            heads(into, 0), heads(into, H), dw[0].data_ptr(), dw[1].data_ptr(), work.data_ptr(), size,
+            ctypes.c_void_p(s._stream(0))) == 0
+        assert torch.equal(into[:, :H], grads[0]) and torch.equal(into[:, H:], grads[1])
+        assert torch.equal(dw[0], grads[2]) and torch.equal(dw[1], grads[3])
+
+
 # ---- attention -----------------------------------------------------------------------------------
 
 def attention_reference(q, k, v, a, lens, scale, S0=None, d_out=None, dS=None):

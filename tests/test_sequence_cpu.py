@@ -78,7 +78,7 @@ def forward(shape, dtype=0, q=None, k=None, v=None, first=None, out=C, last=None
 
 
 @pytest.mark.parametrize("change,word", [
-    (dict(n_tokens=-1), "n_tokens"), (dict(n_rows=1 << 31), "n_rows"), (dict(q_heads=3), "multiple"),
+    (dict(n_tokens=-1), "n_tokens"), (dict(n_rows=(1 << 30) + 1), "n_rows"), (dict(q_heads=3), "multiple"),
     (dict(k_heads=0), "multiple"), (dict(k_width=129), "k_width"), (dict(v_width=0), "v_width"),
     (dict(scale=math.inf), "scale"), (dict(log_decay=None), "log_decay"), (dict(row_ptr=None), "row_ptr"),
     (dict(n_rows=0), "without rows")])
@@ -88,6 +88,7 @@ def test_attention_shapes(change, word):
 
 @pytest.mark.parametrize("change,word", [
     (dict(dtype=-1), "dtype"), (dict(v=_Heads(None, 64, 32)), "NULL"), (dict(out=None), "out"),
+    (dict(q=_Heads(A, (1 << 22) + 1, 64)), "token_stride"), (dict(k=_Heads(A, 1 << 50, 64)), "stride"),
     (dict(out=C + 1), "aligned"), (dict(out=A + 1024), "overlaps"), (dict(first=D, last=D + 64), "overlaps"),
     (dict(size=16), "workspace"), (dict(work=None), "workspace"), (dict(work=W + 4), "aligned")])
 def test_attention_tensors(change, word):
@@ -114,6 +115,7 @@ def test_attention_backward_and_step():
     refused(step(None, 3, None, C), "NULL")
     refused(step(B, 0, A, C), "without a state")
     refused(step(B, 3, None, C, A), "overlaps an input")
+    refused(step(B, 3, None, C, B + 16), "overlaps a state")
 
 
 def beams(**kw):
@@ -135,12 +137,14 @@ def test_beam_shapes(change, word):
 def test_beam_tensors():
     need = lib.als_beam_select_workspace(beams())
     call = lambda s=beams(), dtype=0, x=A, done=None, to=C, work=W, size=need: lib.als_beam_select(  # noqa: E731
-        s, dtype, x, B, done, C, C, to, D, work, size, None)
+        s, dtype, x, B, done, C + 4096, C + 8192, to, D, work, size, None)
     refused(call(dtype=7), "dtype")
     refused(call(x=None), "NULL")
     refused(call(x=A + 2), "aligned")
     refused(call(done=A), "end_token")
-    refused(call(to=B), "input itself")
+    refused(call(to=B + 8), "overlaps an input")
+    refused(call(to=C + 4096), "two outputs")
+    refused(call(to=C + 2), "aligned")
     refused(call(size=need - 1), "workspace")
     refused(lib.als_reorder_states(2, 4, 4, 64, A, A + 64, B, None), "overlaps")
     refused(lib.als_reorder_states(2, 4, 5, 64, A, A, B, None), "overlaps")
@@ -182,3 +186,67 @@ def test_structures_match_the_header():
         for f, _ in t._fields_:
             assert int(said[f"{c}.{f}"]) == getattr(t, f).offset
     assert sequence.MAX_BEAMS == 32
+
+
+# ---- grids: launches of more threads than one HIP grid holds (2^32 - 1) go in slices ---------------
+
+LAUNCH = """
+import ctypes, sys
+ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+sys.path.insert(0, sys.argv[2])
+lib = ctypes.CDLL(sys.argv[3])
+lib.als_last_error.restype = ctypes.c_char_p
+class H(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("t", ctypes.c_int64), ("h", ctypes.c_int64)]
+class S(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_int64), ("b", ctypes.c_int64), ("p", ctypes.c_void_p), ("l", ctypes.c_void_p),
+                ("qh", ctypes.c_int32), ("kh", ctypes.c_int32), ("k", ctypes.c_int32), ("v", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+class B(ctypes.Structure):
+    _fields_ = [("lists", ctypes.c_int64), ("items", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("beams", ctypes.c_int32), ("width", ctypes.c_int32), ("end", ctypes.c_int32)]
+P, i64 = ctypes.c_void_p, ctypes.c_int64
+at = lambda n: (n + 1) << 50
+case, n = sys.argv[4], int(sys.argv[5])
+if case == "rows":  # n rows of one token
+    s = S(n, n, at(0), at(1), 4, 4, 8, 8, 1.0)
+    h = lambda i: H(at(i), 32, 8)
+    lib.als_decay_attention.argtypes = [P, ctypes.c_int, H, H, H, P, P, P, P, i64, P]
+    st = lib.als_decay_attention(ctypes.byref(s), 0, h(2), h(3), h(4), None, at(5), None, at(6), 1 << 50, None)
+elif case == "step":
+    s = S(0, n, None, at(1), 4, 4, 8, 8, 1.0)
+    h = lambda i: H(at(i), 32, 8)
+    lib.als_decay_attention_step.argtypes = [P, ctypes.c_int, H, H, H, P, i64, P, P, P, P]
+    st = lib.als_decay_attention_step(ctypes.byref(s), 0, h(2), h(3), h(4), at(5), n, None, at(6), at(7), None)
+else:
+    s = B(n, 5000, 5000, 2, 2, -1)
+    lib.als_beam_select.argtypes = [P, ctypes.c_int] + [P] * 8 + [i64, P]
+    st = lib.als_beam_select(ctypes.byref(s), 0, at(0), at(1), None, at(2), at(3), at(4), at(5), at(6), 1 << 50, None)
+if st:
+    sys.exit(lib.als_last_error(None).decode())
+"""
+
+
+@pytest.mark.parametrize("case,n,totals", [
+    # places (4 rows a block), segments' states, their join, outputs: heads * slots
+    ("rows", 3_000_000, None), ("rows", 400_000_000, None),
+    ("step", 1000, {256: 4000}), ("step", 5_000_000, {256: 20_000_000}),
+    ("beam", 1000, {256: 4000, 1024: 1000}), ("beam", 6_000_000, {256: 24_000_000, 1024: 6_000_000})])
+def test_grids_hold_their_threads(case, n, totals, tmp_path):
+    import os
+    import subprocess
+    import sys
+
+    here = os.path.dirname(os.path.abspath(__file__))
+    so = str(tmp_path / "librecorder.so")
+    subprocess.check_call(["gcc", "-O1", "-shared", "-fPIC", "-o", so, os.path.join(here, "launch_recorder.c")])
+    r = subprocess.run([sys.executable, "-c", LAUNCH, so, os.path.dirname(here), p.LIB_PATH, case, str(n)],
+                       capture_output=True, text=True, env=dict(os.environ, RECORDED_ARGS="0"))
+    assert r.returncode == 0, r.stderr
+    out = [[int(w) for w in line.split()] for line in r.stdout.splitlines()]
+    assert out and all(threads * blocks < 2 ** 32 for threads, blocks in out)
+    if totals:
+        seen = {}
+        for threads, blocks in out:
+            seen[threads] = seen.get(threads, 0) + blocks
+        assert seen == totals
