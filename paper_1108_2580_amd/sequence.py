@@ -79,8 +79,9 @@ def _check(status):
         raise ALSError(status, lib.als_last_error(None).decode())
 
 
-# A token's calls are bound by the host. The current stream's handle by itself takes a fifth of the
-# time of the Stream object around it.
+# A token's calls are bound by the host: the current device and the current stream's handle by
+# themselves take a fifth of the time of what torch.cuda has around them.
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -92,7 +93,7 @@ def _device(t, name):
     """The current device's index, on which t has to lie."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    device = torch.cuda.current_device()
+    device = _raw_device()
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, not on the current device")
     return device
@@ -115,12 +116,12 @@ def _heads(t, name, dtype, device):
         _device(t, name)
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != 3:
+    stride = t.stride()
+    if len(stride) != 3:
         raise ValueError(f"{name} must have the dimensions tokens, heads, width")
-    token, head, feature = t.stride()
-    if feature != 1 and t.shape[2] > 1:
+    if stride[2] != 1 and t.shape[2] > 1:
         raise TypeError(f"the features of {name} must be contiguous")
-    return _Heads(t.data_ptr(), token, head)
+    return _Heads(t.data_ptr(), stride[0], stride[1])
 
 
 def _dtype(t, name):
@@ -173,8 +174,8 @@ def _rotation(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours):
 
 def _packed(t):
     """A new tensor like t, tokens one after the other, and its strides."""
-    out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
     _, H, D = t.shape
+    out = t.new_empty(t.shape)
     return out, _Heads(out.data_ptr(), H * D, D)
 
 
@@ -246,11 +247,13 @@ class _NormRotate(torch.autograd.Function):
 def _attention(q, k, v, log_decay, row_ptr, scale):
     dev = _device(q, "q")
     code = _dtype(q, "q")
-    hq, hk, hv = (_heads(t, n, q.dtype, dev) for t, n in ((q, "q"), (k, "k"), (v, "v")))
+    dtype = q.dtype
+    hq, hk, hv = _heads(q, "q", dtype, dev), _heads(k, "k", dtype, dev), _heads(v, "v", dtype, dev)
     N, Hq, K = q.shape
-    _, Hk, V = v.shape
-    _shaped(k, "k", (N, Hk, K))
-    _shaped(v, "v", (N, Hk, V))
+    n, Hk, V = v.shape
+    if n != N or k.shape != (N, Hk, K):
+        raise ValueError(f"q, k and v have shapes {tuple(q.shape)}, {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
     rows = N
     if row_ptr is not None:
         if not isinstance(row_ptr, torch.Tensor) or row_ptr.dim() != 1 or row_ptr.numel() < 1:
@@ -274,7 +277,7 @@ def _new_state(shape, device):
 def _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state):
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
     first = _state_ptr(initial_state, "initial_state", shape, dev)
-    out = torch.empty((q.shape[0], shape.q_heads, shape.v_width), dtype=q.dtype, device=q.device)
+    out = q.new_empty((q.shape[0], shape.q_heads, shape.v_width))
     state = _new_state(shape, q.device) if return_state else None
     size = lib.als_decay_attention_workspace(shape)
     work = _workspace(size, q.device)
@@ -314,7 +317,7 @@ def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, ini
     _shaped(d_out, "d_out", (q.shape[0], shape.q_heads, shape.v_width))
     first = _state_ptr(initial_state, "initial_state", shape, dev)
     last = _state_ptr(dstate, "dstate", shape, dev)
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     wanted = initial_state is not None if d_initial is None else d_initial
     dfirst = _new_state(shape, q.device) if wanted else None
     size = lib.als_decay_attention_backward_workspace(shape)
@@ -354,19 +357,17 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
     parent; one outside it gives NaN); ``state`` may then have another number of rows, and
     ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out)."""
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
-    _device(state, "state")
-    if state.dim() != 4:
-        raise ValueError("state must have the dimensions rows, heads, key width, value width")
-    N, one = shape.n_rows, (shape.q_heads, shape.k_width, shape.v_width)
+    N, H, K, V = shape.n_rows, shape.q_heads, shape.k_width, shape.v_width
     sources, src = N, None
     if source is not None:
-        sources = state.shape[0]
+        _device(state, "state")
+        sources = state.shape[0] if state.dim() else 0
         src = _array(source, "source", torch.int32, (N,), dev)
-    sp = _array(state, "state", torch.float32, (sources, *one), dev)
+    sp = _array(state, "state", torch.float32, (sources, H, K, V), dev)
     if state_out is None:
         state_out = state if source is None else _new_state(shape, q.device)
-    to = _array(state_out, "state_out", torch.float32, (N, *one), dev)
-    out = torch.empty((N, one[0], one[2]), dtype=q.dtype, device=q.device)
+    to = sp if state_out is state else _array(state_out, "state_out", torch.float32, (N, H, K, V), dev)
+    out = q.new_empty((N, H, V))
     _check(lib.als_decay_attention_step(shape, code, hq, hk, hv, sp, sources, src, to, out.data_ptr(),
                                         _stream(dev)))
     return out, state_out
@@ -406,8 +407,7 @@ def beam_select(logits, scores, finished=None, end_token=-1, width=None):
     if size < 0:
         raise ALSError(ALS_ERR_INVALID_ARG, lib.als_last_error(None).decode())
     device = logits.device
-    parents = torch.empty((B, width), dtype=torch.int32, device=device)
-    tokens = torch.empty((B, width), dtype=torch.int32, device=device)
+    parents, tokens = torch.empty((2, B, width), dtype=torch.int32, device=device).unbind()
     new = torch.empty((B, width), device=device)
     done = torch.empty((B, width), dtype=torch.bool, device=device)
     work = _workspace(size, device)
