@@ -43,31 +43,39 @@ template <typename T, int VW> struct Run {
   using V = T __attribute__((ext_vector_type(VW)));
   using U = V __attribute__((aligned(sizeof(T))));
 };
-// VW values from p, zero past `left` of them.
-template <typename T, int VW> __device__ __forceinline__ void load(const T *p, int left, float (&x)[VW]) {
+// VW values from p, zero past `left` of them. Without CUT there are VW or none.
+template <typename T, int VW, bool CUT>
+__device__ __forceinline__ void load(const T *p, int left, float (&x)[VW]) {
   if (left >= VW) {
     const typename Run<T, VW>::V v = *(const typename Run<T, VW>::U *)p;
 #pragma unroll
     for (int e = 0; e < VW; ++e) x[e] = (float)v[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < VW - 1; ++e) x[e] = e < left ? (float)p[e] : 0.f;
-    x[VW - 1] = 0.f;
+    for (int e = 0; e < VW; ++e) x[e] = CUT && e < VW - 1 && e < left ? (float)p[e] : 0.f;
   }
 }
-template <typename T, int VW>
+template <typename T, int VW, bool CUT>
 __device__ __forceinline__ void store(T *p, int left, const float (&x)[VW]) {
   if (left >= VW) {
     typename Run<T, VW>::V v;
 #pragma unroll
     for (int e = 0; e < VW; ++e) v[e] = (T)x[e];
     *(typename Run<T, VW>::U *)p = v;
-  } else {
+  } else if (CUT) {
 #pragma unroll
     for (int e = 0; e < VW - 1; ++e)
       if (e < left) p[e] = (T)x[e];
   }
 }
+
+// How a row's runs of VW values meet its end, and a half's:
+enum Ends {
+  kWhole,   // they end with it
+  kOver,    // the last one starts early, over values of the run before it, which both lanes form and
+            // write alike; `skip` of them count in the other lane's sums alone
+  kCut,     // the last one is short and goes value by value: rows and halves shorter than a run
+};
 
 // Where a lane's unit lies in a row: two runs of VW values. Of a lane group, runs a lie side by side,
 // and so do runs b, so that each load and store of the group is one piece of memory. Turned pairs lie
@@ -75,30 +83,36 @@ __device__ __forceinline__ void store(T *p, int left, const float (&x)[VW]) {
 struct Unit {
   int a, b;            // first features of the runs
   int left_a, left_b;  // values there, at most VW count
+  int skip_a, skip_b;
   bool turned;
 };
-template <int VW, bool NEXT, int G>
+template <int VW, bool NEXT, Ends ENDS, int G>
 __device__ __forceinline__ Unit unit_of(int lane, int width, int half) {
   Unit x;
-  if (NEXT) {
-    x.a = lane * VW;
-    x.b = x.a + G * VW;
-    x.left_a = width - x.a;
-    x.left_b = width - x.b;
-    x.turned = true;
-  } else {
-    const int pairs = (half + VW - 1) / VW;
-    x.turned = lane < pairs;
-    if (x.turned) {
-      x.a = lane * VW;
-      x.b = half + lane * VW;
-      x.left_a = x.left_b = half - lane * VW;
-    } else {
-      x.a = 2 * half + (lane - pairs) * 2 * VW;
-      x.b = x.a + VW;
-      x.left_a = width - x.a;
-      x.left_b = width - x.b;
+  x.skip_a = x.skip_b = 0;
+  const auto run = [&](int from, int end, int &at, int &left, int &skip) {
+    at = from;
+    left = end - from;
+    if (ENDS == kOver && left > 0 && left < VW) {
+      skip = VW - left;
+      at = end - VW;
+      left = VW;
     }
+  };
+  const int pairs = (half + VW - 1) / VW;
+  x.turned = NEXT || lane < pairs;
+  if (NEXT) {
+    run(lane * VW, width, x.a, x.left_a, x.skip_a);
+    run(lane * VW + G * VW, width, x.b, x.left_b, x.skip_b);
+  } else if (x.turned) {
+    run(lane * VW, half, x.a, x.left_a, x.skip_a);
+    x.b = half + x.a;
+    x.left_b = x.left_a;
+    x.skip_b = x.skip_a;
+  } else {
+    const int from = 2 * half + (lane - pairs) * 2 * VW;
+    run(from, width, x.a, x.left_a, x.skip_a);
+    run(from + VW, width, x.b, x.left_b, x.skip_b);
   }
   return x;
 }
@@ -153,14 +167,14 @@ template <int G> __device__ __forceinline__ float group_sum(float x) {
 }
 
 // blockIdx.y: queries or keys; blockIdx.x: a run of tokens. G lanes a row, a unit a lane.
-template <typename T, int VW, bool NEXT, int G, bool BACK>
+template <typename T, int VW, bool NEXT, Ends ENDS, int G, bool BACK>
 __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
   const Side &S = R.side[blockIdx.y];
   const int tid = (int)threadIdx.x, lane = tid % G;
   const int64_t t0 = (int64_t)blockIdx.x * R.tokens_per_block;
   const int64_t t1 = t0 + R.tokens_per_block < R.n_tokens ? t0 + R.tokens_per_block : R.n_tokens;
   const int rows = (int)(t1 > t0 ? t1 - t0 : 0) * S.heads;
-  const Unit u = unit_of<VW, NEXT, G>(lane, R.width, R.half);
+  const Unit u = unit_of<VW, NEXT, ENDS, G>(lane, R.width, R.half);
   float wa[VW], wb[VW], ga[VW], gb[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
@@ -181,15 +195,18 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     const bool ok = at >= 0 && at < R.n_positions;
     const float *cs = R.cos + (ok ? at : 0) * R.half, *sn = R.sin + (ok ? at : 0) * R.half;
     float xa[VW], xb[VW], da[VW], db[VW];
-    load<T, VW>(x + u.a, u.left_a, xa);
-    load<T, VW>(x + u.b, u.left_b, xb);
+    load<T, VW, ENDS == kCut>(x + u.a, u.left_a, xa);
+    load<T, VW, ENDS == kCut>(x + u.b, u.left_b, xb);
     if (BACK) {
-      load<T, VW>(dy + u.a, u.left_a, da);
-      load<T, VW>(dy + u.b, u.left_b, db);
+      load<T, VW, ENDS == kCut>(dy + u.a, u.left_a, da);
+      load<T, VW, ENDS == kCut>(dy + u.b, u.left_b, db);
     }
     float squares = 0.f, along = 0.f;
 #pragma unroll
-    for (int e = 0; e < VW; ++e) squares = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], squares));
+    for (int e = 0; e < VW; ++e) {
+      if (e >= u.skip_a) squares = fmaf(xa[e], xa[e], squares);
+      if (e >= u.skip_b) squares = fmaf(xb[e], xb[e], squares);
+    }
     squares = group_sum<G>(squares);
     // a position outside the tables makes its rows NaN
     const float r = ok ? 1.f / sqrtf(squares / (float)R.width + R.eps) : __builtin_nanf("");
@@ -208,7 +225,8 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
         gb[e] = fmaf(db[e], xb[e] * r, gb[e]);
         da[e] *= wa[e];
         db[e] *= wb[e];
-        along = fmaf(da[e], xa[e], fmaf(db[e], xb[e], along));
+        if (e >= u.skip_a) along = fmaf(da[e], xa[e], along);
+        if (e >= u.skip_b) along = fmaf(db[e], xb[e], along);
       }
       along = group_sum<G>(along);
       const float f = r * r * r * (along / (float)R.width);
@@ -218,8 +236,8 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
         xb[e] = db[e] * r - xb[e] * f;
       }
     }
-    store<T, VW>(out + u.a, u.left_a, xa);
-    store<T, VW>(out + u.b, u.left_b, xb);
+    store<T, VW, ENDS == kCut>(out + u.a, u.left_a, xa);
+    store<T, VW, ENDS == kCut>(out + u.b, u.left_b, xb);
     token += token_step;
     head += head_step;
     if (head >= S.heads) {
@@ -236,9 +254,9 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
     }
     __syncthreads();
     for (int i = tid; i < G * 2 * VW; i += kBlock) {
-      const Unit v = unit_of<VW, NEXT, G>(i / (2 * VW), R.width, R.half);
+      const Unit v = unit_of<VW, NEXT, ENDS, G>(i / (2 * VW), R.width, R.half);
       const int run = i / VW % 2, e = i % VW;
-      if (e >= (run ? v.left_b : v.left_a)) continue;
+      if (e >= (run ? v.left_b : v.left_a) || e < (run ? v.skip_b : v.skip_a)) continue;
       float sum = 0.f;
       for (int j = 0; j < kBlock / G; ++j) sum += sums[j][i];
       S.partial[(int64_t)blockIdx.x * R.width + (run ? v.b : v.a) + e] = sum;
@@ -261,11 +279,11 @@ __global__ __launch_bounds__(256) void k_sum_partials(Rotate R, int blocks) {
   if (threadIdx.x == 0) S.dweight[blockIdx.x] = (float)sums[0];
 }
 
-template <typename T, int VW, bool NEXT, bool BACK>
+template <typename T, int VW, bool NEXT, Ends ENDS, bool BACK>
 hipError_t launch_vw(const Rotate &R, int blocks, hipStream_t s) {
   const int units = units_in<VW, NEXT>(R.width, R.half);
   const dim3 grid((unsigned)blocks, 2);
-#define ROTATE(G) hipLaunchKernelGGL((k_rotate<T, VW, NEXT, G, BACK>), grid, dim3(kBlock), 0, s, R)
+#define ROTATE(G) hipLaunchKernelGGL((k_rotate<T, VW, NEXT, ENDS, G, BACK>), grid, dim3(kBlock), 0, s, R)
   if (units <= 4) ROTATE(4);
   else if (units <= 8) ROTATE(8);
   else if (units <= 16) ROTATE(16);
@@ -277,8 +295,7 @@ hipError_t launch_vw(const Rotate &R, int blocks, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Whether every run is whole and aligned at 16 bytes. Others go four values at a time: with eight
-// bf16, the values past a row's last whole run take up to seven loads of their own.
+// Whether every run is whole and aligned at 16 bytes.
 bool whole_runs(const Rotate &R, bool next, bool back, int size) {
   const int vw = 16 / size;
   bool fits = R.width % vw == 0 && (next || R.half % vw == 0);
@@ -287,12 +304,20 @@ bool whole_runs(const Rotate &R, bool next, bool back, int size) {
       fits = fits && (uintptr_t)x->data % 16 == 0 && x->token_stride % vw == 0 && x->head_stride % vw == 0;
   return fits;
 }
+// Whether the last run of the row and of each half can start early.
+bool over_runs(const Rotate &R, bool next, int vw) {
+  const int rest = R.width - 2 * R.half;
+  return next ? R.width >= vw && R.width % 2 == 0
+              : (R.half == 0 || R.half >= vw) && (rest == 0 || rest >= vw);
+}
 
 template <typename T, bool NEXT, bool BACK>
 hipError_t launch_next(const Rotate &R, int blocks, hipStream_t s) {
-  if (sizeof(T) == 4 || !whole_runs(R, NEXT, BACK, sizeof(T)))
-    return launch_vw<T, 4, NEXT, BACK>(R, blocks, s);
-  return launch_vw<T, 16 / sizeof(T), NEXT, BACK>(R, blocks, s);
+  constexpr int VW = 16 / sizeof(T);
+  if (whole_runs(R, NEXT, BACK, sizeof(T))) return launch_vw<T, VW, NEXT, kWhole, BACK>(R, blocks, s);
+  if (over_runs(R, NEXT, VW)) return launch_vw<T, VW, NEXT, kOver, BACK>(R, blocks, s);
+  // cut runs of eight would take seven loads each
+  return launch_vw<T, 4, NEXT, kCut, BACK>(R, blocks, s);
 }
 
 }  // namespace

@@ -83,7 +83,9 @@ ROTATE = [  # tokens, heads, key heads, width, rotated, neighbours
     (1, 1, 1, 1, 0, False), (1, 2, 1, 2, 2, True), (3, 4, 2, 64, 64, False), (5, 8, 8, 64, 32, True),
     (130, 3, 1, 100, 100, False), (67, 5, 5, 33, 30, False), (67, 2, 1, 33, 32, True),
     (1000, 4, 4, 128, 128, False), (33, 2, 2, 256, 250, False), (20, 2, 2, 255, 254, True),
-    (4099, 2, 1, 20, 8, False), (9, 1, 1, 20, 0, False)]
+    (4099, 2, 1, 20, 8, False), (9, 1, 1, 20, 0, False),
+    (40, 3, 2, 100, 60, True), (70, 2, 1, 42, 38, True), (90, 2, 2, 77, 40, False), (33, 1, 1, 12, 0, False),
+    (50, 2, 2, 90, 90, True), (21, 4, 1, 9, 8, True)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -171,15 +173,15 @@ def test_norm_rotate_without_tokens():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("nb", [False, True])
-def test_norm_rotate_in_place(nb, dtype):
+@pytest.mark.parametrize("nb,D,R", [(False, 37, 30), (True, 37, 30), (False, 44, 22), (True, 44, 26)])
+def test_norm_rotate_in_place(nb, D, R, dtype):
     """Through the C entries, outputs that are the inputs themselves (views of one projection)."""
     import ctypes
 
     import paper_1108_2580_amd as p
     from paper_1108_2580_amd import sequence as s
 
-    N, H, Hk, D, R = 50, 3, 2, 37, 30
+    N, H, Hk = 50, 3, 2
     both = torch.randn(N, H + Hk, D, device="cuda:0").to(DTYPES[dtype])
     w = torch.rand(D, device="cuda:0") + 0.5
     cos, sin = p.rotary_tables(9, R)
