@@ -357,16 +357,30 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   }
 };
 
-// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, three where
-// LDS holds no more, two where few threads hold the pieces.
-template <typename T> constexpr int waves_for(int VP) {
-  return VP == 32 ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
+// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, three for
+// f32's parts at 64 wide, two where few threads hold the pieces; never more than LDS has room for.
+template <typename T> constexpr int waves_for(int KP, int VP) {
+  constexpr int C = chunk_tokens<T>(), NT = C / 16;
+  const int bytes = kParts<T> * (4 * C * padded<bf16>(KP) + NT * (NT + 1) * 256) +
+                    C * padded<T>(VP) * (int)sizeof(T);
+  const int room = (160 * 1024 / bytes * (VP / 16) + 3) / 4;
+  const int most = VP == 32 ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
+  return room < most ? room : most;
 }
 
 // One block: one head of one segment. STATES: only the state after the segment, for all segments of
 // a row but its last.
+//
+// What bounds it: neither HBM nor MFMA alone. A wave's chunk is a chain (LDS writes, barrier, weights,
+// barrier, products, update) that the other blocks of its CU have to cover: four of four waves for bf16
+// at 64 wide. Measured there, 4096 rows of 263 tokens, 8 heads: 1283 us forward (q, k, v and o move at
+// 3.4 TB/s of a copy's 4.8), 2807 us for the three passes backward (the seven tensors at 2.7 TB/s; read
+// from HBM once for all passes that share them, since those run side by side); one row of 62496: 61 us
+// after 28 us of states. f32 at 128 wide, 100 rows of 1000, 8 heads to 2 key heads: 532 us forward, 1754
+// us backward at two blocks a CU, which LDS allows. One chunk a row (2000 f32 rows of 25 at 33 x 50):
+// 132 us, the latency of a block from its first load to its last store, three blocks a CU.
 template <typename T, int KP, int VP, bool STATES, bool VEC>
-__global__ __launch_bounds__(VP * 4, waves_for<T>(VP)) void k_attention(Args A) {
+__global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
   constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<bf16>(KP), LV = padded<T>(VP);
   constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, KPART = C * LK;
@@ -701,7 +715,8 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(VP)) void k_attention(Args A) 
 }
 
 // States after each segment alone -> states before each segment: one block (of blockIdx.y parts) a
-// head of a row, one thread four values of the state.
+// head of a row, one thread four values of the state. Bound by the latency of a long row's reads, 16 at
+// a time: 15 us for 8 heads' 122 states of 64 x 64 (31 MB moved); where rows are many, by HBM.
 __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float *second_pass,
                                                        const int64_t *row_ptr,
                                                        int64_t row0, int64_t n_tokens,
@@ -739,7 +754,10 @@ __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float 
   }
 }
 
-// The gradients of shared heads: blockIdx.y: of k, of v.
+// The gradients of shared heads: blockIdx.y: of k, of v. A group's heads are other blocks of the pass,
+// with decays of their own, so each leaves its part in fp32 and they are added here in their order
+// (atomics would change the result from run to run). Bound by HBM: 217 us for 8 heads to 2 of 100 003
+// tokens at 128 wide in f32, 4.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ of_k,
                                                     const float *__restrict__ of_v, int64_t n_heads,
@@ -759,7 +777,8 @@ __global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ of
 }
 
 // One token: S' = e^a S + k v^T, o = scale S'^T q. One block a head of a row; the state is read and
-// written once. Thread: VW neighbouring columns, every (256 / lanes)-th row.
+// written once. Thread: VW neighbouring columns, every (256 / lanes)-th row. Bound by HBM: 188 us for
+// 4096 rows of 8 heads of 64 x 64, 5.7 TB/s; 4.7 us, a launch, for 8 rows.
 template <typename T, int VW>
 __global__ __launch_bounds__(256) void k_step(int64_t row0, int heads, int group, int K, int V, als_heads q,
                                               als_heads k, als_heads v,
@@ -887,10 +906,11 @@ template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t
 
 // Short segments fill the chip where tokens are few; each costs a pass over its k and v and a state
 // written and read. From four chunks up, as many as leave 1024 blocks (bf16: what the chip holds at
-// a time) or 2048 (f32, whose chunks are half as long), at most 2048 tokens. Us with segments of 256, 512, 1024
-// and 2048: one row of 62496 bf16 tokens, 8 heads of 64 142, 126, 115, -; forward and backward of 4096
-// rows of 263 -, 5800, 5275, 5213 (4096: 5640); 100 f32 rows of 1000 at 128 wide -, 3860, 4037, -; 8
-// bf16 rows of 250 33, 42, 72, -.
+// a time) or 2048 (f32, whose chunks are half as long), at most 2048 tokens. Us with segments of 256,
+// 512, 1024 and 2048 tokens: one row of 62496 bf16 tokens, 8 heads of 64: 133, 119, 120, 169; forward
+// and backward of 4096 such rows of 263: 5430, 4620, 4180, 4000 (4096: 3990); of 100 f32 rows of 1000,
+// 8 heads of 128: 2900, 2650, 2590, 2810, of 1000 f32 rows of 262, 8 heads of 64: 2450, 2230, 2110,
+// 2160; forward of 8 bf16 rows of 250: 32, 47, 78, 77.
 int attention_shift(als_dtype dtype, int64_t n_tokens, int32_t heads) {
   int shift = dtype == ALS_F32 ? 7 : 8;
   while (shift < 11 && (n_tokens >> shift) * heads > (dtype == ALS_F32 ? 2048 : 1024)) ++shift;

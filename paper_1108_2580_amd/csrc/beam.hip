@@ -76,6 +76,10 @@ struct SliceStats {
   float max, sum;  // of the slice; sum of exp(x - max)
 };
 
+// Bound by reading the logits: 72 us for 8 lists of 16 beams of 624 961 items in f32, a tenth of them
+// finished: 4.0 TB/s, what a large sum reaches; 13.7 us for 32 lists of 8 of 50 000 in bf16, where few
+// waves of blocks leave the latency of each one's load, maximum and ranking in sight; 4.7 us for one
+// list of 4 of 1000.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_slices(const T *__restrict__ logits, int64_t n_items,
                                                      int64_t row_stride, int slices, int width,
@@ -207,6 +211,8 @@ __device__ __forceinline__ bool better(const Candidate &a, const Candidate &b) {
   return a.score > b.score || (a.score == b.score && a.place < b.place);
 }
 
+// One block a list, for whom it is a chain of latencies (statistics, log-sum-exp, heads, candidates,
+// ranks): 6.7 us for 4 lists of candidates, 7.1 us for 104 (8 beams), 14.5 us for 2448 (16 beams).
 __global__ __launch_bounds__(kMergeThreads) void k_merge(
     int64_t list0, int beams, int width, int slices, const float *__restrict__ scores,
     const uint8_t *__restrict__ finished, int32_t end, const SliceStats *__restrict__ stats,
@@ -354,7 +360,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
   }
 }
 
-// Copies rows of `bytes` bytes, a V at a time: row w of list b from row parents[b, w].
+// Copies rows of `bytes` bytes, a V at a time: row w of list b from row parents[b, w]. 10.2 us for 256
+// rows of 131 kB, 6.6 TB/s (some of it from the caches).
 template <typename V>
 __global__ __launch_bounds__(256) void k_reorder(const V *src, V *dst, int64_t n, int64_t row0,
                                                  int beams, int width,
