@@ -186,6 +186,12 @@ __device__ __forceinline__ constexpr int state_row(int kt, int g, int e) {
 // Padding of a staged row: with it the four lane groups and the rows of one LDS read fall on
 // different banks.
 template <typename T> constexpr int padded(int width) { return width + (sizeof(T) == 2 ? 16 : 4); }
+// Of rows of q and k. Three parts of them at up to 64 wide leave a CU a fourth block with half the
+// padding, which is worth more than the conflicts cost: 2000 rows of 25 at 33 x 50 171 -> 155 us, forward
+// and backward of 400 rows of 250 at 32 x 32 463 -> 440 us; at 128 wide it frees nothing (2860 -> 2970).
+template <typename T> constexpr int key_row(int KP, int VP) {
+  return KP + (sizeof(T) == 4 && KP < 128 && VP < 128 ? 8 : 16);
+}
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
@@ -357,14 +363,14 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   }
 };
 
-// Waves a SIMD to compile for: four (128 registers) where the pieces of a chunk fit them, three for
-// f32's parts at 64 wide, two where few threads hold the pieces; never more than LDS has room for.
+// Waves a SIMD to compile for: four (128 registers), two where few threads hold the pieces of a chunk,
+// and never more than LDS has room for.
 template <typename T> constexpr int waves_for(int KP, int VP) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16;
-  const int bytes = kParts<T> * (4 * C * padded<bf16>(KP) + NT * (NT + 1) * 256) +
+  const int bytes = kParts<T> * (4 * C * key_row<T>(KP, VP) + NT * (NT + 1) * 256) +
                     C * padded<T>(VP) * (int)sizeof(T);
   const int room = (160 * 1024 / bytes * (VP / 16) + 3) / 4;
-  const int most = VP == 32 ? 2 : sizeof(T) == 4 && VP == 64 ? 3 : 4;
+  const int most = VP == 32 ? 2 : 4;
   return room < most ? room : most;
 }
 
@@ -378,11 +384,11 @@ template <typename T> constexpr int waves_for(int KP, int VP) {
 // from HBM once for all passes that share them, since those run side by side); one row of 62496: 61 us
 // after 28 us of states. f32 at 128 wide, 100 rows of 1000, 8 heads to 2 key heads: 532 us forward, 1754
 // us backward at two blocks a CU, which LDS allows. One chunk a row (2000 f32 rows of 25 at 33 x 50):
-// 132 us, the latency of a block from its first load to its last store, three blocks a CU.
+// 117 us, the latency of a block from its first load to its last store, four blocks a CU.
 template <typename T, int KP, int VP, bool STATES, bool VEC>
 __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
-  constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = padded<bf16>(KP), LV = padded<T>(VP);
+  constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = key_row<T>(KP, VP), LV = padded<T>(VP);
   constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, KPART = C * LK;
   using V4 = typename Vec4<T>::type;
   using TK = Tile<T, C, KP, THREADS, VEC>;
