@@ -724,13 +724,20 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
 // head of a row, one thread four values of the state. Bound by the latency of a long row's reads, 16 at
 // a time: 15 us for 8 heads' 122 states of 64 x 64 (31 MB moved); where rows are many, by HBM.
 __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float *second_pass,
-                                                       const int64_t *row_ptr,
-                                                       int64_t row0, int64_t n_tokens,
+                                                       const int64_t *row_ptr, int64_t n_rows,
+                                                       int64_t index0, int64_t n_tokens,
                                                        int64_t n_slots, int shift, int heads,
-                                                       const float *log_decay, int64_t floats) {
+                                                       const float *log_decay, int64_t floats,
+                                                       const Place *places, const int32_t *entries) {
   float *segments = blockIdx.z ? second_pass : first_pass;
-  const int64_t row = row0 + blockIdx.x / heads;
+  int64_t row = index0 + blockIdx.x / heads;
   const int head = (int)(blockIdx.x % heads);
+  if (entries) {  // of a row's, the first one's block
+    const int32_t at = entries[row];
+    if (at < 0 || at >= n_slots || places[at].segment != 0) return;
+    row = places[at].row;
+    if (row < 0 || row >= n_rows) return;
+  }
   const int64_t first = clamped(row_ptr[row], 0, n_tokens);
   const int64_t len = clamped(row_ptr[row + 1], first, n_tokens) - first;
   const int64_t slot = (first >> shift) + row;
@@ -877,14 +884,19 @@ template <typename T, int KP, int VP> hipError_t launch_kv(Args A, bool split, h
     states(own);  // of one pass, or two
     const AttentionPass &P = own.p[0];
     const int64_t floats = (int64_t)KP * VP, per = max_blocks(256) / heads;
-    for (int64_t r = 0; r < P.n_rows; r += per) {
-      const int64_t n = P.n_rows - r < per ? P.n_rows - r : per;
+    // over the rows or, where those are fewer and known, the entries: most rows may be one segment
+    const int64_t n_entries = P.n_tokens >> A.shift;
+    const bool of_entries = A.places && n_entries < P.n_rows;
+    const int64_t count = of_entries ? n_entries : P.n_rows;
+    for (int64_t r = 0; r < count; r += per) {
+      const int64_t n = count - r < per ? count - r : per;
       // parts of a state: as many as fill the chip, where rows and heads alone do not
-      const int64_t parts = n * heads >= 1024 ? 1 : (floats + 1023) / 1024;
+      const int64_t parts = n * heads >= 4096 ? 1 : (floats + 1023) / 1024;
       hipLaunchKernelGGL(k_join_segments,
                          dim3((unsigned)(n * heads), (unsigned)parts, (unsigned)own.n), dim3(256), 0, s,
-                         P.segments, own.n > 1 ? own.p[1].segments : nullptr, P.row_ptr, r, P.n_tokens,
-                         A.n_slots, A.shift, heads, P.log_decay, floats);
+                         P.segments, own.n > 1 ? own.p[1].segments : nullptr, P.row_ptr, P.n_rows, r,
+                         P.n_tokens, A.n_slots, A.shift, heads, P.log_decay, floats,
+                         of_entries ? A.places : nullptr, of_entries ? A.entries : nullptr);
     }
   }
   outputs(A);
