@@ -769,9 +769,10 @@ __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float 
 
 // The gradients of shared heads: blockIdx.y: of k, of v. A group's heads are other blocks of the pass,
 // with decays of their own, so each leaves its part in fp32 and they are added here in their order
-// (atomics would change the result from run to run). Bound by HBM: 217 us for 8 heads to 2 of 100 003
-// tokens at 128 wide in f32, 4.7 TB/s.
-template <typename T>
+// (atomics would change the result from run to run). Bound by HBM: 189 us for 8 heads to 2 of 100 003
+// tokens at 128 wide in f32, 5.4 TB/s (a value a thread: 217).
+// A thread holds VW neighbouring values of its heads (four or, of widths not a multiple of it, one).
+template <typename T, int VW>
 __global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ of_k,
                                                     const float *__restrict__ of_v, int64_t n_heads,
                                                     int group, int k_width, int v_width,
@@ -779,13 +780,18 @@ __global__ __launch_bounds__(256) void k_sum_groups(const float *__restrict__ of
   const float *x = blockIdx.y ? of_v : of_k;
   T *out = blockIdx.y ? dv : dk;
   const int width = blockIdx.y ? v_width : k_width;
-  const int64_t n = n_heads * width;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t head = i / width;
-    const float *p = x + head * group * width + (i - head * width);
-    float sum = p[0];
-    for (int j = 1; j < group; ++j) sum += p[(int64_t)j * width];
-    out[i] = (T)sum;
+  using F = float __attribute__((ext_vector_type(VW)));
+  using O = T __attribute__((ext_vector_type(VW)));
+  const int pieces = width / VW, heads = 256 / pieces;  // of a block
+  const int tid = (int)threadIdx.x, mine = tid / pieces, c = tid % pieces * VW;
+  if (mine >= heads) return;
+  for (int64_t head = (int64_t)blockIdx.x * heads + mine; head < n_heads;
+       head += (int64_t)gridDim.x * heads) {
+    const float *p = x + head * group * width + c;
+    F sum = *(const F *)p;
+#pragma unroll 4
+    for (int j = 1; j < group; ++j) sum += *(const F *)(p + j * width);
+    *(O *)(out + head * width + c) = __builtin_convertvector(sum, O);
   }
 }
 
@@ -998,14 +1004,18 @@ hipError_t launch_sum_groups(als_dtype dtype, const float *of_k, const float *of
                              void *dv, hipStream_t s) {
   const int64_t n_heads = n_tokens * (heads / group);
   if (n_heads == 0) return hipSuccess;
-  const int64_t blocks = (n_heads * (k_width > v_width ? k_width : v_width) + 255) / 256;
+  const bool vec = (k_width | v_width) % 4 == 0 &&
+                   (((uintptr_t)of_k | (uintptr_t)of_v | (uintptr_t)dk | (uintptr_t)dv) % 16 == 0);
+  const int wide = (k_width > v_width ? k_width : v_width) / (vec ? 4 : 1);
+  const int64_t blocks = (n_heads + 256 / wide - 1) / (256 / wide);
   const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192), 2);
+  const auto sum = [&](auto kernel, auto *k, auto *v) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, of_k, of_v, n_heads, group, k_width, v_width, k, v);
+  };
   if (dtype == ALS_F32)
-    hipLaunchKernelGGL(k_sum_groups<float>, grid, dim3(256), 0, s, of_k, of_v, n_heads, group, k_width,
-                       v_width, (float *)dk, (float *)dv);
+    sum(vec ? k_sum_groups<float, 4> : k_sum_groups<float, 1>, (float *)dk, (float *)dv);
   else
-    hipLaunchKernelGGL(k_sum_groups<bf16>, grid, dim3(256), 0, s, of_k, of_v, n_heads, group, k_width,
-                       v_width, (bf16 *)dk, (bf16 *)dv);
+    sum(vec ? k_sum_groups<bf16, 4> : k_sum_groups<bf16, 1>, (bf16 *)dk, (bf16 *)dv);
   return hipGetLastError();
 }
 
