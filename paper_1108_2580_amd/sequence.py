@@ -301,7 +301,8 @@ def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
         raise ValueError("log_decay takes no gradient")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (q, k, v, initial_state)):
-        out, state = _DecayAttention.apply(q, k, v, initial_state, log_decay, row_ptr, scale)
+        out, state = _DecayAttention.apply(q, k, v, initial_state, log_decay, row_ptr, scale,
+                                           return_state)
     else:
         out, state = _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
     return (out, state) if return_state else out
@@ -330,11 +331,11 @@ def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, ini
 
 class _DecayAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, initial_state, log_decay, row_ptr, scale):
+    def forward(ctx, q, k, v, initial_state, log_decay, row_ptr, scale, return_state):
         ctx.save_for_backward(q, k, v, log_decay, row_ptr, initial_state)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
-        return _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, True)
+        return _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -345,7 +346,7 @@ class _DecayAttention(torch.autograd.Function):
         dstate = None if dstate is None else dstate.contiguous()
         grads = decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale,
                                          initial_state, dstate, d_initial=ctx.needs_input_grad[3])
-        return (*grads, None, None, None)
+        return (*grads, None, None, None, None)
 
 
 def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, state_out=None):
@@ -355,7 +356,8 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
     ``state``: fp32 [rows, heads, key width, value width], updated in place unless ``state_out`` is
     given. ``source``: int32 [rows], the row of ``state`` that each row goes on from (a beam's
     parent; one outside it gives NaN); ``state`` may then have another number of rows, and
-    ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out)."""
+    ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out), neither of
+    which carries a gradient."""
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
     N, H, K, V = shape.n_rows, shape.q_heads, shape.k_width, shape.v_width
     sources, src = N, None

@@ -627,3 +627,38 @@ def test_calls_replay_in_a_graph():
         torch.cuda.synchronize()
         for x, y in zip(held, want):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("wanted", ["out", "state", "both"])
+def test_autograd_of_a_training_step(wanted):
+    """norm_rotate and decay_attention in a graph of torch's, from keys that all rows share, with the
+    loss on the outputs, the states, or both: what the operators' own backward calls give."""
+    import paper_1108_2580_amd as p
+
+    lens, H, Hk, K, V = [40, 0, 71], 4, 2, 32, 24
+    q, k, v, a, ptr, d_out, S0, dS = attention_inputs(lens, H, Hk, K, V, "f32", 11)
+    N = sum(lens)
+    w = torch.ones(K, device="cuda:0")
+    cos, sin = p.rotary_tables(N, K)
+    pos = torch.arange(N, dtype=torch.int32, device="cuda:0")
+    one = k[:1].clone().requires_grad_()  # broadcast over the tokens
+    q, v = q.clone().requires_grad_(), v.clone().requires_grad_()
+    keys = one.expand(N, Hk, K)
+    q1, k1 = p.norm_rotate(q, keys, w, w, cos, sin, pos)
+    got = p.decay_attention(q1, k1, v, a, ptr, return_state=wanted != "out")
+    out, state = got if wanted != "out" else (got, None)
+    loss = 0.0
+    if wanted != "state":
+        loss = loss + (out * d_out).sum()
+    if wanted != "out":
+        loss = loss + (state * dS).sum()
+    grads = torch.autograd.grad(loss, (q, one, v))
+    with torch.no_grad():
+        dq1, dk1, dv, _ = p.decay_attention_backward(
+            d_out if wanted != "state" else torch.zeros_like(d_out), q1, k1, v, a, ptr,
+            dstate=dS if wanted != "out" else None)
+        dq, dk, _, _ = p.norm_rotate_backward(dq1, dk1, q, keys, w, w, cos, sin, pos)
+    assert torch.equal(grads[0], dq) and torch.equal(grads[2], dv)
+    # a sum over the tokens in some other order
+    bound = N * 2.0 ** -24 * dk.abs().sum(0, keepdim=True) + 1e-30
+    assert ((grads[1] - dk.sum(0, keepdim=True)).abs() <= 2 * bound).all()
