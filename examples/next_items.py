@@ -62,18 +62,21 @@ class NextItems(torch.nn.Module):
 
     def forward(self, item, position, row_ptr):
         q, k, v = self.tokens(item, position)
-        out, state = decay_attention(q, k, v, self.log_decay, row_ptr, return_state=True)
-        return self.logits(out), state
+        return self.logits(decay_attention(q, k, v, self.log_decay, row_ptr))
 
 
 @torch.no_grad()
 def answer(model, item, position, row_ptr, beams, length, end):
     """The best lists of `length` items for every row: (items [rows, beams, length], scores)."""
-    logits, state = model(item, position, row_ptr)
+    q, k, v = model.tokens(item, position)
+    out, state = decay_attention(q, k, v, model.log_decay, row_ptr, return_state=True)
     B = row_ptr.numel() - 1
     last = (row_ptr[1:] - 1).clamp(min=0)
+    # an empty history says nothing: all items alike
+    empty = (row_ptr[1:] == row_ptr[:-1])[:, None, None]
+    logits = model.logits(out[last].masked_fill(empty, 0.0))
     scores = torch.zeros(B, 1, device=DEV)
-    parents, token, scores, done = beam_select(logits[last][:, None], scores, None, end, width=beams)
+    parents, token, scores, done = beam_select(logits[:, None], scores, None, end, width=beams)
     lists = token[..., None]
     first = torch.arange(B, device=DEV, dtype=torch.int32)[:, None]
     source = (first + parents).flatten()  # rows of `state`: one a user, then one a beam
@@ -116,7 +119,7 @@ def main(users=500, items=1000, steps=20, beams=4, length=5, seed=7):
     step = torch.optim.AdamW(model.parameters(), lr=3e-2)
     losses = []
     for i in range(steps):
-        logits, _ = model(item, position, row_ptr)
+        logits = model(item, position, row_ptr)
         loss = F.cross_entropy(logits[has_next], target)
         step.zero_grad()
         loss.backward()
