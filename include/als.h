@@ -494,7 +494,8 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   log_decay      device fp32[q_heads], <= 0 (-inf forgets at once); a head above 0 or NaN gives NaN.
  *   initial_state, final_state  device fp32 [n_rows, q_heads, k_width, v_width], nullable.
  *   out            device [n_tokens, q_heads, v_width], packed.
- * bf16 inputs: products of bf16 with fp32 sums; the products of q and k with their decay, and the
+ * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
+ * NaN. bf16 inputs: products of bf16 with fp32 sums; the products of q and k with their decay, and the
  * state as q reads it, are rounded to bf16. The state itself is kept in fp32.
  */
 typedef struct {

@@ -135,6 +135,9 @@ als_status check_both(const als_rotation *s, als_dtype dtype, const als_heads *x
     const Span other = span(out[1 - i], s->n_tokens, heads[1 - i], s->width, size);
     REQUIRE(out[0].data != out[1].data || s->n_tokens == 0, "q_out and k_out are the same");
     REQUIRE(!packed || !overlap(o, other), "q_out and k_out overlap");
+    REQUIRE(!packed || (!overlap(o, span(x[1 - i], s->n_tokens, heads[1 - i], s->width, size)) &&
+                        !(dy && overlap(o, span(dy[1 - i], s->n_tokens, heads[1 - i], s->width, size)))),
+            "the output of %s overlaps %s or its gradient", i ? "k" : "q", i ? "q" : "k");
   }
   return ALS_OK;
 }

@@ -51,6 +51,13 @@ def test_norm_rotate_tensors(change, word):
     refused(norm_rotate(rotation(), **change), word)
 
 
+@pytest.mark.parametrize("change", [
+    dict(ko=_Heads(A, 128, 64)), dict(qo=_Heads(B, 256, 64)), dict(q=_Heads(A, 256, 64), k=_Heads(A, 128, 64),
+                                                                   qo=_Heads(A, 256, 64))])
+def test_norm_rotate_output_on_the_other_sides_input(change):
+    refused(norm_rotate(rotation(), **change), "overlaps")
+
+
 def test_norm_rotate_backward_workspace():
     s = rotation()
     need = lib.als_norm_rotate_workspace(s)
