@@ -683,21 +683,17 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
         w[1][e] *= vc[s].get(4 + e);
       }
       const Frag<3> x = as_frag<3>(w[0], w[1]);
-      const auto update = [&](int parts) {  // of x, where k has one
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const Frag<NP> kf =
-              frag_col<NP, 8>(lk + s * 32 * LK + kt / 2 * 32 + kt % 2 * 4, LK, KPART, lane);
-          if constexpr (NP == 3) {
-            S[kt] = mma(kf, x, S[kt]);
-          } else {
-            for (int n = 0; n < parts; ++n) S[kt] = mma(kf.p[0], x.p[n], S[kt]);
-          }
+      for (int kt = 0; kt < KT; ++kt) {
+        const Frag<NP> kf =
+            frag_col<NP, 8>(lk + s * 32 * LK + kt / 2 * 32 + kt % 2 * 4, LK, KPART, lane);
+        if constexpr (NP == 3) {
+          S[kt] = mma(kf, x, S[kt]);
+        } else {
+#pragma unroll
+          for (int n = 2; n >= 0; --n) S[kt] = mma(kf.p[0], x.p[n], S[kt]);
         }
-      };
-      // a state that only bf16 products read needs no more than 16 bits of what is added
-      if (NP == 3 || P.last_state) update(3);
-      else update(2);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   }
