@@ -496,7 +496,7 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   out            device [n_tokens, q_heads, v_width], packed.
  * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
  * NaN. bf16 inputs: products of bf16 with fp32 sums; the products of q and k with their decay, and the
- * state as q reads it, are rounded to bf16. The state itself is kept in fp32.
+ * state as q reads it, enter as two bf16 values each (off by 2^-16 at most). The state is kept in fp32.
  */
 typedef struct {
   int64_t n_tokens;

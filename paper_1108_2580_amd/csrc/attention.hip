@@ -21,10 +21,11 @@
 // A reversed pass reads its state one step nearer and adds to it one step further
 // (read e^{a i}, add e^{a (C - j)}).
 //
-// Rounding. Products have sums in fp32. bf16 inputs: the weights and the state are rounded once more
-// where they enter a product, which is as much again as the output's own rounding; what a token adds
-// to the state is split into three bf16 parts (24 bits), so that the state, an output in fp32, has no
-// bf16 rounding in it. fp32 inputs: all operands are split so.
+// Rounding. Products have sums in fp32. bf16 inputs: the weights and the state enter a product in two
+// bf16 parts, which are off by 2^-16 at most, so that an output is rounded once, on its way out (as one
+// bf16 value they would cost as much again as that rounding); what a token adds to the state is split
+// into three parts (24 bits), so that the state, an output in fp32, has no bf16 rounding in it. fp32
+// inputs: all operands are split so.
 #include <type_traits>
 
 #include "internal.h"
@@ -51,6 +52,9 @@ constexpr float kMinLogDecay = -1e4f;
 // a product is the sum of six products of parts, which leaves out 2^-24 of it: six MFMAs of 16 cycles
 // where the fp32 MFMAs of the same tile take 256.
 template <typename T> constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+// Of the weights, and of the state where a query reads it. Their second part costs bf16 a second MFMA,
+// 14 of 57 in a wave's chunk at 64 wide.
+template <typename T> constexpr int kReadParts = sizeof(T) == 2 ? 2 : 3;
 template <int NP> struct Frag { bf16x8 p[NP]; };
 
 template <typename T> struct Vec4;
@@ -65,6 +69,10 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 mma(const Frag<1> &a, const Frag<1> &b, f32x4 c) {
+  return mma(a.p[0], b.p[0], c);
+}
+__device__ __forceinline__ f32x4 mma(const Frag<1> &a, const Frag<2> &b, f32x4 c) {
+  c = mma(a.p[0], b.p[1], c);
   return mma(a.p[0], b.p[0], c);
 }
 __device__ __forceinline__ f32x4 mma(const Frag<3> &a, const Frag<3> &b, f32x4 c) {
@@ -119,10 +127,21 @@ __device__ __forceinline__ void split3(f32x4 x, bf16x4 *part) {
     }
   }
 }
-// As an operand: rounded, or in three parts.
+// Four values in two: the first cut off, so that the largest finite ones stay finite, the second rounded.
+__device__ __forceinline__ void split2(f32x4 x, bf16x4 *part) {
+  using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+  const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]), c = __float_as_uint(x[2]),
+                 d = __float_as_uint(x[3]);
+  const u32x2 out = {__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
+  part[0] = __builtin_bit_cast(bf16x4, out);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+  part[1] = __builtin_convertvector(x, bf16x4);
+}
+// As an operand, in two or three parts.
 template <int NP> __device__ __forceinline__ void as_parts(f32x4 x, bf16x4 *part) {
-  if constexpr (NP == 1)
-    part[0] = __builtin_convertvector(x, bf16x4);
+  if constexpr (NP == 2)
+    split2(x, part);
   else
     split3(x, part);
 }
@@ -367,7 +386,7 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 // and never more than LDS has room for.
 template <typename T> constexpr int waves_for(int KP, int VP) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16;
-  const int bytes = kParts<T> * (4 * C * key_row<T>(KP, VP) + NT * (NT + 1) * 256) +
+  const int bytes = kParts<T> * 4 * C * key_row<T>(KP, VP) + kReadParts<T> * NT * (NT + 1) * 256 +
                     C * padded<T>(VP) * (int)sizeof(T);
   const int room = (160 * 1024 / bytes * (VP / 16) + 3) / 4;
   const int most = VP == 32 ? 2 : 4;
@@ -389,14 +408,14 @@ template <typename T, int KP, int VP, bool STATES, bool VEC>
 __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
   constexpr int KT = KP / 16, KF = KP / 32, SF = C / 32, LK = key_row<T>(KP, VP), LV = padded<T>(VP);
-  constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, KPART = C * LK;
+  constexpr int PT = NT * (NT + 1) / 2, NP = kParts<T>, RP = kReadParts<T>, KPART = C * LK;
   using V4 = typename Vec4<T>::type;
   using TK = Tile<T, C, KP, THREADS, VEC>;
   using TV = Tile<T, C, VP, THREADS, VEC>;
   __shared__ __align__(16) bf16 lq[STATES ? 1 : NP * KPART];
   __shared__ __align__(16) bf16 lk[NP * KPART];
   __shared__ __align__(16) T lv[C * LV];
-  __shared__ __align__(16) bf16 lp[STATES ? 1 : PT * NP * 256];  // by tile, part, lane
+  __shared__ __align__(16) bf16 lp[STATES ? 1 : PT * RP * 256];  // by tile, part, lane
 
   const AttentionPass &P = A.p[blockIdx.x % (unsigned)A.n];
   const unsigned block = blockIdx.x / (unsigned)A.n;
@@ -550,10 +569,10 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] *= far * near[e];
         }
-        bf16x4 part[NP];
-        as_parts<NP>(w, part);
+        bf16x4 part[RP];
+        as_parts<RP>(w, part);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) *(bf16x4 *)(lp + (tile * NP + n) * 256 + lane * 4) = part[n];
+        for (int n = 0; n < RP; ++n) *(bf16x4 *)(lp + (tile * RP + n) * 256 + lane * 4) = part[n];
       }
       __syncthreads();
     }
@@ -576,56 +595,56 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
       }
       const bf16x4 zero = {(bf16)0.f, (bf16)0.f, (bf16)0.f, (bf16)0.f};
       const int c0 = wave * 16 + g * 4;
-      // rows c0 + e of v, column 16 i + m: what the state before the chunk gives. In parts the state
-      // is one operand at a time, as bf16 all of it and one column.
-      Frag<NP> sf[NP == 1 ? KF : 1], vf[SF];
-      f32x4 all[NP == 1 ? 1 : NT];
-      if constexpr (NP == 1) {
+      // rows c0 + e of v, column 16 i + m: what the state before the chunk gives, 32 rows of the state at
+      // a time
+      Frag<NP> vf[SF];
+      f32x4 all[NT];
 #pragma unroll
-        for (int d = 0; d < KF; ++d) sf[d] = as_frag<NP>(S[2 * d], S[2 * d + 1]);
-      } else {
+      for (int i = 0; i < NT; ++i) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NT; ++i) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int d = 0; d < KF; ++d) {
+        const Frag<RP> sf = as_frag<RP>(S[2 * d], S[2 * d + 1]);
+        const auto q_of = [&](int i) { return frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane); };
+        if constexpr (NP == 1) {  // two tiles side by side: a product waits for the one before it of its tile
 #pragma unroll
-        for (int d = 0; d < KF; ++d) {
-          sf[0] = as_frag<NP>(S[2 * d], S[2 * d + 1]);
+          for (int i = 0; i < NT; i += 2) {
+            const Frag<NP> q0 = q_of(i), q1 = q_of(i + 1);
 #pragma unroll
-          for (int i = 0; i < NT; ++i)
-            all[i] = mma(sf[0], frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane), all[i]);
-          __builtin_amdgcn_sched_barrier(0);
+            for (int n = RP - 1; n >= 0; --n) {
+              all[i] = mma(sf.p[n], q0.p[0], all[i]);
+              all[i + 1] = mma(sf.p[n], q1.p[0], all[i + 1]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < NT; ++i) all[i] = mma(sf, q_of(i), all[i]);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int s = 0; s < SF; ++s) vf[s] = vc[s].frag();
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (NP == 1) {
-#pragma unroll
-          for (int d = 0; d < KF; ++d)
-            o = mma(sf[d], frag_row<NP>(lq + i * 16 * LK + d * 32, LK, KPART, lane), o);
-        } else {
-          o = all[i];
-        }
+        f32x4 o = all[i];
         o *= P.read_scale * exp2_fast(a2 * (float)(16 * i + m + read_off));
 #pragma unroll
         for (int s = 0; s <= i / 2; ++s) {
-          const bf16 *t = lp + (i * (i + 1) / 2 + 2 * s) * NP * 256 + lane * 4;
-          Frag<NP> pf;
+          const bf16 *t = lp + (i * (i + 1) / 2 + 2 * s) * RP * 256 + lane * 4;
+          Frag<RP> pf;
 #pragma unroll
-          for (int n = 0; n < NP; ++n)
+          for (int n = 0; n < RP; ++n)
             pf.p[n] = joined(*(const bf16x4 *)(t + n * 256),
-                             2 * s + 1 <= i ? *(const bf16x4 *)(t + (NP + n) * 256) : zero);
+                             2 * s + 1 <= i ? *(const bf16x4 *)(t + (RP + n) * 256) : zero);
           o = mma(vf[s], pf, o);
         }
         const int place = 16 * i + m;
         if (!all_finite) {
 #pragma unroll 1
           for (int j = 0; j <= place; ++j) {
-            const bf16 *t = lp + (i * (i + 1) / 2 + j / 16) * NP * 256 + (m + j % 16 / 4 * 16) * 4 + j % 4;
+            const bf16 *t = lp + (i * (i + 1) / 2 + j / 16) * RP * 256 + (m + j % 16 / 4 * 16) * 4 + j % 4;
             float w = 0.f;
 #pragma unroll
-            for (int n = NP - 1; n >= 0; --n) w += (float)t[n * 256];
+            for (int n = RP - 1; n >= 0; --n) w += (float)t[n * 256];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x = (float)lv[j * LV + c0 + e];
