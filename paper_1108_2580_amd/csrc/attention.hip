@@ -49,8 +49,8 @@ constexpr float kMinLogDecay = -1e4f;
 // in such an order (frag_col's STEP 8) that a pair of them is an operand of the first order.
 //
 // bf16 values are held as they are. fp32 values are held in three bf16 parts, whose sum they are, and
-// a product is the sum of six products of parts, which leaves out 2^-24 of it: six MFMAs of 16 cycles
-// where the fp32 MFMAs of the same tile take 256.
+// a product is the sum of six products of parts, which leaves out 2^-22 of it at most, in either
+// direction: six MFMAs of 16 cycles where the fp32 MFMAs of the same tile take 256.
 template <typename T> constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
 // Of the weights, and of the state where a query reads it. Their second part costs bf16 a second MFMA,
 // 14 of 57 in a wave's chunk at 64 wide.
@@ -108,47 +108,35 @@ __device__ __forceinline__ Frag<NP> frag_col(const bf16 *x, int ld, int part, in
   return f;
 }
 
-// Four values in three bf16 parts: each is the leading 8 bits of what is left (cut off, so that it is
-// exact), and 3 * 8 bits are all that fp32 has.
-__device__ __forceinline__ void split3(f32x4 x, bf16x4 *part) {
+// Four values in two or three bf16 parts of 8 bits. The first is cut off, so that the largest finite values
+// stay finite. The second is rounded (of three by an integer sum, which takes less time than the
+// conversion), so that what it leaves, 2^-16 of the value at most, leans to neither side: with a second part
+// cut off as well, fp32 products were all short, by 2^-24 on average. A third takes exactly what is left of
+// fp32's 24 bits. Where the other operand is one part (ONE), nothing is left out and all are cut off.
+template <int NP, bool ONE = false> __device__ __forceinline__ void as_parts(f32x4 x, bf16x4 *part) {
   using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int n = 0; n < 3; ++n) {
-    const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]), c = __float_as_uint(x[2]),
-                   d = __float_as_uint(x[3]);
-    // the upper halves of b and a, and of d and c
-    const u32x2 out = {__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
-    part[n] = __builtin_bit_cast(bf16x4, out);
-    if (n < 2) {
-      x[0] -= __uint_as_float(a & 0xffff0000u);
-      x[1] -= __uint_as_float(b & 0xffff0000u);
-      x[2] -= __uint_as_float(c & 0xffff0000u);
-      x[3] -= __uint_as_float(d & 0xffff0000u);
+  for (int n = 0; n < NP; ++n) {
+    if (NP == 2 && n == 1) {
+      part[1] = __builtin_convertvector(x, bf16x4);
+      return;
     }
+    uint32_t bits[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bits[e] = __float_as_uint(x[e]) + (n == 1 && !ONE ? 0x8000u : 0u);
+    // the upper halves
+    const u32x2 out = {__builtin_amdgcn_perm(bits[1], bits[0], 0x07060302),
+                       __builtin_amdgcn_perm(bits[3], bits[2], 0x07060302)};
+    part[n] = __builtin_bit_cast(bf16x4, out);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float(bits[e] & 0xffff0000u);
   }
 }
-// Four values in two: the first cut off, so that the largest finite ones stay finite, the second rounded.
-__device__ __forceinline__ void split2(f32x4 x, bf16x4 *part) {
-  using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
-  const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]), c = __float_as_uint(x[2]),
-                 d = __float_as_uint(x[3]);
-  const u32x2 out = {__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
-  part[0] = __builtin_bit_cast(bf16x4, out);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
-  part[1] = __builtin_convertvector(x, bf16x4);
-}
-// As an operand, in two or three parts.
-template <int NP> __device__ __forceinline__ void as_parts(f32x4 x, bf16x4 *part) {
-  if constexpr (NP == 2)
-    split2(x, part);
-  else
-    split3(x, part);
-}
-template <int NP> __device__ __forceinline__ Frag<NP> as_frag(f32x4 lo, f32x4 hi) {
+template <int NP, bool ONE = false>
+__device__ __forceinline__ Frag<NP> as_frag(f32x4 lo, f32x4 hi) {
   bf16x4 a[NP], b[NP];
-  as_parts<NP>(lo, a);
-  as_parts<NP>(hi, b);
+  as_parts<NP, ONE>(lo, a);
+  as_parts<NP, ONE>(hi, b);
   Frag<NP> f;
 #pragma unroll
   for (int n = 0; n < NP; ++n) f.p[n] = joined(a[n], b[n]);
@@ -373,7 +361,7 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
         if (ROWS <= C || r0 < C) {
           const Piece p = piece(x, i, r0 + i * ROWS, c);
           bf16x4 part[3];
-          split3(f32x4{p.v[0], p.v[1], p.v[2], p.v[3]}, part);
+          as_parts<3>(f32x4{p.v[0], p.v[1], p.v[2], p.v[3]}, part);
 #pragma unroll
           for (int n = 0; n < 3; ++n)
             *(bf16x4 *)(lds + n * C * ld + (r0 + i * ROWS) * ld + c) = part[n];
@@ -701,7 +689,7 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
         w[0][e] *= vc[s].get(e);
         w[1][e] *= vc[s].get(4 + e);
       }
-      const Frag<3> x = as_frag<3>(w[0], w[1]);
+      const Frag<3> x = as_frag<3, NP == 1>(w[0], w[1]);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         const Frag<NP> kf =
