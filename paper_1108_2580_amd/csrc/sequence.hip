@@ -163,9 +163,12 @@ als_status check_attention(const als_attention *s, als_dtype dtype, bool step) {
   return ALS_OK;
 }
 
-als_status check_input(const char *name, const als_heads &x, int64_t n, int size) {
+// One token's stride means nothing and may be anything (a slice of a large tensor has its own): it is taken
+// out, since a pass from the last token to the first addresses its rows from those that would lie below.
+als_status check_input(const char *name, als_heads &x, int64_t n, int size) {
+  if (n <= 1) x.token_stride = 0;
   const char *w = wrong(x, n, size);
-  if (!w && n > 1 && x.token_stride > als::kMaxTokenStride) w = "a token_stride above 2^22";
+  if (!w && x.token_stride > als::kMaxTokenStride) w = "a token_stride above 2^22";
   return w ? fail_without_context(ALS_ERR_INVALID_ARG, "%s has %s", name, w) : ALS_OK;
 }
 

@@ -1,0 +1,23 @@
+"""Attention on views with strides far above their widths."""
+import pytest
+
+from .test_gpu_sequence import attention_inputs
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("stride", [1 << 22, 1 << 27, 1 << 40])
+def test_one_token_of_any_stride(stride, dtype):
+    """A slice of one token keeps the stride of the tensor that it was cut from, which no pass may use."""
+    import paper_1108_2580_amd as p
+
+    q, k, v, a, ptr, d_out, S0, dS = attention_inputs([1], 4, 2, 64, 48, dtype, 30)
+    far = lambda t: t.as_strided(t.shape, (stride, *t.stride()[1:]))  # noqa: E731
+    want = [*p.decay_attention(q, k, v, a, ptr, None, S0, return_state=True),
+            *p.decay_attention_backward(d_out, q, k, v, a, ptr, None, S0, dS)]
+    got = [*p.decay_attention(far(q), far(k), far(v), a, ptr, None, S0, return_state=True),
+           *p.decay_attention_backward(far(d_out), far(q), far(k), far(v), a, ptr, None, S0, dS)]
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
