@@ -3,7 +3,8 @@
 // and the first R features of y in pairs (a, b), turned by the angle of the token's position:
 //   a' = a cos - b sin,  b' = b cos + a sin.
 // Backward, with g = dy turned back: dw = sum g x r,
-//   dx = r g w - x r^3 mean(g w x).
+//   dx = r (g w - n mean(g w n)),  n = x r
+// (formed from n, of unit size at any scale of x: r^3 alone leaves fp32's range from about 1e13 and 1e-13 on).
 //
 // Every byte is read and written once; the arithmetic is small, so memory bounds it. A group of G
 // lanes shares a row (one head of one token), and a lane holds whole pairs: VW values of each half
@@ -224,19 +225,21 @@ __global__ __launch_bounds__(kBlock) void k_rotate(Rotate R) {
       turn<VW, NEXT, -1>(u, da, db, cs, sn, R.half);
 #pragma unroll
       for (int e = 0; e < VW; ++e) {
-        ga[e] = fmaf(da[e], xa[e] * r, ga[e]);
-        gb[e] = fmaf(db[e], xb[e] * r, gb[e]);
+        xa[e] *= r;
+        xb[e] *= r;
+        ga[e] = fmaf(da[e], xa[e], ga[e]);
+        gb[e] = fmaf(db[e], xb[e], gb[e]);
         da[e] *= wa[e];
         db[e] *= wb[e];
         if (e >= u.skip_a) along = fmaf(da[e], xa[e], along);
         if (e >= u.skip_b) along = fmaf(db[e], xb[e], along);
       }
       along = group_sum<G>(along);
-      const float f = r * r * r * (along / (float)R.width);
+      const float mean = along / (float)R.width;
 #pragma unroll
       for (int e = 0; e < VW; ++e) {
-        xa[e] = da[e] * r - xa[e] * f;
-        xb[e] = db[e] * r - xb[e] * f;
+        xa[e] = r * (da[e] - xa[e] * mean);
+        xb[e] = r * (db[e] - xb[e] * mean);
       }
     }
     store<T, VW, ENDS == kCut>(out + u.a, u.left_a, xa);
