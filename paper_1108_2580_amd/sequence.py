@@ -10,7 +10,9 @@ Argument marshalling only: the work runs in the HIP kernels of ``csrc/``. Every 
 the current HIP stream of the current device, on which its tensors have to lie, and nothing is
 synchronised. Inputs are fp32 or bf16 tensors whose features are contiguous; tokens and heads may
 have any strides. Where an input of ``norm_rotate`` or ``decay_attention`` requires a gradient, the
-result carries it.
+result carries it, or the call raises where there is none for that input (``cos``, ``sin``,
+``log_decay``). The other operators' results carry none. What a call writes to a caller's tensor counts as
+an in-place operation.
 """
 from __future__ import annotations
 
@@ -144,6 +146,23 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _no_gradient(t, name):
+    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} takes no gradient")
+
+
+def _writable(t, name):
+    """Refuses a caller's tensor whose gradient a write by a kernel would lose unseen."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which writing to it would lose")
+
+
+def _written(t):
+    """As after torch's in-place operations, a graph that has saved the tensor notices."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 # ---- norm and rotation -------------------------------------------------------------------------
 
 def rotary_tables(n_positions, rotated, base=10_000.0, device="cuda"):
@@ -196,7 +215,9 @@ def norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps=1e-6, neighbo
     ``q_weight``, ``k_weight``: fp32 [width]; ``cos``, ``sin``: fp32 [positions, pairs]
     (``rotary_tables``); ``positions``: int32 [tokens], a row of the tables each (one outside them
     makes its token NaN). ``neighbours``: pair p is features 2 p and 2 p + 1 instead of p and
-    p + pairs. Returns new (q, k)."""
+    p + pairs. Returns new (q, k). ``cos`` and ``sin`` take no gradient."""
+    _no_gradient(cos, "cos")
+    _no_gradient(sin, "sin")
     if torch.is_grad_enabled() and (
             q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad):
         return _NormRotate.apply(q, k, q_weight, k_weight, cos, sin, positions, eps, neighbours)
@@ -297,8 +318,7 @@ def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
     ``scale``: 1 / sqrt(key width) if None. ``initial_state``: fp32 [rows, heads, key width, value
     width], zero if None. Returns out [tokens, heads, value width], with ``return_state`` (out, the
     states after the rows' last tokens). ``log_decay`` takes no gradient."""
-    if log_decay.requires_grad and torch.is_grad_enabled():
-        raise ValueError("log_decay takes no gradient")
+    _no_gradient(log_decay, "log_decay")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (q, k, v, initial_state)):
         out, state = _DecayAttention.apply(q, k, v, initial_state, log_decay, row_ptr, scale,
@@ -357,7 +377,8 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
     given. ``source``: int32 [rows], the row of ``state`` that each row goes on from (a beam's
     parent; one outside it gives NaN); ``state`` may then have another number of rows, and
     ``state_out`` (a new tensor if None) must not overlap it. Returns (out, state_out), neither of
-    which carries a gradient."""
+    which carries a gradient; a ``state`` or ``state_out`` that requires one is written only under
+    ``torch.no_grad()``."""
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, None, scale)
     N, H, K, V = shape.n_rows, shape.q_heads, shape.k_width, shape.v_width
     sources, src = N, None
@@ -369,9 +390,11 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
     if state_out is None:
         state_out = state if source is None else _new_state(shape, q.device)
     to = sp if state_out is state else _array(state_out, "state_out", torch.float32, (N, H, K, V), dev)
+    _writable(state_out, "state" if state_out is state else "state_out")
     out = q.new_empty((N, H, V))
     _check(lib.als_decay_attention_step(shape, code, hq, hk, hv, sp, sources, src, to, out.data_ptr(),
                                         _stream(dev)))
+    _written(state_out)
     return out, state_out
 
 
@@ -385,7 +408,7 @@ def beam_select(logits, scores, finished=None, end_token=-1, width=None):
     beams that go on with ``end_token`` alone at their own score. A candidate scores its beam's score
     plus the log-softmax of its item; equal scores go by the lowest beam, then the lowest item.
     Returns (parents int32, tokens int32, scores fp32, finished bool), each [lists, width] by
-    descending score; where candidates run out: 0, -1, -inf and False."""
+    descending score; where candidates run out: 0, -1, -inf and False. None carries a gradient."""
     dev = _device(logits, "logits")
     code = _dtype(logits, "logits")
     if logits.dim() != 3:
@@ -422,7 +445,9 @@ def beam_select(logits, scores, finished=None, end_token=-1, width=None):
 def reorder_states(states, parents, out=None):
     """The beams' states in their new order: out[b, w] = states[b, parents[b, w]] for ``states``
     [lists, beams, ...] of any type, contiguous, and ``parents`` int32 [lists, width]. ``out`` (a new
-    tensor if None) may be ``states`` itself where width equals beams."""
+    tensor if None) may be ``states`` itself where width equals beams; one that requires a gradient is
+    written only under ``torch.no_grad()``. A parent outside [0, beams) leaves its row of ``out`` as it is.
+    The result carries no gradient."""
     dev = _device(states, "states")
     if states.dim() < 2 or not states.is_contiguous():
         raise TypeError("states must be contiguous with the dimensions lists, beams, ...")
@@ -436,7 +461,9 @@ def reorder_states(states, parents, out=None):
         out = torch.empty(shape, dtype=states.dtype, device=states.device)
     else:
         _array(out, "out", states.dtype, shape, dev)
+        _writable(out, "out")
     size = math.prod(rest) * states.element_size()
     _check(lib.als_reorder_states(B, W, width, size, states.data_ptr(), out.data_ptr(), pp,
                                   _stream(dev)))
+    _written(out)
     return out
