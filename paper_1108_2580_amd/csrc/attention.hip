@@ -205,7 +205,8 @@ template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 
 // Rows are cut into segments of L = 2^shift tokens, which run side by side. Row b's segments have the
 // slots row_ptr[b] / L + b onwards: at least as many as it has segments, one for an empty row, and
 // never another row's. The segments that are not their row's last, whose states the later ones need,
-// have the entries row_ptr[b] / L onwards, again never another row's.
+// have the entries row_ptr[b] / L onwards, again never another row's. States are kept by entry (a batch of
+// short rows has few): at first of the entry's segment alone, then before the segment after it.
 struct Place {
   int64_t first;    // of the row's tokens
   int32_t len;      // tokens of the row
@@ -409,23 +410,22 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
   const unsigned block = blockIdx.x / (unsigned)A.n;
   const int lane0 = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   const int lane = lane0, g = lane >> 4, m = lane & 15;
-  int64_t slot = A.slot0 + block / P.heads;
+  const int64_t index = A.slot0 + block / P.heads;
   const int head = (int)(block % P.heads);
   Place at;
   if (STATES) {
     if (A.places) {
-      slot = A.entries[slot];
+      const int32_t slot = A.entries[index];
       if (slot < 0 || slot >= A.n_slots) return;
       at = A.places[slot];
     } else {
-      at = find_place<true>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, slot, lane);
-      slot += at.row;
+      at = find_place<true>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, index, lane);
     }
   } else {
-    at = A.places ? A.places[slot]
-                  : find_place<false>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, slot, lane);
+    at = A.places ? A.places[index]
+                  : find_place<false>(P.row_ptr, P.n_rows, P.n_tokens, A.shift, index, lane);
   }
-  // a row_ptr that decreases leaves places unwritten: nothing is taken from them unchecked
+  // where row_ptr decreases, two rows write a place, in any mixture: nothing is taken from it unchecked
   if (at.row < 0 || at.row >= P.n_rows || at.first < 0 || at.len < 0 ||
       at.first + at.len > P.n_tokens)
     return;
@@ -467,9 +467,11 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
   f32x4 S[KT];
   const int64_t state = ((int64_t)at.row * P.heads + head) * (int64_t)P.k_width * P.v_width;
   const int col = wave * 16 + m;
-  // a segment's: row r, column c at r * segment_ld[0] + c * segment_ld[1]
-  float *slot_state = P.segments + (slot * P.heads + head) * (int64_t)(KP * VP);
-  const auto in_slot = [&](int kt, int e) {
+  // an entry's: row r, column c at r * segment_ld[0] + c * segment_ld[1]. This segment's own or, for
+  // outputs, the one before it; at.first + at.len <= n_tokens keeps it below n_tokens >> shift.
+  const int64_t entry = (at.first >> A.shift) + at.segment - (STATES ? 0 : 1);
+  float *entry_state = P.segments + (entry * P.heads + head) * (int64_t)(KP * VP);
+  const auto in_entry = [&](int kt, int e) {
     return (unsigned)(state_row(kt, g, e) * P.segment_ld[0] + col * P.segment_ld[1]);
   };
 #pragma unroll
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[kt][e] = slot_state[in_slot(kt, e)];
+      for (int e = 0; e < 4; ++e) S[kt][e] = entry_state[in_entry(kt, e)];
   } else if (at.segment == 0 && P.first_state) {
     const float *from = P.first_state + state;
 #pragma unroll
@@ -709,7 +711,7 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) slot_state[in_slot(kt, e)] = S[kt][e];
+      for (int e = 0; e < 4; ++e) entry_state[in_entry(kt, e)] = S[kt][e];
   } else if (last && P.last_state) {
     float *to = P.last_state + state;
 #pragma unroll
@@ -743,28 +745,27 @@ __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float 
   }
   const int64_t first = clamped(row_ptr[row], 0, n_tokens);
   const int64_t len = clamped(row_ptr[row + 1], first, n_tokens) - first;
-  const int64_t slot = (first >> shift) + row;
-  const int64_t n = (len + (1LL << shift) - 1) >> shift;
-  if (n < 2 || slot + n > n_slots) return;
+  const int64_t entry = first >> shift, n = segments_of(len, shift) - 1;  // the row's entries
+  if (n < 2 || entry + n > n_tokens >> shift) return;
   const float raw = log_decay[head];
   const float a2 = (raw <= 0.f ? fmaxf(raw, kMinLogDecay) : __builtin_nanf("")) * kLog2e;
   const float whole = exp2_fast(a2 * (float)(1 << shift));
   const int64_t stride = heads * floats;
   for (int64_t x = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; x < floats;
        x += (int64_t)gridDim.y * 1024) {
-    float *p = segments + (slot * heads + head) * floats + x;
+    float *p = segments + (entry * heads + head) * floats + x;
     f32x4 state = *(const f32x4 *)p;
     constexpr int kAhead = 16;  // states on their way: the sums wait for each other, the reads need not
     for (int64_t j = 1; j < n; j += kAhead) {
       f32x4 own[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        own[i] = j + i + 1 < n ? *(const f32x4 *)(p + (j + i) * stride) : f32x4{0.f, 0.f, 0.f, 0.f};
+        own[i] = j + i < n ? *(const f32x4 *)(p + (j + i) * stride) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
         if (j + i < n) {
-          *(f32x4 *)(p + (j + i) * stride) = state;
           state = state * whole + own[i];
+          *(f32x4 *)(p + (j + i) * stride) = state;
         }
     }
   }
@@ -954,7 +955,7 @@ AttentionSpace attention_space(als_dtype dtype, int64_t n_tokens, int64_t n_rows
     x.entries = (entries * 4 + 15) / 16 * 16;
   }
   if (n_tokens > 1LL << shift)  // else no row is longer than a segment
-    x.states = slots * heads * padded_width3(k_width) * padded_width3(v_width) * 4;
+    x.states = entries * heads * padded_width3(k_width) * padded_width3(v_width) * 4;
   return x;
 }
 
