@@ -546,7 +546,8 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
 /*
  * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores
  *   scores[w] + logits[w, v] - log sum_u exp(logits[w, u]),
- * and the best `width` of all (w, v) go on, equal scores by the lowest (w, v).
+ * and the best `width` of all (w, v) go on; of equal scores (in fp64) the lowest beam's, then the
+ * largest logit's, then the lowest item's.
  *   beams, width   1 .. 32. n_items 1 .. 2^31 - 1. n_lists 0 .. 2^31 - 1. Outputs overlap no input.
  *   logits         device [n_lists * beams, n_items], rows row_stride values apart. -inf and NaN mask
  *                  an item; +inf counts as the largest finite value.

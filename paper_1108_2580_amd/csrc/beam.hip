@@ -2,15 +2,19 @@
 //
 // A list (one user's answer) is kept as W beams. Beam w extended by item v has the score
 //   c_w + x_wv - max_v x - log sum_v exp(x_wv - max_v x),
-// with the beam's score c and its logits x; the best `width` of the W V candidates go on, equal
-// scores by the lowest (w, v). A finished beam has one candidate: the end item, at its own score.
-// Masked items (-inf or NaN) and dead beams (a score of -inf or NaN) have none.
+// with the beam's score c and its logits x; the best `width` of the W V candidates go on. A finished
+// beam has one candidate: the end item, at its own score. Masked items (-inf or NaN) and dead beams (a
+// score of -inf or NaN) have none.
+//
+// Order: score in fp64, then the lowest beam, the largest logit, the lowest item. Scores of one beam
+// never order against its logits, but beside a logit (or under a score) some 2^53 times larger they may
+// be equal where those differ; with the logit in the order, each beam's is that of its logits, as each
+// slice finds it without knowing the score.
 //
 // The logits are read once, by k_slices: a block keeps a slice of a row in registers, takes its
-// maximum and its sum of exponentials, and writes the slice's best `width` items. Within a row
-// scores order as logits do, so those are all that can be chosen. k_merge takes one list's slices,
-// forms log-sum-exp and scores in fp64 from them (so that two candidates tie only where their
-// logits do) and ranks those that reach the width-th best head of the sorted slices.
+// maximum and its sum of exponentials, and writes the slice's best `width` items, which are all that
+// can be chosen of it. k_merge takes one list's slices, forms log-sum-exp and scores in fp64 from them
+// and ranks those that reach the width-th best head of the sorted slices.
 #include <cfloat>
 
 #include "internal.h"
@@ -205,11 +209,14 @@ __global__ __launch_bounds__(kThreads) void k_slices(const T *__restrict__ logit
 
 struct Candidate {
   double score;
-  uint64_t place;  // beam << 32 | item
+  uint64_t key;   // of the logit and the item
+  uint32_t beam;  // kMaxBeams: no candidate
 };
 __device__ __forceinline__ bool better(const Candidate &a, const Candidate &b) {
-  return a.score > b.score || (a.score == b.score && a.place < b.place);
+  return a.score > b.score ||
+         (a.score == b.score && (a.beam < b.beam || (a.beam == b.beam && a.key > b.key)));
 }
+__device__ __forceinline__ uint32_t item_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
 // One block a list, for whom it is a chain of latencies (statistics, log-sum-exp, heads, candidates,
 // ranks): 6.7 us for 4 lists of candidates, 7.1 us for 104 (8 beams), 14.5 us for 2448 (16 beams).
@@ -262,20 +269,19 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
   __syncthreads();
   // Every (beam, slice) list is sorted, so that `width` of the lists' heads reach a bound, and no
   // candidate below it can be chosen: those that reach it are gathered and ranked at once.
-  const Candidate none = {-INFINITY, ~0ull};
+  const Candidate none = {-INFINITY, 0, kMaxBeams};
   const auto of_key = [&](int l, int j, uint64_t key) {  // candidate j of list l, whose key this is
     const int w = l / slices;
     if (kind[w] == 2)  // finished
-      return l == w * slices && j == 0 ? Candidate{base[w], (uint64_t)w << 32 | (uint32_t)end} : none;
+      return l == w * slices && j == 0 ? Candidate{base[w], key_of(0.f, (uint32_t)end), (uint32_t)w} : none;
     if (kind[w] == 0 || !key) return none;
-    return Candidate{base[w] + ((double)from_ordered((uint32_t)(key >> 32)) - top[w]),
-                     (uint64_t)w << 32 | (0xffffffffu - (uint32_t)key)};
+    return Candidate{base[w] + ((double)from_ordered((uint32_t)(key >> 32)) - top[w]), key, (uint32_t)w};
   };
   const auto head = [&](int l, int j) { return of_key(l, j, best[(int64_t)l * width + j]); };
   const auto write = [&](int i, const Candidate &c) {
-    const bool any = c.place != ~0ull;
-    const int p = any ? (int)(c.place >> 32) : 0;
-    const int t = any ? (int)(uint32_t)c.place : -1;
+    const bool any = c.beam < kMaxBeams;
+    const int p = any ? (int)c.beam : 0;
+    const int t = any ? (int)item_of(c.key) : -1;
     const int64_t to = list * width + i;
     parents[to] = p;
     tokens[to] = t;
@@ -311,7 +317,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const Candidate c = of_key(l, j + i, keys[i]);
-        if (c.place == ~0ull || ordered((float)c.score) < most) return;
+        if (c.beam == kMaxBeams || ordered((float)c.score) < most) return;
         const int n = atomicAdd(&n_found, 1);
         if (n < kFound) found[n] = c;
       }
@@ -334,20 +340,20 @@ __global__ __launch_bounds__(kMergeThreads) void k_merge(
     return;
   }
   // many equal scores: one at a time
-  Candidate last = {INFINITY, 0};
+  Candidate last = none;
   for (int i = 0; i < width; ++i) {
     Candidate mine = none;
     for (int l = tid; l < lists; l += kMergeThreads)
       for (int j = 0; j < width; ++j) {
         const Candidate c = head(l, j);
-        if (c.place == ~0ull) break;
+        if (c.beam == kMaxBeams) break;
         if (i == 0 || better(last, c)) {
           if (better(c, mine)) mine = c;
           break;
         }
       }
     for (int o = 32; o > 0; o >>= 1) {
-      const Candidate c = {__shfl_xor(mine.score, o), __shfl_xor(mine.place, o)};
+      const Candidate c = {__shfl_xor(mine.score, o), __shfl_xor(mine.key, o), __shfl_xor(mine.beam, o)};
       if (better(c, mine)) mine = c;
     }
     if (lane == 0) found[wave] = mine;

@@ -406,7 +406,8 @@ def beam_select(logits, scores, finished=None, end_token=-1, width=None):
     ``logits``: fp32 or bf16 [lists, beams, items] (-inf and NaN mask an item); ``scores``: fp32
     [lists, beams], -inf for a beam without candidates; ``finished``: bool or uint8 [lists, beams],
     beams that go on with ``end_token`` alone at their own score. A candidate scores its beam's score
-    plus the log-softmax of its item; equal scores go by the lowest beam, then the lowest item.
+    plus the log-softmax of its item; equal scores (in fp64) go by the lowest beam, then the largest
+    logit, then the lowest item.
     Returns (parents int32, tokens int32, scores fp32, finished bool), each [lists, width] by
     descending score; where candidates run out: 0, -1, -inf and False. None carries a gradient."""
     dev = _device(logits, "logits")
