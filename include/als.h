@@ -486,7 +486,7 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,
  * S being k_width x v_width; S before the first token is zero or initial_state.
  *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^30.
- *   q, k, v        token strides at most 2^22 values.
+ *   q, k, v        token strides at most 2^22 values (d_out too; any where n_tokens is 1).
  *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
  *                  values out of [0, n_tokens] are taken as the nearest bound.
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
@@ -529,7 +529,8 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
                                         void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /*
- * One token of each of n_rows rows (n_tokens and row_ptr of shape are not read):
+ * One token of each of n_rows rows (n_tokens and row_ptr of shape are not read; q, k and v may have any
+ * strides):
  *   state_out = exp(log_decay) state[source] + k v^T,   out = scale state_out^T q.
  *   state        device fp32 [n_sources, q_heads, k_width, v_width].
  *   source       nullable (row r goes on from state r, n_sources = n_rows): device int32[n_rows], the

@@ -165,10 +165,11 @@ als_status check_attention(const als_attention *s, als_dtype dtype, bool step) {
 
 // One token's stride means nothing and may be anything (a slice of a large tensor has its own): it is taken
 // out, since a pass from the last token to the first addresses its rows from those that would lie below.
-als_status check_input(const char *name, als_heads &x, int64_t n, int size) {
+// A step addresses its rows in 64 bits, at any stride.
+als_status check_input(const char *name, als_heads &x, int64_t n, int size, bool step = false) {
   if (n <= 1) x.token_stride = 0;
   const char *w = wrong(x, n, size);
-  if (!w && x.token_stride > als::kMaxTokenStride) w = "a token_stride above 2^22";
+  if (!w && !step && x.token_stride > als::kMaxTokenStride) w = "a token_stride above 2^22";
   return w ? fail_without_context(ALS_ERR_INVALID_ARG, "%s has %s", name, w) : ALS_OK;
 }
 
@@ -413,9 +414,9 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
   if (als_status st = check_attention(shape, dtype, true)) return st;
   const als_attention *s = shape;
   const int size = size_of(dtype);
-  if (als_status st = check_input("q", q, s->n_rows, size)) return st;
-  if (als_status st = check_input("k", k, s->n_rows, size)) return st;
-  if (als_status st = check_input("v", v, s->n_rows, size)) return st;
+  if (als_status st = check_input("q", q, s->n_rows, size, true)) return st;
+  if (als_status st = check_input("k", k, s->n_rows, size, true)) return st;
+  if (als_status st = check_input("v", v, s->n_rows, size, true)) return st;
   REQUIRE(n_sources >= 0 && n_sources <= kMax31, "n_sources %lld out of range", (long long)n_sources);
   REQUIRE(source || n_sources == s->n_rows, "%lld states for %lld rows without source",
           (long long)n_sources, (long long)s->n_rows);

@@ -21,3 +21,21 @@ def test_one_token_of_any_stride(stride, dtype):
            *p.decay_attention_backward(far(d_out), far(q), far(k), far(v), a, ptr, None, S0, dS)]
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_steps_of_rows_far_apart(dtype):
+    """Rows more than 2^22 values apart, as one token of each history in a padded batch."""
+    import paper_1108_2580_amd as p
+
+    q, k, v, a, _, _, S0, _ = attention_inputs([1, 1, 1], 4, 2, 64, 48, dtype, 31)
+    apart = (1 << 22) + 8
+
+    def far(t):
+        n = t[0].numel()
+        x = torch.empty(2 * apart + n, dtype=t.dtype, device=t.device).as_strided((3, n), (apart, 1))
+        return x.copy_(t.flatten(1)).unflatten(1, t.shape[1:])
+
+    want = p.decay_attention_step(q, k, v, a, S0.clone())
+    got = p.decay_attention_step(far(q), far(k), far(v), a, S0.clone())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -76,3 +76,11 @@ def test_two_tokens_strides_are_bounded(recorder, case, dtype):
     assert 63 * (1 << 22) * 4 < 1 << 31
     r, out = launches(recorder, 48, case, dtype, 2, 1 << 22)
     assert r.returncode == 0 and out, r.stderr
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("stride", [(1 << 22) + 64, 1 << 30])
+def test_a_steps_rows_may_lie_any_distance_apart(recorder, dtype, stride):
+    """As one token of each history in a padded batch does. The step addresses its rows in 64 bits."""
+    r, out = launches(recorder, 1, "step", dtype, 3, stride)
+    assert r.returncode == 0 and len(out) == 1, r.stderr
