@@ -9,10 +9,10 @@ A next-item model reads a user's ratings in the order of time and answers with l
 Argument marshalling only: the work runs in the HIP kernels of ``csrc/``. Every call is enqueued on
 the current HIP stream of the current device, on which its tensors have to lie, and nothing is
 synchronised. Inputs are fp32 or bf16 tensors whose features are contiguous; tokens and heads may
-have any strides. Where an input of ``norm_rotate`` or ``decay_attention`` requires a gradient, the
-result carries it, or the call raises where there is none for that input (``cos``, ``sin``,
-``log_decay``). The other operators' results carry none. What a call writes to a caller's tensor counts as
-an in-place operation.
+have any strides (tokens of ``decay_attention`` up to 2^22 values). Where an input of ``norm_rotate`` or
+``decay_attention`` requires a gradient, the result carries it, or the call raises where there is none
+for that input (``cos``, ``sin``, ``log_decay``). The other operators' results carry none. What a call
+writes to a caller's tensor counts as an in-place operation.
 """
 from __future__ import annotations
 
@@ -244,9 +244,13 @@ def norm_rotate_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, 
     return q_out, k_out, dwq, dwk
 
 
+MAX_TOKEN_STRIDE = 1 << 22  # of decay_attention
+
+
 def _dense(t):
-    """A gradient as the operators take it: contiguous features."""
-    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+    """A gradient, which has the strides that its graph gives it, as the operators take it."""
+    fits = (t.stride(-1) == 1 or t.shape[-1] == 1) and t.stride(0) <= MAX_TOKEN_STRIDE
+    return t if fits else t.contiguous()
 
 
 class _NormRotate(torch.autograd.Function):

@@ -39,3 +39,17 @@ def test_steps_of_rows_far_apart(dtype):
     want = p.decay_attention_step(q, k, v, a, S0.clone())
     got = p.decay_attention_step(far(q), far(k), far(v), a, S0.clone())
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_gradient_of_tokens_far_apart():
+    """The output's gradient has the strides that a graph gives it, whatever those of the call were."""
+    import paper_1108_2580_amd as p
+
+    q, k, v, a, ptr, d_out, *_ = attention_inputs([2, 1], 2, 2, 16, 16, "f32", 32)
+    q = q.clone().requires_grad_()
+    o = p.decay_attention(q, k, v, a, ptr)
+    apart = (1 << 22) + 8
+    far = torch.empty(2 * apart + 32, device="cuda:0").as_strided((3, 2, 16), (apart, 16, 1)).copy_(d_out)
+    want, = torch.autograd.grad(o, q, d_out, retain_graph=True)
+    got, = torch.autograd.grad(o, q, far)
+    assert torch.equal(got, want)
