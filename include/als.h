@@ -424,7 +424,8 @@ als_status als_tensor_sample_alpha(als_ctx *ctx, const float *U, const float *V,
  * reused as soon as the call's work on the stream is done), allocates nothing and synchronises
  * nothing. Everything is checked that the host can see; the values of row_ptr, positions, parents and
  * sources lie on the device, where one out of range is handled as stated and touches no memory
- * outside the buffers. Messages: als_last_error(NULL). Results are bitwise reproducible.
+ * outside the buffers. What a call writes overlaps nothing that it reads or writes elsewhere, but where
+ * stated. Messages: als_last_error(NULL). Results are bitwise reproducible.
  */
 typedef enum {
   ALS_F32 = 0,

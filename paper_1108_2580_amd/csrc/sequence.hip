@@ -34,7 +34,10 @@ Span span(const als_heads &x, int64_t n, int32_t heads, int32_t width, int size)
   return span(x.data,
               ((n - 1) * x.token_stride + (heads - 1) * x.head_stride + width) * (int64_t)size);
 }
-bool overlap(Span a, Span b) { return a.first < b.last && b.first < a.last; }
+bool overlap(Span a, Span b) {
+  return a.first < a.last && b.first < b.last && a.first < b.last && b.first < a.last;
+}
+Span optional(const void *p, int64_t bytes) { return p ? span(p, bytes) : Span{0, 0}; }
 bool same(const als_heads &a, const als_heads &b) {
   return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
 }
@@ -259,6 +262,14 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
   if (als_status st = check_both(shape, dtype, x, dy, out, weight)) return st;
   REQUIRE(dq_weight && dk_weight, "a NULL gradient of a weight");
   REQUIRE(dq_weight != dk_weight, "the weights' gradients are the same");
+  const Span dw[2] = {span(dq_weight, 4 * shape->width), span(dk_weight, 4 * shape->width)};
+  REQUIRE(!overlap(dw[0], dw[1]), "the weights' gradients overlap");
+  for (int i = 0; i < 2; ++i) {
+    const Span o = span(out[i], shape->n_tokens, i ? shape->k_heads : shape->q_heads, shape->width,
+                        size_of(dtype));
+    REQUIRE(!overlap(o, dw[0]) && !overlap(o, dw[1]), "a weight's gradient overlaps the output of %s",
+            i ? "k" : "q");
+  }
   if (als_status st = check_workspace(workspace, workspace_bytes, als_norm_rotate_workspace(shape)))
     return st;
   return launched(als::launch_rotate(dtype, true, *shape, x, dy, out, weight, dweight,
@@ -288,9 +299,13 @@ als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_
               !overlap(o, span(v, s->n_tokens, s->k_heads, s->v_width, size)),
           "out overlaps an input");
   const int64_t states = 4 * s->n_rows * s->q_heads * s->k_width * s->v_width;
-  REQUIRE(!initial_state || !final_state ||
-              !overlap(span(initial_state, states), span(final_state, states)),
-          "final_state overlaps initial_state");
+  const Span first = optional(initial_state, states), last = optional(final_state, states);
+  REQUIRE(!overlap(first, last), "final_state overlaps initial_state");
+  REQUIRE(!overlap(o, first) && !overlap(o, last), "out overlaps a state");
+  REQUIRE(!overlap(last, span(q, s->n_tokens, s->q_heads, s->k_width, size)) &&
+              !overlap(last, span(k, s->n_tokens, s->k_heads, s->k_width, size)) &&
+              !overlap(last, span(v, s->n_tokens, s->k_heads, s->v_width, size)),
+          "final_state overlaps an input");
   if (als_status st = check_workspace(workspace, workspace_bytes, space_bytes(s))) return st;
   AttentionPass p = pass_of(s, dtype, workspace);
   p.group = p.v_group = s->q_heads / s->k_heads;
@@ -342,12 +357,12 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
     REQUIRE(!overlap(outs[i], outs[(i + 1) % 3]), "two gradients overlap");
   }
   const int64_t states = 4 * s->n_rows * s->q_heads * s->k_width * s->v_width;
-  REQUIRE(!d_initial_state ||
-              ((!initial_state ||
-                !overlap(span(initial_state, states), span(d_initial_state, states))) &&
-               (!d_final_state ||
-                !overlap(span(d_final_state, states), span(d_initial_state, states)))),
-          "d_initial_state overlaps another state");
+  const Span first = optional(initial_state, states), last = optional(d_final_state, states),
+             d_first = optional(d_initial_state, states);
+  REQUIRE(!overlap(first, d_first) && !overlap(last, d_first), "d_initial_state overlaps another state");
+  for (const Span &x : outs)
+    REQUIRE(!overlap(x, first) && !overlap(x, last) && !overlap(x, d_first), "a gradient overlaps a state");
+  for (const Span &x : ins) REQUIRE(!overlap(d_first, x), "d_initial_state overlaps an input");
   if (als_status st = check_workspace(workspace, workspace_bytes,
                                       als_decay_attention_backward_workspace(s)))
     return st;
@@ -436,6 +451,11 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
               !overlap(o, span(k, s->n_rows, s->k_heads, s->k_width, size)) &&
               !overlap(o, span(v, s->n_rows, s->k_heads, s->v_width, size)),
           "out overlaps an input");
+  const Span to = span(state_out, s->n_rows * one);
+  REQUIRE(!overlap(to, span(q, s->n_rows, s->q_heads, s->k_width, size)) &&
+              !overlap(to, span(k, s->n_rows, s->k_heads, s->k_width, size)) &&
+              !overlap(to, span(v, s->n_rows, s->k_heads, s->v_width, size)),
+          "state_out overlaps an input");
   return launched(als::launch_attention_step(dtype, s->n_rows, s->q_heads, s->q_heads / s->k_heads,
                                              s->k_width, s->v_width, q, k, v, s->log_decay, s->scale,
                                              state, source, n_sources, state_out, out,
