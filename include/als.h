@@ -489,7 +489,8 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   n_tokens       all rows' tokens, 0 .. 2^31 - 1; n_rows 0 .. 2^30.
  *   q, k, v        token strides at most 2^22 values (d_out too; any where n_tokens is 1).
  *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
- *                  values out of [0, n_tokens] are taken as the nearest bound.
+ *                  values out of [0, n_tokens] are taken as the nearest bound. What out and the gradients
+ *                  hold for a token of no row stays as it is.
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
  *                  head h of k and v. k_width, v_width 1 .. 128.
  *   log_decay      device fp32[q_heads], <= 0 (-inf forgets at once); a head above 0 or NaN gives NaN.

@@ -194,8 +194,9 @@ __device__ __forceinline__ constexpr int state_row(int kt, int g, int e) {
 // different banks.
 template <typename T> constexpr int padded(int width) { return width + (sizeof(T) == 2 ? 16 : 4); }
 // Of rows of q and k. Three parts of them at up to 64 wide leave a CU a fourth block with half the
-// padding, which is worth more than the conflicts cost: 2000 rows of 25 at 33 x 50 171 -> 155 us, forward
-// and backward of 400 rows of 250 at 32 x 32 463 -> 440 us; at 128 wide it frees nothing (2860 -> 2970).
+// padding, which is worth more than the conflicts cost: 2000 rows of 25 at 33 x 50 174 -> 156 us, forward
+// and backward of 400 rows of 250 at 32 x 32 474 -> 452 us; at 128 wide it frees nothing (2290 -> 2400 us for
+// 100 rows of 1000, 8 heads).
 template <typename T> constexpr int key_row(int KP, int VP) {
   return KP + (sizeof(T) == 4 && KP < 128 && VP < 128 ? 8 : 16);
 }
@@ -385,14 +386,16 @@ template <typename T> constexpr int waves_for(int KP, int VP) {
 // One block: one head of one segment. STATES: only the state after the segment, for all segments of
 // a row but its last.
 //
-// What bounds it: neither HBM nor MFMA alone. A wave's chunk is a chain (LDS writes, barrier, weights,
-// barrier, products, update) that the other blocks of its CU have to cover: four of four waves for bf16
-// at 64 wide. Measured there, 4096 rows of 263 tokens, 8 heads: 1283 us forward (q, k, v and o move at
-// 3.4 TB/s of a copy's 4.8), 2807 us for the three passes backward (the seven tensors at 2.7 TB/s; read
-// from HBM once for all passes that share them, since those run side by side); one row of 62496: 61 us
-// after 28 us of states. f32 at 128 wide, 100 rows of 1000, 8 heads to 2 key heads: 532 us forward, 1754
-// us backward at two blocks a CU, which LDS allows. One chunk a row (2000 f32 rows of 25 at 33 x 50):
-// 117 us, the latency of a block from its first load to its last store, four blocks a CU.
+// What bounds it: vector instructions above all, and the chain of a wave's chunk (LDS writes, barrier,
+// weights, barrier, products, update) that the other blocks of its CU have to cover: four of four waves for
+// bf16 at 64 wide. Measured there, 4096 rows of 263 tokens, 8 heads: 1350 us forward (q, k, v and o move at
+// 3.3 TB/s of a copy's 4.8), 2910 us for the three passes backward (the seven tensors at 2.6 TB/s); vector
+// instructions issue in 72 and 82 % of the SIMDs' cycles, MFMA is busy in 25 and 29 %. The passes backward
+// read past L2 what each of them needs (9.9 GB), since a row's three blocks lie on three XCDs. One row of
+// 62496: 63 us after 27 us of states. f32 at 128 wide, 100 rows of 1000, 8 heads to 2 key heads: 570 us
+// forward, 1480 us backward (issue 69 and 70 %, MFMA 42 %) at two blocks a CU, which LDS allows. One chunk
+// a row (2000 f32 rows of 25 at 33 x 50): 119 us, the latency of a block from its first load to its last
+// store, four blocks a CU.
 template <typename T, int KP, int VP, bool STATES, bool VEC>
 __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args A) {
   constexpr int C = chunk_tokens<T>(), NT = C / 16, NW = VP / 16, THREADS = NW * 64;
@@ -727,7 +730,7 @@ __global__ __launch_bounds__(VP * 4, waves_for<T>(KP, VP)) void k_attention(Args
 
 // States after each segment alone -> states before each segment: one block (of blockIdx.y parts) a
 // head of a row, one thread four values of the state. Bound by the latency of a long row's reads, 16 at
-// a time: 15 us for 8 heads' 122 states of 64 x 64 (31 MB moved); where rows are many, by HBM.
+// a time: 14 us for 8 heads' 121 states of 64 x 64 (32 MB moved); where rows are many, by HBM.
 __global__ __launch_bounds__(256) void k_join_segments(float *first_pass, float *second_pass,
                                                        const int64_t *row_ptr, int64_t n_rows,
                                                        int64_t index0, int64_t n_tokens,
@@ -935,10 +938,10 @@ template <typename T> hipError_t launch_t(const Args &A, bool split, hipStream_t
 // Short segments fill the chip where tokens are few; each costs a pass over its k and v and a state
 // written and read. From four chunks up, as many as leave 1024 blocks (bf16: what the chip holds at
 // a time) or 2048 (f32, whose chunks are half as long), at most 2048 tokens. Us with segments of 256,
-// 512, 1024 and 2048 tokens: one row of 62496 bf16 tokens, 8 heads of 64: 133, 119, 120, 169; forward
-// and backward of 4096 such rows of 263: 5430, 4620, 4180, 4000 (4096: 3990); of 100 f32 rows of 1000,
-// 8 heads of 128: 2900, 2650, 2590, 2810, of 1000 f32 rows of 262, 8 heads of 64: 2450, 2230, 2110,
-// 2160; forward of 8 bf16 rows of 250: 32, 47, 78, 77.
+// 512, 1024 and 2048 tokens: one row of 62496 bf16 tokens, 8 heads of 64: 138, 126, 125, 163; forward
+// and backward of 4096 such rows of 263: 5700, 4990, 4570, 4430; of 100 f32 rows of 1000, 8 heads of 128
+// to 2: 2860, 2630, 2660, 2890, of 1000 f32 rows of 262, 8 heads of 64: 2400, 2200, 2110, 2270; forward
+// of 8 bf16 rows of 250: 32, 49, 79, 85.
 int attention_shift(als_dtype dtype, int64_t n_tokens, int32_t heads) {
   int shift = dtype == ALS_F32 ? 7 : 8;
   while (shift < 11 && (n_tokens >> shift) * heads > (dtype == ALS_F32 ? 2048 : 1024)) ++shift;

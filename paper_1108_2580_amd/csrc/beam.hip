@@ -6,10 +6,10 @@
 // beam has one candidate: the end item, at its own score. Masked items (-inf or NaN) and dead beams (a
 // score of -inf or NaN) have none.
 //
-// Order: score in fp64, then the lowest beam, the largest logit, the lowest item. Scores of one beam
-// never order against its logits, but beside a logit (or under a score) some 2^53 times larger they may
-// be equal where those differ; with the logit in the order, each beam's is that of its logits, as each
-// slice finds it without knowing the score.
+// Order: score in fp64, then the lowest beam, the largest logit, the lowest item. A beam's scores rise
+// with its logits, but beside a logit (or under a score) some 2^53 times larger they may be equal where
+// the logits differ; with the logit in the order, a beam's candidates go by their logits in any case, as
+// a slice orders them without knowing the score.
 //
 // The logits are read once, by k_slices: a block keeps a slice of a row in registers, takes its
 // maximum and its sum of exponentials, and writes the slice's best `width` items, which are all that
@@ -219,7 +219,7 @@ __device__ __forceinline__ bool better(const Candidate &a, const Candidate &b) {
 __device__ __forceinline__ uint32_t item_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
 // One block a list, for whom it is a chain of latencies (statistics, log-sum-exp, heads, candidates,
-// ranks): 6.7 us for 4 lists of candidates, 7.1 us for 104 (8 beams), 14.5 us for 2448 (16 beams).
+// ranks): 7.2 us for 4 lists of candidates, 7.9 us for 104 (8 beams), 15.3 us for 2448 (16 beams).
 __global__ __launch_bounds__(kMergeThreads) void k_merge(
     int64_t list0, int beams, int width, int slices, const float *__restrict__ scores,
     const uint8_t *__restrict__ finished, int32_t end, const SliceStats *__restrict__ stats,

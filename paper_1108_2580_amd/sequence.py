@@ -318,7 +318,9 @@ def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
 
     ``q``: [tokens, heads, key width]; ``k``, ``v``: [tokens, key heads, width], each key head shared
     by heads / key heads query heads; widths up to 128. ``log_decay``: fp32 [heads], <= 0.
-    ``row_ptr``: int64 [rows + 1] on the device, row b holding tokens row_ptr[b] .. row_ptr[b + 1].
+    ``row_ptr``: int64 [rows + 1] on the device, from 0 to the number of tokens, row b holding tokens
+    row_ptr[b] .. row_ptr[b + 1] - 1; a token that no row holds (padding behind the last row) is not
+    worked on, and its place in the new tensors, outputs and gradients, is left unset.
     ``scale``: 1 / sqrt(key width) if None. ``initial_state``: fp32 [rows, heads, key width, value
     width], zero if None. Returns out [tokens, heads, value width], with ``return_state`` (out, the
     states after the rows' last tokens). ``log_decay`` takes no gradient."""
