@@ -547,6 +547,89 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
                                     void *hip_stream);
 
 /*
+ * Softmax attention with a bias for each bucket of the gap of time between two tokens: for the tokens
+ * j <= i of a row, t their positions,
+ *   s_ij = scale q_i . k_j + bias[h, #{bounds <= t_i - t_j}],   o_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij).
+ * A token all of whose scores are -inf has the output zero.
+ *   n_tokens       all rows' tokens, 0 .. 2^31 - 256; n_rows 0 .. 2^30.
+ *   q, k, v        token strides at most 2^22 values (d_out too; any where n_tokens is 1).
+ *   row_ptr        as for als_decay_attention; it is not read beyond its n_rows + 1 values.
+ *   positions      device int32[n_tokens], any values; a gap below 0 is in bucket 0, one that does not fit 32
+ *                  bits counts as the largest that does.
+ *   buckets        1 .. 64; bounds: host int32[buckets - 1], >= 1 and ascending, the first gap of each bucket but
+ *                  the first. They are read within the call. (Up to 8191 a table in LDS holds the gaps' buckets;
+ *                  larger ones are searched, which takes longer.)
+ *   bias           device fp32[q_heads, buckets]; -inf masks a bucket.
+ *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
+ *                  head h of k and v. width 1 .. 128.
+ *   out            device [n_tokens, q_heads, width], packed.
+ *   stats, rest    what the gradients read, both nullable: stats device fp32 [2, q_heads, n_tokens], rest
+ *                  like out (bf16 only), what out's rounding left out.
+ * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
+ * NaN. Scores, weights and sums are fp32; weights of bf16 values enter their product as two bf16 values (off by
+ * 2^-16 at most).
+ */
+typedef struct {
+  int64_t n_tokens;
+  int64_t n_rows;
+  const int64_t *row_ptr;
+  const int32_t *positions;
+  const float *bias;
+  const int32_t *bounds;
+  int32_t q_heads;
+  int32_t k_heads;
+  int32_t width;
+  int32_t buckets;
+  float scale;
+} als_gaps;
+
+int64_t als_gap_attention_workspace(const als_gaps *shape);
+als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q, als_heads k, als_heads v,
+                             void *out, float *stats, void *rest, void *workspace, int64_t workspace_bytes,
+                             void *hip_stream);
+
+/*
+ * Gradients of als_gap_attention: dq [n_tokens, q_heads, width], dk and dv [n_tokens, k_heads, width], packed,
+ * and dbias fp32 [q_heads, buckets], from that of its output (d_out), its outputs (packed) and what it left in
+ * stats and rest. Without rest (nullable) the gradients take in out's rounding.
+ */
+int64_t als_gap_attention_backward_workspace(const als_gaps *shape);
+als_status als_gap_attention_backward(const als_gaps *shape, als_dtype dtype, als_heads d_out, als_heads q,
+                                      als_heads k, als_heads v, const void *out, const float *stats,
+                                      const void *rest, void *dq, void *dk, void *dv, float *dbias,
+                                      void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * One token of each beam of n_rows lists (q_positions its position): als_gap_attention's output over all tokens
+ * of the list's row of k, v and positions, which its beams share (strides of any size), and the `steps` tokens
+ * of the beam's own path.
+ *   beams          1 .. 32; n_rows * beams 0 .. 2^31 - 1. steps 0 .. 2^20.
+ *   q, q_positions, out  of n_rows * beams tokens, a list's beams one after the other; out packed.
+ *   k, v           of path: values of step s at data + s * k_step (v_step), a token each list and beam.
+ *   positions      of path: device int32 [steps, n_rows * beams].
+ *   path           device int32 [n_rows * beams, steps], rows path_stride apart: the beam of the list that holds
+ *                  each step of a beam's path; one outside [0, beams) gives NaN.
+ * With steps 0 the path's tensors are not read.
+ */
+typedef struct {
+  int32_t beams;
+  int32_t steps;
+  const int32_t *q_positions;
+  als_heads k;
+  als_heads v;
+  int64_t k_step;
+  int64_t v_step;
+  const int32_t *positions;
+  const int32_t *path;
+  int64_t path_stride;
+} als_gap_path;
+
+int64_t als_gap_attention_step_workspace(const als_gaps *shape, const als_gap_path *path);
+als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *path, als_dtype dtype, als_heads q,
+                                  als_heads k, als_heads v, void *out, void *workspace,
+                                  int64_t workspace_bytes, void *hip_stream);
+
+/*
  * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores
  *   scores[w] + logits[w, v] - log sum_u exp(logits[w, u]),
  * and the best `width` of all (w, v) go on; of equal scores (in fp64) the lowest beam's, then the

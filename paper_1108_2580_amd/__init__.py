@@ -40,6 +40,9 @@ EXPORTS = ("als_create", "als_half_sweep", "als_last_rmse_in", "als_rmse", "als_
            "als_norm_rotate", "als_norm_rotate_workspace", "als_norm_rotate_backward",
            "als_decay_attention", "als_decay_attention_workspace", "als_decay_attention_backward",
            "als_decay_attention_backward_workspace", "als_decay_attention_step",
+           "als_gap_attention", "als_gap_attention_workspace", "als_gap_attention_backward",
+           "als_gap_attention_backward_workspace", "als_gap_attention_step",
+           "als_gap_attention_step_workspace",
            "als_beam_select", "als_beam_select_workspace", "als_reorder_states",
            "als_destroy", "als_status_str", "als_last_error")
 
@@ -498,5 +501,6 @@ class ALS:
 
 # the sequence operators, which need no rating matrix
 from .sequence import (beam_select, decay_attention, decay_attention_backward,  # noqa: E402
-                       decay_attention_step, norm_rotate, norm_rotate_backward, reorder_states,
+                       decay_attention_step, gap_attention, gap_attention_backward,
+                       gap_attention_step, norm_rotate, norm_rotate_backward, reorder_states,
                        rotary_tables)

@@ -1,0 +1,235 @@
+// What the kernels of attention over gaps of time share (gap.hip: forward, gap_back.hip: gradients,
+// gap_step.hip: one token of each beam): the rows of tokens, the buckets of gaps, and fragments of
+// queries that lie in global memory.
+#pragma once
+
+#include "tiles.h"
+
+namespace als {
+
+// The keys [first, i] that a token i reads as a query, and the queries [i, end) that read it as a key.
+// Of a token that no row holds: neither.
+struct Span2 {
+  int32_t first, end;
+};
+constexpr int32_t kNoRow = 0x7fffffff;  // first of a token without a row
+
+// Up to as many rows a block counts those that begin at its tokens or before; for more there is a
+// table, whose launch costs about as much as 64 rows' counting in each block.
+constexpr int64_t kCountedRows = 64;
+
+__device__ __forceinline__ Span2 span_from(const int64_t *row_ptr, int64_t n_rows, int64_t n_tokens,
+                                           int64_t row, int64_t t) {
+  Span2 s = {kNoRow, 0};
+  if (row >= 0 && row < n_rows) {
+    const int64_t first = clamped(row_ptr[row], 0, n_tokens), end = clamped(row_ptr[row + 1], first, n_tokens);
+    if (t >= first && t < end) {
+      s.first = (int32_t)first;
+      s.end = (int32_t)end;
+    }
+  }
+  return s;
+}
+__device__ __forceinline__ Span2 span_of(const GapShape &G, const Span2 *spans, int64_t t) {
+  if (t >= G.n_tokens) return {kNoRow, 0};
+  if (spans) return spans[t];
+  int64_t row = -1;
+  for (int64_t r = 0; r < G.n_rows; ++r) row += G.row_ptr[r] <= t ? 1 : 0;
+  return span_from(G.row_ptr, G.n_rows, G.n_tokens, row, t);
+}
+
+// a - b, at the ends of the range where it does not fit
+__device__ __forceinline__ int32_t gap_of(int32_t a, int32_t b) { return __builtin_elementwise_sub_sat(a, b); }
+
+// ---- buckets --------------------------------------------------------------------------------------
+// The bucket of a gap is the number of bounds at it or below. Up to kTableGaps a table holds it for each
+// gap, a byte each; where the last bound is larger the bounds are searched. Either way the bias comes from
+// a second read, whose 64 places are 64 banks.
+constexpr int kTableGaps = 8192;
+constexpr float kLargest = 3.402823466e38f;
+
+struct Buckets {
+  uint32_t kinds[kTableGaps / 4];  // a byte a gap
+  int32_t bounds[64];
+  float bias[64];                  // times log2 e, finite where it was
+
+  // by the first 64 threads, with a barrier before fill
+  __device__ __forceinline__ void start(const GapShape &G, int head, int tid) {
+    if (tid < 64) {
+      const float b = tid < G.buckets ? G.bias[(int64_t)head * G.buckets + tid] : 0.f;
+      float x = b * kLog2e;
+      if (fabsf(b) <= kLargest) x = fminf(fmaxf(x, -kLargest), kLargest);
+      bias[tid] = x;
+      bounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+    }
+  }
+  // `most`: no larger gap is asked for
+  __device__ __forceinline__ void fill(const GapShape &G, int32_t most, int tid, int threads) {
+    if (G.last_bound >= kTableGaps) return;
+    const int32_t top = most < G.last_bound ? most : G.last_bound;
+    for (int w = tid; w <= top / 4; w += threads) {
+      int n = 0;  // bounds at the word's first gap or below, then at the others
+#pragma unroll
+      for (int step = 32; step > 0; step >>= 1)
+        if (bounds[n + step - 1] <= w * 4) n += step;
+      uint32_t word = (uint32_t)n;
+#pragma unroll
+      for (int e = 1; e < 4; ++e) {
+        while (n < G.buckets - 1 && bounds[n] <= w * 4 + e) ++n;
+        word |= (uint32_t)n << (8 * e);
+      }
+      kinds[w] = word;
+    }
+  }
+  template <bool TABLE> __device__ __forceinline__ int kind(const GapShape &G, int32_t gap) const {
+    if (TABLE) {
+      const int32_t g = gap < 0 ? 0 : gap > G.last_bound ? G.last_bound : gap;
+      return ((const uint8_t *)kinds)[g];
+    }
+    int n = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1)
+      if (bounds[n + step - 1] <= gap) n += step;
+    return n < G.buckets - 1 ? n : G.buckets - 1;
+  }
+  __device__ __forceinline__ int kind(const GapShape &G, int32_t gap) const {
+    return G.last_bound < kTableGaps ? kind<true>(G, gap) : kind<false>(G, gap);
+  }
+};
+// Up to this bias a score's largest is as good as the score itself: exponents may take their
+// difference first.
+constexpr float kPlainBias = 16777216.f;
+
+// ---- fragments of a row in global memory ---------------------------------------------------------
+// 8 values from column c of the row at p as they lie there, zero past `width`.
+template <typename T> struct Raw8 {
+  T v[8];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *p, int c, int width, bool vec) {
+  Raw8<T> x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x.v[e] = (T)0.f;
+  if (vec) {
+    constexpr int E = 16 / sizeof(T);
+    struct alignas(16) Piece { T v[E]; };
+#pragma unroll
+    for (int n = 0; n < 8; n += E)
+      if (c + n < width) __builtin_memcpy(x.v + n, (const Piece *)(p + c + n), 16);
+  } else if (c + 8 <= width) {  // at any alignment of the type
+    __builtin_memcpy(x.v, p + c, 8 * sizeof(T));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < width) x.v[e] = p[c + e];
+  }
+  return x;
+}
+template <typename T> __device__ __forceinline__ f32x4 low4(const Raw8<T> &x) {
+  return f32x4{(float)x.v[0], (float)x.v[1], (float)x.v[2], (float)x.v[3]};
+}
+template <typename T> __device__ __forceinline__ f32x4 high4(const Raw8<T> &x) {
+  return f32x4{(float)x.v[4], (float)x.v[5], (float)x.v[6], (float)x.v[7]};
+}
+// as operands: bf16 values as they are, fp32 ones in three parts
+template <typename T> __device__ __forceinline__ Frag<kParts<T>> operand(const Raw8<T> &x) {
+  if constexpr (sizeof(T) == 4) {
+    return as_frag<3>(low4(x), high4(x));
+  } else {
+    return Frag<1>{{__builtin_bit_cast(bf16x8, x)}};
+  }
+}
+template <int NP> __device__ __forceinline__ Frag<NP> negated(Frag<NP> f) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) f.p[n] = -f.p[n];
+  return f;
+}
+template <typename T, int D>
+__device__ __forceinline__ void load_row(const T *p, int width, bool vec, int lane,
+                                         Frag<kParts<T>> *f) {
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) f[d] = operand(load8(p, d * 32 + (lane >> 4) * 8, width, vec));
+}
+
+// Four values at p, at any alignment of the type, of which `n` belong to the row.
+template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 x, int n) {
+  using V4 = typename Vec4<T>::type;
+  const V4 r = __builtin_convertvector(x, V4);
+  if (n >= 4) {
+    __builtin_memcpy(p, &r, sizeof r);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = (T)x[e];
+  }
+}
+
+__device__ __forceinline__ bool finite4(f32x4 x) {
+  return x[0] * 0.f + x[1] * 0.f + (x[2] * 0.f + x[3] * 0.f) == 0.f;
+}
+
+// Over the lanes of a column (lane & 15): the sum or the largest.
+__device__ __forceinline__ float column_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float column_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int n = 1; n < 64; n <<= 1) x = min(x, __shfl_xor(x, n));
+  return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int n = 1; n < 64; n <<= 1) x = max(x, __shfl_xor(x, n));
+  return x;
+}
+
+// to[c] += rows 16 c + 4 g .. 4 g + 3 of x^T W, g the lane's group, for x in LDS and 16-row tiles of weights W
+// as MFMA leaves them (a lane: column m = lane & 15, rows 4 g .. 4 g + 3). In a tile of which a mask leaves
+// only the places that ok(row) names, W is zero elsewhere, which an infinity or NaN in x would turn into
+// NaN: where a sum is not finite it is formed again over the places that are left, one row at a time.
+template <int NP, int TILES, int C, typename Columns, typename OK>
+__device__ __forceinline__ void add_kept(const f32x4 *w, const bf16 *x, int ld, int part, int lane,
+                                         Columns product, OK ok, f32x4 *to) {
+  f32x4 sum[C];
+  bool finite = true;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    sum[c] = product(c, f32x4{0.f, 0.f, 0.f, 0.f});
+    finite = finite && finite4(sum[c]);
+  }
+  if (__any(!finite)) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) sum[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int r = 0; r < 16 * TILES; ++r) {
+      float weight = 0.f;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (r / 16 == t && r % 4 == e) weight = w[t][e];
+      weight = __shfl(weight, r % 16 / 4 * 16 + (lane & 15));
+      if (ok(r)) {
+        const bf16 *p = x + r * ld + (lane >> 4) * 4;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float v = 0.f;
+#pragma unroll
+            for (int n = NP - 1; n >= 0; --n) v += (float)p[n * part + c * 16 + e];
+            sum[c][e] = fmaf(weight, v, sum[c][e]);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) to[c] += sum[c];
+}
+
+}  // namespace als

@@ -1,0 +1,352 @@
+// Softmax attention over packed rows of tokens (a user's ratings in the order of time), with a bias that
+// each head learns for each bucket of the gap of time between two tokens: for the tokens j <= i of a row,
+//   s_ij = scale q_i . k_j + bias[bucket(t_i - t_j)],  p_ij = exp(s_ij) / sum_j exp(s_ij),
+//   o_i = sum_j p_ij v_j.
+//
+// One pass over the keys: a block holds 64 or 128 queries of a head, reads keys and values in tiles through
+// LDS, and keeps the largest score and the sum of the exponentials so far. Both products are on MFMA with
+// the queries as columns, so that the weights are operands of the second as they lie in registers. A block's
+// queries are neighbours in the packed order, of one row or of several: a token's row says which keys it
+// reads, so that short rows share tiles.
+//
+// Rounding. Scores, weights, sums and outputs are fp32; bf16 weights enter their product in two bf16 parts,
+// off by 2^-16 at most (one would cost an output as much again as its own rounding).
+#include "gap.h"
+#include "internal.h"
+
+namespace als {
+
+namespace {
+
+__global__ __launch_bounds__(256) void k_gap_spans(GapShape G, Span2 *__restrict__ spans) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= G.n_tokens) return;
+  int64_t lo = 0, hi = G.n_rows + 1;  // rows that begin at t or before
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (G.row_ptr[mid] <= t) lo = mid + 1; else hi = mid;
+  }
+  spans[t] = span_from(G.row_ptr, G.n_rows, G.n_tokens, lo - 1, t);
+}
+
+struct ReadArgs {
+  GapShape G;
+  als_heads q, k, v;
+  const Span2 *spans;  // nullable: counted
+  void *out, *rest;    // rest nullable
+  float *stats;        // nullable
+  int64_t tile0, n_tiles;
+  bool vec_q;
+};
+
+template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 32; }
+// Columns of 16 queries a wave.
+template <typename T> constexpr int query_tiles() { return sizeof(T) == 2 ? 2 : 1; }
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
+  constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+  constexpr int NP = kParts<T>, RP = kReadParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
+  using Staged = Tile<T, KN, D, 256, VEC>;
+  __shared__ __align__(16) bf16 lk[NP * PART];
+  __shared__ __align__(16) bf16 lv[NP * PART];
+  __shared__ __align__(16) int32_t lpos[KN];
+  __shared__ int32_t lrange[2];
+  __shared__ Buckets lb;
+
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  const int head = (int)(blockIdx.x % (unsigned)G.heads);
+  // a row's last tokens have the most keys: they go first
+  const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
+  const int64_t t0 = tile * BQ;
+
+  lb.start(G, head, tid);
+  // the block's keys: from its first row's first token to its last token that has a row
+  int span_first[QT], block_first = kNoRow, block_last = -1;
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int64_t t = t0 + n * 64 + lane;
+    span_first[n] = span_of(G, A.spans, t).first;
+    block_first = min(block_first, span_first[n]);
+    if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
+  }
+  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
+  block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
+  if (block_last < 0) return;
+
+  // this wave's queries, one a lane and tile
+  const int i0 = (int)t0 + wave * 16 * QT;
+  int at[QT], first[QT], pos[QT];
+  unsigned before[QT];
+  int first_min = kNoRow, first_max = 0, last = -1, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
+  Frag<NP> qf[QT][DF];
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int index = wave * 16 * QT + n * 16 + m;  // in the block
+    at[n] = (int)t0 + index;
+    first[n] = __shfl(span_first[0], index & 63);
+    if (QT > 1 && wave >= 2) first[n] = __shfl(span_first[QT - 1], index & 63);
+    const bool real = first[n] != kNoRow;
+    before[n] = real ? (unsigned)(at[n] - first[n]) : 0u;
+    first_min = min(first_min, first[n]);
+    first_max = max(first_max, first[n]);
+    if (real) last = max(last, at[n]);
+    const int64_t t = real ? at[n] : block_last;
+    pos[n] = G.positions[t];
+    pos_min = min(pos_min, pos[n]);
+    pos_max = max(pos_max, pos[n]);
+    load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_q,
+                   lane, qf[n]);
+    if (G.scale < 0.f) {
+#pragma unroll
+      for (int d = 0; d < DF; ++d) qf[n][d] = negated(qf[n][d]);
+    }
+  }
+  first_min = __builtin_amdgcn_readfirstlane(wave_min(first_min));
+  first_max = __builtin_amdgcn_readfirstlane(wave_max(first_max));
+  last = __builtin_amdgcn_readfirstlane(wave_max(last));
+  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
+  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  const float scale = fabsf(G.scale) * kLog2e;
+
+  const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
+  const char *v = (const char *)((const T *)A.v.data + head / G.group * A.v.head_stride);
+  const int64_t k_row = A.k.token_stride * (int)sizeof(T), v_row = A.v.token_stride * (int)sizeof(T);
+  Staged hk, hv;
+  int hpos = 0;
+  const auto rows_of = [&](const char *x, int64_t bytes, int k0) {
+    return typename Staged::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
+                                 block_last + 1 - k0 < KN ? block_last + 1 - k0 : KN, G.width};
+  };
+  const auto fetch = [&](int k0) {
+    hk.fetch(rows_of(k, k_row, k0), tid);
+    hv.fetch(rows_of(v, v_row, k0), tid);
+    if (wave == 0) hpos = G.positions[min(k0 + lane % KN, block_last)];
+  };
+  fetch(block_first);
+  __syncthreads();
+  lb.fill(G, 0x7fffffff, tid, 256);
+
+  f32x4 o[QT][DT];
+  float top[QT], base[QT], sum[QT];
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    top[n] = -__builtin_inff();
+    base[n] = sum[n] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int k0 = block_first; k0 <= block_last; k0 += KN) {
+    __syncthreads();
+    hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
+    hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
+    if (wave == 0) {
+      const int lo = wave_min(hpos), hi = wave_max(hpos);
+      if (lane < KN) lpos[lane] = hpos;
+      if (lane == 0) {
+        lrange[0] = lo;
+        lrange[1] = hi;
+      }
+    }
+    __syncthreads();
+    if (k0 + KN <= block_last) fetch(k0 + KN);
+    if (k0 > last || k0 + KN <= first_min) continue;
+
+    const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
+    f32x4 s[QT][KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+      for (int n = 0; n < QT; ++n) s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < DF; ++d) {
+        const Frag<NP> kf = frag_row<NP>(lk + t * 16 * LD + d * 32, LD, PART, lane);
+#pragma unroll
+        for (int n = 0; n < QT; ++n) s[n][t] = mma(kf, qf[n][d], s[n][t]);
+      }
+    }
+
+    // one bucket for the tile's gaps, or one for each
+    const int near = lb.kind(G, gap_of(pos_min, lrange[1])), far = lb.kind(G, gap_of(pos_max, lrange[0]));
+    const float b = lb.bias[near];
+    const bool one = __builtin_amdgcn_readfirstlane(near) == __builtin_amdgcn_readfirstlane(far);
+    const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+    float most[QT];
+    if (plain) {
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        most[n] = s[n][0][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most[n] = fmaxf(most[n], s[n][t][e]);
+        most[n] = fmaf(most[n], scale, b);
+      }
+    } else {
+      const auto biased = [&](auto bias_of) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n) most[n] = -__builtin_inff();
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          int kpos[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kpos[e] = lpos[t * 16 + g * 4 + e];
+#pragma unroll
+          for (int n = 0; n < QT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x = fmaf(s[n][t][e], scale, bias_of(pos[n], kpos[e]));
+              const int j = k0 + t * 16 + g * 4 + e;
+              if (partial && (unsigned)(j - first[n]) > before[n]) x = -__builtin_inff();
+              s[n][t][e] = x;
+              most[n] = fmaxf(most[n], x);
+            }
+        }
+      };
+      if (one)
+        biased([&](int, int) { return b; });
+      else if (G.last_bound < kTableGaps)
+        biased([&](int i, int j) { return lb.bias[lb.kind<true>(G, gap_of(i, j))]; });
+      else
+        biased([&](int i, int j) { return lb.bias[lb.kind<false>(G, gap_of(i, j))]; });
+    }
+
+    // The largest score so far is followed only where it has grown by 8: exponentials up to 2^8 keep
+    // their precision, and most tiles leave the sums as they are.
+    bool grown = false;
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      most[n] = column_max(most[n]);
+      grown = grown || most[n] > top[n] + 8.f;
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        const bool none = top[n] == -__builtin_inff();  // so far: there is nothing to scale
+        top[n] = fmaxf(top[n], most[n]);
+        const float next = top[n] == -__builtin_inff() ? 0.f : top[n];
+        const float factor = none ? 0.f : exp2_fast(base[n] - next);
+        base[n] = next;
+        sum[n] *= factor;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) o[n][c] *= factor;
+      }
+    }
+
+    Frag<RP> pf[QT][KS];
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      const float shift = b - base[n];
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = exp2_fast(plain ? fmaf(s[n][t][e], scale, shift) : s[n][t][e] - base[n]);
+          s[n][t][e] = x;
+          sum[n] += x;
+        }
+#pragma unroll
+      for (int w = 0; w < KS; ++w) pf[n][w] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
+    }
+    if (!partial) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+          const Frag<NP> vf = frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane);
+#pragma unroll
+          for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n][w], o[n][c]);
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < QT; ++n)
+        add_kept<NP, KT, DT>(
+            s[n], lv, LD, PART, lane,
+            [&](int c, f32x4 x) {
+#pragma unroll
+              for (int w = 0; w < KS; ++w)
+                x = mma(frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane), pf[n][w], x);
+              return x;
+            },
+            [&](int r) { return (unsigned)(k0 + r - first[n]) <= before[n]; }, o[n]);
+    }
+  }
+
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const float total = column_sum(sum[n]);
+    if (first[n] == kNoRow) continue;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      const int d = c * 16 + g * 4;
+      if (d >= G.width) continue;
+      const f32x4 x = o[n][c] * inv;
+      store4((T *)A.out + row + d, x, G.width - d);
+      if constexpr (sizeof(T) == 2) {
+        if (A.rest) {
+          f32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = x[e] - (float)(T)x[e];
+          store4((T *)A.rest + row + d, y, G.width - d);
+        }
+      }
+    }
+    if (A.stats && g == 0) {
+      float *to = A.stats + (int64_t)head * G.n_tokens + at[n];
+      to[0] = base[n];
+      to[(int64_t)G.heads * G.n_tokens] = total == 0.f ? __builtin_inff() : __log2f(total);
+    }
+  }
+}
+
+template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStream_t s) {
+  constexpr int BQ = 64 * query_tiles<T>();
+  A.n_tiles = (A.G.n_tokens + BQ - 1) / BQ;
+  const int64_t per = max_blocks(256) / A.G.heads;
+  for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
+    const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
+    const dim3 grid((unsigned)(n * A.G.heads));
+    if (vec)
+      hipLaunchKernelGGL((k_gap_read<T, D, true>), grid, dim3(256), 0, s, A);
+    else
+      hipLaunchKernelGGL((k_gap_read<T, D, false>), grid, dim3(256), 0, s, A);
+  }
+  return hipGetLastError();
+}
+template <typename T> hipError_t launch_read(const ReadArgs &A, bool vec, hipStream_t s) {
+  return A.G.width <= 32   ? launch_read<T, 32>(A, vec, s)
+         : A.G.width <= 64 ? launch_read<T, 64>(A, vec, s)
+                           : launch_read<T, 128>(A, vec, s);
+}
+
+}  // namespace
+
+int64_t gap_spans_bytes(int64_t n_tokens, int64_t n_rows) {
+  return n_rows > kCountedRows ? (n_tokens * (int64_t)sizeof(Span2) + 15) / 16 * 16 : 0;
+}
+
+hipError_t launch_gap_spans(const GapShape &G, void *spans, hipStream_t s) {
+  if (!spans || G.n_tokens == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_gap_spans, dim3((unsigned)((G.n_tokens + 255) / 256)), dim3(256), 0, s, G,
+                     (Span2 *)spans);
+  return hipGetLastError();
+}
+
+hipError_t launch_gap_read(als_dtype dtype, const GapShape &G, const als_heads &q, const als_heads &k,
+                           const als_heads &v, const void *spans, void *out, float *stats, void *rest,
+                           hipStream_t s) {
+  if (G.n_tokens == 0) return hipSuccess;
+  const int size = dtype == ALS_F32 ? 4 : 2;
+  const auto vec = [&](const als_heads &x) {
+    return aligned16(x.data, x.token_stride, x.head_stride, G.width, size);
+  };
+  ReadArgs A{G, q, k, v, (const Span2 *)spans, out, rest, stats, 0, 0, vec(q)};
+  const bool all = vec(k) && vec(v);
+  return dtype == ALS_F32 ? launch_read<float>(A, all, s) : launch_read<bf16>(A, all, s);
+}
+
+}  // namespace als

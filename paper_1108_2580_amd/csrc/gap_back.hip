@@ -1,0 +1,612 @@
+// Gradients of the attention over gaps of time (gap.hip). With do the gradient of the outputs, p_ij the
+// weights, formed anew from the saved largest scores and sums, and delta_i = do_i . o_i,
+//   ds_ij = p_ij (do_i . v_j - delta_i),
+//   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij do_i,
+//   dbias[b] = sum of ds_ij over the pairs whose gap is in bucket b.
+//
+// Two kernels, each with sums that stay in the registers of the block that owns them, so that no result
+// depends on an order of atomics: one over the keys of a block's queries (dq, dbias; it also leaves delta for
+// the other), one over the queries of a block's keys and, in turn, of the query heads that share them
+// (dk, dv). Scores and do . v are formed in both.
+//
+// Rounding. As forward: weights and ds enter products in two bf16 parts where the inputs are bf16. delta takes
+// what the outputs' rounding left out as well, so that dbias, fp32 whatever the inputs, does not hold it.
+#include "gap.h"
+#include "internal.h"
+
+namespace als {
+
+namespace {
+
+struct BackArgs {
+  GapShape G;
+  als_heads q, k, v, d_out;
+  const Span2 *spans;
+  const void *out, *rest;  // packed; rest nullable
+  const float *stats;
+  float *delta;            // [heads, n_tokens]
+  float *dbias_parts;      // [heads, buckets, n_tiles]
+  void *dq, *dk, *dv;      // packed
+  int64_t tile0, n_tiles;
+  bool vec_rows, vec_out;  // rows read from global memory as operands; out and rest
+};
+
+template <typename T> constexpr int tile_tokens() { return sizeof(T) == 2 ? 64 : 32; }
+template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 ? 2 : 1; }
+
+// ---- over keys: dq and dbias ---------------------------------------------------------------------
+
+// Sums by bucket: 32 columns a wave, two lanes each, which add one after the other: the order of a
+// column's terms is that of the program.
+constexpr int kColumns = 32;
+
+__device__ __forceinline__ void add_to(float *x, float y) {
+  __hip_atomic_fetch_add(x, y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
+  constexpr int KN = tile_tokens<T>(), QT = columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+  constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
+  using Staged = Tile<T, KN, D, 256, VEC>;
+  __shared__ __align__(16) bf16 lk[NP * PART];
+  __shared__ __align__(16) bf16 lv[NP * PART];
+  __shared__ __align__(16) int32_t lpos[KN];
+  __shared__ int32_t lrange[2];
+  __shared__ Buckets lb;
+  extern __shared__ float lsums[];  // [waves, buckets, kColumns]
+
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  const int head = (int)(blockIdx.x % (unsigned)G.heads);
+  const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
+  const int64_t t0 = tile * BQ;
+
+  lb.start(G, head, tid);
+  for (int n = tid; n < 4 * G.buckets * kColumns; n += 256) lsums[n] = 0.f;
+  int span_first[QT], block_first = kNoRow, block_last = -1;
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int64_t t = t0 + n * 64 + lane;
+    span_first[n] = span_of(G, A.spans, t).first;
+    block_first = min(block_first, span_first[n]);
+    if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
+  }
+  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
+  block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
+  float *parts = A.dbias_parts + (int64_t)head * G.buckets * A.n_tiles + tile;
+  if (block_last < 0) {
+    if (tid < G.buckets) parts[tid * A.n_tiles] = 0.f;
+    return;
+  }
+
+  const int i0 = (int)t0 + wave * 16 * QT;
+  int at[QT], first[QT], pos[QT];
+  unsigned before[QT];
+  float top[QT], logsum[QT], delta[QT];
+  int first_min = kNoRow, first_max = 0, last = -1, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
+  Frag<NP> qf[QT][DF], of[QT][DF];
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int index = wave * 16 * QT + n * 16 + m;
+    at[n] = (int)t0 + index;
+    first[n] = __shfl(span_first[0], index & 63);
+    if (QT > 1 && wave >= 2) first[n] = __shfl(span_first[QT - 1], index & 63);
+    const bool real = first[n] != kNoRow;
+    before[n] = real ? (unsigned)(at[n] - first[n]) : 0u;
+    first_min = min(first_min, first[n]);
+    first_max = max(first_max, first[n]);
+    if (real) last = max(last, at[n]);
+    const int64_t t = real ? at[n] : block_last;
+    pos[n] = G.positions[t];
+    pos_min = min(pos_min, pos[n]);
+    pos_max = max(pos_max, pos[n]);
+    load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_rows,
+                   lane, qf[n]);
+    const float *stats = A.stats + (int64_t)head * G.n_tokens + t;
+    top[n] = stats[0];
+    logsum[n] = stats[(int64_t)G.heads * G.n_tokens];
+    // delta, and do as operands
+    float x = 0.f;
+    const int64_t row = (t * G.heads + head) * G.width;
+#pragma unroll
+    for (int d = 0; d < DF; ++d) {
+      const int c = d * 32 + g * 8;
+      const Raw8<T> y = load8((const T *)A.d_out.data + t * A.d_out.token_stride + head * A.d_out.head_stride,
+                              c, G.width, A.vec_rows);
+      const Raw8<T> z = load8((const T *)A.out + row, c, G.width, A.vec_out);
+      f32x4 o[2] = {low4(z), high4(z)};
+      if constexpr (sizeof(T) == 2) {
+        if (A.rest) {
+          const Raw8<T> r = load8((const T *)A.rest + row, c, G.width, A.vec_out);
+          o[0] += low4(r);
+          o[1] += high4(r);
+        }
+      }
+      const f32x4 lo = low4(y), hi = high4(y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x = fmaf(lo[e], o[0][e], fmaf(hi[e], o[1][e], x));
+      of[n][d] = operand(y);
+      if (G.scale < 0.f) qf[n][d] = negated(qf[n][d]);
+    }
+    delta[n] = column_sum(x);
+    if (g == 0 && real) A.delta[(int64_t)head * G.n_tokens + t] = delta[n];
+  }
+  first_min = __builtin_amdgcn_readfirstlane(wave_min(first_min));
+  first_max = __builtin_amdgcn_readfirstlane(wave_max(first_max));
+  last = __builtin_amdgcn_readfirstlane(wave_max(last));
+  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
+  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  const float scale = fabsf(G.scale) * kLog2e;
+
+  const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
+  const char *v = (const char *)((const T *)A.v.data + head / G.group * A.v.head_stride);
+  const int64_t k_row = A.k.token_stride * (int)sizeof(T), v_row = A.v.token_stride * (int)sizeof(T);
+  Staged hk, hv;
+  int hpos = 0;
+  const auto rows_of = [&](const char *x, int64_t bytes, int k0) {
+    return typename Staged::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
+                                 block_last + 1 - k0 < KN ? block_last + 1 - k0 : KN, G.width};
+  };
+  const auto fetch = [&](int k0) {
+    hk.fetch(rows_of(k, k_row, k0), tid);
+    hv.fetch(rows_of(v, v_row, k0), tid);
+    if (wave == 0) hpos = G.positions[min(k0 + lane % KN, block_last)];
+  };
+  fetch(block_first);
+  __syncthreads();
+  lb.fill(G, 0x7fffffff, tid, 256);
+
+  f32x4 dq[QT][DT];
+#pragma unroll
+  for (int n = 0; n < QT; ++n)
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float *sums = lsums + wave * G.buckets * kColumns + (lane & (kColumns - 1));
+  const auto add_sum = [&](int kind, float x) {
+    if (lane < 32) add_to(sums + kind * kColumns, x);
+    if (lane >= 32) add_to(sums + kind * kColumns, x);
+  };
+  float run = 0.f;  // of the tiles so far whose gaps were all in bucket run_kind
+  int run_kind = 0;
+
+  for (int k0 = block_first; k0 <= block_last; k0 += KN) {
+    __syncthreads();
+    hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
+    hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
+    if (wave == 0) {
+      const int lo = wave_min(hpos), hi = wave_max(hpos);
+      if (lane < KN) lpos[lane] = hpos;
+      if (lane == 0) {
+        lrange[0] = lo;
+        lrange[1] = hi;
+      }
+    }
+    __syncthreads();
+    if (k0 + KN <= block_last) fetch(k0 + KN);
+    if (k0 > last || k0 + KN <= first_min) continue;
+
+    const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
+    const int near = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(pos_min, lrange[1])));
+    const int far = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(pos_max, lrange[0])));
+    const float b = lb.bias[near];
+    const bool one = near == far;
+    const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+    if (one && near != run_kind) {
+      add_sum(run_kind, run);
+      run = 0.f;
+      run_kind = near;
+    }
+#pragma unroll 1
+    for (int w = 0; w < KS; ++w) {  // 32 keys at a time
+      const bf16 *wk = lk + w * 32 * LD, *wv = lv + w * 32 * LD;
+      f32x4 s[QT][2], dp[QT][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n) s[n][t] = dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DF; ++d) {
+          const Frag<NP> kf = frag_row<NP>(wk + t * 16 * LD + d * 32, LD, PART, lane);
+          const Frag<NP> vf = frag_row<NP>(wv + t * 16 * LD + d * 32, LD, PART, lane);
+#pragma unroll
+          for (int n = 0; n < QT; ++n) {
+            s[n][t] = mma(kf, qf[n][d], s[n][t]);
+            dp[n][t] = mma(vf, of[n][d], dp[n][t]);
+          }
+        }
+      }
+      if (plain) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n) {
+          const float shift = b - top[n] - logsum[n];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = exp2_fast(fmaf(s[n][t][e], scale, shift));
+              s[n][t][e] = p * (dp[n][t][e] - delta[n]);
+              run += s[n][t][e];
+            }
+        }
+      } else {
+        const auto biased = [&](auto kind_of) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            int kpos[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kpos[e] = lpos[w * 32 + t * 16 + g * 4 + e];
+#pragma unroll
+            for (int n = 0; n < QT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int kind = kind_of(pos[n], kpos[e]);
+                const float x = fmaf(s[n][t][e], scale, one ? b : lb.bias[kind]);
+                const float p = exp2_fast(x - top[n] - logsum[n]);
+                float ds = p * (dp[n][t][e] - delta[n]);
+                const int j = k0 + w * 32 + t * 16 + g * 4 + e;
+                if (partial && (unsigned)(j - first[n]) > before[n]) ds = 0.f;
+                s[n][t][e] = ds;
+                if (one) run += ds; else add_sum(kind, ds);
+              }
+          }
+        };
+        if (one)
+          biased([&](int, int) { return near; });
+        else if (G.last_bound < kTableGaps)
+          biased([&](int i, int j) { return lb.kind<true>(G, gap_of(i, j)); });
+        else
+          biased([&](int i, int j) { return lb.kind<false>(G, gap_of(i, j)); });
+      }
+      Frag<RP> df[QT];
+#pragma unroll
+      for (int n = 0; n < QT; ++n) df[n] = as_frag<RP>(s[n][0], s[n][1]);
+      if (!partial) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          const Frag<NP> kf = frag_col<NP, 4>(wk + c * 16, LD, PART, lane);
+#pragma unroll
+          for (int n = 0; n < QT; ++n) dq[n][c] = mma(kf, df[n], dq[n][c]);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < QT; ++n)
+          add_kept<NP, 2, DT>(
+              s[n], wk, LD, PART, lane,
+              [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wk + c * 16, LD, PART, lane), df[n], x); },
+              [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, dq[n]);
+      }
+    }
+  }
+
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    if (first[n] == kNoRow) continue;
+    const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      const int d = c * 16 + g * 4;
+      if (d < G.width) store4((T *)A.dq + row + d, dq[n][c] * G.scale, G.width - d);
+    }
+  }
+  add_sum(run_kind, run);
+  __syncthreads();
+  // four threads a bucket, a wave's columns each
+  for (int n = tid; n < 4 * G.buckets; n += 256) {
+    const float *x = lsums + ((n & 3) * G.buckets + n / 4) * kColumns;
+    float sum = 0.f;
+    for (int c = 0; c < kColumns; ++c) sum += x[(c + n) & (kColumns - 1)];
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if ((n & 3) == 0) parts[n / 4 * A.n_tiles] = sum;
+  }
+}
+
+// dbias[h, b]: the blocks' parts, in fp64. One block a head and bucket.
+__global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ parts, int64_t n_tiles,
+                                                   float *__restrict__ dbias) {
+  __shared__ double sums[4];
+  const float *x = parts + blockIdx.x * n_tiles;
+  double sum = 0.0;
+  for (int64_t t = threadIdx.x; t < n_tiles; t += 256) sum += (double)x[t];
+#pragma unroll
+  for (int n = 1; n < 64; n <<= 1) sum += __shfl_xor(sum, n);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) dbias[blockIdx.x] = (float)(sums[0] + sums[1] + (sums[2] + sums[3]));
+}
+
+// ---- over queries: dk and dv ---------------------------------------------------------------------
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
+  constexpr int QN = tile_tokens<T>(), CT = columns<T, D>(), BK = 64 * CT, LD = D + 16, PART = QN * LD;
+  constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
+  using Staged = Tile<T, QN, D, 256, VEC>;
+  __shared__ __align__(16) bf16 lq[NP * PART];
+  __shared__ __align__(16) bf16 lo[NP * PART];
+  __shared__ __align__(16) int32_t lpos[QN];
+  __shared__ __align__(16) float ltop[QN], llog[QN], ldelta[QN];
+  __shared__ int32_t lrange[2];
+  __shared__ Buckets lb;
+
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  const int k_heads = G.heads / G.group;
+  const int k_head = (int)(blockIdx.x % (unsigned)k_heads);
+  const int64_t t0 = (A.tile0 + blockIdx.x / (unsigned)k_heads) * BK;
+
+  // the block's queries: from its first token that has a row to its last row's end
+  int span_end[CT], block_first = kNoRow, block_end = 0;
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    const int64_t t = t0 + n * 64 + lane;
+    span_end[n] = span_of(G, A.spans, t).end;
+    if (span_end[n] > 0) block_first = min(block_first, (int)t);
+    block_end = max(block_end, span_end[n]);
+  }
+  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
+  block_end = __builtin_amdgcn_readfirstlane(wave_max(block_end));
+  if (block_end == 0) return;
+
+  // this wave's keys, one a lane and tile
+  const int j0 = (int)t0 + wave * 16 * CT;
+  int at[CT], pos[CT];
+  unsigned after[CT];  // queries from the key on
+  int end_min = kNoRow, end_max = 0, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
+  Frag<NP> kf[CT][DF], vf[CT][DF];
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    const int index = wave * 16 * CT + n * 16 + m;
+    at[n] = (int)t0 + index;
+    int end = __shfl(span_end[0], index & 63);
+    if (CT > 1 && wave >= 2) end = __shfl(span_end[CT - 1], index & 63);
+    after[n] = end > 0 ? (unsigned)(end - at[n]) : 0u;
+    end_min = min(end_min, end);
+    end_max = max(end_max, end);
+    const int64_t t = end > 0 ? at[n] : block_first;
+    pos[n] = G.positions[t];
+    pos_min = min(pos_min, pos[n]);
+    pos_max = max(pos_max, pos[n]);
+    load_row<T, D>((const T *)A.k.data + t * A.k.token_stride + k_head * A.k.head_stride, G.width, A.vec_rows,
+                   lane, kf[n]);
+    load_row<T, D>((const T *)A.v.data + t * A.v.token_stride + k_head * A.v.head_stride, G.width, A.vec_rows,
+                   lane, vf[n]);
+    if (G.scale < 0.f) {
+#pragma unroll
+      for (int d = 0; d < DF; ++d) kf[n][d] = negated(kf[n][d]);
+    }
+  }
+  end_min = __builtin_amdgcn_readfirstlane(wave_min(end_min));
+  end_max = __builtin_amdgcn_readfirstlane(wave_max(end_max));
+  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
+  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  const float scale = fabsf(G.scale) * kLog2e;
+  const int64_t q_row = A.q.token_stride * (int)sizeof(T), o_row = A.d_out.token_stride * (int)sizeof(T);
+
+  f32x4 dk[CT][DT], dv[CT][DT];
+#pragma unroll
+  for (int n = 0; n < CT; ++n)
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int head = k_head * G.group; head < (k_head + 1) * G.group; ++head) {
+    __syncthreads();
+    lb.start(G, head, tid);
+    if (head == k_head * G.group) {
+      __syncthreads();
+      lb.fill(G, 0x7fffffff, tid, 256);
+    }
+    const char *q = (const char *)((const T *)A.q.data + head * A.q.head_stride);
+    const char *o = (const char *)((const T *)A.d_out.data + head * A.d_out.head_stride);
+    const float *stats = A.stats + (int64_t)head * G.n_tokens;
+    const float *log_stats = stats + (int64_t)G.heads * G.n_tokens;
+    const float *deltas = A.delta + (int64_t)head * G.n_tokens;
+    Staged hq, ho;
+    int hpos = 0;
+    float hstat = 0.f;
+    const auto rows_of = [&](const char *x, int64_t bytes, int q0) {
+      return typename Staged::Rows{x + q0 * bytes, (uint32_t)bytes, 0,
+                                   block_end - q0 < QN ? block_end - q0 : QN, G.width};
+    };
+    const auto fetch = [&](int q0) {
+      hq.fetch(rows_of(q, q_row, q0), tid);
+      ho.fetch(rows_of(o, o_row, q0), tid);
+      const int t = min(q0 + lane % QN, block_end - 1);
+      if (wave == 0) hpos = G.positions[t];
+      if (wave == 1) hstat = stats[t];
+      if (wave == 2) hstat = log_stats[t];
+      if (wave == 3) hstat = deltas[t];
+    };
+    fetch(block_first);
+
+    for (int q0 = block_first; q0 < block_end; q0 += QN) {
+      __syncthreads();
+      hq.put_parts(lq, LD, rows_of(q, q_row, q0), tid);
+      ho.put_parts(lo, LD, rows_of(o, o_row, q0), tid);
+      if (wave == 0) {
+        const int low = wave_min(hpos), high = wave_max(hpos);
+        if (lane < QN) lpos[lane] = hpos;
+        if (lane == 0) {
+          lrange[0] = low;
+          lrange[1] = high;
+        }
+      } else if (lane < QN) {
+        (wave == 1 ? ltop : wave == 2 ? llog : ldelta)[lane] = hstat;
+      }
+      __syncthreads();
+      if (q0 + QN < block_end) fetch(q0 + QN);
+      if (q0 + QN <= j0 || q0 >= end_max) continue;
+
+      const bool partial = q0 < j0 + 16 * CT - 1 || q0 + QN > end_min;
+      const int near = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(lrange[0], pos_max)));
+      const int far = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(lrange[1], pos_min)));
+      const float b = lb.bias[near];
+      const bool one = near == far;
+      const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+#pragma unroll 1
+      for (int w = 0; w < QS; ++w) {  // 32 queries at a time
+        const bf16 *wq = lq + w * 32 * LD, *wo = lo + w * 32 * LD;
+        f32x4 s[CT][2], dp[CT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int n = 0; n < CT; ++n) s[n][t] = dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int d = 0; d < DF; ++d) {
+            const Frag<NP> qf = frag_row<NP>(wq + t * 16 * LD + d * 32, LD, PART, lane);
+            const Frag<NP> of = frag_row<NP>(wo + t * 16 * LD + d * 32, LD, PART, lane);
+#pragma unroll
+            for (int n = 0; n < CT; ++n) {
+              s[n][t] = mma(qf, kf[n][d], s[n][t]);
+              dp[n][t] = mma(of, vf[n][d], dp[n][t]);
+            }
+          }
+        }
+        const auto weigh = [&](auto bias_of) {  // s, dp -> p, ds
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int r = w * 32 + t * 16 + g * 4;
+            const f32x4 top = *(const f32x4 *)(ltop + r), logsum = *(const f32x4 *)(llog + r),
+                        delta = *(const f32x4 *)(ldelta + r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float shift = b - top[e] - logsum[e];
+              const int qpos = lpos[r + e];
+#pragma unroll
+              for (int n = 0; n < CT; ++n) {
+                const float x =
+                    plain ? fmaf(s[n][t][e], scale, shift)
+                          : fmaf(s[n][t][e], scale, bias_of(qpos, pos[n])) - top[e] - logsum[e];
+                float p = exp2_fast(x), ds = p * (dp[n][t][e] - delta[e]);
+                if (partial && (unsigned)(q0 + r + e - at[n]) >= after[n]) p = ds = 0.f;
+                s[n][t][e] = p;
+                dp[n][t][e] = ds;
+              }
+            }
+          }
+        };
+        if (one)
+          weigh([&](int, int) { return b; });
+        else if (G.last_bound < kTableGaps)
+          weigh([&](int i, int j) { return lb.bias[lb.kind<true>(G, gap_of(i, j))]; });
+        else
+          weigh([&](int i, int j) { return lb.bias[lb.kind<false>(G, gap_of(i, j))]; });
+        Frag<RP> pf[CT], df[CT];
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+          pf[n] = as_frag<RP>(s[n][0], s[n][1]);
+          df[n] = as_frag<RP>(dp[n][0], dp[n][1]);
+        }
+        if (!partial) {
+#pragma unroll
+          for (int c = 0; c < DT; ++c) {
+            const Frag<NP> of = frag_col<NP, 4>(wo + c * 16, LD, PART, lane);
+            const Frag<NP> qf = frag_col<NP, 4>(wq + c * 16, LD, PART, lane);
+#pragma unroll
+            for (int n = 0; n < CT; ++n) {
+              dv[n][c] = mma(of, pf[n], dv[n][c]);
+              dk[n][c] = mma(qf, df[n], dk[n][c]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < CT; ++n) {
+            const auto ok = [&](int r) { return (unsigned)(q0 + w * 32 + r - at[n]) < after[n]; };
+            add_kept<NP, 2, DT>(
+                s[n], wo, LD, PART, lane,
+                [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wo + c * 16, LD, PART, lane), pf[n], x); },
+                ok, dv[n]);
+            add_kept<NP, 2, DT>(
+                dp[n], wq, LD, PART, lane,
+                [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wq + c * 16, LD, PART, lane), df[n], x); },
+                ok, dk[n]);
+          }
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    if (after[n] == 0) continue;
+    const int64_t row = ((int64_t)at[n] * k_heads + k_head) * G.width;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      const int d = c * 16 + g * 4;
+      if (d >= G.width) continue;
+      store4((T *)A.dk + row + d, dk[n][c] * G.scale, G.width - d);
+      store4((T *)A.dv + row + d, dv[n][c], G.width - d);
+    }
+  }
+}
+
+template <typename T, int D> constexpr int block_tokens() { return 64 * columns<T, D>(); }
+
+template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float *dbias, hipStream_t s) {
+  constexpr int B = block_tokens<T, D>();
+  A.n_tiles = (A.G.n_tokens + B - 1) / B;
+  const auto each = [&](auto kernel, int heads, size_t lds) {
+    const int64_t per = max_blocks(256) / heads;
+    for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
+      const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(n * heads)), dim3(256), lds, s, A);
+    }
+  };
+  each(vec ? k_gap_dq<T, D, true> : k_gap_dq<T, D, false>, A.G.heads,
+       4 * A.G.buckets * kColumns * sizeof(float));
+  hipLaunchKernelGGL(k_gap_dbias, dim3((unsigned)(A.G.heads * A.G.buckets)), dim3(256), 0, s, A.dbias_parts,
+                     A.n_tiles, dbias);
+  each(vec ? k_gap_dkv<T, D, true> : k_gap_dkv<T, D, false>, A.G.heads / A.G.group, 0);
+  return hipGetLastError();
+}
+template <typename T> hipError_t launch_back(const BackArgs &A, bool vec, float *dbias, hipStream_t s) {
+  return A.G.width <= 32   ? launch_back<T, 32>(A, vec, dbias, s)
+         : A.G.width <= 64 ? launch_back<T, 64>(A, vec, dbias, s)
+                           : launch_back<T, 128>(A, vec, dbias, s);
+}
+
+int64_t rounded(int64_t x) { return (x + 15) / 16 * 16; }
+
+}  // namespace
+
+GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t buckets) {
+  // tiles of 64 tokens at least
+  return {gap_spans_bytes(n_tokens, n_rows), rounded(4 * n_tokens * heads),
+          rounded(4 * ((n_tokens + 63) / 64) * heads * buckets)};
+}
+
+hipError_t launch_gap_back(als_dtype dtype, const GapShape &G, const als_heads &d_out, const als_heads &q,
+                           const als_heads &k, const als_heads &v, const void *out, const float *stats,
+                           const void *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
+                           hipStream_t s) {
+  const GapBackSpace x = gap_back_space(G.n_tokens, G.n_rows, G.heads, G.buckets);
+  char *w = (char *)workspace;
+  BackArgs A{};
+  A.G = G;
+  A.q = q;
+  A.k = k;
+  A.v = v;
+  A.d_out = d_out;
+  A.spans = x.spans ? (const Span2 *)w : nullptr;
+  A.out = out;
+  A.rest = rest;
+  A.stats = stats;
+  A.delta = (float *)(w + x.spans);
+  A.dbias_parts = (float *)(w + x.spans + x.delta);
+  A.dq = dq;
+  A.dk = dk;
+  A.dv = dv;
+  const int size = dtype == ALS_F32 ? 4 : 2;
+  const auto vec = [&](const als_heads &h) {
+    return aligned16(h.data, h.token_stride, h.head_stride, G.width, size);
+  };
+  A.vec_rows = vec(q) && vec(k) && vec(v) && vec(d_out);
+  A.vec_out = ((uintptr_t)out | (uintptr_t)rest | (uint64_t)(G.width * size)) % 16 == 0;
+  hipError_t e = launch_gap_spans(G, x.spans ? w : nullptr, s);
+  if (e != hipSuccess) return e;
+  return dtype == ALS_F32 ? launch_back<float>(A, A.vec_rows, dbias, s)
+                          : launch_back<bf16>(A, A.vec_rows, dbias, s);
+}
+
+}  // namespace als

@@ -1,0 +1,431 @@
+// One token of each beam of each list, over the list's row of the history (gap.hip's scores) and the
+// tokens that the beam has chosen itself: those lie by step and beam, and a table says which beam holds
+// each step of a beam's path, so that nothing is copied where beams fork.
+//
+// The history is read once for all beams of a list and all query heads that share a key head: they are the
+// columns of the products. Rows are cut into segments that run side by side; a second kernel joins a beam's
+// segments with its path. Bound by HBM: every key and value is read once.
+#include "gap.h"
+#include "internal.h"
+
+namespace als {
+
+namespace {
+
+struct StepArgs {
+  GapShape G;
+  GapPath P;
+  als_heads q, k, v;
+  void *out;
+  float *parts;   // [slots, heads, beams, width]
+  float *stats;   // [slots, heads, beams, 2]: the largest score (-inf: none) and the sum
+  int64_t slot0, row0;
+  int shift, passes;
+  bool vec, vec_path;
+};
+
+// Partials of slot, head, beam.
+__device__ __forceinline__ int64_t part_index(const StepArgs &A, int64_t slot, int head, int beam) {
+  return (slot * A.G.heads + head) * A.P.beams + beam;
+}
+
+// One block: a segment, a key head and up to 16 CT of its columns (beams and the head's query heads). A wave
+// takes every fourth 32 keys.
+template <typename T, int D, int CT>
+__global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
+  constexpr int LD = D + 16, PART = 32 * LD, NP = kParts<T>, RP = kReadParts<T>, DF = D / 32, DT = D / 16;
+  constexpr int COLS = 16 * CT, V8 = D / 8, ROWS = 64 / V8, VN = 32 / ROWS, LB = 65;
+  __shared__ __align__(16) bf16 lv[4][NP * PART];
+  __shared__ __align__(16) int32_t lkind[4][32];
+  __shared__ int32_t lbounds[64];
+  __shared__ float lbias[COLS * LB];
+  __shared__ float ltop[4][COLS], lsum[4][COLS];
+  __shared__ __align__(16) float lout[COLS * D];
+
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  const int k_heads = G.heads / G.group, columns = A.P.beams * G.group;
+  unsigned block = blockIdx.x;
+  const int col0 = (int)(block % (unsigned)A.passes) * COLS;
+  block /= (unsigned)A.passes;
+  const int k_head = (int)(block % (unsigned)k_heads);
+  const int64_t slot = A.slot0 + block / (unsigned)k_heads;
+  const Place at = find_place<false>(G.row_ptr, G.n_rows, G.n_tokens, A.shift, slot, lane);
+  const int64_t begin = at.segment << A.shift;
+  if (at.segment < 0 || begin >= at.len) return;
+  const int count = (int)(at.len - begin < 1LL << A.shift ? at.len - begin : 1LL << A.shift);
+  const int64_t token0 = at.first + begin;
+
+  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+  for (int x = tid; x < COLS * G.buckets; x += 256) {
+    const int c = x / G.buckets, n = x % G.buckets, col = min(col0 + c, columns - 1);
+    const float b = G.bias[(int64_t)(k_head * G.group + col % G.group) * G.buckets + n];
+    float y = b * kLog2e;
+    if (fabsf(b) <= kLargest) y = fminf(fmaxf(y, -kLargest), kLargest);
+    lbias[c * LB + n] = y;
+  }
+
+  Frag<NP> qf[CT][DF];
+  int pos[CT];
+  bool alike = true;
+  const int64_t rows = (int64_t)at.row * A.P.beams;
+  const int pos0 = A.P.q_positions[rows];
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    const int col = min(col0 + n * 16 + m, columns - 1);
+    const int64_t row = rows + col / G.group;
+    pos[n] = A.P.q_positions[row];
+    alike = alike && pos[n] == pos0;
+    load_row<T, D>((const T *)A.q.data + row * A.q.token_stride +
+                       (k_head * G.group + col % G.group) * A.q.head_stride,
+                   G.width, A.vec, lane, qf[n]);
+    if (G.scale < 0.f) {
+#pragma unroll
+      for (int d = 0; d < DF; ++d) qf[n][d] = negated(qf[n][d]);
+    }
+  }
+  alike = __all(alike);
+  const float scale = fabsf(G.scale) * kLog2e;
+  const T *k = (const T *)A.k.data + token0 * A.k.token_stride + k_head * A.k.head_stride;
+  const T *v = (const T *)A.v.data + token0 * A.v.token_stride + k_head * A.v.head_stride;
+
+  // 32 keys: rows m and 16 + m as operands; rows of v eight values a lane
+  Raw8<T> hk[2][DF], hv[VN];
+  int hpos = 0;
+  const auto fetch = [&](int j0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int j = min(j0 + 16 * t + m, count - 1);
+#pragma unroll
+      for (int d = 0; d < DF; ++d)
+        hk[t][d] = load8(k + j * A.k.token_stride, d * 32 + g * 8, G.width, A.vec);
+    }
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      const int j = j0 + i * ROWS + lane / V8;
+      hv[i] = load8(v + min(j, count - 1) * A.v.token_stride, lane % V8 * 8, j < count ? G.width : 0, A.vec);
+    }
+    hpos = G.positions[token0 + min(j0 + (lane & 31), count - 1)];
+  };
+  f32x4 o[CT][DT];
+  float top[CT], base[CT], sum[CT];
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    top[n] = -__builtin_inff();
+    base[n] = sum[n] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const auto kind_of = [&](int gap) {
+    int n = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1)
+      if (lbounds[n + step - 1] <= gap) n += step;
+    return n < G.buckets - 1 ? n : G.buckets - 1;
+  };
+  if (wave * 32 < count) fetch(wave * 32);
+  __syncthreads();
+
+  for (int j0 = wave * 32; j0 < count; j0 += 128) {
+    Frag<NP> kf[2][DF];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < DF; ++d) kf[t][d] = operand(hk[t][d]);
+    bf16 *mine = lv[wave];
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      const Frag<NP> x = operand(hv[i]);
+      bf16 *to = mine + (i * ROWS + lane / V8) * LD + lane % V8 * 8;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) *(bf16x8 *)(to + n * PART) = x.p[n];
+    }
+    // where the beams' positions are alike, a lane finds the bucket of one key, for all columns
+    if (lane < 32) lkind[wave][lane] = alike ? kind_of(gap_of(pos0, hpos)) : hpos;
+    if (j0 + 128 < count) fetch(j0 + 128);
+    __builtin_amdgcn_wave_barrier();
+
+    f32x4 s[CT][2];
+    float most[CT];
+#pragma unroll
+    for (int n = 0; n < CT; ++n) {
+      most[n] = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DF; ++d) s[n][t] = mma(kf[t][d], qf[n][d], s[n][t]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = t * 16 + g * 4 + e, x = lkind[wave][r];
+          const float b = lbias[(n * 16 + m) * LB + (alike ? x : kind_of(gap_of(pos[n], x)))];
+          const float y = j0 + r < count ? fmaf(s[n][t][e], scale, b) : -__builtin_inff();
+          s[n][t][e] = y;
+          most[n] = fmaxf(most[n], y);
+        }
+      }
+    }
+    bool grown = false;
+#pragma unroll
+    for (int n = 0; n < CT; ++n) {
+      most[n] = column_max(most[n]);
+      grown = grown || most[n] > top[n] + 8.f;
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int n = 0; n < CT; ++n) {
+        const bool none = top[n] == -__builtin_inff();
+        top[n] = fmaxf(top[n], most[n]);
+        const float next = top[n] == -__builtin_inff() ? 0.f : top[n];
+        const float factor = none ? 0.f : exp2_fast(base[n] - next);
+        base[n] = next;
+        sum[n] *= factor;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) o[n][c] *= factor;
+      }
+    }
+    Frag<RP> pf[CT];
+#pragma unroll
+    for (int n = 0; n < CT; ++n) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[n][t][e] = exp2_fast(s[n][t][e] - base[n]);
+          sum[n] += s[n][t][e];
+        }
+      pf[n] = as_frag<RP>(s[n][0], s[n][1]);
+    }
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      const Frag<NP> vf = frag_col<NP, 4>(mine + c * 16, LD, PART, lane);
+#pragma unroll
+      for (int n = 0; n < CT; ++n) o[n][c] = mma(vf, pf[n], o[n][c]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // the waves' parts on one base, added in their order
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    sum[n] = column_sum(sum[n]);
+    if (g == 0) {
+      ltop[wave][n * 16 + m] = top[n] == -__builtin_inff() && sum[n] == 0.f ? -__builtin_inff() : base[n];
+      lsum[wave][n * 16 + m] = sum[n];
+    }
+  }
+  __syncthreads();
+  float total[CT], highest[CT];
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    const int c = n * 16 + m;
+    highest[n] = fmaxf(fmaxf(ltop[0][c], ltop[1][c]), fmaxf(ltop[2][c], ltop[3][c]));
+    const float to = highest[n] == -__builtin_inff() ? 0.f : highest[n];
+    total[n] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total[n] += lsum[w][c] * exp2_fast(ltop[w][c] - to);
+    const float factor = exp2_fast(ltop[wave][c] - to);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[n][d] *= factor;
+  }
+#pragma unroll 1
+  for (int w = 0; w < 4; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int n = 0; n < CT; ++n)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f32x4 *to = (f32x4 *)(lout + (n * 16 + m) * D + d * 16 + g * 4);
+          *to = w == 0 ? o[n][d] : *to + o[n][d];
+        }
+      if (w == 0 && g == 0) {
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+          const int col = col0 + n * 16 + m;
+          if (col < columns) {
+            float *to = A.stats + 2 * part_index(A, slot, k_head * G.group + col % G.group, col / G.group);
+            to[0] = highest[n];
+            to[1] = total[n];
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+  for (int x = tid; x < COLS * D; x += 256) {
+    const int col = col0 + x / D, d = x % D;
+    if (col < columns && d < G.width)
+      A.parts[part_index(A, slot, k_head * G.group + col % G.group, col / G.group) * G.width + d] = lout[x];
+  }
+}
+
+// A beam's head: its segments and its path. A wave each; D / 8 lanes a key (or segment), eight values a
+// lane.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
+  constexpr int L = D / 8, KEYS = 64 / L;
+  __shared__ int32_t lbounds[64];
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, sub = lane / L, c = lane % L * 8;
+  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+  __syncthreads();
+  const int64_t index = A.row0 * G.heads + (int64_t)blockIdx.x * 4 + tid / 64;
+  const int64_t row = index / G.heads;
+  if (row >= G.n_rows * A.P.beams) return;
+  const int head = (int)(index % G.heads), beam = (int)(row % A.P.beams);
+  const int64_t list = row / A.P.beams;
+
+  const Raw8<T> raw = load8((const T *)A.q.data + row * A.q.token_stride + head * A.q.head_stride, c, G.width,
+                            A.vec);
+  const f32x4 q[2] = {low4(raw), high4(raw)};
+  const float scale = G.scale * kLog2e;
+  float top = -__builtin_inff(), sum = 0.f;
+  f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  // takes a part whose weights are `by` at the largest score `score`
+  const auto take = [&](float score, float by, const f32x4 *x) {
+    const float next = fmaxf(top, score), to = next == -__builtin_inff() ? 0.f : next;
+    const float mine = top == next ? 1.f : exp2_fast(top - to), its = exp2_fast(score - to);
+    top = next;
+    sum = sum * mine + by * its;
+    o[0] = o[0] * mine + x[0] * its;
+    o[1] = o[1] * mine + x[1] * its;
+  };
+  const int64_t first = clamped(G.row_ptr[list], 0, G.n_tokens);
+  const int64_t len = clamped(G.row_ptr[list + 1], first, G.n_tokens) - first;
+  const int64_t slot = (first >> A.shift) + list, n_slots = segments_of(len, A.shift);
+  for (int64_t n = sub; n < n_slots; n += KEYS) {
+    const int64_t part = part_index(A, slot + n, head, beam);
+    const float *x = A.parts + part * G.width;
+    const Raw8<float> raw = load8(x, c, G.width, G.width % 4 == 0);
+    const f32x4 y[2] = {low4(raw), high4(raw)};
+    take(A.stats[2 * part], A.stats[2 * part + 1], y);
+  }
+  const int32_t at = A.P.q_positions[row];
+  for (int t = sub; t < A.P.steps; t += KEYS) {
+    const int32_t holder = A.P.path[row * A.P.path_stride + t];
+    const bool ok = holder >= 0 && holder < A.P.beams;
+    const int64_t from = list * A.P.beams + (ok ? holder : 0);
+    const Raw8<T> rk = load8((const T *)A.P.k.data + t * A.P.k_step + from * A.P.k.token_stride +
+                                 head / G.group * A.P.k.head_stride,
+                             c, G.width, A.vec_path);
+    const Raw8<T> rv = load8((const T *)A.P.v.data + t * A.P.v_step + from * A.P.v.token_stride +
+                                 head / G.group * A.P.v.head_stride,
+                             c, G.width, A.vec_path);
+    const f32x4 k[2] = {low4(rk), high4(rk)}, v[2] = {low4(rv), high4(rv)};
+    const int gap = gap_of(at, A.P.positions[t * (G.n_rows * A.P.beams) + from]);
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = fmaf(q[0][e], k[0][e], fmaf(q[1][e], k[1][e], x));
+#pragma unroll
+    for (int n = 1; n < L; n <<= 1) x += __shfl_xor(x, n);
+    int kind = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1)
+      if (lbounds[kind + step - 1] <= gap) kind += step;
+    kind = kind < G.buckets - 1 ? kind : G.buckets - 1;
+    const float b = G.bias[(int64_t)head * G.buckets + kind];
+    float y = b * kLog2e;
+    if (fabsf(b) <= kLargest) y = fminf(fmaxf(y, -kLargest), kLargest);
+    y = fmaf(x, scale, y);
+    if (!ok) y = __builtin_nanf("");
+    take(y, 1.f, v);
+  }
+#pragma unroll
+  for (int n = L; n < 64; n <<= 1) {
+    const float score = __shfl_xor(top, n), by = __shfl_xor(sum, n);
+    f32x4 x[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[0][e] = __shfl_xor(o[0][e], n);
+      x[1][e] = __shfl_xor(o[1][e], n);
+    }
+    take(score, by, x);
+  }
+  if (sub == 0 && c < G.width) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T *to = (T *)A.out + (row * G.heads + head) * G.width + c;
+    store4(to, o[0] * inv, G.width - c);
+    if (c + 4 < G.width) store4(to + 4, o[1] * inv, G.width - c - 4);
+  }
+}
+
+// Short segments fill the chip where tokens are few; each leaves a part of every beam's and head's sums.
+int step_shift(int64_t n_tokens, int32_t k_heads) {
+  int shift = 7;
+  while (shift < 12 && (n_tokens >> shift) * k_heads > 2048) ++shift;
+  return shift;
+}
+
+template <typename T, int D, int CT> void launch_history(StepArgs A, hipStream_t s) {
+  const int k_heads = A.G.heads / A.G.group, columns = A.P.beams * A.G.group;
+  A.passes = (columns + 16 * CT - 1) / (16 * CT);
+  const int64_t slots = (A.G.n_tokens >> A.shift) + A.G.n_rows;
+  const int64_t per = max_blocks(256) / ((int64_t)k_heads * A.passes);
+  for (A.slot0 = 0; A.slot0 < slots; A.slot0 += per) {
+    const int64_t n = slots - A.slot0 < per ? slots - A.slot0 : per;
+    hipLaunchKernelGGL((k_gap_history<T, D, CT>), dim3((unsigned)(n * k_heads * A.passes)), dim3(256), 0, s, A);
+  }
+}
+template <typename T, int D> hipError_t launch_step(StepArgs A, hipStream_t s) {
+  const int columns = A.P.beams * A.G.group;
+  if (A.G.n_tokens > 0) {
+    // as many columns as fit the registers beside a tile of keys and one of values
+    constexpr int MOST = D == 128 ? (sizeof(T) == 4 ? 1 : 2) : (sizeof(T) == 4 ? 2 : 4);
+    if (columns <= 16 || MOST == 1)
+      launch_history<T, D, 1>(A, s);
+    else if (columns <= 32 || MOST == 2)
+      launch_history<T, D, MOST < 2 ? 1 : 2>(A, s);
+    else
+      launch_history<T, D, MOST>(A, s);
+  }
+  const int64_t rows = A.G.n_rows * A.P.beams, per = max_blocks(256) * 4 / A.G.heads;
+  for (A.row0 = 0; A.row0 < rows; A.row0 += per) {
+    const int64_t n = rows - A.row0 < per ? rows - A.row0 : per;
+    hipLaunchKernelGGL((k_gap_path<T, D>), dim3((unsigned)((n * A.G.heads + 3) / 4)), dim3(256), 0, s, A);
+  }
+  return hipGetLastError();
+}
+template <typename T> hipError_t launch_step(const StepArgs &A, hipStream_t s) {
+  return A.G.width <= 32   ? launch_step<T, 32>(A, s)
+         : A.G.width <= 64 ? launch_step<T, 64>(A, s)
+                           : launch_step<T, 128>(A, s);
+}
+
+int64_t part_bytes(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t k_heads, int32_t beams,
+                   int64_t values) {
+  const int64_t slots = (n_tokens >> step_shift(n_tokens, k_heads)) + n_lists;
+  return n_tokens > 0 ? (slots * heads * beams * values * 4 + 15) / 16 * 16 : 0;
+}
+
+}  // namespace
+
+int64_t gap_step_space(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t k_heads, int32_t beams,
+                       int32_t width) {
+  return part_bytes(n_tokens, n_lists, heads, k_heads, beams, width) +
+         part_bytes(n_tokens, n_lists, heads, k_heads, beams, 2);
+}
+
+hipError_t launch_gap_step(als_dtype dtype, const GapShape &G, const GapPath &P, const als_heads &q,
+                           const als_heads &k, const als_heads &v, void *out, void *workspace, hipStream_t s) {
+  if (G.n_rows == 0) return hipSuccess;
+  const int32_t k_heads = G.heads / G.group;
+  StepArgs A{};
+  A.G = G;
+  A.P = P;
+  A.q = q;
+  A.k = k;
+  A.v = v;
+  A.out = out;
+  A.parts = (float *)workspace;
+  A.stats = (float *)((char *)workspace + part_bytes(G.n_tokens, G.n_rows, G.heads, k_heads, P.beams, G.width));
+  A.shift = step_shift(G.n_tokens, k_heads);
+  const int size = dtype == ALS_F32 ? 4 : 2;
+  const auto vec = [&](const als_heads &h) {
+    return aligned16(h.data, h.token_stride, h.head_stride, G.width, size);
+  };
+  A.vec = vec(q) && vec(k) && vec(v);
+  A.vec_path = vec(P.k) && vec(P.v) && (P.k_step * size) % 16 == 0 && (P.v_step * size) % 16 == 0;
+  return dtype == ALS_F32 ? launch_step<float>(A, s) : launch_step<bf16>(A, s);
+}
+
+}  // namespace als

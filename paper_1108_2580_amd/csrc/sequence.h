@@ -85,6 +85,52 @@ hipError_t launch_attention_step(als_dtype dtype, int64_t n_rows, int32_t heads,
                                  float scale, const float *state, const int32_t *source,
                                  int64_t n_sources, float *state_out, void *out, hipStream_t s);
 
+// Attention over gaps of time (gap.hip, gap_back.hip, gap_step.hip): what all its calls share.
+struct GapShape {
+  int64_t n_tokens, n_rows;
+  const int64_t *row_ptr;
+  const int32_t *positions;
+  const float *bias;       // [heads, buckets]
+  int32_t heads, group;    // heads of q, and how many of them share one head of k and v
+  int32_t width, buckets;
+  float scale;
+  int32_t last_bound;      // bounds[buckets - 2], 0 where there is one bucket
+  int32_t bounds[63];
+};
+// Bytes of the table of the tokens' rows, which calls over more than a few rows need.
+int64_t gap_spans_bytes(int64_t n_tokens, int64_t n_rows);
+hipError_t launch_gap_spans(const GapShape &g, void *spans, hipStream_t s);
+// stats: nullable, fp32 [2, heads, n_tokens], the largest score (times log2 e) and the log2 of the sum;
+// rest: nullable, like out, what its rounding left out.
+hipError_t launch_gap_read(als_dtype dtype, const GapShape &g, const als_heads &q, const als_heads &k,
+                           const als_heads &v, const void *spans, void *out, float *stats, void *rest,
+                           hipStream_t s);
+
+// Bytes of the gradients' workspace, by part, each a multiple of 16.
+struct GapBackSpace {
+  int64_t spans, delta, dbias;
+  int64_t total() const { return spans + delta + dbias; }
+};
+GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t buckets);
+hipError_t launch_gap_back(als_dtype dtype, const GapShape &g, const als_heads &d_out, const als_heads &q,
+                           const als_heads &k, const als_heads &v, const void *out, const float *stats,
+                           const void *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
+                           hipStream_t s);
+
+// One token of each beam: what it reads besides its list's row of the history.
+struct GapPath {
+  int32_t beams, steps;
+  const int32_t *q_positions;  // [lists * beams]
+  als_heads k, v;              // [steps, lists * beams, heads, width]
+  int64_t k_step, v_step;      // values from step to step
+  const int32_t *positions;    // [steps, lists * beams]
+  const int32_t *path;         // [lists * beams, steps], rows path_stride apart: the beam that holds each step
+  int64_t path_stride;
+};
+int64_t gap_step_space(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t k_heads, int32_t beams,
+                       int32_t width);
+hipError_t launch_gap_step(als_dtype dtype, const GapShape &g, const GapPath &p, const als_heads &q,
+                           const als_heads &k, const als_heads &v, void *out, void *workspace, hipStream_t s);
 
 // Blocks of a pass of norm and rotation: partial sums of the weights' gradients (rotate.hip).
 int64_t rotate_blocks(int64_t n_tokens);

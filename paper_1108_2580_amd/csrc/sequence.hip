@@ -226,6 +226,75 @@ AttentionPass pass_of(const als_attention *s, als_dtype dtype, void *workspace) 
   return p;
 }
 
+// ---- attention over gaps of time -------------------------------------------------------------------
+
+constexpr int64_t kMaxGapTokens = kMax31 - 255;  // a block's tokens are counted in 32 bits
+
+bool sane(const als_gaps *s) {
+  return s && s->n_tokens >= 0 && s->n_tokens <= kMaxGapTokens && s->n_rows >= 0 && s->n_rows <= kMaxRows &&
+         s->q_heads >= 1 && s->q_heads <= 1024 && s->k_heads >= 1 && s->q_heads % s->k_heads == 0 &&
+         s->width >= 1 && s->width <= 128 && s->buckets >= 1 && s->buckets <= 64;
+}
+
+als_status check_gaps(const als_gaps *s, als_dtype dtype) {
+  REQUIRE(s, "shape is NULL");
+  if (als_status st = check_dtype(dtype)) return st;
+  REQUIRE(s->n_tokens >= 0 && s->n_tokens <= kMaxGapTokens, "n_tokens %lld out of range",
+          (long long)s->n_tokens);
+  REQUIRE(s->n_rows >= 0 && s->n_rows <= kMaxRows, "n_rows %lld out of range", (long long)s->n_rows);
+  REQUIRE(s->q_heads >= 1 && s->q_heads <= 1024 && s->k_heads >= 1 && s->q_heads % s->k_heads == 0,
+          "q_heads %d is not in [1, 1024] and a multiple of k_heads %d", s->q_heads, s->k_heads);
+  REQUIRE(s->width >= 1 && s->width <= 128, "width %d outside [1, 128]", s->width);
+  REQUIRE(s->buckets >= 1 && s->buckets <= 64, "buckets %d outside [1, 64]", s->buckets);
+  REQUIRE(s->buckets == 1 || s->bounds, "bounds is NULL");
+  for (int b = 0; b + 1 < s->buckets; ++b)
+    REQUIRE(s->bounds[b] >= 1 && (b == 0 || s->bounds[b] > s->bounds[b - 1]),
+            "bounds[%d] = %d is below 1 or not above the one before it", b, s->bounds[b]);
+  REQUIRE(std::isfinite(s->scale), "scale %g is not finite", s->scale);
+  REQUIRE(s->bias, "bias is NULL");
+  REQUIRE(s->row_ptr, "row_ptr is NULL");
+  REQUIRE(s->n_tokens == 0 || s->positions, "positions is NULL");
+  REQUIRE(s->n_rows > 0 || s->n_tokens == 0, "tokens without rows");
+  return ALS_OK;
+}
+
+als::GapShape gap_shape(const als_gaps *s) {
+  als::GapShape g{};
+  g.n_tokens = s->n_tokens;
+  g.n_rows = s->n_rows;
+  g.row_ptr = s->row_ptr;
+  g.positions = s->positions;
+  g.bias = s->bias;
+  g.heads = s->q_heads;
+  g.group = s->q_heads / s->k_heads;
+  g.width = s->width;
+  g.buckets = s->buckets;
+  g.scale = s->scale;
+  for (int b = 0; b + 1 < s->buckets; ++b) g.last_bound = g.bounds[b] = s->bounds[b];
+  return g;
+}
+
+// A tensor of a call, by name.
+struct Named {
+  const char *name;
+  Span at;
+};
+// What a call writes lies on nothing else of it.
+als_status check_apart(const Named *written, int n_written, const Named *read, int n_read) {
+  for (int i = 0; i < n_written; ++i) {
+    for (int j = 0; j < i; ++j)
+      REQUIRE(!overlap(written[i].at, written[j].at), "%s overlaps %s", written[i].name, written[j].name);
+    for (int j = 0; j < n_read; ++j)
+      REQUIRE(!overlap(written[i].at, read[j].at), "%s overlaps %s", written[i].name, read[j].name);
+  }
+  return ALS_OK;
+}
+als_status check_packed(const char *name, const void *p, int64_t n, int size) {
+  REQUIRE(n == 0 || p, "%s is NULL", name);
+  REQUIRE((uintptr_t)p % size == 0, "%s is not aligned to its type", name);
+  return ALS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -476,6 +545,161 @@ static als_status check_beams(const als_beams *s) {
   REQUIRE(s->end_token >= -1 && s->end_token < s->n_items, "end_token %d outside [-1, n_items)",
           s->end_token);
   return ALS_OK;
+}
+
+int64_t als_gap_attention_workspace(const als_gaps *shape) {
+  return sane(shape) ? als::gap_spans_bytes(shape->n_tokens, shape->n_rows) : -1;
+}
+
+als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q, als_heads k, als_heads v,
+                             void *out, float *stats, void *rest, void *workspace, int64_t workspace_bytes,
+                             void *hip_stream) {
+  if (als_status st = check_gaps(shape, dtype)) return st;
+  const als_gaps *s = shape;
+  const int size = size_of(dtype);
+  const int64_t n = s->n_tokens, values = n * s->q_heads * s->width;
+  if (als_status st = check_input("q", q, n, size)) return st;
+  if (als_status st = check_input("k", k, n, size)) return st;
+  if (als_status st = check_input("v", v, n, size)) return st;
+  if (als_status st = check_packed("out", out, n, size)) return st;
+  if (als_status st = check_packed("stats", stats, 0, 4)) return st;
+  if (als_status st = check_packed("rest", rest, 0, size)) return st;
+  REQUIRE(!rest || dtype == ALS_BF16, "rest is for bf16 outputs");
+  const int64_t needed = als::gap_spans_bytes(n, s->n_rows);
+  if (als_status st = check_workspace(workspace, workspace_bytes, needed)) return st;
+  const Named written[] = {{"out", span(out, values * size)},
+                           {"stats", optional(stats, 8 * n * s->q_heads)},
+                           {"rest", optional(rest, values * size)},
+                           {"the workspace", span(workspace, needed)}};
+  const Named read[] = {{"q", span(q, n, s->q_heads, s->width, size)},
+                        {"k", span(k, n, s->k_heads, s->width, size)},
+                        {"v", span(v, n, s->k_heads, s->width, size)},
+                        {"bias", span(s->bias, 4LL * s->q_heads * s->buckets)},
+                        {"positions", span(s->positions, 4 * n)},
+                        {"row_ptr", span(s->row_ptr, 8 * (s->n_rows + 1))}};
+  if (als_status st = check_apart(written, 4, read, 6)) return st;
+  const als::GapShape g = gap_shape(s);
+  void *spans = needed ? workspace : nullptr;
+  hipError_t e = als::launch_gap_spans(g, spans, (hipStream_t)hip_stream);
+  if (e == hipSuccess)
+    e = als::launch_gap_read(dtype, g, q, k, v, spans, out, stats, rest, (hipStream_t)hip_stream);
+  return launched(e, "als_gap_attention");
+}
+
+int64_t als_gap_attention_backward_workspace(const als_gaps *shape) {
+  return sane(shape)
+             ? als::gap_back_space(shape->n_tokens, shape->n_rows, shape->q_heads, shape->buckets).total()
+             : -1;
+}
+
+als_status als_gap_attention_backward(const als_gaps *shape, als_dtype dtype, als_heads d_out, als_heads q,
+                                      als_heads k, als_heads v, const void *out, const float *stats,
+                                      const void *rest, void *dq, void *dk, void *dv, float *dbias,
+                                      void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  if (als_status st = check_gaps(shape, dtype)) return st;
+  const als_gaps *s = shape;
+  const int size = size_of(dtype);
+  const int64_t n = s->n_tokens, q_bytes = n * s->q_heads * s->width * size,
+                k_bytes = n * s->k_heads * s->width * size;
+  if (als_status st = check_input("d_out", d_out, n, size)) return st;
+  if (als_status st = check_input("q", q, n, size)) return st;
+  if (als_status st = check_input("k", k, n, size)) return st;
+  if (als_status st = check_input("v", v, n, size)) return st;
+  if (als_status st = check_packed("out", out, n, size)) return st;
+  if (als_status st = check_packed("stats", stats, n, 4)) return st;
+  if (als_status st = check_packed("rest", rest, 0, size)) return st;
+  REQUIRE(!rest || dtype == ALS_BF16, "rest is for bf16 outputs");
+  if (als_status st = check_packed("dq", dq, n, size)) return st;
+  if (als_status st = check_packed("dk", dk, n, size)) return st;
+  if (als_status st = check_packed("dv", dv, n, size)) return st;
+  if (als_status st = check_packed("dbias", dbias, 1, 4)) return st;
+  const int64_t needed = als_gap_attention_backward_workspace(s);
+  if (als_status st = check_workspace(workspace, workspace_bytes, needed)) return st;
+  const int64_t bias_bytes = 4LL * s->q_heads * s->buckets;
+  const Named written[] = {{"dq", span(dq, q_bytes)},
+                           {"dk", span(dk, k_bytes)},
+                           {"dv", span(dv, k_bytes)},
+                           {"dbias", span(dbias, bias_bytes)},
+                           {"the workspace", span(workspace, needed)}};
+  const Named read[] = {{"d_out", span(d_out, n, s->q_heads, s->width, size)},
+                        {"q", span(q, n, s->q_heads, s->width, size)},
+                        {"k", span(k, n, s->k_heads, s->width, size)},
+                        {"v", span(v, n, s->k_heads, s->width, size)},
+                        {"out", span(out, q_bytes)},
+                        {"stats", span(stats, 8 * n * s->q_heads)},
+                        {"rest", optional(rest, q_bytes)},
+                        {"bias", span(s->bias, bias_bytes)},
+                        {"positions", span(s->positions, 4 * n)},
+                        {"row_ptr", span(s->row_ptr, 8 * (s->n_rows + 1))}};
+  if (als_status st = check_apart(written, 5, read, 10)) return st;
+  return launched(als::launch_gap_back(dtype, gap_shape(s), d_out, q, k, v, out, stats, rest, dq, dk, dv, dbias,
+                                       workspace, (hipStream_t)hip_stream),
+                  "als_gap_attention_backward");
+}
+
+int64_t als_gap_attention_step_workspace(const als_gaps *shape, const als_gap_path *path) {
+  return sane(shape) && path && path->beams >= 1 && path->beams <= als::kMaxBeams
+             ? als::gap_step_space(shape->n_tokens, shape->n_rows, shape->q_heads, shape->k_heads, path->beams,
+                                   shape->width)
+             : -1;
+}
+
+als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *path, als_dtype dtype, als_heads q,
+                                  als_heads k, als_heads v, void *out, void *workspace,
+                                  int64_t workspace_bytes, void *hip_stream) {
+  const als_gaps *s = shape;
+  if (als_status st = check_gaps(s, dtype)) return st;
+  REQUIRE(path, "path is NULL");
+  const als_gap_path *p = path;
+  REQUIRE(p->beams >= 1 && p->beams <= als::kMaxBeams, "beams %d outside [1, %d]", p->beams, als::kMaxBeams);
+  REQUIRE(p->steps >= 0 && p->steps <= 1 << 20, "steps %d out of range", p->steps);
+  const int64_t rows = s->n_rows * p->beams;
+  REQUIRE(rows <= kMax31, "%lld lists of %d beams", (long long)s->n_rows, p->beams);
+  const int size = size_of(dtype);
+  const int64_t n = s->n_tokens, path_rows = p->steps > 0 ? rows : 0;
+  REQUIRE(rows == 0 || p->q_positions, "q_positions is NULL");
+  if (als_status st = check_input("q", q, rows, size, true)) return st;
+  if (als_status st = check_input("k", k, n, size, true)) return st;
+  if (als_status st = check_input("v", v, n, size, true)) return st;
+  als::GapPath g{p->beams, p->steps, p->q_positions, p->k, p->v, p->k_step, p->v_step, p->positions, p->path,
+                 p->path_stride};
+  if (als_status st = check_input("the path's k", g.k, path_rows, size, true)) return st;
+  if (als_status st = check_input("the path's v", g.v, path_rows, size, true)) return st;
+  if (path_rows > 0) {
+    REQUIRE(p->k_step >= 0 && p->v_step >= 0 && p->k_step <= (1LL << 56) / p->steps &&
+                p->v_step <= (1LL << 56) / p->steps,
+            "a step's stride of the path's k or v is negative or out of range");
+    REQUIRE(p->positions, "the path's positions are NULL");
+    REQUIRE(p->path, "path is NULL");
+    REQUIRE(p->path_stride >= p->steps && p->path_stride <= 1LL << 24, "path_stride %lld out of range",
+            (long long)p->path_stride);
+  }
+  if (als_status st = check_packed("out", out, rows, size)) return st;
+  const int64_t needed = als::gap_step_space(n, s->n_rows, s->q_heads, s->k_heads, p->beams, s->width);
+  if (als_status st = check_workspace(workspace, workspace_bytes, needed)) return st;
+  const auto path_span = [&](const als_heads &x, int64_t step) {
+    if (path_rows == 0) return Span{0, 0};
+    return span(x.data, ((p->steps - 1) * step + (rows - 1) * x.token_stride +
+                         (s->k_heads - 1) * x.head_stride + s->width) * (int64_t)size);
+  };
+  const Named written[] = {{"out", span(out, rows * s->q_heads * s->width * size)},
+                           {"the workspace", span(workspace, needed)}};
+  const Named read[] = {{"q", span(q, rows, s->q_heads, s->width, size)},
+                        {"k", span(k, n, s->k_heads, s->width, size)},
+                        {"v", span(v, n, s->k_heads, s->width, size)},
+                        {"bias", span(s->bias, 4LL * s->q_heads * s->buckets)},
+                        {"positions", span(s->positions, 4 * n)},
+                        {"row_ptr", span(s->row_ptr, 8 * (s->n_rows + 1))},
+                        {"q_positions", span(p->q_positions, 4 * rows)},
+                        {"the path's k", path_span(g.k, p->k_step)},
+                        {"the path's v", path_span(g.v, p->v_step)},
+                        {"the path's positions", span(p->positions, 4 * p->steps * path_rows)},
+                        {"path", path_rows ? span(p->path, 4 * ((rows - 1) * p->path_stride + p->steps))
+                                           : Span{0, 0}}};
+  if (als_status st = check_apart(written, 2, read, 11)) return st;
+  return launched(als::launch_gap_step(dtype, gap_shape(s), g, q, k, v, out, workspace,
+                                       (hipStream_t)hip_stream),
+                  "als_gap_attention_step");
 }
 
 int64_t als_beam_select_workspace(const als_beams *shape) {

@@ -46,13 +46,24 @@ class _Attention(ctypes.Structure):
                 ("scale", _f32)]
 
 
+class _Gaps(ctypes.Structure):
+    _fields_ = [("n_tokens", _i64), ("n_rows", _i64), ("row_ptr", _P), ("positions", _P), ("bias", _P),
+                ("bounds", _P), ("q_heads", _i32), ("k_heads", _i32), ("width", _i32), ("buckets", _i32),
+                ("scale", _f32)]
+
+
+class _GapPath(ctypes.Structure):
+    _fields_ = [("beams", _i32), ("steps", _i32), ("q_positions", _P), ("k", _Heads), ("v", _Heads),
+                ("k_step", _i64), ("v_step", _i64), ("positions", _P), ("path", _P), ("path_stride", _i64)]
+
+
 class _Beams(ctypes.Structure):
     _fields_ = [("n_lists", _i64), ("n_items", _i64), ("row_stride", _i64), ("beams", _i32),
                 ("width", _i32), ("end_token", _i32)]
 
 
 def _declare():
-    R, A, B = (ctypes.POINTER(t) for t in (_Rotation, _Attention, _Beams))
+    R, A, B, G, GP = (ctypes.POINTER(t) for t in (_Rotation, _Attention, _Beams, _Gaps, _GapPath))
     H, st = _Heads, ctypes.c_int
     for name, args in (
             ("als_norm_rotate", [R, st, H, H, _P, _P, H, H, _P]),
@@ -62,15 +73,23 @@ def _declare():
             ("als_decay_attention_backward",
              [A, st, H, H, H, H, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_decay_attention_step", [A, st, H, H, H, _P, _i64, _P, _P, _P, _P]),
+            ("als_gap_attention", [G, st, H, H, H, _P, _P, _P, _P, _i64, _P]),
+            ("als_gap_attention_backward",
+             [G, st, H, H, H, H, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
+            ("als_gap_attention_step", [G, GP, st, H, H, H, _P, _P, _i64, _P]),
             ("als_beam_select", [B, st, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_reorder_states", [_i64, _i32, _i32, _i64, _P, _P, _P, _P])):
         f = getattr(lib, name)
         f.argtypes, f.restype = args, st
     for name, arg in (("als_norm_rotate_workspace", R), ("als_decay_attention_workspace", A),
                       ("als_decay_attention_backward_workspace", A),
+                      ("als_gap_attention_workspace", G),
+                      ("als_gap_attention_backward_workspace", G),
                       ("als_beam_select_workspace", B)):
         f = getattr(lib, name)
         f.argtypes, f.restype = [arg], _i64
+    f = lib.als_gap_attention_step_workspace
+    f.argtypes, f.restype = [G, GP], _i64
 
 
 _declare()
@@ -402,6 +421,168 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, sta
                                         _stream(dev)))
     _written(state_out)
     return out, state_out
+
+
+# ---- attention over gaps of time -----------------------------------------------------------------
+
+def _gaps(q, k, v, bias, bounds, positions, row_ptr, scale):
+    """What the calls share: the shape as the library takes it, without q's tokens."""
+    dev = _device(q, "q")
+    code = _dtype(q, "q")
+    dtype = q.dtype
+    hq, hk, hv = _heads(q, "q", dtype, dev), _heads(k, "k", dtype, dev), _heads(v, "v", dtype, dev)
+    _, Hq, D = q.shape
+    N, Hk, _ = k.shape
+    if k.shape != (N, Hk, D) or v.shape != (N, Hk, D):
+        raise ValueError(f"q, k and v have shapes {tuple(q.shape)}, {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
+    if not isinstance(bounds, torch.Tensor) or bounds.device.type != "cpu" or bounds.dtype != torch.int32 or \
+            bounds.dim() != 1 or not bounds.is_contiguous():
+        raise TypeError("bounds must be a contiguous int32 tensor of one dimension on the host")
+    if not isinstance(row_ptr, torch.Tensor) or row_ptr.dim() != 1 or row_ptr.numel() < 1:
+        raise ValueError("row_ptr must have one more entry than there are rows")
+    rows, buckets = row_ptr.numel() - 1, bounds.numel() + 1
+    shape = _Gaps(N, rows, _array(row_ptr, "row_ptr", torch.int64, (rows + 1,), dev),
+                  _array(positions, "positions", torch.int32, (N,), dev),
+                  _array(bias, "bias", torch.float32, (Hq, buckets), dev), bounds.data_ptr(), Hq, Hk, D,
+                  buckets, D ** -0.5 if scale is None else scale)
+    return dev, code, shape, hq, hk, hv
+
+
+def _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, save):
+    dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
+    _shaped(q, "q", (shape.n_tokens, shape.q_heads, shape.width))
+    out = q.new_empty(q.shape)
+    stats = rest = None
+    if save:
+        stats = torch.empty((2, shape.q_heads, shape.n_tokens), device=q.device)
+        rest = torch.empty_like(out) if code == ALS_BF16 else None
+    size = lib.als_gap_attention_workspace(shape)
+    work = _workspace(size, q.device)
+    _check(lib.als_gap_attention(shape, code, hq, hk, hv, out.data_ptr(), _ptr(stats), _ptr(rest), _ptr(work),
+                                 size, _stream(dev)))
+    return out, stats, rest
+
+
+def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_saved=False):
+    """Softmax attention over packed rows of tokens with a learned bias for each bucket of the gap of time
+    between two tokens: a token i reads the tokens j <= i of its row by softmax over j of
+    scale q_i . k_j + bias[head, #{bounds <= positions[i] - positions[j]}].
+
+    ``q``: [tokens, heads, width]; ``k``, ``v``: [tokens, key heads, width], each key head shared by
+    heads / key heads query heads; widths up to 128. ``bias``: fp32 [heads, buckets], up to 64 buckets;
+    -inf masks a bucket, and a token left without a key has the output zero. ``bounds``: int32
+    [buckets - 1] on the host, ascending from 1 or more, the first gap of each bucket but the first.
+    ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``: as for
+    ``decay_attention``; a token that no row holds is not worked on, and its place in the new tensors,
+    outputs and gradients, is left unset. ``scale``: 1 / sqrt(width) if None. Returns out [tokens,
+    heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or bias.requires_grad):
+        out, *saved = _GapAttention.apply(q, k, v, bias, bounds, positions, row_ptr, scale)
+    else:
+        out, *saved = _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, return_saved)
+    return (out, tuple(saved)) if return_saved else out
+
+
+def gap_attention_backward(d_out, out, saved, q, k, v, bias, bounds, positions, row_ptr, scale=None):
+    """Gradients (dq, dk, dv, dbias) of ``gap_attention`` from that of its output, its output (contiguous)
+    and what it saved."""
+    dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
+    shaped = (shape.n_tokens, shape.q_heads, shape.width)
+    _shaped(q, "q", shaped)
+    hdo = _heads(d_out, "d_out", q.dtype, dev)
+    _shaped(d_out, "d_out", shaped)
+    stats, rest = saved
+    op = _array(out, "out", q.dtype, shaped, dev)
+    sp = _array(stats, "saved[0]", torch.float32, (2, shape.q_heads, shape.n_tokens), dev)
+    rp = None if rest is None else _array(rest, "saved[1]", q.dtype, shaped, dev)
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+    dbias = torch.empty_like(bias)
+    size = lib.als_gap_attention_backward_workspace(shape)
+    work = _workspace(size, q.device)
+    _check(lib.als_gap_attention_backward(shape, code, hdo, hq, hk, hv, op, sp, rp, dq.data_ptr(),
+                                          dk.data_ptr(), dv.data_ptr(), dbias.data_ptr(), _ptr(work), size,
+                                          _stream(dev)))
+    return dq, dk, dv, dbias
+
+
+class _GapAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, bias, bounds, positions, row_ptr, scale):
+        out, stats, rest = _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, True)
+        # the host's bounds are kept as they are now
+        ctx.save_for_backward(out, stats, rest, q, k, v, bias, bounds.clone(), positions, row_ptr)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*(t for t in (stats, rest) if t is not None))
+        return out, stats, rest
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out, *_):
+        if d_out is None:
+            return (None,) * 8
+        out, stats, rest, *args = ctx.saved_tensors
+        return (*gap_attention_backward(_dense(d_out), out, (stats, rest), *args, ctx.scale), None, None, None,
+                None)
+
+
+def gap_attention_step(q, k, v, bias, bounds, q_positions, positions, row_ptr, k_path=None, v_path=None,
+                       path_positions=None, path=None, scale=None):
+    """One token of each beam: ``gap_attention``'s output for ``q`` [lists * beams, heads, width] at
+    ``q_positions`` int32 [lists * beams], over all tokens of its list's row of ``k``, ``v`` [tokens, key
+    heads, width] and ``positions`` int32 [tokens] (the user's history, read once for all beams of the
+    list) and over its own path.
+
+    ``row_ptr``: int64 [lists + 1]. The path (none if ``path`` is None) is kept by step and beam, as it
+    was appended: ``k_path``, ``v_path`` [steps, lists * beams, key heads, width] and ``path_positions``
+    int32 [steps, lists * beams]; ``path``: int32 [lists, beams, steps], the beam that holds each step of
+    a beam's path (one outside [0, beams) gives NaN). Where beams fork nothing but ``path`` moves:
+    ``reorder_states`` on it, then the beams' own numbers at the step that they append. The tensors may
+    be parts of longer ones ([:steps], and [..., :steps] of ``path``). Up to 32 beams. Returns out
+    [lists * beams, heads, width], which carries no gradient."""
+    dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
+    rows, lists, Hk, D = q.shape[0], shape.n_rows, shape.k_heads, shape.width
+    if path is None:
+        if lists == 0 or rows % lists != 0 or rows == 0:
+            raise ValueError(f"{rows} tokens are no whole number of beams of {lists} lists")
+        at = _GapPath(rows // lists, 0)
+    else:
+        _device(path, "path")
+        if path.dtype != torch.int32 or path.dim() != 3:
+            raise TypeError("path must be int32 with the dimensions lists, beams, steps")
+        n, beams, steps = path.shape
+        if n != lists or n * beams != rows:
+            raise ValueError(f"path has shape {tuple(path.shape)} for {lists} lists and {rows} tokens")
+        apart, stride, unit = path.stride()
+        if beams == 1:
+            stride = apart if n > 1 else steps
+        if (steps > 1 and unit != 1) or (n > 1 and apart != beams * stride):
+            raise TypeError("path must have contiguous steps and evenly spaced beams")
+        heads = []
+        for t, name in ((k_path, "k_path"), (v_path, "v_path")):
+            if not isinstance(t, torch.Tensor) or t.dim() != 4:
+                raise ValueError(f"{name} must have the dimensions steps, tokens, heads, width")
+            _shaped(t, name, (steps, rows, Hk, D))
+            if t.get_device() != dev:
+                _device(t, name)
+            if t.dtype != q.dtype:
+                raise TypeError(f"{name} must be {q.dtype}, not {t.dtype}")
+            step, token, head, feature = t.stride()
+            if feature != 1 and D > 1:
+                raise TypeError(f"the features of {name} must be contiguous")
+            heads.append((_Heads(t.data_ptr(), token, head), step))
+        (hkp, k_step), (hvp, v_step) = heads
+        at = _GapPath(beams, steps, 0, hkp, hvp, k_step, v_step,
+                      _array(path_positions, "path_positions", torch.int32, (steps, rows), dev),
+                      path.data_ptr(), stride)
+    at.q_positions = _array(q_positions, "q_positions", torch.int32, (rows,), dev)
+    out = q.new_empty(q.shape)
+    size = lib.als_gap_attention_step_workspace(shape, at)
+    work = _workspace(size, q.device)
+    _check(lib.als_gap_attention_step(shape, at, code, hq, hk, hv, out.data_ptr(), _ptr(work), size,
+                                      _stream(dev)))
+    return out
 
 
 # ---- beams ---------------------------------------------------------------------------------------
