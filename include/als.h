@@ -564,7 +564,7 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
  *                  head h of k and v. width 1 .. 128.
  *   out            device [n_tokens, q_heads, width], packed.
  *   stats, rest    what the gradients read, both nullable: stats device fp32 [2, q_heads, n_tokens], rest
- *                  like out (bf16 only), what out's rounding left out.
+ *                  device int16 like out (bf16 only), what out's rounding left out.
  * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
  * NaN. Scores, weights and sums are fp32; weights of bf16 values enter their product as two bf16 values (off by
  * 2^-16 at most).
@@ -585,7 +585,7 @@ typedef struct {
 
 int64_t als_gap_attention_workspace(const als_gaps *shape);
 als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q, als_heads k, als_heads v,
-                             void *out, float *stats, void *rest, void *workspace, int64_t workspace_bytes,
+                             void *out, float *stats, int16_t *rest, void *workspace, int64_t workspace_bytes,
                              void *hip_stream);
 
 /*
@@ -596,7 +596,7 @@ als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q
 int64_t als_gap_attention_backward_workspace(const als_gaps *shape);
 als_status als_gap_attention_backward(const als_gaps *shape, als_dtype dtype, als_heads d_out, als_heads q,
                                       als_heads k, als_heads v, const void *out, const float *stats,
-                                      const void *rest, void *dq, void *dk, void *dv, float *dbias,
+                                      const int16_t *rest, void *dq, void *dk, void *dv, float *dbias,
                                       void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /*

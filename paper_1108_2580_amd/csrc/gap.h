@@ -109,7 +109,7 @@ template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T *p, int c, int width, bool vec) {
   Raw8<T> x;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x.v[e] = (T)0.f;
+  for (int e = 0; e < 8; ++e) x.v[e] = (T)0;
   if (vec) {
     constexpr int E = 16 / sizeof(T);
     struct alignas(16) Piece { T v[E]; };
@@ -162,6 +162,29 @@ template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 x, int 
     for (int e = 0; e < 3; ++e)
       if (e < n) p[e] = (T)x[e];
   }
+}
+
+// What rounding to bf16 leaves out, as the distance of the bit patterns: 16 more bits, so that value and rest
+// together are the fp32 value (one bit short of it where a tie went down).
+__device__ __forceinline__ void store_rest(int16_t *p, f32x4 x, int n) {
+  using s16x4 = int16_t __attribute__((ext_vector_type(4)));
+  s16x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int32_t far = (int32_t)(__float_as_uint(x[e]) -
+                                  ((uint32_t)__builtin_bit_cast(uint16_t, (bf16)x[e]) << 16));
+    r[e] = (int16_t)(far > 32767 ? 32767 : far < -32768 ? -32768 : far);
+  }
+  if (n >= 4) {
+    __builtin_memcpy(p, &r, sizeof r);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = r[e];
+  }
+}
+__device__ __forceinline__ float with_rest(bf16 x, int16_t rest) {
+  return __uint_as_float(((uint32_t)__builtin_bit_cast(uint16_t, x) << 16) + (uint32_t)(int32_t)rest);
 }
 
 __device__ __forceinline__ bool finite4(f32x4 x) {

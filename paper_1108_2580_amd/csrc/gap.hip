@@ -33,7 +33,8 @@ struct ReadArgs {
   GapShape G;
   als_heads q, k, v;
   const Span2 *spans;  // nullable: counted
-  void *out, *rest;    // rest nullable
+  void *out;
+  int16_t *rest;       // nullable
   float *stats;        // nullable
   int64_t tile0, n_tiles;
   bool vec_q;
@@ -287,18 +288,13 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
       const f32x4 x = o[n][c] * inv;
       store4((T *)A.out + row + d, x, G.width - d);
       if constexpr (sizeof(T) == 2) {
-        if (A.rest) {
-          f32x4 y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = x[e] - (float)(T)x[e];
-          store4((T *)A.rest + row + d, y, G.width - d);
-        }
+        if (A.rest) store_rest(A.rest + row + d, x, G.width - d);
       }
     }
     if (A.stats && g == 0) {
       float *to = A.stats + (int64_t)head * G.n_tokens + at[n];
       to[0] = base[n];
-      to[(int64_t)G.heads * G.n_tokens] = total == 0.f ? __builtin_inff() : __log2f(total);
+      to[(int64_t)G.heads * G.n_tokens] = inv;
     }
   }
 }
@@ -337,7 +333,7 @@ hipError_t launch_gap_spans(const GapShape &G, void *spans, hipStream_t s) {
 }
 
 hipError_t launch_gap_read(als_dtype dtype, const GapShape &G, const als_heads &q, const als_heads &k,
-                           const als_heads &v, const void *spans, void *out, float *stats, void *rest,
+                           const als_heads &v, const void *spans, void *out, float *stats, int16_t *rest,
                            hipStream_t s) {
   if (G.n_tokens == 0) return hipSuccess;
   const int size = dtype == ALS_F32 ? 4 : 2;

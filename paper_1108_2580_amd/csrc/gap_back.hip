@@ -22,7 +22,8 @@ struct BackArgs {
   GapShape G;
   als_heads q, k, v, d_out;
   const Span2 *spans;
-  const void *out, *rest;  // packed; rest nullable
+  const void *out;         // packed
+  const int16_t *rest;     // nullable
   const float *stats;
   float *delta;            // [heads, n_tokens]
   float *dbias_parts;      // [heads, buckets, n_tiles]
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   const int i0 = (int)t0 + wave * 16 * QT;
   int at[QT], first[QT], pos[QT];
   unsigned before[QT];
-  float top[QT], logsum[QT], delta[QT];
+  float top[QT], inv[QT], delta[QT];
   int first_min = kNoRow, first_max = 0, last = -1, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
   Frag<NP> qf[QT][DF], of[QT][DF];
 #pragma unroll
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
                    lane, qf[n]);
     const float *stats = A.stats + (int64_t)head * G.n_tokens + t;
     top[n] = stats[0];
-    logsum[n] = stats[(int64_t)G.heads * G.n_tokens];
+    inv[n] = stats[(int64_t)G.heads * G.n_tokens];
     // delta, and do as operands
     float x = 0.f;
     const int64_t row = (t * G.heads + head) * G.width;
@@ -118,9 +119,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       f32x4 o[2] = {low4(z), high4(z)};
       if constexpr (sizeof(T) == 2) {
         if (A.rest) {
-          const Raw8<T> r = load8((const T *)A.rest + row, c, G.width, A.vec_out);
-          o[0] += low4(r);
-          o[1] += high4(r);
+          const Raw8<int16_t> r = load8(A.rest + row, c, G.width, A.vec_out);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            o[0][e] = with_rest(z.v[e], r.v[e]);
+            o[1][e] = with_rest(z.v[4 + e], r.v[4 + e]);
+          }
         }
       }
       const f32x4 lo = low4(y), hi = high4(y);
@@ -167,8 +171,20 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
     if (lane < 32) add_to(sums + kind * kColumns, x);
     if (lane >= 32) add_to(sums + kind * kColumns, x);
   };
-  float run = 0.f;  // of the tiles so far whose gaps were all in bucket run_kind
+  // of the tiles so far whose gaps were all in bucket run_kind, before the queries' own factors
+  float run[QT];
+#pragma unroll
+  for (int n = 0; n < QT; ++n) run[n] = 0.f;
   int run_kind = 0;
+  const auto end_run = [&]() {
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      sum = fmaf(run[n], inv[n], sum);
+      run[n] = 0.f;
+    }
+    add_sum(run_kind, sum);
+  };
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
     __syncthreads();
@@ -193,8 +209,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
     const bool one = near == far;
     const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
     if (one && near != run_kind) {
-      add_sum(run_kind, run);
-      run = 0.f;
+      end_run();
       run_kind = near;
     }
 #pragma unroll 1
@@ -219,14 +234,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       if (plain) {
 #pragma unroll
         for (int n = 0; n < QT; ++n) {
-          const float shift = b - top[n] - logsum[n];
+          const float shift = b - top[n];
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float p = exp2_fast(fmaf(s[n][t][e], scale, shift));
               s[n][t][e] = p * (dp[n][t][e] - delta[n]);
-              run += s[n][t][e];
+              run[n] += s[n][t][e];
             }
         }
       } else {
@@ -242,12 +257,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
               for (int e = 0; e < 4; ++e) {
                 const int kind = kind_of(pos[n], kpos[e]);
                 const float x = fmaf(s[n][t][e], scale, one ? b : lb.bias[kind]);
-                const float p = exp2_fast(x - top[n] - logsum[n]);
+                const float p = exp2_fast(x - top[n]);
                 float ds = p * (dp[n][t][e] - delta[n]);
                 const int j = k0 + w * 32 + t * 16 + g * 4 + e;
                 if (partial && (unsigned)(j - first[n]) > before[n]) ds = 0.f;
                 s[n][t][e] = ds;
-                if (one) run += ds; else add_sum(kind, ds);
+                if (one) run[n] += ds; else add_sum(kind, ds * inv[n]);
               }
           }
         };
@@ -286,10 +301,10 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
       const int d = c * 16 + g * 4;
-      if (d < G.width) store4((T *)A.dq + row + d, dq[n][c] * G.scale, G.width - d);
+      if (d < G.width) store4((T *)A.dq + row + d, dq[n][c] * (G.scale * inv[n]), G.width - d);
     }
   }
-  add_sum(run_kind, run);
+  end_run();
   __syncthreads();
   // four threads a bucket, a wave's columns each
   for (int n = tid; n < 4 * G.buckets; n += 256) {
@@ -322,11 +337,14 @@ template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   constexpr int QN = tile_tokens<T>(), CT = columns<T, D>(), BK = 64 * CT, LD = D + 16, PART = QN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
+  // A query's factor of the weights goes into the exponent: good for 2^-21, which bf16 does not see, and a
+  // product less a weight.
+  constexpr bool LOG = sizeof(T) == 2;
   using Staged = Tile<T, QN, D, 256, VEC>;
   __shared__ __align__(16) bf16 lq[NP * PART];
   __shared__ __align__(16) bf16 lo[NP * PART];
   __shared__ __align__(16) int32_t lpos[QN];
-  __shared__ __align__(16) float ltop[QN], llog[QN], ldelta[QN];
+  __shared__ __align__(16) float ltop[QN], linv[QN], ldelta[QN];
   __shared__ int32_t lrange[2];
   __shared__ Buckets lb;
 
@@ -400,7 +418,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
     const char *q = (const char *)((const T *)A.q.data + head * A.q.head_stride);
     const char *o = (const char *)((const T *)A.d_out.data + head * A.d_out.head_stride);
     const float *stats = A.stats + (int64_t)head * G.n_tokens;
-    const float *log_stats = stats + (int64_t)G.heads * G.n_tokens;
+    const float *inv_stats = stats + (int64_t)G.heads * G.n_tokens;
     const float *deltas = A.delta + (int64_t)head * G.n_tokens;
     Staged hq, ho;
     int hpos = 0;
@@ -415,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
       const int t = min(q0 + lane % QN, block_end - 1);
       if (wave == 0) hpos = G.positions[t];
       if (wave == 1) hstat = stats[t];
-      if (wave == 2) hstat = log_stats[t];
+      if (wave == 2) hstat = LOG ? __log2f(inv_stats[t]) : inv_stats[t];
       if (wave == 3) hstat = deltas[t];
     };
     fetch(block_first);
@@ -432,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
           lrange[1] = high;
         }
       } else if (lane < QN) {
-        (wave == 1 ? ltop : wave == 2 ? llog : ldelta)[lane] = hstat;
+        (wave == 1 ? ltop : wave == 2 ? linv : ldelta)[lane] = hstat;
       }
       __syncthreads();
       if (q0 + QN < block_end) fetch(q0 + QN);
@@ -467,18 +485,18 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int r = w * 32 + t * 16 + g * 4;
-            const f32x4 top = *(const f32x4 *)(ltop + r), logsum = *(const f32x4 *)(llog + r),
+            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r),
                         delta = *(const f32x4 *)(ldelta + r);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float shift = b - top[e] - logsum[e];
+              const float shift = b - top[e] + (LOG ? inv[e] : 0.f);
               const int qpos = lpos[r + e];
 #pragma unroll
               for (int n = 0; n < CT; ++n) {
                 const float x =
                     plain ? fmaf(s[n][t][e], scale, shift)
-                          : fmaf(s[n][t][e], scale, bias_of(qpos, pos[n])) - top[e] - logsum[e];
-                float p = exp2_fast(x), ds = p * (dp[n][t][e] - delta[e]);
+                          : fmaf(s[n][t][e], scale, bias_of(qpos, pos[n])) - top[e] + (LOG ? inv[e] : 0.f);
+                float p = LOG ? exp2_fast(x) : exp2_fast(x) * inv[e], ds = p * (dp[n][t][e] - delta[e]);
                 if (partial && (unsigned)(q0 + r + e - at[n]) >= after[n]) p = ds = 0.f;
                 s[n][t][e] = p;
                 dp[n][t][e] = ds;
@@ -578,7 +596,7 @@ GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int
 
 hipError_t launch_gap_back(als_dtype dtype, const GapShape &G, const als_heads &d_out, const als_heads &q,
                            const als_heads &k, const als_heads &v, const void *out, const float *stats,
-                           const void *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
+                           const int16_t *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
                            hipStream_t s) {
   const GapBackSpace x = gap_back_space(G.n_tokens, G.n_rows, G.heads, G.buckets);
   char *w = (char *)workspace;

@@ -100,10 +100,10 @@ struct GapShape {
 // Bytes of the table of the tokens' rows, which calls over more than a few rows need.
 int64_t gap_spans_bytes(int64_t n_tokens, int64_t n_rows);
 hipError_t launch_gap_spans(const GapShape &g, void *spans, hipStream_t s);
-// stats: nullable, fp32 [2, heads, n_tokens], the largest score (times log2 e) and the log2 of the sum;
-// rest: nullable, like out, what its rounding left out.
+// stats: nullable, fp32 [2, heads, n_tokens], the largest score (times log2 e) and one over the sum;
+// rest: nullable, like out, what its rounding to bf16 left out.
 hipError_t launch_gap_read(als_dtype dtype, const GapShape &g, const als_heads &q, const als_heads &k,
-                           const als_heads &v, const void *spans, void *out, float *stats, void *rest,
+                           const als_heads &v, const void *spans, void *out, float *stats, int16_t *rest,
                            hipStream_t s);
 
 // Bytes of the gradients' workspace, by part, each a multiple of 16.
@@ -114,7 +114,7 @@ struct GapBackSpace {
 GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t buckets);
 hipError_t launch_gap_back(als_dtype dtype, const GapShape &g, const als_heads &d_out, const als_heads &q,
                            const als_heads &k, const als_heads &v, const void *out, const float *stats,
-                           const void *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
+                           const int16_t *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,
                            hipStream_t s);
 
 // One token of each beam: what it reads besides its list's row of the history.

@@ -552,7 +552,7 @@ int64_t als_gap_attention_workspace(const als_gaps *shape) {
 }
 
 als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q, als_heads k, als_heads v,
-                             void *out, float *stats, void *rest, void *workspace, int64_t workspace_bytes,
+                             void *out, float *stats, int16_t *rest, void *workspace, int64_t workspace_bytes,
                              void *hip_stream) {
   if (als_status st = check_gaps(shape, dtype)) return st;
   const als_gaps *s = shape;
@@ -594,7 +594,7 @@ int64_t als_gap_attention_backward_workspace(const als_gaps *shape) {
 
 als_status als_gap_attention_backward(const als_gaps *shape, als_dtype dtype, als_heads d_out, als_heads q,
                                       als_heads k, als_heads v, const void *out, const float *stats,
-                                      const void *rest, void *dq, void *dk, void *dv, float *dbias,
+                                      const int16_t *rest, void *dq, void *dk, void *dv, float *dbias,
                                       void *workspace, int64_t workspace_bytes, void *hip_stream) {
   if (als_status st = check_gaps(shape, dtype)) return st;
   const als_gaps *s = shape;

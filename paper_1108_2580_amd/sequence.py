@@ -456,7 +456,7 @@ def _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, save):
     stats = rest = None
     if save:
         stats = torch.empty((2, shape.q_heads, shape.n_tokens), device=q.device)
-        rest = torch.empty_like(out) if code == ALS_BF16 else None
+        rest = torch.empty_like(out, dtype=torch.int16) if code == ALS_BF16 else None
     size = lib.als_gap_attention_workspace(shape)
     work = _workspace(size, q.device)
     _check(lib.als_gap_attention(shape, code, hq, hk, hv, out.data_ptr(), _ptr(stats), _ptr(rest), _ptr(work),
@@ -495,7 +495,7 @@ def gap_attention_backward(d_out, out, saved, q, k, v, bias, bounds, positions, 
     stats, rest = saved
     op = _array(out, "out", q.dtype, shaped, dev)
     sp = _array(stats, "saved[0]", torch.float32, (2, shape.q_heads, shape.n_tokens), dev)
-    rp = None if rest is None else _array(rest, "saved[1]", q.dtype, shaped, dev)
+    rp = None if rest is None else _array(rest, "saved[1]", torch.int16, shaped, dev)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     dbias = torch.empty_like(bias)
     size = lib.als_gap_attention_backward_workspace(shape)

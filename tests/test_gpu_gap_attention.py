@@ -12,7 +12,7 @@ products' sizes and its bias), D the width and n the longest row:
   formula over absolute values), two bf16 parts of a weight by 2^-16 of it, and its own rounding;
 - ds = p (do . v - do . o): with A = p (sum |do| |v| + sum |do| |o's size|), it is off by A times the weight's
   error, (D + 8) E for each product, the outputs' error (n E and twice the scores') and, in bf16, what rest
-  leaves of them (U U = 2^-16);
+  leaves of them (2^-24);
 - a gradient by that and n E (its sum) of the sum of its terms' sizes, 2^-16 for two parts, and its rounding.
 """
 import math
