@@ -3,9 +3,13 @@
 // queries that lie in global memory.
 #pragma once
 
+#include <type_traits>
+
 #include "tiles.h"
 
 namespace als {
+
+using i32x4 = int32_t __attribute__((ext_vector_type(4)));
 
 // The keys [first, i] that a token i reads as a query, and the queries [i, end) that read it as a key.
 // Of a token that no row holds: neither.
@@ -42,60 +46,81 @@ __device__ __forceinline__ Span2 span_of(const GapShape &G, const Span2 *spans, 
 __device__ __forceinline__ int32_t gap_of(int32_t a, int32_t b) { return __builtin_elementwise_sub_sat(a, b); }
 
 // ---- buckets --------------------------------------------------------------------------------------
-// The bucket of a gap is the number of bounds at it or below. Up to kTableGaps a table holds it for each
-// gap, a byte each; where the last bound is larger the bounds are searched. Either way the bias comes from
-// a second read, whose 64 places are 64 banks.
+// The bucket of a gap is the number of bounds at it or below. Where the last bound is below kTableGaps a table
+// in LDS holds for each gap the bias itself (Entry float: one read a score) or the bucket (uint8_t: a quarter of
+// the LDS, and a second read for the bias, whose 64 places are 64 banks); larger bounds are searched (Entry void).
 constexpr int kTableGaps = 8192;
 constexpr float kLargest = 3.402823466e38f;
 
-struct Buckets {
-  uint32_t kinds[kTableGaps / 4];  // a byte a gap
-  int32_t bounds[64];
-  float bias[64];                  // times log2 e, finite where it was
+// A bias as scores take it: times log2 e, finite where it was.
+__device__ __forceinline__ float bias2(float b) {
+  const float x = b * kLog2e;
+  return fabsf(b) <= kLargest ? fminf(fmaxf(x, -kLargest), kLargest) : x;
+}
 
-  // by the first 64 threads, with a barrier before fill
+// The number of 63 ascending bounds at the gap or below.
+__device__ __forceinline__ int bucket_of(const int32_t *bounds, int buckets, int32_t gap) {
+  int n = 0;
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1) n += bounds[n + step - 1] <= gap ? step : 0;
+  return n < buckets - 1 ? n : buckets - 1;
+}
+
+template <typename Entry> struct Table { Entry of[kTableGaps]; };
+template <> struct Table<void> {};
+
+template <typename Entry> struct Buckets : Table<Entry> {
+  static constexpr bool SEARCHED = std::is_void<Entry>::value, DIRECT = std::is_same<Entry, float>::value;
+  int32_t bounds[64];
+  float bias[64];
+
+  // by the first 64 threads, with a barrier before anything else
   __device__ __forceinline__ void start(const GapShape &G, int head, int tid) {
     if (tid < 64) {
-      const float b = tid < G.buckets ? G.bias[(int64_t)head * G.buckets + tid] : 0.f;
-      float x = b * kLog2e;
-      if (fabsf(b) <= kLargest) x = fminf(fmaxf(x, -kLargest), kLargest);
-      bias[tid] = x;
+      bias[tid] = bias2(tid < G.buckets ? G.bias[(int64_t)head * G.buckets + tid] : 0.f);
       bounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
     }
   }
-  // `most`: no larger gap is asked for
-  __device__ __forceinline__ void fill(const GapShape &G, int32_t most, int tid, int threads) {
-    if (G.last_bound >= kTableGaps) return;
-    const int32_t top = most < G.last_bound ? most : G.last_bound;
-    for (int w = tid; w <= top / 4; w += threads) {
-      int n = 0;  // bounds at the word's first gap or below, then at the others
-#pragma unroll
-      for (int step = 32; step > 0; step >>= 1)
-        if (bounds[n + step - 1] <= w * 4) n += step;
-      uint32_t word = (uint32_t)n;
-#pragma unroll
-      for (int e = 1; e < 4; ++e) {
-        while (n < G.buckets - 1 && bounds[n] <= w * 4 + e) ++n;
-        word |= (uint32_t)n << (8 * e);
+  // a wave a bucket in turn
+  __device__ __forceinline__ void fill(const GapShape &G, int wave, int lane) {
+    if constexpr (!SEARCHED) {
+      for (int b = wave; b < G.buckets; b += 4) {
+        const int lo = b ? bounds[b - 1] : 0, hi = b < G.buckets - 1 ? bounds[b] : G.last_bound + 1;
+        if constexpr (DIRECT) {
+          const float x = bias[b];
+          for (int g = lo + lane; g < hi; g += 64) this->of[g] = x;
+        } else {
+          for (int g = lo + lane; g < hi; g += 64) this->of[g] = (uint8_t)b;
+        }
       }
-      kinds[w] = word;
     }
   }
-  template <bool TABLE> __device__ __forceinline__ int kind(const GapShape &G, int32_t gap) const {
-    if (TABLE) {
-      const int32_t g = gap < 0 ? 0 : gap > G.last_bound ? G.last_bound : gap;
-      return ((const uint8_t *)kinds)[g];
-    }
-    int n = 0;
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1)
-      if (bounds[n + step - 1] <= gap) n += step;
-    return n < G.buckets - 1 ? n : G.buckets - 1;
+  __device__ __forceinline__ int clipped(const GapShape &G, int32_t gap) const {
+    const int g = gap < G.last_bound ? gap : G.last_bound;
+    return g > 0 ? g : 0;
   }
+  // not of a DIRECT table's scores, whose bias comes without it
   __device__ __forceinline__ int kind(const GapShape &G, int32_t gap) const {
-    return G.last_bound < kTableGaps ? kind<true>(G, gap) : kind<false>(G, gap);
+    if constexpr (SEARCHED || DIRECT)
+      return bucket_of(bounds, G.buckets, gap);
+    else
+      return this->of[clipped(G, gap)];
+  }
+  __device__ __forceinline__ float bias_of(const GapShape &G, int32_t gap) const {
+    if constexpr (DIRECT)
+      return this->of[clipped(G, gap)];
+    else
+      return bias[kind(G, gap)];
   }
 };
+// The bucket of two gaps, low <= high, if it is one for both, else -1; the same in all lanes. Lane l looks at
+// bound l.
+template <typename B>
+__device__ __forceinline__ int one_bucket(const B &b, const GapShape &G, int32_t low, int32_t high, int lane) {
+  const int32_t bound = b.bounds[lane];
+  const int at = __popcll(__ballot(bound <= low && lane < G.buckets - 1));
+  return at == __popcll(__ballot(bound <= high && lane < G.buckets - 1)) ? at : -1;
+}
 // Up to this bias a score's largest is as good as the score itself: exponents may take their
 // difference first.
 constexpr float kPlainBias = 16777216.f;

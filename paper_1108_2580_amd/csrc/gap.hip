@@ -44,7 +44,7 @@ template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 3
 // Columns of 16 queries a wave.
 template <typename T> constexpr int query_tiles() { return sizeof(T) == 2 ? 2 : 1; }
 
-template <typename T, int D, bool VEC>
+template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   __shared__ __align__(16) bf16 lv[NP * PART];
   __shared__ __align__(16) int32_t lpos[KN];
   __shared__ int32_t lrange[2];
-  __shared__ Buckets lb;
+  __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   };
   fetch(block_first);
   __syncthreads();
-  lb.fill(G, 0x7fffffff, tid, 256);
+  lb.fill(G, wave, lane);
 
   f32x4 o[QT][DT];
   float top[QT], base[QT], sum[QT];
@@ -170,10 +170,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
     }
 
     // one bucket for the tile's gaps, or one for each
-    const int near = lb.kind(G, gap_of(pos_min, lrange[1])), far = lb.kind(G, gap_of(pos_max, lrange[0]));
-    const float b = lb.bias[near];
-    const bool one = __builtin_amdgcn_readfirstlane(near) == __builtin_amdgcn_readfirstlane(far);
-    const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+    const int kind = one_bucket(lb, G, gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]), lane);
+    const float b = kind >= 0 ? lb.bias[kind] : 0.f;
+    const bool plain = kind >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
     float most[QT];
     if (plain) {
 #pragma unroll
@@ -191,27 +190,27 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
         for (int n = 0; n < QT; ++n) most[n] = -__builtin_inff();
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
-          int kpos[4];
+          const i32x4 kpos = *(const i32x4 *)(lpos + t * 16 + g * 4);
+          f32x4 add[QT];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kpos[e] = lpos[t * 16 + g * 4 + e];
+          for (int n = 0; n < QT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add[n][e] = bias_of(gap_of(pos[n], kpos[e]));
 #pragma unroll
           for (int n = 0; n < QT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float x = fmaf(s[n][t][e], scale, bias_of(pos[n], kpos[e]));
-              const int j = k0 + t * 16 + g * 4 + e;
-              if (partial && (unsigned)(j - first[n]) > before[n]) x = -__builtin_inff();
+              const bool kept = (unsigned)(k0 + t * 16 + g * 4 + e - first[n]) <= before[n];
+              const float x = kept ? fmaf(s[n][t][e], scale, add[n][e]) : -__builtin_inff();
               s[n][t][e] = x;
               most[n] = fmaxf(most[n], x);
             }
         }
       };
-      if (one)
-        biased([&](int, int) { return b; });
-      else if (G.last_bound < kTableGaps)
-        biased([&](int i, int j) { return lb.bias[lb.kind<true>(G, gap_of(i, j))]; });
+      if (kind >= 0)
+        biased([&](int) { return b; });
       else
-        biased([&](int i, int j) { return lb.bias[lb.kind<false>(G, gap_of(i, j))]; });
+        biased([&](int gap) { return lb.bias_of(G, gap); });
     }
 
     // The largest score so far is followed only where it has grown by 8: exponentials up to 2^8 keep
@@ -301,15 +300,19 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
 
 template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStream_t s) {
   constexpr int BQ = 64 * query_tiles<T>();
+  // a table of biases, where it leaves a CU two blocks
+  using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, float>::type;
   A.n_tiles = (A.G.n_tokens + BQ - 1) / BQ;
   const int64_t per = max_blocks(256) / A.G.heads;
   for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
     const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
     const dim3 grid((unsigned)(n * A.G.heads));
-    if (vec)
-      hipLaunchKernelGGL((k_gap_read<T, D, true>), grid, dim3(256), 0, s, A);
+    if (A.G.last_bound >= kTableGaps)
+      hipLaunchKernelGGL((k_gap_read<T, D, false, void>), grid, dim3(256), 0, s, A);
+    else if (vec)
+      hipLaunchKernelGGL((k_gap_read<T, D, true, Entry>), grid, dim3(256), 0, s, A);
     else
-      hipLaunchKernelGGL((k_gap_read<T, D, false>), grid, dim3(256), 0, s, A);
+      hipLaunchKernelGGL((k_gap_read<T, D, false, Entry>), grid, dim3(256), 0, s, A);
   }
   return hipGetLastError();
 }

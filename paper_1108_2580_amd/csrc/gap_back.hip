@@ -37,15 +37,23 @@ template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 ? 2
 
 // ---- over keys: dq and dbias ---------------------------------------------------------------------
 
-// Sums by bucket: 32 columns a wave, two lanes each, which add one after the other: the order of a
-// column's terms is that of the program.
-constexpr int kColumns = 32;
+// Sums by bucket: a column each lane, so that no two lanes add to the same place and the order of a sum's
+// terms is that of the program. LDS adds floats by itself at 3 cycles a lane (194 a wave's instruction, where
+// a read and a write take 8), so a lane reads, adds and writes: four places at a time, each with what the
+// ones before it give the same place, so that the last write to a place has all of them.
+constexpr int kColumns = 64;
 
-__device__ __forceinline__ void add_to(float *x, float y) {
-  __hip_atomic_fetch_add(x, y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+__device__ __forceinline__ void add_sums(float *column, i32x4 kind, f32x4 x) {
+  x[1] += kind[1] == kind[0] ? x[0] : 0.f;
+  x[2] += kind[2] == kind[1] ? x[1] : kind[2] == kind[0] ? x[0] : 0.f;
+  x[3] += kind[3] == kind[2] ? x[2] : kind[3] == kind[1] ? x[1] : kind[3] == kind[0] ? x[0] : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] += column[kind[e] * kColumns];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) column[kind[e] * kColumns] = x[e];
 }
 
-template <typename T, int D, bool VEC>
+template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   constexpr int KN = tile_tokens<T>(), QT = columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
@@ -54,7 +62,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   __shared__ __align__(16) bf16 lv[NP * PART];
   __shared__ __align__(16) int32_t lpos[KN];
   __shared__ int32_t lrange[2];
-  __shared__ Buckets lb;
+  __shared__ Buckets<Entry> lb;
   extern __shared__ float lsums[];  // [waves, buckets, kColumns]
 
   const GapShape &G = A.G;
@@ -159,18 +167,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   };
   fetch(block_first);
   __syncthreads();
-  lb.fill(G, 0x7fffffff, tid, 256);
+  lb.fill(G, wave, lane);
 
   f32x4 dq[QT][DT];
 #pragma unroll
   for (int n = 0; n < QT; ++n)
 #pragma unroll
     for (int c = 0; c < DT; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float *sums = lsums + wave * G.buckets * kColumns + (lane & (kColumns - 1));
-  const auto add_sum = [&](int kind, float x) {
-    if (lane < 32) add_to(sums + kind * kColumns, x);
-    if (lane >= 32) add_to(sums + kind * kColumns, x);
-  };
+  float *sums = lsums + wave * G.buckets * kColumns + lane;
   // of the tiles so far whose gaps were all in bucket run_kind, before the queries' own factors
   float run[QT];
 #pragma unroll
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       sum = fmaf(run[n], inv[n], sum);
       run[n] = 0.f;
     }
-    add_sum(run_kind, sum);
+    sums[run_kind * kColumns] += sum;
   };
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
@@ -203,14 +207,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
     if (k0 > last || k0 + KN <= first_min) continue;
 
     const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
-    const int near = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(pos_min, lrange[1])));
-    const int far = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(pos_max, lrange[0])));
-    const float b = lb.bias[near];
-    const bool one = near == far;
-    const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
-    if (one && near != run_kind) {
+    const int one = one_bucket(lb, G, gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]), lane);
+    const float b = one >= 0 ? lb.bias[one] : 0.f;
+    const bool plain = one >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+    if (one >= 0 && one != run_kind) {
       end_run();
-      run_kind = near;
+      run_kind = one;
     }
 #pragma unroll 1
     for (int w = 0; w < KS; ++w) {  // 32 keys at a time
@@ -245,33 +247,48 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
             }
         }
       } else {
-        const auto biased = [&](auto kind_of) {
+        i32x4 kind[QT][2];
+        f32x4 add[QT][2];
+        if (one < 0) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            int kpos[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) kpos[e] = lpos[w * 32 + t * 16 + g * 4 + e];
+            const i32x4 kpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
 #pragma unroll
             for (int n = 0; n < QT; ++n)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int kind = kind_of(pos[n], kpos[e]);
-                const float x = fmaf(s[n][t][e], scale, one ? b : lb.bias[kind]);
-                const float p = exp2_fast(x - top[n]);
-                float ds = p * (dp[n][t][e] - delta[n]);
-                const int j = k0 + w * 32 + t * 16 + g * 4 + e;
-                if (partial && (unsigned)(j - first[n]) > before[n]) ds = 0.f;
-                s[n][t][e] = ds;
-                if (one) run[n] += ds; else add_sum(kind, ds * inv[n]);
-              }
+              for (int e = 0; e < 4; ++e) kind[n][t][e] = lb.kind(G, gap_of(pos[n], kpos[e]));
           }
-        };
-        if (one)
-          biased([&](int, int) { return near; });
-        else if (G.last_bound < kTableGaps)
-          biased([&](int i, int j) { return lb.kind<true>(G, gap_of(i, j)); });
-        else
-          biased([&](int i, int j) { return lb.kind<false>(G, gap_of(i, j)); });
+        }
+#pragma unroll
+        for (int n = 0; n < QT; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add[n][t][e] = one >= 0 ? b : lb.bias[kind[n][t][e]];
+#pragma unroll
+        for (int n = 0; n < QT; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = exp2_fast(fmaf(s[n][t][e], scale, add[n][t][e]) - top[n]);
+              const bool kept = (unsigned)(k0 + w * 32 + t * 16 + g * 4 + e - first[n]) <= before[n];
+              s[n][t][e] = kept ? p * (dp[n][t][e] - delta[n]) : 0.f;
+            }
+        if (one >= 0) {
+#pragma unroll
+          for (int n = 0; n < QT; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) run[n] += s[n][t][e];
+        } else {
+#pragma unroll
+          for (int n = 0; n < QT; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              add_sums(sums, kind[n][t], s[n][t] * inv[n]);
+        }
       }
       Frag<RP> df[QT];
 #pragma unroll
@@ -333,7 +350,7 @@ __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ par
 
 // ---- over queries: dk and dv ---------------------------------------------------------------------
 
-template <typename T, int D, bool VEC>
+template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   constexpr int QN = tile_tokens<T>(), CT = columns<T, D>(), BK = 64 * CT, LD = D + 16, PART = QN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
@@ -346,7 +363,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   __shared__ __align__(16) int32_t lpos[QN];
   __shared__ __align__(16) float ltop[QN], linv[QN], ldelta[QN];
   __shared__ int32_t lrange[2];
-  __shared__ Buckets lb;
+  __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
@@ -411,9 +428,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   for (int head = k_head * G.group; head < (k_head + 1) * G.group; ++head) {
     __syncthreads();
     lb.start(G, head, tid);
-    if (head == k_head * G.group) {
+    if (Buckets<Entry>::DIRECT || head == k_head * G.group) {
       __syncthreads();
-      lb.fill(G, 0x7fffffff, tid, 256);
+      lb.fill(G, wave, lane);
     }
     const char *q = (const char *)((const T *)A.q.data + head * A.q.head_stride);
     const char *o = (const char *)((const T *)A.d_out.data + head * A.d_out.head_stride);
@@ -457,11 +474,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
       if (q0 + QN <= j0 || q0 >= end_max) continue;
 
       const bool partial = q0 < j0 + 16 * CT - 1 || q0 + QN > end_min;
-      const int near = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(lrange[0], pos_max)));
-      const int far = __builtin_amdgcn_readfirstlane(lb.kind(G, gap_of(lrange[1], pos_min)));
-      const float b = lb.bias[near];
-      const bool one = near == far;
-      const bool plain = one && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+      const int one = one_bucket(lb, G, gap_of(lrange[0], pos_max), gap_of(lrange[1], pos_min), lane);
+      const float b = one >= 0 ? lb.bias[one] : 0.f;
+      const bool plain = one >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
 #pragma unroll 1
       for (int w = 0; w < QS; ++w) {  // 32 queries at a time
         const bf16 *wq = lq + w * 32 * LD, *wo = lo + w * 32 * LD;
@@ -481,35 +496,50 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
             }
           }
         }
-        const auto weigh = [&](auto bias_of) {  // s, dp -> p, ds
+        // s, dp -> p, ds
+        if (plain) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int r = w * 32 + t * 16 + g * 4;
+            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r),
+                        delta = *(const f32x4 *)(ldelta + r);
+            const f32x4 shift = LOG ? b - top + inv : b - top;
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float x = exp2_fast(fmaf(s[n][t][e], scale, shift[e])), p = LOG ? x : x * inv[e];
+                s[n][t][e] = p;
+                dp[n][t][e] = p * (dp[n][t][e] - delta[e]);
+              }
+          }
+        } else {
+          f32x4 add[CT][2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const i32x4 qpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) add[n][t][e] = one >= 0 ? b : lb.bias_of(G, gap_of(qpos[e], pos[n]));
+          }
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int r = w * 32 + t * 16 + g * 4;
             const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r),
                         delta = *(const f32x4 *)(ldelta + r);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float shift = b - top[e] + (LOG ? inv[e] : 0.f);
-              const int qpos = lpos[r + e];
+            for (int n = 0; n < CT; ++n)
 #pragma unroll
-              for (int n = 0; n < CT; ++n) {
-                const float x =
-                    plain ? fmaf(s[n][t][e], scale, shift)
-                          : fmaf(s[n][t][e], scale, bias_of(qpos, pos[n])) - top[e] + (LOG ? inv[e] : 0.f);
-                float p = LOG ? exp2_fast(x) : exp2_fast(x) * inv[e], ds = p * (dp[n][t][e] - delta[e]);
-                if (partial && (unsigned)(q0 + r + e - at[n]) >= after[n]) p = ds = 0.f;
-                s[n][t][e] = p;
-                dp[n][t][e] = ds;
+              for (int e = 0; e < 4; ++e) {
+                const float x = fmaf(s[n][t][e], scale, add[n][t][e]) - top[e];
+                const float p = LOG ? exp2_fast(x + inv[e]) : exp2_fast(x) * inv[e];
+                const bool kept = (unsigned)(q0 + r + e - at[n]) < after[n];
+                s[n][t][e] = kept ? p : 0.f;
+                dp[n][t][e] = kept ? p * (dp[n][t][e] - delta[e]) : 0.f;
               }
-            }
           }
-        };
-        if (one)
-          weigh([&](int, int) { return b; });
-        else if (G.last_bound < kTableGaps)
-          weigh([&](int i, int j) { return lb.bias[lb.kind<true>(G, gap_of(i, j))]; });
-        else
-          weigh([&](int i, int j) { return lb.bias[lb.kind<false>(G, gap_of(i, j))]; });
+        }
         Frag<RP> pf[CT], df[CT];
 #pragma unroll
         for (int n = 0; n < CT; ++n) {
@@ -571,11 +601,19 @@ template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float 
       hipLaunchKernelGGL(kernel, dim3((unsigned)(n * heads)), dim3(256), lds, s, A);
     }
   };
-  each(vec ? k_gap_dq<T, D, true> : k_gap_dq<T, D, false>, A.G.heads,
-       4 * A.G.buckets * kColumns * sizeof(float));
+  // tables of biases, where they leave a CU two blocks
+  using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, float>::type;
+  const bool searched = A.G.last_bound >= kTableGaps;
+  each(searched ? k_gap_dq<T, D, false, void>
+       : vec    ? k_gap_dq<T, D, true, uint8_t>
+                : k_gap_dq<T, D, false, uint8_t>,
+       A.G.heads, 4 * A.G.buckets * kColumns * sizeof(float));
   hipLaunchKernelGGL(k_gap_dbias, dim3((unsigned)(A.G.heads * A.G.buckets)), dim3(256), 0, s, A.dbias_parts,
                      A.n_tiles, dbias);
-  each(vec ? k_gap_dkv<T, D, true> : k_gap_dkv<T, D, false>, A.G.heads / A.G.group, 0);
+  each(searched ? k_gap_dkv<T, D, false, void>
+       : vec    ? k_gap_dkv<T, D, true, Entry>
+                : k_gap_dkv<T, D, false, Entry>,
+       A.G.heads / A.G.group, 0);
   return hipGetLastError();
 }
 template <typename T> hipError_t launch_back(const BackArgs &A, bool vec, float *dbias, hipStream_t s) {

@@ -59,10 +59,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
   if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
   for (int x = tid; x < COLS * G.buckets; x += 256) {
     const int c = x / G.buckets, n = x % G.buckets, col = min(col0 + c, columns - 1);
-    const float b = G.bias[(int64_t)(k_head * G.group + col % G.group) * G.buckets + n];
-    float y = b * kLog2e;
-    if (fabsf(b) <= kLargest) y = fminf(fmaxf(y, -kLargest), kLargest);
-    lbias[c * LB + n] = y;
+    lbias[c * LB + n] = bias2(G.bias[(int64_t)(k_head * G.group + col % G.group) * G.buckets + n]);
   }
 
   Frag<NP> qf[CT][DF];
@@ -116,13 +113,6 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const auto kind_of = [&](int gap) {
-    int n = 0;
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1)
-      if (lbounds[n + step - 1] <= gap) n += step;
-    return n < G.buckets - 1 ? n : G.buckets - 1;
-  };
   if (wave * 32 < count) fetch(wave * 32);
   __syncthreads();
 
@@ -141,7 +131,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
       for (int n = 0; n < NP; ++n) *(bf16x8 *)(to + n * PART) = x.p[n];
     }
     // where the beams' positions are alike, a lane finds the bucket of one key, for all columns
-    if (lane < 32) lkind[wave][lane] = alike ? kind_of(gap_of(pos0, hpos)) : hpos;
+    if (lane < 32) lkind[wave][lane] = alike ? bucket_of(lbounds, G.buckets, gap_of(pos0, hpos)) : hpos;
     if (j0 + 128 < count) fetch(j0 + 128);
     __builtin_amdgcn_wave_barrier();
 
@@ -158,7 +148,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = t * 16 + g * 4 + e, x = lkind[wave][r];
-          const float b = lbias[(n * 16 + m) * LB + (alike ? x : kind_of(gap_of(pos[n], x)))];
+          const float b = lbias[(n * 16 + m) * LB + (alike ? x : bucket_of(lbounds, G.buckets, gap_of(pos[n], x)))];
           const float y = j0 + r < count ? fmaf(s[n][t][e], scale, b) : -__builtin_inff();
           s[n][t][e] = y;
           most[n] = fmaxf(most[n], y);
@@ -318,15 +308,8 @@ __global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
     for (int e = 0; e < 4; ++e) x = fmaf(q[0][e], k[0][e], fmaf(q[1][e], k[1][e], x));
 #pragma unroll
     for (int n = 1; n < L; n <<= 1) x += __shfl_xor(x, n);
-    int kind = 0;
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1)
-      if (lbounds[kind + step - 1] <= gap) kind += step;
-    kind = kind < G.buckets - 1 ? kind : G.buckets - 1;
-    const float b = G.bias[(int64_t)head * G.buckets + kind];
-    float y = b * kLog2e;
-    if (fabsf(b) <= kLargest) y = fminf(fmaxf(y, -kLargest), kLargest);
-    y = fmaf(x, scale, y);
+    const float b = G.bias[(int64_t)head * G.buckets + bucket_of(lbounds, G.buckets, gap)];
+    float y = fmaf(x, scale, bias2(b));
     if (!ok) y = __builtin_nanf("");
     take(y, 1.f, v);
   }
