@@ -212,14 +212,14 @@ __device__ __forceinline__ float with_rest(bf16 x, int16_t rest) {
   return __uint_as_float(((uint32_t)__builtin_bit_cast(uint16_t, x) << 16) + (uint32_t)(int32_t)rest);
 }
 
-__device__ __forceinline__ bool finite4(f32x4 x) {
-  return x[0] * 0.f + x[1] * 0.f + (x[2] * 0.f + x[3] * 0.f) == 0.f;
-}
-
-// Over the lanes of a column (lane & 15): the sum or the largest.
+// Over the lanes of a column (lane & 15): the sum or the largest. The swaps give each lane both halves of a
+// pair of rows of lanes, then of the wave, without a way through LDS.
 __device__ __forceinline__ float column_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  const uint32_t a = __float_as_uint(x);
+  const auto y = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const uint32_t b = __float_as_uint(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+  const auto z = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
 }
 __device__ __forceinline__ float column_sum(float x) {
   x += __shfl_xor(x, 16);
@@ -236,48 +236,49 @@ __device__ __forceinline__ int wave_max(int x) {
   return x;
 }
 
-// to[c] += rows 16 c + 4 g .. 4 g + 3 of x^T W, g the lane's group, for x in LDS and 16-row tiles of weights W
-// as MFMA leaves them (a lane: column m = lane & 15, rows 4 g .. 4 g + 3). In a tile of which a mask leaves
-// only the places that ok(row) names, W is zero elsewhere, which an infinity or NaN in x would turn into
-// NaN: where a sum is not finite it is formed again over the places that are left, one row at a time.
-template <int NP, int TILES, int C, typename Columns, typename OK>
-__device__ __forceinline__ void add_kept(const f32x4 *w, const bf16 *x, int ld, int part, int lane,
-                                         Columns product, OK ok, f32x4 *to) {
-  f32x4 sum[C];
-  bool finite = true;
+// A tile of which a mask leaves some places has weights of zero in the others, which an infinity or NaN there
+// would turn into NaN. So such tiles' rows are looked at, and where one is met the product is formed one row
+// at a time over the places that are left.
+// Whether 32 rows of x in LDS, 16 C wide, are finite (of parts, the first tells).
+template <int C> __device__ __forceinline__ bool finite_rows(const bf16 *x, int ld, int lane) {
+  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+  uint32_t carry = 0;  // into either half's sign: its exponent was all ones
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    sum[c] = product(c, f32x4{0.f, 0.f, 0.f, 0.f});
-    finite = finite && finite4(sum[c]);
+    const u32x4 bits = __builtin_bit_cast(u32x4, frag_col<1, 4>(x + c * 16, ld, 0, lane).p[0]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) carry |= (bits[e] & 0x7fff7fffu) + 0x00800080u;
   }
-  if (__any(!finite)) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) sum[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  return !__any((carry & 0x80008000u) != 0);
+}
+// to[c] += rows 16 c + 4 g .. 4 g + 3 of x^T W, g the lane's group, for 32 rows of x in LDS and W as MFMA leaves
+// it (two tiles; a lane: column lane & 15, rows 4 g .. 4 g + 3), over the places of the lane's column that
+// ok(row) leaves.
+template <int NP, int C, typename OK>
+__device__ __forceinline__ void add_rows(const f32x4 *w, const bf16 *x, int ld, int part, int lane, OK ok,
+                                         f32x4 *to) {
 #pragma unroll 1
-    for (int r = 0; r < 16 * TILES; ++r) {
-      float weight = 0.f;
+  for (int r = 0; r < 32; ++r) {
+    float weight = 0.f;
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r / 16 == t && r % 4 == e) weight = w[t][e];
-      weight = __shfl(weight, r % 16 / 4 * 16 + (lane & 15));
-      if (ok(r)) {
-        const bf16 *p = x + r * ld + (lane >> 4) * 4;
+      for (int e = 0; e < 4; ++e)
+        if (r / 16 == t && r % 4 == e) weight = w[t][e];
+    weight = __shfl(weight, r % 16 / 4 * 16 + (lane & 15));
+    if (ok(r)) {
+      const bf16 *p = x + r * ld + (lane >> 4) * 4;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float v = 0.f;
+        for (int e = 0; e < 4; ++e) {
+          float v = 0.f;
 #pragma unroll
-            for (int n = NP - 1; n >= 0; --n) v += (float)p[n * part + c * 16 + e];
-            sum[c][e] = fmaf(weight, v, sum[c][e]);
-          }
-      }
+          for (int n = NP - 1; n >= 0; --n) v += (float)p[n * part + c * 16 + e];
+          to[c][e] = fmaf(weight, v, to[c][e]);
+        }
     }
   }
-#pragma unroll
-  for (int c = 0; c < C; ++c) to[c] += sum[c];
 }
 
 }  // namespace als

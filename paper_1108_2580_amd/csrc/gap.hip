@@ -56,7 +56,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  int tid = (int)threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = (int)(blockIdx.x % (unsigned)G.heads);
   // a row's last tokens have the most keys: they go first
   const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
@@ -140,6 +141,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   }
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
+    // addresses are formed anew in each tile: held across tiles they would cost a block its place on the CU
+    asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));
     __syncthreads();
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
@@ -235,42 +238,37 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
       }
     }
 
-    Frag<RP> pf[QT][KS];
 #pragma unroll
-    for (int n = 0; n < QT; ++n) {
-      const float shift = b - base[n];
+    for (int w = 0; w < KS; ++w) {  // 32 keys at a time
+      __builtin_amdgcn_sched_barrier(0);
+      const bf16 *wv = lv + w * 32 * LD;
+      Frag<RP> pf[QT];
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
+      for (int n = 0; n < QT; ++n) {
+        const float by = plain ? scale : 1.f, shift = plain ? b - base[n] : -base[n];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = exp2_fast(plain ? fmaf(s[n][t][e], scale, shift) : s[n][t][e] - base[n]);
-          s[n][t][e] = x;
-          sum[n] += x;
+        for (int t = 2 * w; t < 2 * w + 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = exp2_fast(fmaf(s[n][t][e], by, shift));
+            s[n][t][e] = x;
+            sum[n] += x;
+          }
+        pf[n] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
+      }
+      if (!partial || finite_rows<DT>(wv, LD, lane)) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          const Frag<NP> vf = frag_col<NP, 4>(wv + c * 16, LD, PART, lane);
+#pragma unroll
+          for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n], o[n][c]);
         }
+      } else {
 #pragma unroll
-      for (int w = 0; w < KS; ++w) pf[n][w] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
-    }
-    if (!partial) {
-#pragma unroll
-      for (int c = 0; c < DT; ++c)
-#pragma unroll
-        for (int w = 0; w < KS; ++w) {
-          const Frag<NP> vf = frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane);
-#pragma unroll
-          for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n][w], o[n][c]);
-        }
-    } else {
-#pragma unroll
-      for (int n = 0; n < QT; ++n)
-        add_kept<NP, KT, DT>(
-            s[n], lv, LD, PART, lane,
-            [&](int c, f32x4 x) {
-#pragma unroll
-              for (int w = 0; w < KS; ++w)
-                x = mma(frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane), pf[n][w], x);
-              return x;
-            },
-            [&](int r) { return (unsigned)(k0 + r - first[n]) <= before[n]; }, o[n]);
+        for (int n = 0; n < QT; ++n)
+          add_rows<NP, DT>(s[n] + 2 * w, wv, LD, PART, lane,
+                           [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, o[n]);
+      }
     }
   }
 

@@ -33,7 +33,7 @@ struct BackArgs {
 };
 
 template <typename T> constexpr int tile_tokens() { return sizeof(T) == 2 ? 64 : 32; }
-template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 ? 2 : 1; }
+template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 && D < 128 ? 2 : 1; }
 
 // ---- over keys: dq and dbias ---------------------------------------------------------------------
 
@@ -66,7 +66,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   extern __shared__ float lsums[];  // [waves, buckets, kColumns]
 
   const GapShape &G = A.G;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  int tid = (int)threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = (int)(blockIdx.x % (unsigned)G.heads);
   const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
   const int64_t t0 = tile * BQ;
@@ -191,6 +192,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   };
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
+    // addresses are formed anew in each tile: held across tiles they cost registers
+    asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));
     __syncthreads();
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       Frag<RP> df[QT];
 #pragma unroll
       for (int n = 0; n < QT; ++n) df[n] = as_frag<RP>(s[n][0], s[n][1]);
-      if (!partial) {
+      if (!partial || finite_rows<DT>(wk, LD, lane)) {
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
           const Frag<NP> kf = frag_col<NP, 4>(wk + c * 16, LD, PART, lane);
@@ -303,10 +306,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       } else {
 #pragma unroll
         for (int n = 0; n < QT; ++n)
-          add_kept<NP, 2, DT>(
-              s[n], wk, LD, PART, lane,
-              [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wk + c * 16, LD, PART, lane), df[n], x); },
-              [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, dq[n]);
+          add_rows<NP, DT>(s[n], wk, LD, PART, lane,
+                           [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, dq[n]);
       }
     }
   }
@@ -366,7 +367,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+  int tid = (int)threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int k_heads = G.heads / G.group;
   const int k_head = (int)(blockIdx.x % (unsigned)k_heads);
   const int64_t t0 = (A.tile0 + blockIdx.x / (unsigned)k_heads) * BK;
@@ -456,6 +458,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
     fetch(block_first);
 
     for (int q0 = block_first; q0 < block_end; q0 += QN) {
+      asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));  // as above
       __syncthreads();
       hq.put_parts(lq, LD, rows_of(q, q_row, q0), tid);
       ho.put_parts(lo, LD, rows_of(o, o_row, q0), tid);
@@ -546,7 +549,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
           pf[n] = as_frag<RP>(s[n][0], s[n][1]);
           df[n] = as_frag<RP>(dp[n][0], dp[n][1]);
         }
-        if (!partial) {
+        if (!partial || (finite_rows<DT>(wo, LD, lane) && finite_rows<DT>(wq, LD, lane))) {
 #pragma unroll
           for (int c = 0; c < DT; ++c) {
             const Frag<NP> of = frag_col<NP, 4>(wo + c * 16, LD, PART, lane);
@@ -561,14 +564,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll
           for (int n = 0; n < CT; ++n) {
             const auto ok = [&](int r) { return (unsigned)(q0 + w * 32 + r - at[n]) < after[n]; };
-            add_kept<NP, 2, DT>(
-                s[n], wo, LD, PART, lane,
-                [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wo + c * 16, LD, PART, lane), pf[n], x); },
-                ok, dv[n]);
-            add_kept<NP, 2, DT>(
-                dp[n], wq, LD, PART, lane,
-                [&](int c, f32x4 x) { return mma(frag_col<NP, 4>(wq + c * 16, LD, PART, lane), df[n], x); },
-                ok, dk[n]);
+            add_rows<NP, DT>(s[n], wo, LD, PART, lane, ok, dv[n]);
+            add_rows<NP, DT>(dp[n], wq, LD, PART, lane, ok, dk[n]);
           }
         }
       }

@@ -166,7 +166,7 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   static constexpr int E = 16 / sizeof(T), ROW = WP / E;
   static constexpr int ROWS = THREADS / ROW, N = (C + ROWS - 1) / ROWS;
   static_assert(THREADS % ROW == 0 && (ROWS >= C || C % ROWS == 0), "whole rows a pass");
-  struct alignas(16) Piece { T v[E]; };
+  using Piece = uint32_t __attribute__((ext_vector_type(4)));  // E values
   struct Rows {  // of one chunk
     const char *base;
     uint32_t bytes;  // from row to row
@@ -182,8 +182,7 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = r0 + i * ROWS;
-#pragma unroll
-      for (int e = 0; e < E; ++e) held[i].v[e] = (T)0.f;
+      held[i] = Piece{0, 0, 0, 0};
       if (r < x.size && c < x.width) {
         if (VEC)
           held[i] = *(const Piece *)x.at(r, c);
@@ -196,11 +195,11 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   __device__ __forceinline__ Piece piece(const Rows &x, int i, int r, int c) const {
     if (VEC) return held[i];
     if (x.width < E) {  // too narrow for any whole piece
-      Piece p;
+      struct { T v[E]; } p;
 #pragma unroll
       for (int e = 0; e < E; ++e)
         p.v[e] = r < x.size && c + e < x.width ? ((const T *)x.at(r, 0))[e] : (T)0.f;
-      return p;
+      return __builtin_bit_cast(Piece, p);
     }
     int bits = (c + E > x.width ? c + E - x.width : 0) * (int)sizeof(T) * 8;
     uint64_t w[2];
@@ -232,9 +231,8 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (ROWS <= C || r0 < C) {
-          const Piece p = piece(x, i, r0 + i * ROWS, c);
           bf16x4 part[3];
-          as_parts<3>(f32x4{p.v[0], p.v[1], p.v[2], p.v[3]}, part);
+          as_parts<3>(__builtin_bit_cast(f32x4, piece(x, i, r0 + i * ROWS, c)), part);
 #pragma unroll
           for (int n = 0; n < 3; ++n)
             *(bf16x4 *)(lds + n * C * ld + (r0 + i * ROWS) * ld + c) = part[n];
