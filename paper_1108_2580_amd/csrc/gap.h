@@ -113,17 +113,73 @@ template <typename Entry> struct Buckets : Table<Entry> {
       return bias[kind(G, gap)];
   }
 };
-// The bucket of two gaps, low <= high, if it is one for both, else -1; the same in all lanes. Lane l looks at
-// bound l.
-template <typename B>
-__device__ __forceinline__ int one_bucket(const B &b, const GapShape &G, int32_t low, int32_t high, int lane) {
-  const int32_t bound = b.bounds[lane];
-  const int at = __popcll(__ballot(bound <= low && lane < G.buckets - 1));
-  return at == __popcll(__ballot(bound <= high && lane < G.buckets - 1)) ? at : -1;
-}
 // Up to this bias a score's largest is as good as the score itself: exponents may take their
 // difference first.
 constexpr float kPlainBias = 16777216.f;
+
+// Lane l's bound and bias: whether two gaps have one bucket takes two comparisons over the wave.
+struct BucketLanes {
+  int32_t bound;
+  float bias;
+  uint64_t plain;  // buckets whose bias is below kPlainBias
+  int last;        // bucket
+  template <typename B> __device__ __forceinline__ void read(const B &b, const GapShape &G, int lane) {
+    bound = b.bounds[lane];
+    bias = b.bias[lane];
+    plain = __ballot(fabsf(bias) < kPlainBias);
+    last = G.buckets - 1;
+  }
+  // of the gaps low <= high; -1: more than one. The same in all lanes.
+  __device__ __forceinline__ int kind(int32_t low, int32_t high) const {
+    const int at = __popcll(__ballot(bound <= low)), to = __popcll(__ballot(bound <= high));
+    return at == to ? (at < last ? at : last) : -1;
+  }
+  __device__ __forceinline__ bool is_plain(int kind) const { return kind >= 0 && (plain >> kind & 1); }
+  __device__ __forceinline__ float bias_of(int kind) const {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(bias), kind < 0 ? 0 : kind));
+  }
+};
+// ---- tiles on their way to LDS ----------------------------------------------------------------
+// Tile (tiles.h) for rows that are whole pieces of 16 bytes: rows past `size` are taken as the last one, since
+// masks leave them out anyway, so that no load has a condition and no register is cleared.
+template <typename T, int C, int WP, bool VEC> struct Staged : Tile<T, C, WP, 256, VEC> {
+  using Base = Tile<T, C, WP, 256, VEC>;
+  using Rows = typename Base::Rows;
+  using Piece = typename Base::Piece;
+  __device__ __forceinline__ void fetch(const Rows &x, int tid) {
+    if constexpr (!VEC) {
+      Base::fetch(x, tid);
+    } else {
+      const int r0 = tid / Base::ROW, c = tid % Base::ROW * Base::E, col = c < x.width ? c : 0;
+#pragma unroll
+      for (int i = 0; i < Base::N; ++i) {
+        const int r = r0 + i * Base::ROWS;
+        this->held[i] = *(const Piece *)x.at(r < x.size ? r : x.size - 1, col);
+      }
+    }
+  }
+  __device__ __forceinline__ void put_parts(bf16 *lds, int ld, const Rows &x, int tid) {
+    if constexpr (VEC) {
+      if (x.width < WP && tid % Base::ROW * Base::E >= x.width) {
+#pragma unroll
+        for (int i = 0; i < Base::N; ++i) this->held[i] = Piece{0, 0, 0, 0};
+      }
+    }
+    Base::put_parts(lds, ld, x, tid);
+  }
+  // Whether what is held has infinities or NaN (columns past the width may be anything).
+  __device__ __forceinline__ bool nonfinite() const {
+    constexpr uint32_t mask = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;  // exponents; all ones carry
+    constexpr uint32_t one = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
+    constexpr uint32_t carry = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < Base::N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (this->held[i][e] & mask) + one;
+    return (any & carry) != 0;
+  }
+};
 
 // ---- fragments of a row in global memory ---------------------------------------------------------
 // 8 values from column c of the row at p as they lie there, zero past `width`.
@@ -214,12 +270,17 @@ __device__ __forceinline__ float with_rest(bf16 x, int16_t rest) {
 
 // Over the lanes of a column (lane & 15): the sum or the largest. The swaps give each lane both halves of a
 // pair of rows of lanes, then of the wave, without a way through LDS.
+__device__ __forceinline__ float larger(uint32_t a, uint32_t b) {  // without a first pass for signalling NaNs
+  float x;
+  asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(a), "v"(b));
+  return x;
+}
 __device__ __forceinline__ float column_max(float x) {
   const uint32_t a = __float_as_uint(x);
   const auto y = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  const uint32_t b = __float_as_uint(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+  const uint32_t b = __float_as_uint(larger(y[0], y[1]));
   const auto z = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+  return larger(z[0], z[1]);
 }
 __device__ __forceinline__ float column_sum(float x) {
   x += __shfl_xor(x, 16);
@@ -237,47 +298,35 @@ __device__ __forceinline__ int wave_max(int x) {
 }
 
 // A tile of which a mask leaves some places has weights of zero in the others, which an infinity or NaN there
-// would turn into NaN. So such tiles' rows are looked at, and where one is met the product is formed one row
-// at a time over the places that are left.
-// Whether 32 rows of x in LDS, 16 C wide, are finite (of parts, the first tells).
-template <int C> __device__ __forceinline__ bool finite_rows(const bf16 *x, int ld, int lane) {
+// would turn into NaN. Where such a tile's rows have any, they are summed by weight without those values, and
+// the sums that do read them become NaN at the end.
+template <int NP> __device__ __forceinline__ Frag<NP> cleaned(Frag<NP> f) {
   using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
-  uint32_t carry = 0;  // into either half's sign: its exponent was all ones
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const u32x4 bits = __builtin_bit_cast(u32x4, frag_col<1, 4>(x + c * 16, ld, 0, lane).p[0]);
+  for (int n = 0; n < NP; ++n) {
+    u32x4 x = __builtin_bit_cast(u32x4, f.p[n]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) carry |= (bits[e] & 0x7fff7fffu) + 0x00800080u;
+    for (int e = 0; e < 4; ++e)
+      x[e] &= ~(((((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu);
+    f.p[n] = __builtin_bit_cast(bf16x8, x);
   }
-  return !__any((carry & 0x80008000u) != 0);
+  return f;
 }
-// to[c] += rows 16 c + 4 g .. 4 g + 3 of x^T W, g the lane's group, for 32 rows of x in LDS and W as MFMA leaves
-// it (two tiles; a lane: column lane & 15, rows 4 g .. 4 g + 3), over the places of the lane's column that
-// ok(row) leaves.
-template <int NP, int C, typename OK>
-__device__ __forceinline__ void add_rows(const f32x4 *w, const bf16 *x, int ld, int part, int lane, OK ok,
-                                         f32x4 *to) {
+// x: rows `lo` to `hi` are looked at, `ok(row)` tells what the lane's column reads. to[c]: columns 16 c + 4 g
+// onwards, g the lane's group.
+template <typename T, int C, typename OK>
+__device__ __forceinline__ void mark_read(const T *x, int64_t stride, int width, int lo, int hi, int lane, OK ok,
+                                          f32x4 *to) {
 #pragma unroll 1
-  for (int r = 0; r < 32; ++r) {
-    float weight = 0.f;
+  for (int r = lo; r < hi; ++r) {
+    const T *p = x + r * stride + (lane >> 4) * 4;
+    if (!ok(r)) continue;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (r / 16 == t && r % 4 == e) weight = w[t][e];
-    weight = __shfl(weight, r % 16 / 4 * 16 + (lane & 15));
-    if (ok(r)) {
-      const bf16 *p = x + r * ld + (lane >> 4) * 4;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = 0.f;
-#pragma unroll
-          for (int n = NP - 1; n >= 0; --n) v += (float)p[n * part + c * 16 + e];
-          to[c][e] = fmaf(weight, v, to[c][e]);
-        }
-    }
+        if (c * 16 + (lane >> 4) * 4 + e < width && (float)p[c * 16 + e] * 0.f != 0.f)
+          to[c][e] = __builtin_nanf("");
   }
 }
 

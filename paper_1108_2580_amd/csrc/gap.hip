@@ -42,17 +42,17 @@ struct ReadArgs {
 
 template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 32; }
 // Columns of 16 queries a wave.
-template <typename T> constexpr int query_tiles() { return sizeof(T) == 2 ? 2 : 1; }
+template <typename T> constexpr int query_tiles() { return 1; }
 
 template <typename T, int D, bool VEC, typename Entry>
-__global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 : 4) void k_gap_read(ReadArgs A) {
   constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
-  using Staged = Tile<T, KN, D, 256, VEC>;
+  using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
   __shared__ __align__(16) bf16 lv[NP * PART];
   __shared__ __align__(16) int32_t lpos[KN];
-  __shared__ int32_t lrange[2];
+  __shared__ int32_t lrange[2], lbad;
   __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
@@ -64,17 +64,20 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   const int64_t t0 = tile * BQ;
 
   lb.start(G, head, tid);
+  if (tid == 0) lbad = -1;
   // the block's keys: from its first row's first token to its last token that has a row
-  int span_first[QT], block_first = kNoRow, block_last = -1;
+  int span_first[QT], block_first = kNoRow, block_last = -1, rows_first = 0;
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
     const int64_t t = t0 + n * 64 + lane;
     span_first[n] = span_of(G, A.spans, t).first;
     block_first = min(block_first, span_first[n]);
+    rows_first = max(rows_first, span_first[n]);  // the last row's
     if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
   }
   block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
   block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
+  rows_first = __builtin_amdgcn_readfirstlane(wave_max(rows_first));
   if (block_last < 0) return;
 
   // this wave's queries, one a lane and tile
@@ -115,22 +118,25 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
   const char *v = (const char *)((const T *)A.v.data + head / G.group * A.v.head_stride);
   const int64_t k_row = A.k.token_stride * (int)sizeof(T), v_row = A.v.token_stride * (int)sizeof(T);
-  Staged hk, hv;
+  Tiles hk, hv;
   int hpos = 0;
   const auto rows_of = [&](const char *x, int64_t bytes, int k0) {
-    return typename Staged::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
+    return typename Tiles::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
                                  block_last + 1 - k0 < KN ? block_last + 1 - k0 : KN, G.width};
   };
   const auto fetch = [&](int k0) {
     hk.fetch(rows_of(k, k_row, k0), tid);
     hv.fetch(rows_of(v, v_row, k0), tid);
-    if (wave == 0) hpos = G.positions[min(k0 + lane % KN, block_last)];
+    if (wave == 0) hpos = G.positions[min(k0 + (lane & (KN - 1)), block_last)];
   };
   fetch(block_first);
   __syncthreads();
   lb.fill(G, wave, lane);
+  BucketLanes bl;
+  bl.read(lb, G, lane);
 
   f32x4 o[QT][DT];
+  int bad_lo = 0, bad_hi = 0;  // keys among which some values were left out
   float top[QT], base[QT], sum[QT];
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
@@ -142,9 +148,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
     // addresses are formed anew in each tile: held across tiles they would cost a block its place on the CU
-    asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));
+    asm volatile("" : "+v"(tid));
+    tid &= 255;
+    lane = tid & 63;
+    g = lane >> 4;
     __syncthreads();
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
+    const bool masked = k0 + KN - 1 > (int)t0 || k0 < rows_first;  // for some query of the block
+    if (masked && hv.nonfinite()) lbad = k0;
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
     if (wave == 0) {
       const int lo = wave_min(hpos), hi = wave_max(hpos);
@@ -155,8 +166,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
       }
     }
     __syncthreads();
+    const bool bad = masked && __builtin_amdgcn_readfirstlane(lbad) == k0;
+    if (bad) {
+      bad_lo = bad_hi ? bad_lo : k0;
+      bad_hi = min(k0 + KN, block_last + 1);
+    }
     if (k0 + KN <= block_last) fetch(k0 + KN);
     if (k0 > last || k0 + KN <= first_min) continue;
+    __builtin_amdgcn_sched_barrier(0);
 
     const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
     f32x4 s[QT][KT];
@@ -173,10 +190,59 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
     }
 
     // one bucket for the tile's gaps, or one for each
-    const int kind = one_bucket(lb, G, gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]), lane);
-    const float b = kind >= 0 ? lb.bias[kind] : 0.f;
-    const bool plain = kind >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
-    float most[QT];
+    const int kind = bl.kind(gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]));
+    const float b = bl.bias_of(kind);
+    const bool plain = bl.is_plain(kind) && !partial;
+
+    // The largest score so far is followed only where it has grown by 8: exponentials up to 2^8 keep
+    // their precision, and most tiles leave the sums as they are.
+    const auto follow = [&](float *most) {
+      bool grown = false;
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        most[n] = column_max(most[n]);
+        grown = grown || most[n] > top[n] + 8.f;
+      }
+      if (__any(grown)) {
+#pragma unroll
+        for (int n = 0; n < QT; ++n) {
+          const bool none = top[n] == -__builtin_inff();  // so far: there is nothing to scale
+          top[n] = fmaxf(top[n], most[n]);
+          const float next = top[n] == -__builtin_inff() ? 0.f : top[n];
+          const float factor = none ? 0.f : exp2_fast(base[n] - next);
+          base[n] = next;
+          sum[n] *= factor;
+#pragma unroll
+          for (int c = 0; c < DT; ++c) o[n][c] *= factor;
+        }
+      }
+    };
+    // s -> 2^(by s + shift), of 32 keys, as operands
+    const auto weigh = [&](int w, float by, const float *shift, Frag<RP> *pf) {
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+#pragma unroll
+        for (int t = 2 * w; t < 2 * w + 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = exp2_fast(fmaf(s[n][t][e], by, shift[n]));
+            s[n][t][e] = x;
+            sum[n] += x;
+          }
+        asm("" : "+v"(sum[n]));  // now: put off, the sums would hold the weights' registers
+        pf[n] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
+      }
+    };
+    const auto add_values = [&](int w, bool bad, const Frag<RP> *pf) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        Frag<NP> vf = frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane);
+        if (bad) vf = cleaned(vf);
+#pragma unroll
+        for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n], o[n][c]);
+      }
+    };
+    float most[QT], shift[QT];
     if (plain) {
 #pragma unroll
       for (int n = 0; n < QT; ++n) {
@@ -186,6 +252,16 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) most[n] = fmaxf(most[n], s[n][t][e]);
         most[n] = fmaf(most[n], scale, b);
+      }
+      follow(most);
+#pragma unroll
+      for (int n = 0; n < QT; ++n) shift[n] = b - base[n];
+#pragma unroll
+      for (int w = 0; w < KS; ++w) {
+        Frag<RP> pf[QT];
+        weigh(w, scale, shift, pf);
+        add_values(w, false, pf);
+        __builtin_amdgcn_sched_barrier(0);
       }
     } else {
       const auto biased = [&](auto bias_of) {
@@ -208,66 +284,22 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
               s[n][t][e] = x;
               most[n] = fmaxf(most[n], x);
             }
+          __builtin_amdgcn_sched_barrier(0);
         }
       };
       if (kind >= 0)
         biased([&](int) { return b; });
       else
         biased([&](int gap) { return lb.bias_of(G, gap); });
-    }
-
-    // The largest score so far is followed only where it has grown by 8: exponentials up to 2^8 keep
-    // their precision, and most tiles leave the sums as they are.
-    bool grown = false;
+      follow(most);
 #pragma unroll
-    for (int n = 0; n < QT; ++n) {
-      most[n] = column_max(most[n]);
-      grown = grown || most[n] > top[n] + 8.f;
-    }
-    if (__any(grown)) {
+      for (int n = 0; n < QT; ++n) shift[n] = -base[n];
 #pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        const bool none = top[n] == -__builtin_inff();  // so far: there is nothing to scale
-        top[n] = fmaxf(top[n], most[n]);
-        const float next = top[n] == -__builtin_inff() ? 0.f : top[n];
-        const float factor = none ? 0.f : exp2_fast(base[n] - next);
-        base[n] = next;
-        sum[n] *= factor;
-#pragma unroll
-        for (int c = 0; c < DT; ++c) o[n][c] *= factor;
-      }
-    }
-
-#pragma unroll
-    for (int w = 0; w < KS; ++w) {  // 32 keys at a time
-      __builtin_amdgcn_sched_barrier(0);
-      const bf16 *wv = lv + w * 32 * LD;
-      Frag<RP> pf[QT];
-#pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        const float by = plain ? scale : 1.f, shift = plain ? b - base[n] : -base[n];
-#pragma unroll
-        for (int t = 2 * w; t < 2 * w + 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = exp2_fast(fmaf(s[n][t][e], by, shift));
-            s[n][t][e] = x;
-            sum[n] += x;
-          }
-        pf[n] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
-      }
-      if (!partial || finite_rows<DT>(wv, LD, lane)) {
-#pragma unroll
-        for (int c = 0; c < DT; ++c) {
-          const Frag<NP> vf = frag_col<NP, 4>(wv + c * 16, LD, PART, lane);
-#pragma unroll
-          for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n], o[n][c]);
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < QT; ++n)
-          add_rows<NP, DT>(s[n] + 2 * w, wv, LD, PART, lane,
-                           [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, o[n]);
+      for (int w = 0; w < KS; ++w) {
+        Frag<RP> pf[QT];
+        weigh(w, 1.f, shift, pf);
+        add_values(w, bad, pf);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -276,6 +308,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
   for (int n = 0; n < QT; ++n) {
     const float total = column_sum(sum[n]);
     if (first[n] == kNoRow) continue;
+    if (bad_hi)
+      mark_read<T, DT>((const T *)v, A.v.token_stride, G.width, bad_lo, bad_hi, lane,
+                       [&](int j) { return (unsigned)(j - first[n]) <= before[n]; }, o[n]);
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
 #pragma unroll
@@ -299,7 +334,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_read(ReadArgs A) {
 template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStream_t s) {
   constexpr int BQ = 64 * query_tiles<T>();
   // a table of biases, where it leaves a CU two blocks
-  using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, float>::type;
+  using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, uint8_t>::type;
   A.n_tiles = (A.G.n_tokens + BQ - 1) / BQ;
   const int64_t per = max_blocks(256) / A.G.heads;
   for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {

@@ -57,11 +57,11 @@ template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   constexpr int KN = tile_tokens<T>(), QT = columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
-  using Staged = Tile<T, KN, D, 256, VEC>;
+  using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
   __shared__ __align__(16) bf16 lv[NP * PART];
   __shared__ __align__(16) int32_t lpos[KN];
-  __shared__ int32_t lrange[2];
+  __shared__ int32_t lrange[2], lbad;
   __shared__ Buckets<Entry> lb;
   extern __shared__ float lsums[];  // [waves, buckets, kColumns]
 
@@ -73,17 +73,20 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   const int64_t t0 = tile * BQ;
 
   lb.start(G, head, tid);
+  if (tid == 0) lbad = -1;
   for (int n = tid; n < 4 * G.buckets * kColumns; n += 256) lsums[n] = 0.f;
-  int span_first[QT], block_first = kNoRow, block_last = -1;
+  int span_first[QT], block_first = kNoRow, block_last = -1, rows_first = 0;
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
     const int64_t t = t0 + n * 64 + lane;
     span_first[n] = span_of(G, A.spans, t).first;
     block_first = min(block_first, span_first[n]);
+    rows_first = max(rows_first, span_first[n]);
     if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
   }
   block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
   block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
+  rows_first = __builtin_amdgcn_readfirstlane(wave_max(rows_first));
   float *parts = A.dbias_parts + (int64_t)head * G.buckets * A.n_tiles + tile;
   if (block_last < 0) {
     if (tid < G.buckets) parts[tid * A.n_tiles] = 0.f;
@@ -155,20 +158,22 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
   const char *v = (const char *)((const T *)A.v.data + head / G.group * A.v.head_stride);
   const int64_t k_row = A.k.token_stride * (int)sizeof(T), v_row = A.v.token_stride * (int)sizeof(T);
-  Staged hk, hv;
+  Tiles hk, hv;
   int hpos = 0;
   const auto rows_of = [&](const char *x, int64_t bytes, int k0) {
-    return typename Staged::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
+    return typename Tiles::Rows{x + k0 * bytes, (uint32_t)bytes, 0,
                                  block_last + 1 - k0 < KN ? block_last + 1 - k0 : KN, G.width};
   };
   const auto fetch = [&](int k0) {
     hk.fetch(rows_of(k, k_row, k0), tid);
     hv.fetch(rows_of(v, v_row, k0), tid);
-    if (wave == 0) hpos = G.positions[min(k0 + lane % KN, block_last)];
+    if (wave == 0) hpos = G.positions[min(k0 + (lane & (KN - 1)), block_last)];
   };
   fetch(block_first);
   __syncthreads();
   lb.fill(G, wave, lane);
+  BucketLanes bl;
+  bl.read(lb, G, lane);
 
   f32x4 dq[QT][DT];
 #pragma unroll
@@ -181,6 +186,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
   for (int n = 0; n < QT; ++n) run[n] = 0.f;
   int run_kind = 0;
+  int bad_lo = 0, bad_hi = 0;  // keys among which some values were left out
   const auto end_run = [&]() {
     float sum = 0.f;
 #pragma unroll
@@ -193,8 +199,13 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
     // addresses are formed anew in each tile: held across tiles they cost registers
-    asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));
+    asm volatile("" : "+v"(tid));
+    tid &= 255;
+    lane = tid & 63;
+    g = lane >> 4;
     __syncthreads();
+    const bool masked = k0 + KN - 1 > (int)t0 || k0 < rows_first;
+    if (masked && hk.nonfinite()) lbad = k0;
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
     if (wave == 0) {
@@ -206,13 +217,18 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       }
     }
     __syncthreads();
+    const bool bad = masked && __builtin_amdgcn_readfirstlane(lbad) == k0;
+    if (bad) {
+      bad_lo = bad_hi ? bad_lo : k0;
+      bad_hi = min(k0 + KN, block_last + 1);
+    }
     if (k0 + KN <= block_last) fetch(k0 + KN);
     if (k0 > last || k0 + KN <= first_min) continue;
 
     const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
-    const int one = one_bucket(lb, G, gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]), lane);
-    const float b = one >= 0 ? lb.bias[one] : 0.f;
-    const bool plain = one >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+    const int one = bl.kind(gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]));
+    const float b = bl.bias_of(one);
+    const bool plain = bl.is_plain(one) && !partial;
     if (one >= 0 && one != run_kind) {
       end_run();
       run_kind = one;
@@ -296,18 +312,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       Frag<RP> df[QT];
 #pragma unroll
       for (int n = 0; n < QT; ++n) df[n] = as_frag<RP>(s[n][0], s[n][1]);
-      if (!partial || finite_rows<DT>(wk, LD, lane)) {
 #pragma unroll
-        for (int c = 0; c < DT; ++c) {
-          const Frag<NP> kf = frag_col<NP, 4>(wk + c * 16, LD, PART, lane);
+      for (int c = 0; c < DT; ++c) {
+        Frag<NP> kf = frag_col<NP, 4>(wk + c * 16, LD, PART, lane);
+        if (bad) kf = cleaned(kf);
 #pragma unroll
-          for (int n = 0; n < QT; ++n) dq[n][c] = mma(kf, df[n], dq[n][c]);
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < QT; ++n)
-          add_rows<NP, DT>(s[n], wk, LD, PART, lane,
-                           [&](int r) { return (unsigned)(k0 + w * 32 + r - first[n]) <= before[n]; }, dq[n]);
+        for (int n = 0; n < QT; ++n) dq[n][c] = mma(kf, df[n], dq[n][c]);
       }
     }
   }
@@ -315,6 +325,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
     if (first[n] == kNoRow) continue;
+    if (bad_hi)
+      mark_read<T, DT>((const T *)k, A.k.token_stride, G.width, bad_lo, bad_hi, lane,
+                       [&](int j) { return (unsigned)(j - first[n]) <= before[n]; }, dq[n]);
     const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
@@ -358,12 +371,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   // A query's factor of the weights goes into the exponent: good for 2^-21, which bf16 does not see, and a
   // product less a weight.
   constexpr bool LOG = sizeof(T) == 2;
-  using Staged = Tile<T, QN, D, 256, VEC>;
+  using Tiles = Staged<T, QN, D, VEC>;
   __shared__ __align__(16) bf16 lq[NP * PART];
   __shared__ __align__(16) bf16 lo[NP * PART];
   __shared__ __align__(16) int32_t lpos[QN];
   __shared__ __align__(16) float ltop[QN], linv[QN], ldelta[QN];
-  __shared__ int32_t lrange[2];
+  __shared__ int32_t lrange[2], lbad;
   __shared__ Buckets<Entry> lb;
 
   const GapShape &G = A.G;
@@ -374,16 +387,18 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   const int64_t t0 = (A.tile0 + blockIdx.x / (unsigned)k_heads) * BK;
 
   // the block's queries: from its first token that has a row to its last row's end
-  int span_end[CT], block_first = kNoRow, block_end = 0;
+  int span_end[CT], block_first = kNoRow, block_end = 0, rows_end = kNoRow;
 #pragma unroll
   for (int n = 0; n < CT; ++n) {
     const int64_t t = t0 + n * 64 + lane;
     span_end[n] = span_of(G, A.spans, t).end;
     if (span_end[n] > 0) block_first = min(block_first, (int)t);
     block_end = max(block_end, span_end[n]);
+    rows_end = min(rows_end, span_end[n]);  // the first row's
   }
   block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
   block_end = __builtin_amdgcn_readfirstlane(wave_max(block_end));
+  rows_end = __builtin_amdgcn_readfirstlane(wave_min(rows_end));
   if (block_end == 0) return;
 
   // this wave's keys, one a lane and tile
@@ -429,27 +444,29 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 
   for (int head = k_head * G.group; head < (k_head + 1) * G.group; ++head) {
     __syncthreads();
+    if (tid == 0) lbad = -1;
+    int bad_lo = 0, bad_hi = 0;  // queries among which some values were left out
     lb.start(G, head, tid);
-    if (Buckets<Entry>::DIRECT || head == k_head * G.group) {
-      __syncthreads();
-      lb.fill(G, wave, lane);
-    }
+    __syncthreads();
+    if (Buckets<Entry>::DIRECT || head == k_head * G.group) lb.fill(G, wave, lane);
+    BucketLanes bl;
+    bl.read(lb, G, lane);
     const char *q = (const char *)((const T *)A.q.data + head * A.q.head_stride);
     const char *o = (const char *)((const T *)A.d_out.data + head * A.d_out.head_stride);
     const float *stats = A.stats + (int64_t)head * G.n_tokens;
     const float *inv_stats = stats + (int64_t)G.heads * G.n_tokens;
     const float *deltas = A.delta + (int64_t)head * G.n_tokens;
-    Staged hq, ho;
+    Tiles hq, ho;
     int hpos = 0;
     float hstat = 0.f;
     const auto rows_of = [&](const char *x, int64_t bytes, int q0) {
-      return typename Staged::Rows{x + q0 * bytes, (uint32_t)bytes, 0,
+      return typename Tiles::Rows{x + q0 * bytes, (uint32_t)bytes, 0,
                                    block_end - q0 < QN ? block_end - q0 : QN, G.width};
     };
     const auto fetch = [&](int q0) {
       hq.fetch(rows_of(q, q_row, q0), tid);
       ho.fetch(rows_of(o, o_row, q0), tid);
-      const int t = min(q0 + lane % QN, block_end - 1);
+      const int t = min(q0 + (lane & (QN - 1)), block_end - 1);
       if (wave == 0) hpos = G.positions[t];
       if (wave == 1) hstat = stats[t];
       if (wave == 2) hstat = LOG ? __log2f(inv_stats[t]) : inv_stats[t];
@@ -458,8 +475,13 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
     fetch(block_first);
 
     for (int q0 = block_first; q0 < block_end; q0 += QN) {
-      asm volatile("" : "+v"(lane), "+v"(tid), "+v"(g));  // as above
+      asm volatile("" : "+v"(tid));  // as above
+      tid &= 255;
+      lane = tid & 63;
+      g = lane >> 4;
       __syncthreads();
+      const bool masked = q0 < (int)t0 + BK - 1 || q0 + QN > rows_end;  // for some key of the block
+      if (masked && (hq.nonfinite() || ho.nonfinite())) lbad = q0;
       hq.put_parts(lq, LD, rows_of(q, q_row, q0), tid);
       ho.put_parts(lo, LD, rows_of(o, o_row, q0), tid);
       if (wave == 0) {
@@ -473,13 +495,18 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
         (wave == 1 ? ltop : wave == 2 ? linv : ldelta)[lane] = hstat;
       }
       __syncthreads();
+      const bool bad = masked && __builtin_amdgcn_readfirstlane(lbad) == q0;
+      if (bad) {
+        bad_lo = bad_hi ? bad_lo : q0;
+        bad_hi = min(q0 + QN, block_end);
+      }
       if (q0 + QN < block_end) fetch(q0 + QN);
       if (q0 + QN <= j0 || q0 >= end_max) continue;
 
       const bool partial = q0 < j0 + 16 * CT - 1 || q0 + QN > end_min;
-      const int one = one_bucket(lb, G, gap_of(lrange[0], pos_max), gap_of(lrange[1], pos_min), lane);
-      const float b = one >= 0 ? lb.bias[one] : 0.f;
-      const bool plain = one >= 0 && !partial && __builtin_amdgcn_readfirstlane(fabsf(b) < kPlainBias);
+      const int one = bl.kind(gap_of(lrange[0], pos_max), gap_of(lrange[1], pos_min));
+      const float b = bl.bias_of(one);
+      const bool plain = bl.is_plain(one) && !partial;
 #pragma unroll 1
       for (int w = 0; w < QS; ++w) {  // 32 queries at a time
         const bf16 *wq = lq + w * 32 * LD, *wo = lo + w * 32 * LD;
@@ -549,25 +576,28 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
           pf[n] = as_frag<RP>(s[n][0], s[n][1]);
           df[n] = as_frag<RP>(dp[n][0], dp[n][1]);
         }
-        if (!partial || (finite_rows<DT>(wo, LD, lane) && finite_rows<DT>(wq, LD, lane))) {
 #pragma unroll
-          for (int c = 0; c < DT; ++c) {
-            const Frag<NP> of = frag_col<NP, 4>(wo + c * 16, LD, PART, lane);
-            const Frag<NP> qf = frag_col<NP, 4>(wq + c * 16, LD, PART, lane);
-#pragma unroll
-            for (int n = 0; n < CT; ++n) {
-              dv[n][c] = mma(of, pf[n], dv[n][c]);
-              dk[n][c] = mma(qf, df[n], dk[n][c]);
-            }
+        for (int c = 0; c < DT; ++c) {
+          Frag<NP> of = frag_col<NP, 4>(wo + c * 16, LD, PART, lane);
+          Frag<NP> qf = frag_col<NP, 4>(wq + c * 16, LD, PART, lane);
+          if (bad) {
+            of = cleaned(of);
+            qf = cleaned(qf);
           }
-        } else {
 #pragma unroll
           for (int n = 0; n < CT; ++n) {
-            const auto ok = [&](int r) { return (unsigned)(q0 + w * 32 + r - at[n]) < after[n]; };
-            add_rows<NP, DT>(s[n], wo, LD, PART, lane, ok, dv[n]);
-            add_rows<NP, DT>(dp[n], wq, LD, PART, lane, ok, dk[n]);
+            dv[n][c] = mma(of, pf[n], dv[n][c]);
+            dk[n][c] = mma(qf, df[n], dk[n][c]);
           }
         }
+      }
+    }
+    if (bad_hi) {
+#pragma unroll
+      for (int n = 0; n < CT; ++n) {
+        const auto ok = [&](int i) { return (unsigned)(i - at[n]) < after[n]; };
+        mark_read<T, DT>((const T *)o, A.d_out.token_stride, G.width, bad_lo, bad_hi, lane, ok, dv[n]);
+        mark_read<T, DT>((const T *)q, A.q.token_stride, G.width, bad_lo, bad_hi, lane, ok, dk[n]);
       }
     }
   }
