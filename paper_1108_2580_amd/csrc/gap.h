@@ -47,9 +47,9 @@ __device__ __forceinline__ int32_t gap_of(int32_t a, int32_t b) { return __built
 
 // ---- buckets --------------------------------------------------------------------------------------
 // The bucket of a gap is the number of bounds at it or below. Where the last bound is below kTableGaps a table
-// in LDS holds for each gap the bias itself (Entry float: one read a score) or the bucket (uint8_t: a quarter of
+// in LDS holds for each gap the bias itself (Entry float: one read a score) or the bucket (uint8_t, times four: a quarter of
 // the LDS, and a second read for the bias, whose 64 places are 64 banks); larger bounds are searched (Entry void).
-constexpr int kTableGaps = 8192;
+constexpr int kTableGaps = 7680;
 constexpr float kLargest = 3.402823466e38f;
 
 // A bias as scores take it: times log2 e, finite where it was.
@@ -90,27 +90,31 @@ template <typename Entry> struct Buckets : Table<Entry> {
           const float x = bias[b];
           for (int g = lo + lane; g < hi; g += 64) this->of[g] = x;
         } else {
-          for (int g = lo + lane; g < hi; g += 64) this->of[g] = (uint8_t)b;
+          for (int g = lo + lane; g < hi; g += 64) this->of[g] = (uint8_t)(b * 4);
         }
       }
     }
   }
+  // within [0, last_bound], in one instruction
   __device__ __forceinline__ int clipped(const GapShape &G, int32_t gap) const {
-    const int g = gap < G.last_bound ? gap : G.last_bound;
-    return g > 0 ? g : 0;
+    int g;
+    asm("v_med3_i32 %0, %1, 0, %2" : "=v"(g) : "v"(gap), "s"(G.last_bound));
+    return g;
   }
-  // not of a DIRECT table's scores, whose bias comes without it
-  __device__ __forceinline__ int kind(const GapShape &G, int32_t gap) const {
-    if constexpr (SEARCHED || DIRECT)
-      return bucket_of(bounds, G.buckets, gap);
+  // four times the bucket (not of a DIRECT table, whose biases come without it), and its bias
+  __device__ __forceinline__ int kind4(const GapShape &G, int32_t gap) const {
+    static_assert(!DIRECT, "a table of biases");
+    if constexpr (SEARCHED)
+      return 4 * bucket_of(bounds, G.buckets, gap);
     else
       return this->of[clipped(G, gap)];
   }
+  __device__ __forceinline__ float bias4(int kind4) const { return *(const float *)((const char *)bias + kind4); }
   __device__ __forceinline__ float bias_of(const GapShape &G, int32_t gap) const {
     if constexpr (DIRECT)
       return this->of[clipped(G, gap)];
     else
-      return bias[kind(G, gap)];
+      return bias4(kind4(G, gap));
   }
 };
 // Up to this bias a score's largest is as good as the score itself: exponents may take their

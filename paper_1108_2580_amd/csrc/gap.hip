@@ -264,33 +264,27 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      const auto biased = [&](auto bias_of) {
 #pragma unroll
-        for (int n = 0; n < QT; ++n) most[n] = -__builtin_inff();
+      for (int n = 0; n < QT; ++n) most[n] = -__builtin_inff();
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          const i32x4 kpos = *(const i32x4 *)(lpos + t * 16 + g * 4);
-          f32x4 add[QT];
+      for (int t = 0; t < KT; ++t) {
+        const i32x4 kpos = *(const i32x4 *)(lpos + t * 16 + g * 4);
+        f32x4 add[QT];
 #pragma unroll
-          for (int n = 0; n < QT; ++n)
+        for (int n = 0; n < QT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add[n][e] = bias_of(gap_of(pos[n], kpos[e]));
+          for (int e = 0; e < 4; ++e) add[n][e] = lb.bias_of(G, gap_of(pos[n], kpos[e]));
 #pragma unroll
-          for (int n = 0; n < QT; ++n)
+        for (int n = 0; n < QT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const bool kept = (unsigned)(k0 + t * 16 + g * 4 + e - first[n]) <= before[n];
-              const float x = kept ? fmaf(s[n][t][e], scale, add[n][e]) : -__builtin_inff();
-              s[n][t][e] = x;
-              most[n] = fmaxf(most[n], x);
-            }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      };
-      if (kind >= 0)
-        biased([&](int) { return b; });
-      else
-        biased([&](int gap) { return lb.bias_of(G, gap); });
+          for (int e = 0; e < 4; ++e) {
+            const bool kept = (unsigned)(k0 + t * 16 + g * 4 + e - first[n]) <= before[n];
+            const float x = kept ? fmaf(s[n][t][e], scale, add[n][e]) : -__builtin_inff();
+            s[n][t][e] = x;
+            most[n] = fmaxf(most[n], x);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
       follow(most);
 #pragma unroll
       for (int n = 0; n < QT; ++n) shift[n] = -base[n];

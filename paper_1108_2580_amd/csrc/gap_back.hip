@@ -33,7 +33,9 @@ struct BackArgs {
 };
 
 template <typename T> constexpr int tile_tokens() { return sizeof(T) == 2 ? 64 : 32; }
-template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 && D < 128 ? 2 : 1; }
+// Columns of 16 queries (keys) a wave.
+template <typename T, int D> constexpr int query_columns() { return sizeof(T) == 2 && D < 128 ? 2 : 1; }
+template <typename T, int D> constexpr int key_columns() { return 1; }
 
 // ---- over keys: dq and dbias ---------------------------------------------------------------------
 
@@ -43,19 +45,19 @@ template <typename T, int D> constexpr int columns() { return sizeof(T) == 2 && 
 // ones before it give the same place, so that the last write to a place has all of them.
 constexpr int kColumns = 64;
 
-__device__ __forceinline__ void add_sums(float *column, i32x4 kind, f32x4 x) {
-  x[1] += kind[1] == kind[0] ? x[0] : 0.f;
-  x[2] += kind[2] == kind[1] ? x[1] : kind[2] == kind[0] ? x[0] : 0.f;
-  x[3] += kind[3] == kind[2] ? x[2] : kind[3] == kind[1] ? x[1] : kind[3] == kind[0] ? x[0] : 0.f;
+__device__ __forceinline__ void add_sums(float *column, i32x4 kind4, f32x4 x) {
+  x[1] += kind4[1] == kind4[0] ? x[0] : 0.f;
+  x[2] += kind4[2] == kind4[1] ? x[1] : kind4[2] == kind4[0] ? x[0] : 0.f;
+  x[3] += kind4[3] == kind4[2] ? x[2] : kind4[3] == kind4[1] ? x[1] : kind4[3] == kind4[0] ? x[0] : 0.f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] += column[kind[e] * kColumns];
+  for (int e = 0; e < 4; ++e) x[e] += column[kind4[e] * (kColumns / 4)];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) column[kind[e] * kColumns] = x[e];
+  for (int e = 0; e < 4; ++e) column[kind4[e] * (kColumns / 4)] = x[e];
 }
 
 template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
-  constexpr int KN = tile_tokens<T>(), QT = columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+  constexpr int KN = tile_tokens<T>(), QT = query_columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
   using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
     const int one = bl.kind(gap_of(pos_min, lrange[1]), gap_of(pos_max, lrange[0]));
     const float b = bl.bias_of(one);
     const bool plain = bl.is_plain(one) && !partial;
-    if (one >= 0 && one != run_kind) {
+    if (plain && one != run_kind) {
       end_run();
       run_kind = one;
     }
@@ -240,7 +242,10 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int n = 0; n < QT; ++n) s[n][t] = dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < QT; ++n) {
+          s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f} - delta[n];  // do . v - delta is what is asked for
+        }
 #pragma unroll
         for (int d = 0; d < DF; ++d) {
           const Frag<NP> kf = frag_row<NP>(wk + t * 16 * LD + d * 32, LD, PART, lane);
@@ -261,29 +266,27 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float p = exp2_fast(fmaf(s[n][t][e], scale, shift));
-              s[n][t][e] = p * (dp[n][t][e] - delta[n]);
+              s[n][t][e] = p * dp[n][t][e];
               run[n] += s[n][t][e];
             }
         }
       } else {
         i32x4 kind[QT][2];
         f32x4 add[QT][2];
-        if (one < 0) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const i32x4 kpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
+        for (int t = 0; t < 2; ++t) {
+          const i32x4 kpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
 #pragma unroll
-            for (int n = 0; n < QT; ++n)
+          for (int n = 0; n < QT; ++n)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) kind[n][t][e] = lb.kind(G, gap_of(pos[n], kpos[e]));
-          }
+            for (int e = 0; e < 4; ++e) kind[n][t][e] = lb.kind4(G, gap_of(pos[n], kpos[e]));
         }
 #pragma unroll
         for (int n = 0; n < QT; ++n)
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add[n][t][e] = one >= 0 ? b : lb.bias[kind[n][t][e]];
+            for (int e = 0; e < 4; ++e) add[n][t][e] = lb.bias4(kind[n][t][e]);
 #pragma unroll
         for (int n = 0; n < QT; ++n)
 #pragma unroll
@@ -292,22 +295,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
             for (int e = 0; e < 4; ++e) {
               const float p = exp2_fast(fmaf(s[n][t][e], scale, add[n][t][e]) - top[n]);
               const bool kept = (unsigned)(k0 + w * 32 + t * 16 + g * 4 + e - first[n]) <= before[n];
-              s[n][t][e] = kept ? p * (dp[n][t][e] - delta[n]) : 0.f;
+              s[n][t][e] = kept ? p * dp[n][t][e] : 0.f;
             }
-        if (one >= 0) {
 #pragma unroll
-          for (int n = 0; n < QT; ++n)
+        for (int n = 0; n < QT; ++n)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) run[n] += s[n][t][e];
-        } else {
-#pragma unroll
-          for (int n = 0; n < QT; ++n)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-              add_sums(sums, kind[n][t], s[n][t] * inv[n]);
-        }
+          for (int t = 0; t < 2; ++t) add_sums(sums, kind[n][t], s[n][t] * inv[n]);
       }
       Frag<RP> df[QT];
 #pragma unroll
@@ -366,7 +359,7 @@ __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ par
 
 template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
-  constexpr int QN = tile_tokens<T>(), CT = columns<T, D>(), BK = 64 * CT, LD = D + 16, PART = QN * LD;
+  constexpr int QN = tile_tokens<T>(), CT = key_columns<T, D>(), BK = 64 * CT, LD = D + 16, PART = QN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
   // A query's factor of the weights goes into the exponent: good for 2^-21, which bf16 does not see, and a
   // product less a weight.
@@ -470,7 +463,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
       if (wave == 0) hpos = G.positions[t];
       if (wave == 1) hstat = stats[t];
       if (wave == 2) hstat = LOG ? __log2f(inv_stats[t]) : inv_stats[t];
-      if (wave == 3) hstat = deltas[t];
+      if (wave == 3) hstat = -deltas[t];
     };
     fetch(block_first);
 
@@ -514,7 +507,10 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
-          for (int n = 0; n < CT; ++n) s[n][t] = dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int n = 0; n < CT; ++n) {
+            s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            dp[n][t] = *(const f32x4 *)(ldelta + w * 32 + t * 16 + g * 4);  // -delta
+          }
 #pragma unroll
           for (int d = 0; d < DF; ++d) {
             const Frag<NP> qf = frag_row<NP>(wq + t * 16 * LD + d * 32, LD, PART, lane);
@@ -531,8 +527,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int r = w * 32 + t * 16 + g * 4;
-            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r),
-                        delta = *(const f32x4 *)(ldelta + r);
+            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r);
             const f32x4 shift = LOG ? b - top + inv : b - top;
 #pragma unroll
             for (int n = 0; n < CT; ++n)
@@ -540,7 +535,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
               for (int e = 0; e < 4; ++e) {
                 const float x = exp2_fast(fmaf(s[n][t][e], scale, shift[e])), p = LOG ? x : x * inv[e];
                 s[n][t][e] = p;
-                dp[n][t][e] = p * (dp[n][t][e] - delta[e]);
+                dp[n][t][e] = p * dp[n][t][e];
               }
           }
         } else {
@@ -551,13 +546,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll
             for (int n = 0; n < CT; ++n)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) add[n][t][e] = one >= 0 ? b : lb.bias_of(G, gap_of(qpos[e], pos[n]));
+              for (int e = 0; e < 4; ++e) add[n][t][e] = lb.bias_of(G, gap_of(qpos[e], pos[n]));
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int r = w * 32 + t * 16 + g * 4;
-            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r),
-                        delta = *(const f32x4 *)(ldelta + r);
+            const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r);
 #pragma unroll
             for (int n = 0; n < CT; ++n)
 #pragma unroll
@@ -566,7 +560,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
                 const float p = LOG ? exp2_fast(x + inv[e]) : exp2_fast(x) * inv[e];
                 const bool kept = (unsigned)(q0 + r + e - at[n]) < after[n];
                 s[n][t][e] = kept ? p : 0.f;
-                dp[n][t][e] = kept ? p * (dp[n][t][e] - delta[e]) : 0.f;
+                dp[n][t][e] = kept ? p * dp[n][t][e] : 0.f;
               }
           }
         }
@@ -616,12 +610,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   }
 }
 
-template <typename T, int D> constexpr int block_tokens() { return 64 * columns<T, D>(); }
-
 template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float *dbias, hipStream_t s) {
-  constexpr int B = block_tokens<T, D>();
-  A.n_tiles = (A.G.n_tokens + B - 1) / B;
-  const auto each = [&](auto kernel, int heads, size_t lds) {
+  const auto each = [&](auto kernel, int block, int heads, size_t lds) {
+    A.n_tiles = (A.G.n_tokens + block - 1) / block;
     const int64_t per = max_blocks(256) / heads;
     for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
       const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
@@ -634,13 +625,13 @@ template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float 
   each(searched ? k_gap_dq<T, D, false, void>
        : vec    ? k_gap_dq<T, D, true, uint8_t>
                 : k_gap_dq<T, D, false, uint8_t>,
-       A.G.heads, 4 * A.G.buckets * kColumns * sizeof(float));
+       64 * query_columns<T, D>(), A.G.heads, 4 * A.G.buckets * kColumns * sizeof(float));
   hipLaunchKernelGGL(k_gap_dbias, dim3((unsigned)(A.G.heads * A.G.buckets)), dim3(256), 0, s, A.dbias_parts,
                      A.n_tiles, dbias);
   each(searched ? k_gap_dkv<T, D, false, void>
        : vec    ? k_gap_dkv<T, D, true, Entry>
                 : k_gap_dkv<T, D, false, Entry>,
-       A.G.heads / A.G.group, 0);
+       64 * key_columns<T, D>(), A.G.heads / A.G.group, 0);
   return hipGetLastError();
 }
 template <typename T> hipError_t launch_back(const BackArgs &A, bool vec, float *dbias, hipStream_t s) {
