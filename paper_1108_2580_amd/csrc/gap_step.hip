@@ -19,6 +19,7 @@ struct StepArgs {
   void *out;
   float *parts;   // [slots, heads, beams, width]
   float *stats;   // [slots, heads, beams, 2]: the largest score (-inf: none) and the sum
+  const Place *places;  // of the slots; nullable: searched for
   int64_t slot0, row0;
   int shift, passes;
   bool vec, vec_path;
@@ -29,18 +30,38 @@ __device__ __forceinline__ int64_t part_index(const StepArgs &A, int64_t slot, i
   return (slot * A.G.heads + head) * A.P.beams + beam;
 }
 
+__global__ __launch_bounds__(256) void k_gap_places(GapShape G, int shift, int64_t n_slots, Place *places) {
+  const int64_t slot = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (slot >= n_slots) return;
+  int64_t lo = 0, hi = G.n_rows;  // the last row whose slots begin at this one or before
+  while (hi - lo > 1) {
+    const int64_t mid = (lo + hi) / 2;
+    if ((clamped(G.row_ptr[mid], 0, G.n_tokens) >> shift) + mid <= slot) lo = mid; else hi = mid;
+  }
+  Place p;
+  p.row = (int32_t)lo;
+  p.first = clamped(G.row_ptr[lo], 0, G.n_tokens);
+  p.len = (int32_t)(clamped(G.row_ptr[lo + 1], p.first, G.n_tokens) - p.first);
+  p.segment = slot - ((p.first >> shift) + lo);
+  places[slot] = p;
+}
+
 // One block: a segment, a key head and up to 16 CT of its columns (beams and the head's query heads). A wave
 // takes every fourth 32 keys.
 template <typename T, int D, int CT>
 __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
   constexpr int LD = D + 16, PART = 32 * LD, NP = kParts<T>, RP = kReadParts<T>, DF = D / 32, DT = D / 16;
   constexpr int COLS = 16 * CT, V8 = D / 8, ROWS = 64 / V8, VN = 32 / ROWS, LB = 65;
-  __shared__ __align__(16) bf16 lv[4][NP * PART];
+  // values of the waves' tiles, and at the end their sums: of all four side by side where they fit
+  constexpr int TILES = 4 * NP * PART * (int)sizeof(bf16), SUMS = COLS * D * (int)sizeof(float);
+  constexpr int SIDE = 4 * SUMS <= 32768 || 4 * SUMS <= TILES ? 4 : 1;
+  __shared__ __align__(16) char lmem[TILES > SIDE * SUMS ? TILES : SIDE * SUMS];
+  bf16(*lv)[NP * PART] = (bf16(*)[NP * PART])lmem;
+  float *lout = (float *)lmem;
   __shared__ __align__(16) int32_t lkind[4][32];
   __shared__ int32_t lbounds[64];
   __shared__ float lbias[COLS * LB];
   __shared__ float ltop[4][COLS], lsum[4][COLS];
-  __shared__ __align__(16) float lout[COLS * D];
 
   const GapShape &G = A.G;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
@@ -50,39 +71,12 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
   block /= (unsigned)A.passes;
   const int k_head = (int)(block % (unsigned)k_heads);
   const int64_t slot = A.slot0 + block / (unsigned)k_heads;
-  const Place at = find_place<false>(G.row_ptr, G.n_rows, G.n_tokens, A.shift, slot, lane);
+  const Place at = A.places ? A.places[slot]
+                            : find_place<false>(G.row_ptr, G.n_rows, G.n_tokens, A.shift, slot, lane);
   const int64_t begin = at.segment << A.shift;
   if (at.segment < 0 || begin >= at.len) return;
   const int count = (int)(at.len - begin < 1LL << A.shift ? at.len - begin : 1LL << A.shift);
   const int64_t token0 = at.first + begin;
-
-  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
-  for (int x = tid; x < COLS * G.buckets; x += 256) {
-    const int c = x / G.buckets, n = x % G.buckets, col = min(col0 + c, columns - 1);
-    lbias[c * LB + n] = bias2(G.bias[(int64_t)(k_head * G.group + col % G.group) * G.buckets + n]);
-  }
-
-  Frag<NP> qf[CT][DF];
-  int pos[CT];
-  bool alike = true;
-  const int64_t rows = (int64_t)at.row * A.P.beams;
-  const int pos0 = A.P.q_positions[rows];
-#pragma unroll
-  for (int n = 0; n < CT; ++n) {
-    const int col = min(col0 + n * 16 + m, columns - 1);
-    const int64_t row = rows + col / G.group;
-    pos[n] = A.P.q_positions[row];
-    alike = alike && pos[n] == pos0;
-    load_row<T, D>((const T *)A.q.data + row * A.q.token_stride +
-                       (k_head * G.group + col % G.group) * A.q.head_stride,
-                   G.width, A.vec, lane, qf[n]);
-    if (G.scale < 0.f) {
-#pragma unroll
-      for (int d = 0; d < DF; ++d) qf[n][d] = negated(qf[n][d]);
-    }
-  }
-  alike = __all(alike);
-  const float scale = fabsf(G.scale) * kLog2e;
   const T *k = (const T *)A.k.data + token0 * A.k.token_stride + k_head * A.k.head_stride;
   const T *v = (const T *)A.v.data + token0 * A.v.token_stride + k_head * A.v.head_stride;
 
@@ -104,6 +98,37 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
     }
     hpos = G.positions[token0 + min(j0 + (lane & 31), count - 1)];
   };
+  if (wave * 32 < count) fetch(wave * 32);
+
+  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+  {
+    const int c = tid % COLS, col = min(col0 + c, columns - 1);
+    const float *from = G.bias + (int64_t)(k_head * G.group + col % G.group) * G.buckets;
+#pragma unroll 4
+    for (int n = tid / COLS; n < G.buckets; n += 256 / COLS) lbias[c * LB + n] = bias2(from[n]);
+  }
+  Frag<NP> qf[CT][DF];
+  int pos[CT];
+  bool alike = true;
+  const int64_t rows = (int64_t)at.row * A.P.beams;
+  const int pos0 = A.P.q_positions[rows];
+#pragma unroll
+  for (int n = 0; n < CT; ++n) {
+    const int col = min(col0 + n * 16 + m, columns - 1);
+    const int64_t row = rows + col / G.group;
+    pos[n] = A.P.q_positions[row];
+    alike = alike && pos[n] == pos0;
+    load_row<T, D>((const T *)A.q.data + row * A.q.token_stride +
+                       (k_head * G.group + col % G.group) * A.q.head_stride,
+                   G.width, A.vec, lane, qf[n]);
+    if (G.scale < 0.f) {
+#pragma unroll
+      for (int d = 0; d < DF; ++d) qf[n][d] = negated(qf[n][d]);
+    }
+  }
+  alike = __all(alike);
+  const float scale = fabsf(G.scale) * kLog2e;
+
   f32x4 o[CT][DT];
   float top[CT], base[CT], sum[CT];
 #pragma unroll
@@ -113,7 +138,6 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (wave * 32 < count) fetch(wave * 32);
   __syncthreads();
 
   for (int j0 = wave * 32; j0 < count; j0 += 128) {
@@ -218,103 +242,63 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[n][d] *= factor;
   }
+  if (wave == 0 && g == 0) {
+#pragma unroll
+    for (int n = 0; n < CT; ++n) {
+      const int col = col0 + n * 16 + m;
+      if (col < columns) {
+        float *to = A.stats + 2 * part_index(A, slot, k_head * G.group + col % G.group, col / G.group);
+        to[0] = highest[n];
+        to[1] = total[n];
+      }
+    }
+  }
+  // the waves are past their tiles: the barrier above
 #pragma unroll 1
   for (int w = 0; w < 4; ++w) {
-    if (wave == w) {
+    if (SIDE == 4 ? w == 0 : wave == w) {
 #pragma unroll
       for (int n = 0; n < CT; ++n)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          f32x4 *to = (f32x4 *)(lout + (n * 16 + m) * D + d * 16 + g * 4);
-          *to = w == 0 ? o[n][d] : *to + o[n][d];
+          f32x4 *to = (f32x4 *)(lout + (SIDE == 4 ? wave * COLS * D : 0) + (n * 16 + m) * D + d * 16 + g * 4);
+          *to = SIDE == 4 || w == 0 ? o[n][d] : *to + o[n][d];
         }
-      if (w == 0 && g == 0) {
-#pragma unroll
-        for (int n = 0; n < CT; ++n) {
-          const int col = col0 + n * 16 + m;
-          if (col < columns) {
-            float *to = A.stats + 2 * part_index(A, slot, k_head * G.group + col % G.group, col / G.group);
-            to[0] = highest[n];
-            to[1] = total[n];
-          }
-        }
-      }
     }
+    if (SIDE == 4) break;
     __syncthreads();
   }
-  for (int x = tid; x < COLS * D; x += 256) {
+  if (SIDE == 4) __syncthreads();
+  for (int x = tid * 4; x < COLS * D; x += 1024) {
     const int col = col0 + x / D, d = x % D;
+    f32x4 y = *(const f32x4 *)(lout + x);
+#pragma unroll
+    for (int w = 1; w < SIDE; ++w) y += *(const f32x4 *)(lout + w * COLS * D + x);
     if (col < columns && d < G.width)
-      A.parts[part_index(A, slot, k_head * G.group + col % G.group, col / G.group) * G.width + d] = lout[x];
+      store4(A.parts + part_index(A, slot, k_head * G.group + col % G.group, col / G.group) * G.width + d, y,
+             G.width - d);
   }
 }
 
-// A beam's head: its segments and its path. A wave each; D / 8 lanes a key (or segment), eight values a
-// lane.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
-  constexpr int L = D / 8, KEYS = 64 / L;
-  __shared__ int32_t lbounds[64];
-  const GapShape &G = A.G;
-  const int tid = (int)threadIdx.x, lane = tid & 63, sub = lane / L, c = lane % L * 8;
-  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
-  __syncthreads();
-  const int64_t index = A.row0 * G.heads + (int64_t)blockIdx.x * 4 + tid / 64;
-  const int64_t row = index / G.heads;
-  if (row >= G.n_rows * A.P.beams) return;
-  const int head = (int)(index % G.heads), beam = (int)(row % A.P.beams);
-  const int64_t list = row / A.P.beams;
-
-  const Raw8<T> raw = load8((const T *)A.q.data + row * A.q.token_stride + head * A.q.head_stride, c, G.width,
-                            A.vec);
-  const f32x4 q[2] = {low4(raw), high4(raw)};
-  const float scale = G.scale * kLog2e;
-  float top = -__builtin_inff(), sum = 0.f;
-  f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+// What a lane has of a head's softmax so far: eight features.
+struct Sums {
+  float top, sum;
+  f32x4 o[2];
+  __device__ __forceinline__ void clear() {
+    top = -__builtin_inff();
+    sum = 0.f;
+    o[0] = o[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   // takes a part whose weights are `by` at the largest score `score`
-  const auto take = [&](float score, float by, const f32x4 *x) {
+  __device__ __forceinline__ void take(float score, float by, f32x4 lo, f32x4 hi) {
     const float next = fmaxf(top, score), to = next == -__builtin_inff() ? 0.f : next;
     const float mine = top == next ? 1.f : exp2_fast(top - to), its = exp2_fast(score - to);
     top = next;
     sum = sum * mine + by * its;
-    o[0] = o[0] * mine + x[0] * its;
-    o[1] = o[1] * mine + x[1] * its;
-  };
-  const int64_t first = clamped(G.row_ptr[list], 0, G.n_tokens);
-  const int64_t len = clamped(G.row_ptr[list + 1], first, G.n_tokens) - first;
-  const int64_t slot = (first >> A.shift) + list, n_slots = segments_of(len, A.shift);
-  for (int64_t n = sub; n < n_slots; n += KEYS) {
-    const int64_t part = part_index(A, slot + n, head, beam);
-    const float *x = A.parts + part * G.width;
-    const Raw8<float> raw = load8(x, c, G.width, G.width % 4 == 0);
-    const f32x4 y[2] = {low4(raw), high4(raw)};
-    take(A.stats[2 * part], A.stats[2 * part + 1], y);
+    o[0] = o[0] * mine + lo * its;
+    o[1] = o[1] * mine + hi * its;
   }
-  const int32_t at = A.P.q_positions[row];
-  for (int t = sub; t < A.P.steps; t += KEYS) {
-    const int32_t holder = A.P.path[row * A.P.path_stride + t];
-    const bool ok = holder >= 0 && holder < A.P.beams;
-    const int64_t from = list * A.P.beams + (ok ? holder : 0);
-    const Raw8<T> rk = load8((const T *)A.P.k.data + t * A.P.k_step + from * A.P.k.token_stride +
-                                 head / G.group * A.P.k.head_stride,
-                             c, G.width, A.vec_path);
-    const Raw8<T> rv = load8((const T *)A.P.v.data + t * A.P.v_step + from * A.P.v.token_stride +
-                                 head / G.group * A.P.v.head_stride,
-                             c, G.width, A.vec_path);
-    const f32x4 k[2] = {low4(rk), high4(rk)}, v[2] = {low4(rv), high4(rv)};
-    const int gap = gap_of(at, A.P.positions[t * (G.n_rows * A.P.beams) + from]);
-    float x = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x = fmaf(q[0][e], k[0][e], fmaf(q[1][e], k[1][e], x));
-#pragma unroll
-    for (int n = 1; n < L; n <<= 1) x += __shfl_xor(x, n);
-    const float b = G.bias[(int64_t)head * G.buckets + bucket_of(lbounds, G.buckets, gap)];
-    float y = fmaf(x, scale, bias2(b));
-    if (!ok) y = __builtin_nanf("");
-    take(y, 1.f, v);
-  }
-#pragma unroll
-  for (int n = L; n < 64; n <<= 1) {
+  __device__ __forceinline__ void take_lane(int n) {  // of the lane n apart
     const float score = __shfl_xor(top, n), by = __shfl_xor(sum, n);
     f32x4 x[2];
 #pragma unroll
@@ -322,20 +306,167 @@ __global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
       x[0][e] = __shfl_xor(o[0][e], n);
       x[1][e] = __shfl_xor(o[1][e], n);
     }
-    take(score, by, x);
+    take(score, by, x[0], x[1]);
   }
-  if (sub == 0 && c < G.width) {
+  template <typename T> __device__ __forceinline__ void store(T *to, int n) const {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T *to = (T *)A.out + (row * G.heads + head) * G.width + c;
-    store4(to, o[0] * inv, G.width - c);
-    if (c + 4 < G.width) store4(to + 4, o[1] * inv, G.width - c - 4);
+    store4(to, o[0] * inv, n);
+    if (n > 4) store4(to + 4, o[1] * inv, n - 4);
   }
+};
+
+// A token of a beam's path as a lane reads it.
+template <typename T> struct PathToken {
+  Raw8<T> k, v;
+  int32_t position;
+  bool ok;
+  __device__ __forceinline__ void read(const StepArgs &A, int64_t list, int holder, int64_t step, int k_head,
+                                       int c) {
+    ok = holder >= 0 && holder < A.P.beams;
+    const int64_t from = list * A.P.beams + (ok ? holder : 0);
+    k = load8((const T *)A.P.k.data + step * A.P.k_step + from * A.P.k.token_stride + k_head * A.P.k.head_stride,
+              c, A.G.width, A.vec_path);
+    v = load8((const T *)A.P.v.data + step * A.P.v_step + from * A.P.v.token_stride + k_head * A.P.v.head_stride,
+              c, A.G.width, A.vec_path);
+    position = A.P.positions[step * (A.G.n_rows * A.P.beams) + from];
+  }
+  // q . k over the L lanes of a head, with its bias
+  template <int L>
+  __device__ __forceinline__ float score(const GapShape &G, const int32_t *bounds, const f32x4 *q, int32_t at,
+                                         int head) const {
+    const f32x4 a = low4(k), b = high4(k);
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = fmaf(q[0][e], a[e], fmaf(q[1][e], b[e], x));
+#pragma unroll
+    for (int n = 1; n < L; n <<= 1) x += __shfl_xor(x, n);
+    const float bias = G.bias[(int64_t)head * G.buckets + bucket_of(bounds, G.buckets, gap_of(at, position))];
+    return ok ? fmaf(x, G.scale * kLog2e, bias2(bias)) : __builtin_nanf("");
+  }
+};
+
+// The path and the segments' parts of many beams: a wave takes 512 / D heads of one, eight features a lane, so
+// that a step's keys and values are one read each of neighbouring heads; four steps are on their way at a
+// time.
+template <typename T, int D> __global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
+  constexpr int L = D / 8, HEADS = 64 / L, AHEAD = 4;
+  __shared__ int32_t lbounds[64];
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, c = lane % L * 8;
+  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+  __syncthreads();
+  const unsigned per_row = (unsigned)((G.heads + HEADS - 1) / HEADS);
+  const unsigned index = blockIdx.x * 4 + (unsigned)__builtin_amdgcn_readfirstlane(tid / 64);
+  const int64_t row = A.row0 + index / per_row;
+  if (row >= G.n_rows * A.P.beams) return;
+  const int head0 = (int)(index % per_row) * HEADS + lane / L, head = min(head0, G.heads - 1);
+  const int64_t list = row / A.P.beams;
+  const int beam = (int)(row - list * A.P.beams), k_head = head / G.group;
+  const int32_t *path = A.P.path + row * A.P.path_stride;
+
+  const Raw8<T> raw = load8((const T *)A.q.data + row * A.q.token_stride + head * A.q.head_stride, c, G.width,
+                            A.vec);
+  const int32_t at = A.P.q_positions[row];
+  const f32x4 q[2] = {low4(raw), high4(raw)};
+  Sums s;
+  s.clear();
+  for (int t0 = 0; t0 < A.P.steps; t0 += AHEAD) {
+    PathToken<T> x[AHEAD];
+    const int n = min(A.P.steps - t0, AHEAD);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (i < n) x[i].read(A, list, path[t0 + i], t0 + i, k_head, c);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (i < n) s.take(x[i].template score<L>(G, lbounds, q, at, head), 1.f, low4(x[i].v), high4(x[i].v));
+  }
+  const int64_t first = clamped(G.row_ptr[list], 0, G.n_tokens);
+  const int64_t len = clamped(G.row_ptr[list + 1], first, G.n_tokens) - first;
+  const int64_t slot = (first >> A.shift) + list, n_slots = segments_of(len, A.shift);
+  for (int64_t n = 0; n < n_slots; ++n) {
+    const int64_t part = part_index(A, slot + n, head, beam);
+    const Raw8<float> x = load8(A.parts + part * G.width, c, G.width, G.width % 4 == 0);
+    s.take(A.stats[2 * part], A.stats[2 * part + 1], low4(x), high4(x));
+  }
+  if (head0 < G.heads && c < G.width) s.store((T *)A.out + (row * G.heads + head) * G.width + c, G.width - c);
 }
 
-// Short segments fill the chip where tokens are few; each leaves a part of every beam's and head's sums.
+// Of fewer beams: WAVES waves take one head, L = D / 8 lanes a segment or a step.
+template <typename T, int D, int WAVES> __global__ __launch_bounds__(256) void k_gap_path_wide(StepArgs A) {
+  constexpr int L = D / 8, KEYS = 64 * WAVES / L;
+  __shared__ int32_t lbounds[64];
+  __shared__ float lparts[WAVES > 1 ? 3 : 1][L][10];
+  const GapShape &G = A.G;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid / 64, c = lane % L * 8;
+  const int sub = (WAVES == 1 ? lane : tid) / L;
+  if (tid < 64) lbounds[tid] = tid < G.buckets - 1 ? G.bounds[tid] : 0x7fffffff;
+  if (WAVES == 1) __syncthreads();
+  const unsigned index = WAVES == 1 ? blockIdx.x * 4 + (unsigned)wave : blockIdx.x;
+  const int64_t row = A.row0 + index / (unsigned)G.heads;
+  if (row >= G.n_rows * A.P.beams) return;
+  const int head = (int)(index % (unsigned)G.heads);
+  const int64_t list = row / A.P.beams;
+  const int beam = (int)(row - list * A.P.beams);
+  const Raw8<T> raw = load8((const T *)A.q.data + row * A.q.token_stride + head * A.q.head_stride, c, G.width,
+                            A.vec);
+  const int32_t at = A.P.q_positions[row];
+  const int64_t first = clamped(G.row_ptr[list], 0, G.n_tokens);
+  const int64_t len = clamped(G.row_ptr[list + 1], first, G.n_tokens) - first;
+  const int64_t slot = (first >> A.shift) + list, n_slots = segments_of(len, A.shift);
+  const f32x4 q[2] = {low4(raw), high4(raw)};
+  Sums s;
+  s.clear();
+  if (WAVES > 1) __syncthreads();
+  for (int t = sub; t < A.P.steps; t += KEYS) {
+    PathToken<T> x;
+    x.read(A, list, A.P.path[row * A.P.path_stride + t], t, head / G.group, c);
+    s.take(x.template score<L>(G, lbounds, q, at, head), 1.f, low4(x.v), high4(x.v));
+  }
+  for (int64_t n0 = sub; n0 < n_slots; n0 += 2 * KEYS) {
+    Raw8<float> x[2];
+    float score[2], by[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t n = n0 + i * KEYS, part = part_index(A, slot + (n < n_slots ? n : n0), head, beam);
+      x[i] = load8(A.parts + part * G.width, c, G.width, G.width % 4 == 0);
+      score[i] = A.stats[2 * part];
+      by[i] = A.stats[2 * part + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (n0 + i * KEYS < n_slots) s.take(score[i], by[i], low4(x[i]), high4(x[i]));
+  }
+#pragma unroll
+  for (int n = L; n < 64; n <<= 1) s.take_lane(n);
+  if constexpr (WAVES > 1) {
+    if (wave > 0 && lane < L) {
+      float *to = lparts[wave - 1][lane];
+      to[0] = s.top;
+      to[1] = s.sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        to[2 + e] = s.o[0][e];
+        to[6 + e] = s.o[1][e];
+      }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 0; w < 3; ++w) {
+      const float *x = lparts[w][lane % L];
+      s.take(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]}, f32x4{x[6], x[7], x[8], x[9]});
+    }
+  }
+  if (lane < L && c < G.width)
+    s.store((T *)A.out + (row * G.heads + head) * G.width + c, G.width - c);
+}
+
+// Short segments fill the chip where tokens are few, long ones leave fewer parts of every beam's and head's sums:
+// 128 tokens up to 2048 blocks, then as few above 256 as leave 8192. History and join, us, at 2048, 4096, 8192
+// and 16 384 blocks: one list of 62 496 tokens, 8 key heads of 64: 44, 56, 56, 56 (segments of 256, then 128);
+// 1024 lists of 262: 336, 309, 306, 320 (of 2048, 1024, 512, 256).
 int step_shift(int64_t n_tokens, int32_t k_heads) {
-  int shift = 7;
-  while (shift < 12 && (n_tokens >> shift) * k_heads > 2048) ++shift;
+  int shift = (n_tokens >> 7) * k_heads > 2048 ? 8 : 7;
+  while (shift < 12 && (n_tokens >> shift) * k_heads > 8192) ++shift;
   return shift;
 }
 
@@ -361,10 +492,21 @@ template <typename T, int D> hipError_t launch_step(StepArgs A, hipStream_t s) {
     else
       launch_history<T, D, MOST>(A, s);
   }
-  const int64_t rows = A.G.n_rows * A.P.beams, per = max_blocks(256) * 4 / A.G.heads;
+  // Waves a beam: four a head where those are few, one, or one for 512 / D heads. 4, 1 and 1/8 a head, us:
+  // 64 heads of beams with 245 segments 9.6, 19.6, -; 4000 with 3 steps at 50 wide 20, 10, 23; 131 072 with 9
+  // steps at 64 wide -, 178, 100.
+  constexpr int HEADS = 512 / D;
+  const int64_t rows = A.G.n_rows * A.P.beams, heads = rows * A.G.heads;
+  const int64_t waves = heads <= 1024    ? 4 * A.G.heads
+                        : heads <= 16384 ? A.G.heads
+                                         : (A.G.heads + HEADS - 1) / HEADS;
+  const auto kernel = heads <= 1024    ? k_gap_path_wide<T, D, 4>
+                      : heads <= 16384 ? k_gap_path_wide<T, D, 1>
+                                       : k_gap_path<T, D>;
+  const int64_t per = max_blocks(256) / A.G.heads;
   for (A.row0 = 0; A.row0 < rows; A.row0 += per) {
     const int64_t n = rows - A.row0 < per ? rows - A.row0 : per;
-    hipLaunchKernelGGL((k_gap_path<T, D>), dim3((unsigned)((n * A.G.heads + 3) / 4)), dim3(256), 0, s, A);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((n * waves + 3) / 4)), dim3(256), 0, s, A);
   }
   return hipGetLastError();
 }
@@ -380,12 +522,18 @@ int64_t part_bytes(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t k_h
   return n_tokens > 0 ? (slots * heads * beams * values * 4 + 15) / 16 * 16 : 0;
 }
 
+// Of the slots' places, for more rows than a search looks at together.
+int64_t place_bytes(int64_t n_tokens, int64_t n_lists, int32_t k_heads) {
+  const int64_t slots = (n_tokens >> step_shift(n_tokens, k_heads)) + n_lists;
+  return n_tokens > 0 && n_lists > 64 ? (slots * (int64_t)sizeof(Place) + 15) / 16 * 16 : 0;
+}
+
 }  // namespace
 
 int64_t gap_step_space(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t k_heads, int32_t beams,
                        int32_t width) {
   return part_bytes(n_tokens, n_lists, heads, k_heads, beams, width) +
-         part_bytes(n_tokens, n_lists, heads, k_heads, beams, 2);
+         part_bytes(n_tokens, n_lists, heads, k_heads, beams, 2) + place_bytes(n_tokens, n_lists, k_heads);
 }
 
 hipError_t launch_gap_step(als_dtype dtype, const GapShape &G, const GapPath &P, const als_heads &q,
@@ -402,6 +550,14 @@ hipError_t launch_gap_step(als_dtype dtype, const GapShape &G, const GapPath &P,
   A.parts = (float *)workspace;
   A.stats = (float *)((char *)workspace + part_bytes(G.n_tokens, G.n_rows, G.heads, k_heads, P.beams, G.width));
   A.shift = step_shift(G.n_tokens, k_heads);
+  if (place_bytes(G.n_tokens, G.n_rows, k_heads)) {
+    Place *places =
+        (Place *)((char *)A.stats + part_bytes(G.n_tokens, G.n_rows, G.heads, k_heads, P.beams, 2));
+    A.places = places;
+    const int64_t slots = (G.n_tokens >> A.shift) + G.n_rows;  // below 2^31
+    hipLaunchKernelGGL(k_gap_places, dim3((unsigned)((slots + 255) / 256)), dim3(256), 0, s, G, A.shift, slots,
+                       places);
+  }
   const int size = dtype == ALS_F32 ? 4 : 2;
   const auto vec = [&](const als_heads &h) {
     return aligned16(h.data, h.token_stride, h.head_stride, G.width, size);
