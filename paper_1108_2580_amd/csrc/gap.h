@@ -236,6 +236,36 @@ __device__ __forceinline__ void load_row(const T *p, int width, bool vec, int la
   for (int d = 0; d < D / 32; ++d) f[d] = operand(load8(p, d * 32 + (lane >> 4) * 8, width, vec));
 }
 
+// Sums of products. Of parts, the products of first parts have a sum of their own: beside it the others' would be
+// rounded to its last bits, six times a step.
+template <int NP> struct Acc {
+  f32x4 sum;
+  __device__ __forceinline__ void start(f32x4 x) { sum = x; }
+  __device__ __forceinline__ void add(const Frag<NP> &a, const Frag<NP> &b) { sum = mma(a, b, sum); }
+  __device__ __forceinline__ f32x4 value() const { return sum; }
+};
+template <> struct Acc<3> {
+  f32x4 sum, rest;
+  __device__ __forceinline__ void start(f32x4 x) {
+    sum = x;
+    rest = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void add(const Frag<3> &a, const Frag<3> &b) {
+    rest = mma(a.p[0], b.p[2], rest);
+    rest = mma(a.p[2], b.p[0], rest);
+    rest = mma(a.p[1], b.p[1], rest);
+    rest = mma(a.p[0], b.p[1], rest);
+    rest = mma(a.p[1], b.p[0], rest);
+    sum = mma(a.p[0], b.p[0], sum);
+  }
+  __device__ __forceinline__ f32x4 value() const { return sum + rest; }
+};
+__device__ __forceinline__ f32x4 mma(const Frag<1> &a, const Frag<3> &b, f32x4 c) {
+  c = mma(a.p[0], b.p[2], c);
+  c = mma(a.p[0], b.p[1], c);
+  return mma(a.p[0], b.p[0], c);
+}
+
 // Four values at p, at any alignment of the type, of which `n` belong to the row.
 template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 x, int n) {
   using V4 = typename Vec4<T>::type;

@@ -9,8 +9,10 @@
 // queries are neighbours in the packed order, of one row or of several: a token's row says which keys it
 // reads, so that short rows share tiles.
 //
-// Rounding. Scores, weights, sums and outputs are fp32; bf16 weights enter their product in two bf16 parts,
-// off by 2^-16 at most (one would cost an output as much again as its own rounding).
+// Rounding. Scores, weights, sums and outputs are fp32; weights of bf16 values enter their product in two bf16
+// parts, off by 2^-16 at most (one would cost an output as much again as its own rounding), or in three where
+// the gradients are to follow: they take the outputs in 32 bits, and dbias, which sums terms that nearly cancel,
+// was off by 2.3e-6 of its norm with two and is by 1e-7.
 #include "gap.h"
 #include "internal.h"
 
@@ -44,10 +46,11 @@ template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 3
 // Columns of 16 queries a wave.
 template <typename T> constexpr int query_tiles() { return 1; }
 
-template <typename T, int D, bool VEC, typename Entry>
+// RP: parts of a weight.
+template <typename T, int D, bool VEC, typename Entry, int RP>
 __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 : 4) void k_gap_read(ReadArgs A) {
   constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
-  constexpr int NP = kParts<T>, RP = kReadParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
+  constexpr int NP = kParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
   using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
   __shared__ __align__(16) bf16 lv[NP * PART];
@@ -179,14 +182,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
     f32x4 s[QT][KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
+      Acc<NP> qk[QT];
 #pragma unroll
-      for (int n = 0; n < QT; ++n) s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < QT; ++n) qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
       for (int d = 0; d < DF; ++d) {
         const Frag<NP> kf = frag_row<NP>(lk + t * 16 * LD + d * 32, LD, PART, lane);
 #pragma unroll
-        for (int n = 0; n < QT; ++n) s[n][t] = mma(kf, qf[n][d], s[n][t]);
+        for (int n = 0; n < QT; ++n) qk[n].add(kf, qf[n][d]);
       }
+#pragma unroll
+      for (int n = 0; n < QT; ++n) s[n][t] = qk[n].value();
     }
 
     // one bucket for the tile's gaps, or one for each
@@ -334,12 +340,15 @@ template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStr
   for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
     const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
     const dim3 grid((unsigned)(n * A.G.heads));
-    if (A.G.last_bound >= kTableGaps)
-      hipLaunchKernelGGL((k_gap_read<T, D, false, void>), grid, dim3(256), 0, s, A);
-    else if (vec)
-      hipLaunchKernelGGL((k_gap_read<T, D, true, Entry>), grid, dim3(256), 0, s, A);
-    else
-      hipLaunchKernelGGL((k_gap_read<T, D, false, Entry>), grid, dim3(256), 0, s, A);
+    // for gradients, with three parts of a weight
+    constexpr int RP = kReadParts<T>;
+    const auto kernel = A.G.last_bound >= kTableGaps ? A.stats ? k_gap_read<T, D, false, void, 3>
+                                                               : k_gap_read<T, D, false, void, RP>
+                        : vec                        ? A.stats ? k_gap_read<T, D, true, Entry, 3>
+                                                               : k_gap_read<T, D, true, Entry, RP>
+                        : A.stats                    ? k_gap_read<T, D, false, Entry, 3>
+                                                     : k_gap_read<T, D, false, Entry, RP>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, A);
   }
   return hipGetLastError();
 }

@@ -238,13 +238,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll 1
     for (int w = 0; w < KS; ++w) {  // 32 keys at a time
       const bf16 *wk = lk + w * 32 * LD, *wv = lv + w * 32 * LD;
-      f32x4 s[QT][2], dp[QT][2];
+      f32x4 s[QT][2], dp[QT][2];  // do . v - delta
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
+        Acc<NP> qk[QT], ov[QT];
 #pragma unroll
         for (int n = 0; n < QT; ++n) {
-          s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-          dp[n][t] = f32x4{0.f, 0.f, 0.f, 0.f} - delta[n];  // do . v - delta is what is asked for
+          qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
+          ov[n].start(f32x4{0.f, 0.f, 0.f, 0.f} - delta[n]);
         }
 #pragma unroll
         for (int d = 0; d < DF; ++d) {
@@ -252,9 +253,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
           const Frag<NP> vf = frag_row<NP>(wv + t * 16 * LD + d * 32, LD, PART, lane);
 #pragma unroll
           for (int n = 0; n < QT; ++n) {
-            s[n][t] = mma(kf, qf[n][d], s[n][t]);
-            dp[n][t] = mma(vf, of[n][d], dp[n][t]);
+            qk[n].add(kf, qf[n][d]);
+            ov[n].add(vf, of[n][d]);
           }
+        }
+#pragma unroll
+        for (int n = 0; n < QT; ++n) {
+          s[n][t] = qk[n].value();
+          dp[n][t] = ov[n].value();
         }
       }
       if (plain) {
@@ -333,11 +339,11 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   // four threads a bucket, a wave's columns each
   for (int n = tid; n < 4 * G.buckets; n += 256) {
     const float *x = lsums + ((n & 3) * G.buckets + n / 4) * kColumns;
-    float sum = 0.f;
-    for (int c = 0; c < kColumns; ++c) sum += x[(c + n) & (kColumns - 1)];
+    double sum = 0.0;
+    for (int c = 0; c < kColumns; ++c) sum += (double)x[(c + n) & (kColumns - 1)];
     sum += __shfl_xor(sum, 1);
     sum += __shfl_xor(sum, 2);
-    if ((n & 3) == 0) parts[n / 4 * A.n_tiles] = sum;
+    if ((n & 3) == 0) parts[n / 4 * A.n_tiles] = (float)sum;
   }
 }
 
@@ -503,13 +509,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
 #pragma unroll 1
       for (int w = 0; w < QS; ++w) {  // 32 queries at a time
         const bf16 *wq = lq + w * 32 * LD, *wo = lo + w * 32 * LD;
-        f32x4 s[CT][2], dp[CT][2];
+        f32x4 s[CT][2], dp[CT][2];  // do . v - delta
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          Acc<NP> qk[CT], ov[CT];
 #pragma unroll
           for (int n = 0; n < CT; ++n) {
-            s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-            dp[n][t] = *(const f32x4 *)(ldelta + w * 32 + t * 16 + g * 4);  // -delta
+            qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
+            ov[n].start(*(const f32x4 *)(ldelta + w * 32 + t * 16 + g * 4));  // -delta
           }
 #pragma unroll
           for (int d = 0; d < DF; ++d) {
@@ -517,9 +524,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
             const Frag<NP> of = frag_row<NP>(wo + t * 16 * LD + d * 32, LD, PART, lane);
 #pragma unroll
             for (int n = 0; n < CT; ++n) {
-              s[n][t] = mma(qf, kf[n][d], s[n][t]);
-              dp[n][t] = mma(of, vf[n][d], dp[n][t]);
+              qk[n].add(qf, kf[n][d]);
+              ov[n].add(of, vf[n][d]);
             }
+          }
+#pragma unroll
+          for (int n = 0; n < CT; ++n) {
+            s[n][t] = qk[n].value();
+            dp[n][t] = ov[n].value();
           }
         }
         // s, dp -> p, ds
