@@ -40,22 +40,40 @@ template <typename T, int D> constexpr int key_columns() { return 1; }
 // ---- over keys: dq and dbias ---------------------------------------------------------------------
 
 // Sums by bucket: a column each lane, so that no two lanes add to the same place and the order of a sum's
-// terms is that of the program. LDS adds floats by itself at 3 cycles a lane (194 a wave's instruction, where
-// a read and a write take 8), so a lane reads, adds and writes: four places at a time, each with what the
-// ones before it give the same place, so that the last write to a place has all of them.
-constexpr int kColumns = 64;
-
-__device__ __forceinline__ void add_sums(float *column, i32x4 kind4, f32x4 x) {
-  x[1] += kind4[1] == kind4[0] ? x[0] : 0.f;
-  x[2] += kind4[2] == kind4[1] ? x[1] : kind4[2] == kind4[0] ? x[0] : 0.f;
-  x[3] += kind4[3] == kind4[2] ? x[2] : kind4[3] == kind4[1] ? x[1] : kind4[3] == kind4[0] ? x[0] : 0.f;
+// terms is that of the program; or, where that would leave a CU one block, a column each two lanes, which add
+// one after the other. LDS adds floats by itself at 3 cycles a lane (194 a wave's instruction, where a read and
+// a write take 8), so a lane reads, adds and writes: four places at a time, each with what the ones before it
+// give the same place, so that the last write to a place has all of them.
+template <int COLUMNS> struct BucketSums {
+  float *column;
+  int lane;
+  __device__ __forceinline__ float *at(int kind4) const { return column + kind4 * (COLUMNS / 4); }
+  __device__ __forceinline__ void add_now(const i32x4 &kind4, f32x4 x) const {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] += column[kind4[e] * (kColumns / 4)];
+    for (int e = 0; e < 4; ++e) x[e] += *at(kind4[e]);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) column[kind4[e] * (kColumns / 4)] = x[e];
-}
+    for (int e = 0; e < 4; ++e) *at(kind4[e]) = x[e];
+  }
+  __device__ __forceinline__ void add(const i32x4 &kind4, f32x4 x) const {
+    x[1] += kind4[1] == kind4[0] ? x[0] : 0.f;
+    x[2] += kind4[2] == kind4[1] ? x[1] : kind4[2] == kind4[0] ? x[0] : 0.f;
+    x[3] += kind4[3] == kind4[2] ? x[2] : kind4[3] == kind4[1] ? x[1] : kind4[3] == kind4[0] ? x[0] : 0.f;
+    if constexpr (COLUMNS == 64) {
+      add_now(kind4, x);
+    } else {
+      if (lane < 32) add_now(kind4, x);
+      asm volatile("" ::: "memory");  // one half of the wave after the other
+      if (lane >= 32) add_now(kind4, x);
+    }
+  }
+  __device__ __forceinline__ void add(int kind, float x) const {
+    if (COLUMNS == 64 || lane < 32) *at(kind * 4) += x;
+    asm volatile("" ::: "memory");
+    if (COLUMNS == 32 && lane >= 32) *at(kind * 4) += x;
+  }
+};
 
-template <typename T, int D, bool VEC, typename Entry>
+template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
 __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   constexpr int KN = tile_tokens<T>(), QT = query_columns<T, D>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
@@ -65,7 +83,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   __shared__ __align__(16) int32_t lpos[KN];
   __shared__ int32_t lrange[2], lbad;
   __shared__ Buckets<Entry> lb;
-  extern __shared__ float lsums[];  // [waves, buckets, kColumns]
+  extern __shared__ float lsums[];  // [waves, buckets, columns]
 
   const GapShape &G = A.G;
   int tid = (int)threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
@@ -76,7 +94,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 
   lb.start(G, head, tid);
   if (tid == 0) lbad = -1;
-  for (int n = tid; n < 4 * G.buckets * kColumns; n += 256) lsums[n] = 0.f;
+  for (int n = tid; n < 4 * G.buckets * COLUMNS; n += 256) lsums[n] = 0.f;
   int span_first[QT], block_first = kNoRow, block_last = -1, rows_first = 0;
 #pragma unroll
   for (int n = 0; n < QT; ++n) {
@@ -189,7 +207,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   for (int n = 0; n < QT; ++n)
 #pragma unroll
     for (int c = 0; c < DT; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float *sums = lsums + wave * G.buckets * kColumns + lane;
+  const BucketSums<COLUMNS> sums{lsums + wave * G.buckets * COLUMNS + (lane & (COLUMNS - 1)), lane};
   // of the tiles so far whose gaps were all in bucket run_kind, before the queries' own factors
   float run[QT];
 #pragma unroll
@@ -203,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
       sum = fmaf(run[n], inv[n], sum);
       run[n] = 0.f;
     }
-    sums[run_kind * kColumns] += sum;
+    sums.add(run_kind, sum);
   };
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
@@ -313,7 +331,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
 #pragma unroll
         for (int n = 0; n < QT; ++n)
 #pragma unroll
-          for (int t = 0; t < 2; ++t) add_sums(sums, kind[n][t], s[n][t] * inv[n]);
+          for (int t = 0; t < 2; ++t) sums.add(kind[n][t], s[n][t] * inv[n]);
       }
       Frag<RP> df[QT];
 #pragma unroll
@@ -345,9 +363,9 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
   __syncthreads();
   // four threads a bucket, a wave's columns each
   for (int n = tid; n < 4 * G.buckets; n += 256) {
-    const float *x = lsums + ((n & 3) * G.buckets + n / 4) * kColumns;
+    const float *x = lsums + ((n & 3) * G.buckets + n / 4) * COLUMNS;
     double sum = 0.0;
-    for (int c = 0; c < kColumns; ++c) sum += (double)x[(c + n) & (kColumns - 1)];
+    for (int c = 0; c < COLUMNS; ++c) sum += (double)x[(c + n) & (COLUMNS - 1)];
     sum += __shfl_xor(sum, 1);
     sum += __shfl_xor(sum, 2);
     if ((n & 3) == 0) parts[n / 4 * A.n_tiles] = (float)sum;
@@ -641,10 +659,16 @@ template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float 
   // tables of biases, where they leave a CU two blocks
   using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, float>::type;
   const bool searched = A.G.last_bound >= kTableGaps;
-  each(searched ? k_gap_dq<T, D, false, void>
-       : vec    ? k_gap_dq<T, D, true, uint8_t>
-                : k_gap_dq<T, D, false, uint8_t>,
-       64 * query_columns<T, D>(), A.G.heads, 4 * A.G.buckets * kColumns * sizeof(float));
+  // 64 columns where they leave a CU two blocks, beside the tiles of k and v and the table (taken so, training
+  // at 128 wide with 64 buckets 3090 -> 2000 us in this kernel, in fp32 with 32 buckets 1020 -> 720; 32 columns
+  // take 8 % more time where 64 fit)
+  constexpr int tiles = 2 * kParts<T> * tile_tokens<T>() * (D + 16) * (int)sizeof(bf16) + 8704;
+  const bool all = !searched && tiles + 1024 * A.G.buckets <= 80 * 1024;
+  const auto dq = searched ? k_gap_dq<T, D, false, void, 32>
+                  : vec    ? all ? k_gap_dq<T, D, true, uint8_t, 64> : k_gap_dq<T, D, true, uint8_t, 32>
+                  : all    ? k_gap_dq<T, D, false, uint8_t, 64>
+                           : k_gap_dq<T, D, false, uint8_t, 32>;
+  each(dq, 64 * query_columns<T, D>(), A.G.heads, (size_t)(4 * A.G.buckets * (all ? 64 : 32)) * sizeof(float));
   hipLaunchKernelGGL(k_gap_dbias, dim3((unsigned)(A.G.heads * A.G.buckets)), dim3(256), 0, s, A.dbias_parts,
                      A.n_tiles, dbias);
   each(searched ? k_gap_dkv<T, D, false, void>
