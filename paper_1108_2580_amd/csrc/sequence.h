@@ -108,10 +108,11 @@ hipError_t launch_gap_read(als_dtype dtype, const GapShape &g, const als_heads &
 
 // Bytes of the gradients' workspace, by part, each a multiple of 16.
 struct GapBackSpace {
-  int64_t spans, delta, dbias;
-  int64_t total() const { return spans + delta + dbias; }
+  int64_t spans, delta, dbias, heads;
+  int64_t total() const { return spans + delta + dbias + 2 * heads; }
 };
-GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t buckets);
+GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t k_heads, int32_t width,
+                            int32_t buckets);
 hipError_t launch_gap_back(als_dtype dtype, const GapShape &g, const als_heads &d_out, const als_heads &q,
                            const als_heads &k, const als_heads &v, const void *out, const float *stats,
                            const int16_t *rest, void *dq, void *dk, void *dv, float *dbias, void *workspace,

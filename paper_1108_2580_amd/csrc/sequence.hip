@@ -588,7 +588,8 @@ als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q
 
 int64_t als_gap_attention_backward_workspace(const als_gaps *shape) {
   return sane(shape)
-             ? als::gap_back_space(shape->n_tokens, shape->n_rows, shape->q_heads, shape->buckets).total()
+             ? als::gap_back_space(shape->n_tokens, shape->n_rows, shape->q_heads, shape->k_heads, shape->width,
+                                   shape->buckets).total()
              : -1;
 }
 

@@ -137,7 +137,9 @@ SHAPES = [  # lengths, heads, key heads, width, buckets, last bound
     ([128, 129], 4, 2, 128, 64, 5000), ([3, 0, 0, 40, 1, 1, 90], 4, 2, 50, 7, 300), ([300], 2, 2, 33, 2, 100),
     ([2] * 80, 2, 1, 20, 16, 500), ([500, 17], 8, 2, 64, 32, 3000), ([200, 31, 32, 33], 3, 3, 100, 40, 900),
     ([10, 260], 1, 1, 7, 3, 40), ([700], 2, 1, 64, 32, 6000), ([5] * 70 + [150], 2, 2, 8, 5, 1000),
-    ([400], 4, 1, 128, 16, 2000)]
+    ([400], 4, 1, 128, 16, 2000),
+    # as many blocks as take 128 queries and, of a key head, all query heads
+    ([300] * 30, 8, 8, 64, 32, 3000), ([100] * 170, 16, 8, 8, 4, 200), ([90] * 190, 16, 8, 64, 64, 4000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -437,7 +439,10 @@ def check_step(got, want, D, dtype):
 STEPS = [  # lengths, beams, steps, heads, key heads, width, buckets
     ([1], 1, 1, 1, 1, 1, 1), ([262], 8, 5, 8, 8, 64, 32), ([0, 40, 0], 5, 3, 4, 2, 50, 16), ([33, 128, 129, 1], 4, 1, 4, 1, 128, 64),
     ([700, 20], 16, 9, 8, 2, 64, 32), ([300], 32, 20, 4, 4, 32, 9), ([90] * 70, 2, 2, 2, 1, 20, 5),
-    ([150], 16, 2, 8, 1, 64, 8), ([200, 5], 16, 4, 16, 2, 100, 16), ([2000], 3, 7, 2, 2, 7, 40), ([64, 31], 7, 0, 2, 2, 64, 8)]
+    ([150], 16, 2, 8, 1, 64, 8), ([200, 5], 16, 4, 16, 2, 100, 16), ([2000], 3, 7, 2, 2, 7, 40), ([64, 31], 7, 0, 2, 2, 64, 8),
+    # as many beams and heads as take a wave each, or a part of one; segments of 256 tokens
+    ([20] * 40, 16, 3, 4, 2, 50, 16), ([12, 0, 30] * 50, 16, 6, 8, 4, 40, 8), ([40] * 70, 16, 9, 16, 4, 128, 8),
+    ([70_000], 2, 1, 4, 4, 16, 8)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
