@@ -172,7 +172,13 @@ template <typename T, int C, int WP, bool VEC> struct Staged : Tile<T, C, WP, 25
     Base::put_parts(lds, ld, x, tid);
   }
   // Whether what is held has infinities or NaN (columns past the width may be anything).
-  __device__ __forceinline__ bool nonfinite() const {
+  __device__ __forceinline__ bool nonfinite(const Rows &x, int tid) const {
+    if (!VEC && x.width < Base::E) {  // too narrow for a piece: read as they go to LDS
+      bool any = false;
+      for (int r = tid / Base::ROW; r < x.size && r < C; r += Base::ROWS)
+        for (int e = 0; e < x.width; ++e) any = any || !((float)((const T *)x.at(r, 0))[e] * 0.f == 0.f);
+      return any;
+    }
     constexpr uint32_t mask = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;  // exponents; all ones carry
     constexpr uint32_t one = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
     constexpr uint32_t carry = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
     __syncthreads();
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
     const bool masked = k0 + KN - 1 > (int)t0 || k0 < rows_first;  // for some query of the block
-    if (masked && hv.nonfinite()) lbad = k0;
+    if (masked && hv.nonfinite(rows_of(v, v_row, k0), tid)) lbad = k0;
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
     if (wave == 0) {
       const int lo = wave_min(hpos), hi = wave_max(hpos);

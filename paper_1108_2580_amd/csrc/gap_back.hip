@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
     g = lane >> 4;
     __syncthreads();
     const bool masked = k0 + KN - 1 > (int)t0 || k0 < rows_first;
-    if (masked && hk.nonfinite()) lbad = k0;
+    if (masked && hk.nonfinite(rows_of(k, k_row, k0), tid)) lbad = k0;
     hk.put_parts(lk, LD, rows_of(k, k_row, k0), tid);
     hv.put_parts(lv, LD, rows_of(v, v_row, k0), tid);
     if (wave == 0) {
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
       g = lane >> 4;
       __syncthreads();
       const bool masked = q0 < (int)t0 + BK - 1 || q0 + QN > rows_end;  // for some key of the block
-      if (masked && (hq.nonfinite() || ho.nonfinite())) lbad = q0;
+      if (masked && (hq.nonfinite(rows_of(q, q_row, q0), tid) || ho.nonfinite(rows_of(o, o_row, q0), tid))) lbad = q0;
       hq.put_parts(lq, LD, rows_of(q, q_row, q0), tid);
       ho.put_parts(lo, LD, rows_of(o, o_row, q0), tid);
       if (wave == 0) {

@@ -544,6 +544,8 @@ def gap_attention_step(q, k, v, bias, bounds, q_positions, positions, row_ptr, k
     dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
     rows, lists, Hk, D = q.shape[0], shape.n_rows, shape.k_heads, shape.width
     if path is None:
+        if not (k_path is None and v_path is None and path_positions is None):
+            raise ValueError("a path's tensors without path")
         if lists == 0 or rows % lists != 0 or rows == 0:
             raise ValueError(f"{rows} tokens are no whole number of beams of {lists} lists")
         at = _GapPath(rows // lists, 0)

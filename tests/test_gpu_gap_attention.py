@@ -255,7 +255,7 @@ def test_lowest_biases(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("D", [24, 64, 128])
+@pytest.mark.parametrize("D", [3, 24, 50, 64, 128])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_masked_places_reach_nothing(bad, D, dtype):
     """Infinities and NaN in a token's q, k, v and d_out: rows before it and other rows stay as they are."""
@@ -290,6 +290,22 @@ def test_masked_places_reach_nothing(bad, D, dtype):
                     same(name, slice(t + 1, end))
             if which == 2:
                 assert not torch.isfinite(got["out"][t:end, :, D // 2]).any()
+
+
+def test_a_bucket_of_nan_reaches_its_tokens_alone():
+    import paper_1108_2580_amd as p
+
+    q, k, v, bias, bounds, pos, ptr, do = inputs([60, 50], 2, 2, 32, 4, "f32", 24)
+    bias[1, 3] = math.nan
+    got = run(p, q, k, v, bias, bounds, pos, ptr, do, 0.2)
+    far = torch.zeros(110, dtype=torch.bool)
+    for a, e in ((0, 60), (60, 110)):
+        far[a:e] = (torch.tril((kinds(bounds, pos[a:e].cpu(), pos[a:e].cpu()) == 3).long()).sum(1) > 0)
+    assert far.any() and not far.all()
+    for name in ("out", "dq"):
+        nan = torch.isnan(got[name].cpu()).all(-1)
+        assert torch.equal(nan[:, 1], far) and not nan[:, 0].any(), name
+    assert torch.isnan(got["dbias"][1]).any() and torch.isfinite(got["dbias"][0]).all()
 
 
 def test_gradients_by_differences():
