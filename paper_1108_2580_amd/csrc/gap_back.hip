@@ -9,8 +9,8 @@
 // the other), one over the queries of a block's keys and, in turn, of the query heads that share them
 // (dk, dv). Scores and do . v are formed in both.
 //
-// Rounding. As forward: weights and ds enter products in two bf16 parts where the inputs are bf16. delta takes
-// what the outputs' rounding left out as well, so that dbias, fp32 whatever the inputs, does not hold it.
+// Rounding. Weights and ds enter products in two bf16 parts where the inputs are bf16. delta takes what the
+// outputs' rounding left out as well, so that dbias, fp32 whatever the inputs, does not hold it.
 #include "gap.h"
 #include "internal.h"
 

@@ -1,6 +1,6 @@
 // Internal declarations of the sequence operators: norm and rotation of queries and keys
-// (rotate.hip), attention with a decay for each head (attention.hip) and beam selection
-// (beam.hip). Host entries: sequence.hip.
+// (rotate.hip), attention with a decay for each head (attention.hip), attention over gaps of time (gap.hip,
+// gap_back.hip, gap_step.hip) and beam selection (beam.hip). Host entries: sequence.hip.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -2,16 +2,17 @@
 
 A next-item model reads a user's ratings in the order of time and answers with lists of items:
 ``norm_rotate`` prepares queries and keys, ``decay_attention`` runs over the histories
-(``decay_attention_step`` over one new rating), ``beam_select`` extends the lists and
-``reorder_states`` moves the beams' states along. Histories are packed one after the other, with a
-``row_ptr`` like the rating matrix's.
+(``decay_attention_step`` over one new rating), or ``gap_attention`` does, by softmax with a bias for
+each bucket of the gap between two ratings (``gap_attention_step`` over one new item of each beam),
+``beam_select`` extends the lists and ``reorder_states`` moves the beams' states along. Histories are
+packed one after the other, with a ``row_ptr`` like the rating matrix's.
 
 Argument marshalling only: the work runs in the HIP kernels of ``csrc/``. Every call is enqueued on
 the current HIP stream of the current device, on which its tensors have to lie, and nothing is
 synchronised. Inputs are fp32 or bf16 tensors whose features are contiguous; tokens and heads may
-have any strides (tokens of ``decay_attention`` up to 2^22 values). Where an input of ``norm_rotate`` or
-``decay_attention`` requires a gradient, the result carries it, or the call raises where there is none
-for that input (``cos``, ``sin``, ``log_decay``). The other operators' results carry none. What a call
+have any strides (tokens of ``decay_attention`` and ``gap_attention`` up to 2^22 values). Where an input of
+``norm_rotate``, ``decay_attention`` or ``gap_attention`` requires a gradient, the result carries it, or the
+call raises where there is none for that input (``cos``, ``sin``, ``log_decay``). The other operators' results carry none. What a call
 writes to a caller's tensor counts as an in-place operation.
 """
 from __future__ import annotations
@@ -263,7 +264,7 @@ def norm_rotate_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, 
     return q_out, k_out, dwq, dwk
 
 
-MAX_TOKEN_STRIDE = 1 << 22  # of decay_attention
+MAX_TOKEN_STRIDE = 1 << 22  # of decay_attention and gap_attention
 
 
 def _dense(t):
