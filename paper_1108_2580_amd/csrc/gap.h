@@ -164,9 +164,12 @@ template <typename T, int C, int WP, bool VEC> struct Staged : Tile<T, C, WP, 25
   }
   __device__ __forceinline__ void put_parts(bf16 *lds, int ld, const Rows &x, int tid) {
     if constexpr (VEC) {
-      if (x.width < WP && tid % Base::ROW * Base::E >= x.width) {
+      if (x.width < WP) {
+        asm volatile("");  // a branch: selected by condition, the pieces would cost every tile their selects
+        if (tid % Base::ROW * Base::E >= x.width) {
 #pragma unroll
-        for (int i = 0; i < Base::N; ++i) this->held[i] = Piece{0, 0, 0, 0};
+          for (int i = 0; i < Base::N; ++i) this->held[i] = Piece{0, 0, 0, 0};
+        }
       }
     }
     Base::put_parts(lds, ld, x, tid);
