@@ -20,6 +20,7 @@ namespace als {
 
 namespace {
 
+// The table of the tokens' rows: a search each, 14 us for 1 075 431 tokens of 4096 rows.
 __global__ __launch_bounds__(256) void k_gap_spans(GapShape G, Span2 *__restrict__ spans) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (t >= G.n_tokens) return;
@@ -43,10 +44,21 @@ struct ReadArgs {
 };
 
 template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 32; }
-// Columns of 16 queries a wave.
+// Columns of 16 queries a wave. Two would halve what a score reads from LDS, at twice the registers: two blocks
+// of 128 queries a CU took 730 us for 134 219 bf16 tokens of 512 rows, 8 heads of 64, where four of 64 take 570
+// (one row of 62 496: 7.8 and 7.9 ms).
 template <typename T> constexpr int query_tiles() { return 1; }
 
-// RP: parts of a weight.
+// One block: 64 queries of a head. RP: parts of a weight.
+//
+// What bounds it: vector instructions, of which a score takes 7 where a tile has one bucket (three for the two
+// parts of its weight) and about 7 more where it has several, and about 70 a tile and wave. Measured, 8 heads of
+// 64 in bf16: one row of 62 496 tokens 7.9 ms, 500 TFLOP/s of a large product's 1235 (issue 85 %, MFMA 34 %, four
+// blocks a CU, with which the waves' MFMAs and exponentials overlap: three took 8.5); 134 219 tokens of 512 rows
+// 570 us (q, k, v and o at 1 TB/s of a copy's 5.1). fp32 at 128 wide, 25 003 tokens of 100 rows, 8 heads to 2:
+// 500 us (MFMA 31 %, issue 49 %, two blocks, which LDS and registers allow). 2000 rows of 25 at 50 wide: 111 us,
+// the latency of two or three tiles. A byte a gap in LDS (two reads a score) leaves four blocks a CU where the
+// bias itself, 30 KB, leaves two.
 template <typename T, int D, bool VEC, typename Entry, int RP>
 __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 : 4) void k_gap_read(ReadArgs A) {
   constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
@@ -333,8 +345,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
 
 template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStream_t s) {
   constexpr int BQ = 64 * query_tiles<T>();
-  // a table of biases, where it leaves a CU two blocks
-  using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, uint8_t>::type;
+  using Entry = uint8_t;
   A.n_tiles = (A.G.n_tokens + BQ - 1) / BQ;
   const int64_t per = max_blocks(256) / A.G.heads;
   for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {

@@ -30,6 +30,7 @@ __device__ __forceinline__ int64_t part_index(const StepArgs &A, int64_t slot, i
   return (slot * A.G.heads + head) * A.P.beams + beam;
 }
 
+// The places of the segments, a search each: 5 us for 2074.
 __global__ __launch_bounds__(256) void k_gap_places(GapShape G, int shift, int64_t n_slots, Place *places) {
   const int64_t slot = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (slot >= n_slots) return;
@@ -47,7 +48,12 @@ __global__ __launch_bounds__(256) void k_gap_places(GapShape G, int shift, int64
 }
 
 // One block: a segment, a key head and up to 16 CT of its columns (beams and the head's query heads). A wave
-// takes every fourth 32 keys.
+// takes every fourth 32 keys; the next are on their way while it works.
+//
+// What bounds it: a block's chain of reads (its place, the first keys, the next), at the four blocks a CU that
+// 124 registers allow. Measured in bf16, 8 key heads of 64: one list of 62 496 tokens, 8 beams, 33 us (3.9 TB/s);
+// 1024 lists of 262 tokens, 16 beams, 195 us (2.8 TB/s; waves wait 77 % of their time). Two tiles ahead took 40 and
+// 236: their registers leave three blocks.
 template <typename T, int D, int CT>
 __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
   constexpr int LD = D + 16, PART = 32 * LD, NP = kParts<T>, RP = kReadParts<T>, DF = D / 32, DT = D / 16;
@@ -161,8 +167,23 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
 
     f32x4 s[CT][2];
     float most[CT];
+    i32x4 near[2];  // buckets of the lane's keys, or, where positions differ, the keys' positions
+#pragma unroll
+    for (int t = 0; t < 2; ++t) near[t] = *(const i32x4 *)(lkind[wave] + t * 16 + g * 4);
 #pragma unroll
     for (int n = 0; n < CT; ++n) {
+      i32x4 kind[2] = {near[0], near[1]};
+      if (!alike) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kind[t][e] = bucket_of(lbounds, G.buckets, gap_of(pos[n], near[t][e]));
+      }
+      f32x4 add[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) add[t][e] = lbias[(n * 16 + m) * LB + kind[t][e]];
       most[n] = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -171,9 +192,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
         for (int d = 0; d < DF; ++d) s[n][t] = mma(kf[t][d], qf[n][d], s[n][t]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = t * 16 + g * 4 + e, x = lkind[wave][r];
-          const float b = lbias[(n * 16 + m) * LB + (alike ? x : bucket_of(lbounds, G.buckets, gap_of(pos[n], x)))];
-          const float y = j0 + r < count ? fmaf(s[n][t][e], scale, b) : -__builtin_inff();
+          const int r = t * 16 + g * 4 + e;
+          const float y = j0 + r < count ? fmaf(s[n][t][e], scale, add[t][e]) : -__builtin_inff();
           s[n][t][e] = y;
           most[n] = fmaxf(most[n], y);
         }
@@ -347,7 +367,7 @@ template <typename T> struct PathToken {
 
 // The path and the segments' parts of many beams: a wave takes 512 / D heads of one, eight features a lane, so
 // that a step's keys and values are one read each of neighbouring heads; four steps are on their way at a
-// time.
+// time. 104 us for 16 384 beams of 9 steps, 8 heads of 64 (3.9 TB/s with the segments' parts).
 template <typename T, int D> __global__ __launch_bounds__(256) void k_gap_path(StepArgs A) {
   constexpr int L = D / 8, HEADS = 64 / L, AHEAD = 4;
   __shared__ int32_t lbounds[64];
