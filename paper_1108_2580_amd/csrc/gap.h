@@ -168,7 +168,7 @@ template <typename T, int C, int WP, bool VEC> struct Staged : Tile<T, C, WP, 25
         asm volatile("");  // a branch: selected by condition, the pieces would cost every tile their selects
         if (tid % Base::ROW * Base::E >= x.width) {
 #pragma unroll
-          for (int i = 0; i < Base::N; ++i) this->held[i] = Piece{0, 0, 0, 0};
+          for (int i = 0; i < Base::N; ++i) this->held[i] = Piece{};
         }
       }
     }
@@ -189,7 +189,7 @@ template <typename T, int C, int WP, bool VEC> struct Staged : Tile<T, C, WP, 25
 #pragma unroll
     for (int i = 0; i < Base::N; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) any |= (this->held[i][e] & mask) + one;
+      for (int e = 0; e < 4; ++e) any |= (__builtin_bit_cast(u32x4, this->held[i])[e] & mask) + one;
     return (any & carry) != 0;
   }
 };
@@ -355,7 +355,6 @@ __device__ __forceinline__ int wave_max(int x) {
 // would turn into NaN. Where such a tile's rows have any, they are summed by weight without those values, and
 // the sums that do read them become NaN at the end.
 template <int NP> __device__ __forceinline__ Frag<NP> cleaned(Frag<NP> f) {
-  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     u32x4 x = __builtin_bit_cast(u32x4, f.p[n]);

@@ -2,9 +2,13 @@
 // rows' segments, and tiles of tokens on their way to LDS.
 #pragma once
 
+#include <type_traits>
+
 #include "sequence.h"
 
 namespace als {
+
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -166,7 +170,10 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   static constexpr int E = 16 / sizeof(T), ROW = WP / E;
   static constexpr int ROWS = THREADS / ROW, N = (C + ROWS - 1) / ROWS;
   static_assert(THREADS % ROW == 0 && (ROWS >= C || C % ROWS == 0), "whole rows a pass");
-  using Piece = uint32_t __attribute__((ext_vector_type(4)));  // E values
+  // E values: of bf16 as four words, since the compiler takes halves apart where a read has a condition, and
+  // waits for the read to do so
+  struct alignas(16) Values { T v[E]; };
+  using Piece = typename std::conditional<sizeof(T) == 4, Values, u32x4>::type;
   struct Rows {  // of one chunk
     const char *base;
     uint32_t bytes;  // from row to row
@@ -182,7 +189,12 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = r0 + i * ROWS;
-      held[i] = Piece{0, 0, 0, 0};
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) held[i].v[e] = (T)0.f;
+      } else {
+        held[i] = Piece{};
+      }
       if (r < x.size && c < x.width) {
         if (VEC)
           held[i] = *(const Piece *)x.at(r, c);
@@ -195,7 +207,7 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
   __device__ __forceinline__ Piece piece(const Rows &x, int i, int r, int c) const {
     if (VEC) return held[i];
     if (x.width < E) {  // too narrow for any whole piece
-      struct { T v[E]; } p;
+      Values p;
 #pragma unroll
       for (int e = 0; e < E; ++e)
         p.v[e] = r < x.size && c + e < x.width ? ((const T *)x.at(r, 0))[e] : (T)0.f;
@@ -231,8 +243,9 @@ template <typename T, int C, int WP, int THREADS, bool VEC> struct Tile {
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (ROWS <= C || r0 < C) {
+          const Piece p = piece(x, i, r0 + i * ROWS, c);
           bf16x4 part[3];
-          as_parts<3>(__builtin_bit_cast(f32x4, piece(x, i, r0 + i * ROWS, c)), part);
+          as_parts<3>(f32x4{p.v[0], p.v[1], p.v[2], p.v[3]}, part);
 #pragma unroll
           for (int n = 0; n < 3; ++n)
             *(bf16x4 *)(lds + n * C * ld + (r0 + i * ROWS) * ld + c) = part[n];
