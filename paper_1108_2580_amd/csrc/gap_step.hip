@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void k_gap_places(GapShape G, int shift, int64
 // 1024 lists of 262 tokens, 16 beams, 195 us (2.8 TB/s; waves wait 77 % of their time). Two tiles ahead took 40 and
 // 236: their registers leave three blocks.
 template <typename T, int D, int CT>
-__global__ __launch_bounds__(256, 2) void k_gap_history(StepArgs A) {
+__global__ __launch_bounds__(256, D == 128 && sizeof(T) == 4 ? 1 : 2) void k_gap_history(StepArgs A) {
   constexpr int LD = D + 16, PART = 32 * LD, NP = kParts<T>, RP = kReadParts<T>, DF = D / 32, DT = D / 16;
   constexpr int COLS = 16 * CT, V8 = D / 8, ROWS = 64 / V8, VN = 32 / ROWS, LB = 65;
   // values of the waves' tiles, and at the end their sums: of all four side by side where they fit
