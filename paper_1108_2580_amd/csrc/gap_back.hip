@@ -70,16 +70,16 @@ template <int COLUMNS> struct BucketSums {
   }
 };
 
-// One block: 64 QT queries of a head. QT: columns of 16 queries a wave.
+// One block: 64 queries of a head.
 //
 // What bounds it: vector instructions (about 20 a score where a tile has several buckets, 9 where it has one) and
-// waits, at two barriers a tile and at the reads before each write of dbias's sums, with the two blocks a CU that
-// registers and LDS allow. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.5 ms (issue 48 %, MFMA
-// 15 %, waves wait 47 % of their time); four rows of 8000 at 128 wide with 64 buckets 1.8 ms; fp32 at 128 wide,
+// waits, at two barriers a tile and at the reads before each write of dbias's sums, with the three blocks a CU (two
+// at 128 wide) that registers and LDS allow. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.1 ms
+// (128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64 buckets 1.8 ms; fp32 at 128 wide,
 // 25 003 tokens of 100 rows, 670 us.
-template <typename T, int D, bool VEC, typename Entry, int COLUMNS, int QT>
-__global__ __launch_bounds__(256, 2) void k_gap_dq(BackArgs A) {
-  constexpr int KN = tile_tokens<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
+  constexpr int KN = tile_tokens<T>(), QT = 1, BQ = 64 * QT, LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
   using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
@@ -699,8 +699,8 @@ bool splits_heads(int64_t n_tokens, int32_t heads, int32_t k_heads) {
 }
 
 template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float *dbias, hipStream_t s) {
-  const auto each = [&](auto kernel, int block, int heads, size_t lds) {
-    A.n_tiles = (A.G.n_tokens + block - 1) / block;
+  A.n_tiles = (A.G.n_tokens + 63) / 64;
+  const auto each = [&](auto kernel, int heads, size_t lds) {
     const int64_t per = max_blocks(256) / heads;
     for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
       const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;
@@ -710,32 +710,24 @@ template <typename T, int D> hipError_t launch_back(BackArgs A, bool vec, float 
   // tables of biases, where they leave a CU two blocks
   using Entry = typename std::conditional<D == 128 && sizeof(T) == 4, uint8_t, float>::type;
   const bool searched = A.G.last_bound >= kTableGaps;
-  // 64 columns where they leave a CU two blocks, beside the tiles of k and v and the table (taken so, training
-  // at 128 wide with 64 buckets 3090 -> 2000 us in this kernel, in fp32 with 32 buckets 1020 -> 720; 32 columns
-  // take 8 % more time where 64 fit)
+  // 64 columns of dbias's sums where there are few blocks and they leave a CU two, beside the tiles of k and v and
+  // the table; else 32, with which a CU takes three. Us in this kernel with 64 and 32: training on 2001 ratings,
+  // 8 heads of 64, 32 buckets, 44 and 47; on 1 075 431, 7600 and 7100; at 128 wide with 64 buckets 3090 and 1820,
+  // in fp32 with 32 buckets 1020 and 700.
   constexpr int tiles = 2 * kParts<T> * tile_tokens<T>() * (D + 16) * (int)sizeof(bf16) + 8704;
-  const bool all = !searched && tiles + 1024 * A.G.buckets <= 80 * 1024;
-  // 128 queries a block, where that leaves blocks enough and their sums the registers: training on 2001 ratings
-  // takes 62 us in this kernel with them and 50 with 64, on 1 075 431 ratings 7.7 ms and 9
-  const auto launch_dq = [&](auto qt) {
-    constexpr int QT = decltype(qt)::value;
-    const auto dq = searched ? k_gap_dq<T, D, false, void, 32, QT>
-                    : vec    ? all ? k_gap_dq<T, D, true, uint8_t, 64, QT> : k_gap_dq<T, D, true, uint8_t, 32, QT>
-                    : all    ? k_gap_dq<T, D, false, uint8_t, 64, QT>
-                             : k_gap_dq<T, D, false, uint8_t, 32, QT>;
-    each(dq, 64 * QT, A.G.heads, (size_t)(4 * A.G.buckets * (all ? 64 : 32)) * sizeof(float));
-  };
-  constexpr int WIDE = sizeof(T) == 2 && D < 128 ? 2 : 1;
-  if (A.G.n_tokens * A.G.heads >= 512 * 128)
-    launch_dq(std::integral_constant<int, WIDE>());
-  else
-    launch_dq(std::integral_constant<int, 1>());
+  const bool all =
+      !searched && A.G.n_tokens * A.G.heads < 512 * 128 && tiles + 1024 * A.G.buckets <= 80 * 1024;
+  const auto dq = searched ? k_gap_dq<T, D, false, void, 32>
+                  : vec    ? all ? k_gap_dq<T, D, true, uint8_t, 64> : k_gap_dq<T, D, true, uint8_t, 32>
+                  : all    ? k_gap_dq<T, D, false, uint8_t, 64>
+                           : k_gap_dq<T, D, false, uint8_t, 32>;
+  each(dq, A.G.heads, (size_t)(4 * A.G.buckets * (all ? 64 : 32)) * sizeof(float));
   hipLaunchKernelGGL(k_gap_dbias, dim3((unsigned)(A.G.heads * A.G.buckets)), dim3(256), 0, s, A.dbias_parts,
                      A.n_tiles, dbias);
   each(searched ? k_gap_dkv<T, D, false, void>
        : vec    ? k_gap_dkv<T, D, true, Entry>
                 : k_gap_dkv<T, D, false, Entry>,
-       64, A.dk_parts ? A.G.heads : A.G.heads / A.G.group, 0);
+       A.dk_parts ? A.G.heads : A.G.heads / A.G.group, 0);
   if (A.dk_parts) {
     const int64_t values = A.G.n_tokens * (A.G.heads / A.G.group) * ((A.G.width + 3) / 4);
     const int64_t blocks = (values + 255) / 256;
@@ -757,7 +749,7 @@ int64_t rounded(int64_t x) { return (x + 15) / 16 * 16; }
 
 GapBackSpace gap_back_space(int64_t n_tokens, int64_t n_rows, int32_t heads, int32_t k_heads, int32_t width,
                             int32_t buckets) {
-  // tiles of 64 tokens at least
+  // tiles of 64 tokens
   return {gap_spans_bytes(n_tokens, n_rows), rounded(4 * n_tokens * heads),
           rounded(4 * ((n_tokens + 63) / 64) * heads * buckets),
           splits_heads(n_tokens, heads, k_heads) ? rounded(4 * n_tokens * heads * width) : 0};

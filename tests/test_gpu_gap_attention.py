@@ -138,7 +138,7 @@ SHAPES = [  # lengths, heads, key heads, width, buckets, last bound
     ([2] * 80, 2, 1, 20, 16, 500), ([500, 17], 8, 2, 64, 32, 3000), ([200, 31, 32, 33], 3, 3, 100, 40, 900),
     ([10, 260], 1, 1, 7, 3, 40), ([700], 2, 1, 64, 32, 6000), ([5] * 70 + [150], 2, 2, 8, 5, 1000),
     ([400], 4, 1, 128, 16, 2000),
-    # as many blocks as take 128 queries and, of a key head, all query heads
+    # as many blocks as share columns of dbias's sums and go through a key head's query heads in turn
     ([300] * 30, 8, 8, 64, 32, 3000), ([100] * 170, 16, 8, 8, 4, 200), ([90] * 190, 16, 8, 64, 64, 4000)]
 
 
