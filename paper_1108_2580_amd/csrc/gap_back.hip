@@ -75,7 +75,7 @@ template <int COLUMNS> struct BucketSums {
 // What bounds it: vector instructions (about 20 a score where a tile has several buckets, 9 where it has one) and
 // waits, at two barriers a tile and at the reads before each write of dbias's sums, with the three blocks a CU (two
 // at 128 wide) that registers and LDS allow. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.1 ms
-// (128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64 buckets 1.8 ms; fp32 at 128 wide,
+// (issue 56 %, MFMA 16 %; 128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64 buckets 1.8 ms; fp32 at 128 wide,
 // 25 003 tokens of 100 rows, 670 us.
 template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
@@ -376,8 +376,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
   }
 }
 
-// dbias[h, b]: the blocks' parts, in fp64. One block a head and bucket. 15 us for 8403 parts of 8 heads and 32
-// buckets (8.6 MB): the latency of 33 reads a thread.
+// dbias[h, b]: the blocks' parts, in fp64. One block a head and bucket. 27 us for 16 804 parts of 8 heads and
+// 32 buckets (17 MB): the latency of 66 reads a thread.
 __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ parts, int64_t n_tiles,
                                                    float *__restrict__ dbias) {
   __shared__ double sums[4];
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ par
 // One block: 64 keys of a key head, or of one of its query heads.
 //
 // What bounds it: vector instructions (13 a score where a tile has one bucket) with four products on MFMA, two of
-// them of two parts. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.1 ms (issue 64 %, MFMA 26 %,
+// them of two parts. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.0 ms (issue 63 %, MFMA 26 %,
 // three blocks a CU; 128 keys a block took 8.6); four rows of 8000 at 128 wide 2.0 ms; fp32 at 128 wide, 25 003
 // tokens of 100 rows, 8 heads to 2, 720 us (MFMA 40 %, issue 41 %; 16 registers spilled).
 template <typename T, int D, bool VEC, typename Entry>
