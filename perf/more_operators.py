@@ -90,10 +90,6 @@ def draw(rng):
         lists = log_int(1, max(1, min(1_024, tokens // 4)))
         return dict(case, lists=lists, tokens=tokens, beams=beams, steps=steps)
     train = rng.random() < 0.5
-    # A bias's gradients sum to zero over a head's buckets: of a few that hold nearly all of a history what is
-    # left is mostly rounding.
-    if train:
-        case["buckets"] = max(8, case["buckets"])
     # pairs of a query and a key that all heads' products may have, and values of the inputs
     pairs = (2e8 if train else 6e8) * (8 * 64) / (q * width) * (1.0 if dtype == "bf16" else 0.25)
     mean = log_int(16, int(min(40_000, 0.4 * pairs ** 0.5)))
