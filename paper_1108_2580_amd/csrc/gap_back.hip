@@ -176,6 +176,12 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
     }
     delta[n] = column_sum(x);
     if (g == 0 && real) A.delta[(int64_t)head * G.n_tokens + t] = delta[n];
+    // A sum that is no number would make a masked pair's zero one as well, on its way to dbias: the weights are
+    // formed as NaN instead, before the mask.
+    if (!(fabsf(inv[n]) <= kLargest)) {
+      top[n] = __builtin_nanf("");
+      inv[n] = 1.f;
+    }
     delta[n] *= sign;
     inv[n] *= sign;  // with the factor of a query's sums
   }
