@@ -113,7 +113,7 @@ def strip_comments(src):
 
 # no part of any sweep: the sequence operators
 OTHER_SOURCES = {"sequence.h", "sequence.hip", "tiles.h", "rotate.hip", "attention.hip", "beam.hip",
-                 "gap.h", "gap.hip", "gap_back.hip", "gap_step.hip"}
+                 "gap.h", "gap.hip", "gap_back.hip", "gap_step.hip", "unheld.hip"}
 
 
 def kernel_source_hash():

@@ -630,6 +630,16 @@ als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *pat
                                   int64_t workspace_bytes, void *hip_stream);
 
 /*
+ * Zeros in n (1 .. 4) packed device tensors at the tokens that no row holds, those before row_ptr[0] and from
+ * row_ptr[n_rows] on, whose places als_decay_attention, als_gap_attention and their gradients leave as they are:
+ * for results that go on into sums over all tokens. Token t of tensors[i] is the token_bytes[i] (1 .. 2^20)
+ * bytes from t * token_bytes[i] on; tensors and token_bytes lie on the host and are read within the call.
+ * n_tokens 0 .. 2^31 - 1; n_rows 0 .. 2^30; row_ptr as for als_decay_attention.
+ */
+als_status als_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, int32_t n,
+                            void *const *tensors, const int64_t *token_bytes, void *hip_stream);
+
+/*
  * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores
  *   scores[w] + logits[w, v] - log sum_u exp(logits[w, u]),
  * and the best `width` of all (w, v) go on; of equal scores (in fp64) the lowest beam's, then the

@@ -1,6 +1,7 @@
 // Internal declarations of the sequence operators: norm and rotation of queries and keys
 // (rotate.hip), attention with a decay for each head (attention.hip), attention over gaps of time (gap.hip,
-// gap_back.hip, gap_step.hip) and beam selection (beam.hip). Host entries: sequence.hip.
+// gap_back.hip, gap_step.hip), tokens of no row (unheld.hip) and beam selection (beam.hip). Host entries:
+// sequence.hip.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -132,6 +133,15 @@ int64_t gap_step_space(int64_t n_tokens, int64_t n_lists, int32_t heads, int32_t
                        int32_t width);
 hipError_t launch_gap_step(als_dtype dtype, const GapShape &g, const GapPath &p, const als_heads &q,
                            const als_heads &k, const als_heads &v, void *out, void *workspace, hipStream_t s);
+
+// Packed tensors to clear at the tokens that no row holds (unheld.hip).
+struct Unheld {
+  int32_t n;
+  char *data[4];
+  int64_t token_bytes[4];
+};
+hipError_t launch_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, const Unheld &u,
+                               hipStream_t s);
 
 // Blocks of a pass of norm and rotation: partial sums of the weights' gradients (rotate.hip).
 int64_t rotate_blocks(int64_t n_tokens);

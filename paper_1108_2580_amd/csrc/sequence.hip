@@ -703,6 +703,29 @@ als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *pat
                   "als_gap_attention_step");
 }
 
+als_status als_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, int32_t n,
+                            void *const *tensors, const int64_t *token_bytes, void *hip_stream) {
+  REQUIRE(n_tokens >= 0 && n_tokens <= kMax31, "n_tokens %lld out of range", (long long)n_tokens);
+  REQUIRE(n_rows >= 0 && n_rows <= kMaxRows, "n_rows %lld out of range", (long long)n_rows);
+  REQUIRE(row_ptr, "row_ptr is NULL");
+  REQUIRE((uintptr_t)row_ptr % 8 == 0, "row_ptr is not aligned to its type");
+  REQUIRE(n >= 1 && n <= 4, "%d tensors outside [1, 4]", n);
+  REQUIRE(tensors && token_bytes, "tensors or token_bytes is NULL");
+  als::Unheld u{};
+  u.n = n;
+  const Span ptr = span(row_ptr, 8 * (n_rows + 1));
+  for (int i = 0; i < n; ++i) {
+    REQUIRE(token_bytes[i] >= 1 && token_bytes[i] <= 1LL << 20, "token_bytes[%d] = %lld outside [1, 2^20]", i,
+            (long long)token_bytes[i]);
+    REQUIRE(n_tokens == 0 || tensors[i], "tensors[%d] is NULL", i);
+    REQUIRE(!overlap(span(tensors[i], n_tokens * token_bytes[i]), ptr), "tensors[%d] overlaps row_ptr", i);
+    u.data[i] = (char *)tensors[i];
+    u.token_bytes[i] = token_bytes[i];
+  }
+  return launched(als::launch_clear_unheld(n_tokens, n_rows, row_ptr, u, (hipStream_t)hip_stream),
+                  "als_clear_unheld");
+}
+
 int64_t als_beam_select_workspace(const als_beams *shape) {
   if (check_beams(shape) != ALS_OK) return -1;
   return als::beam_workspace(shape->n_lists, shape->beams, shape->width, shape->n_items);

@@ -78,6 +78,7 @@ def _declare():
             ("als_gap_attention_backward",
              [G, st, H, H, H, H, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_gap_attention_step", [G, GP, st, H, H, H, _P, _P, _i64, _P]),
+            ("als_clear_unheld", [_i64, _i64, _P, _i32, ctypes.POINTER(_P), ctypes.POINTER(_i64), _P]),
             ("als_beam_select", [B, st, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_reorder_states", [_i64, _i32, _i32, _i64, _P, _P, _P, _P])):
         f = getattr(lib, name)
@@ -164,6 +165,16 @@ def _workspace(size, device):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _clear_unheld(row_ptr, *tensors):
+    """Zeros new packed tensors [tokens, ...] at the tokens that no row holds, which the attentions' calls leave
+    unset: what autograd goes on with is summed over all tokens."""
+    n = len(tensors)
+    sizes = (t.element_size() * math.prod(t.shape[1:]) for t in tensors)
+    _check(lib.als_clear_unheld(tensors[0].shape[0], row_ptr.numel() - 1, row_ptr.data_ptr(), n,
+                                (_P * n)(*(t.data_ptr() for t in tensors)), (_i64 * n)(*sizes),
+                                _stream(tensors[0].get_device())))
 
 
 def _no_gradient(t, name):
@@ -475,9 +486,9 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
     -inf masks a bucket, and a token left without a key has the output zero. ``bounds``: int32
     [buckets - 1] on the host, ascending from 1 or more, the first gap of each bucket but the first.
     ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``: as for
-    ``decay_attention``; a token that no row holds is not worked on, and its place in the new tensors,
-    outputs and gradients, is left unset. ``scale``: 1 / sqrt(width) if None. Returns out [tokens,
-    heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
+    ``decay_attention``; a token that no row holds is not worked on: where a gradient is recorded, its output and
+    its gradients are zero, and its place in the new tensors is left unset otherwise. ``scale``: 1 / sqrt(width) if
+    None. Returns out [tokens, heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or bias.requires_grad):
         out, *saved = _GapAttention.apply(q, k, v, bias, bounds, positions, row_ptr, scale)
     else:
@@ -487,7 +498,7 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
 
 def gap_attention_backward(d_out, out, saved, q, k, v, bias, bounds, positions, row_ptr, scale=None):
     """Gradients (dq, dk, dv, dbias) of ``gap_attention`` from that of its output, its output (contiguous)
-    and what it saved."""
+    and what it saved. Those of tokens that no row holds are left unset."""
     dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
     shaped = (shape.n_tokens, shape.q_heads, shape.width)
     _shaped(q, "q", shaped)
@@ -511,6 +522,7 @@ class _GapAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, bias, bounds, positions, row_ptr, scale):
         out, stats, rest = _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, True)
+        _clear_unheld(row_ptr, out)
         # the host's bounds are kept as they are now
         ctx.save_for_backward(out, stats, rest, q, k, v, bias, bounds.clone(), positions, row_ptr)
         ctx.scale = scale
@@ -524,8 +536,9 @@ class _GapAttention(torch.autograd.Function):
         if d_out is None:
             return (None,) * 8
         out, stats, rest, *args = ctx.saved_tensors
-        return (*gap_attention_backward(_dense(d_out), out, (stats, rest), *args, ctx.scale), None, None, None,
-                None)
+        dq, dk, dv, dbias = gap_attention_backward(_dense(d_out), out, (stats, rest), *args, ctx.scale)
+        _clear_unheld(args[-1], dq, dk, dv)
+        return dq, dk, dv, dbias, None, None, None, None
 
 
 def gap_attention_step(q, k, v, bias, bounds, q_positions, positions, row_ptr, k_path=None, v_path=None,
