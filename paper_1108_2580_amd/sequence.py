@@ -351,7 +351,8 @@ def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
     by heads / key heads query heads; widths up to 128. ``log_decay``: fp32 [heads], <= 0.
     ``row_ptr``: int64 [rows + 1] on the device, from 0 to the number of tokens, row b holding tokens
     row_ptr[b] .. row_ptr[b + 1] - 1; a token that no row holds (padding behind the last row) is not
-    worked on, and its place in the new tensors, outputs and gradients, is left unset.
+    worked on: where a gradient is recorded, its output and its gradients are zero, and its place in the
+    new tensors is left unset otherwise.
     ``scale``: 1 / sqrt(key width) if None. ``initial_state``: fp32 [rows, heads, key width, value
     width], zero if None. Returns out [tokens, heads, value width], with ``return_state`` (out, the
     states after the rows' last tokens). ``log_decay`` takes no gradient."""
@@ -369,7 +370,7 @@ def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, ini
                              dstate=None, d_initial=None):
     """Gradients (dq, dk, dv, d_initial_state) of ``decay_attention`` from that of its output and,
     if given, of its returned state (``dstate``). The last is None unless there is an
-    ``initial_state`` or ``d_initial`` is true."""
+    ``initial_state`` or ``d_initial`` is true. Those of tokens that no row holds are left unset."""
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
     hdo = _heads(d_out, "d_out", q.dtype, dev)
     _shaped(d_out, "d_out", (q.shape[0], shape.q_heads, shape.v_width))
@@ -392,7 +393,9 @@ class _DecayAttention(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, log_decay, row_ptr, initial_state)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
-        return _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
+        out, state = _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
+        _clear_unheld(row_ptr, out)
+        return out, state
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -401,9 +404,10 @@ class _DecayAttention(torch.autograd.Function):
         if d_out is None:
             d_out = torch.zeros((q.shape[0], q.shape[1], v.shape[2]), dtype=q.dtype, device=q.device)
         dstate = None if dstate is None else dstate.contiguous()
-        grads = decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale,
-                                         initial_state, dstate, d_initial=ctx.needs_input_grad[3])
-        return (*grads, None, None, None, None)
+        dq, dk, dv, d_initial = decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale,
+                                                         initial_state, dstate, d_initial=ctx.needs_input_grad[3])
+        _clear_unheld(row_ptr, dq, dk, dv)
+        return dq, dk, dv, d_initial, None, None, None, None
 
 
 def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, state_out=None):
@@ -485,10 +489,8 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
     heads / key heads query heads; widths up to 128. ``bias``: fp32 [heads, buckets], up to 64 buckets;
     -inf masks a bucket, and a token left without a key has the output zero. ``bounds``: int32
     [buckets - 1] on the host, ascending from 1 or more, the first gap of each bucket but the first.
-    ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``: as for
-    ``decay_attention``; a token that no row holds is not worked on: where a gradient is recorded, its output and
-    its gradients are zero, and its place in the new tensors is left unset otherwise. ``scale``: 1 / sqrt(width) if
-    None. Returns out [tokens, heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
+    ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``, and tokens that no
+    row holds: as for ``decay_attention``. ``scale``: 1 / sqrt(width) if None. Returns out [tokens, heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or bias.requires_grad):
         out, *saved = _GapAttention.apply(q, k, v, bias, bounds, positions, row_ptr, scale)
     else:

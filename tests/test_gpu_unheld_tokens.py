@@ -77,6 +77,33 @@ def test_projections_around_gap_attention(before, lens, after, dtype, poisoned):
     same_sum(grads[1], plain.float().flatten(1), d_y, held)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("before,lens,after", BATCHES)
+def test_projections_around_decay_attention(before, lens, after, dtype, poisoned):
+    import paper_1108_2580_amd as p
+
+    H, Hk, D, W = 4, 2, 24, 16
+    log(f"{before} tokens, rows {lens[:4]}, {after} tokens, {dtype}")
+    g, N, ptr, held, x = batch(before, lens, after, W, 2)
+    weight = dev(torch.randn(W, (H + 2 * Hk) * D, generator=g)).requires_grad_()
+    back = dev(torch.randn(H * D, W, generator=g)).requires_grad_()
+    decay = dev(-torch.rand(H, generator=g))
+    qkv = parts((x @ weight).to(DTYPES[dtype]), H, Hk, D)
+    out = p.decay_attention(*qkv, decay, ptr, 0.2)
+    assert not out[~held].any()
+    d_y = dev(torch.randn(N, W, generator=g)) * held[:, None]
+    grads = torch.autograd.grad(out.float().flatten(1) @ back, (weight, back), d_y)
+    assert all(torch.isfinite(t).all() for t in grads)
+
+    args = (*(t.detach() for t in qkv), decay, ptr, 0.2)
+    plain = p.decay_attention(*args)
+    assert torch.equal(plain[held], out.detach()[held])
+    d_out = (d_y @ back.detach().T).unflatten(1, (H, D)).to(DTYPES[dtype])
+    dq, dk, dv, _ = p.decay_attention_backward(d_out, *args)
+    same_sum(grads[0], x, torch.cat([dq, dk, dv], 1), held)
+    same_sum(grads[1], plain.float().flatten(1), d_y, held)
+
+
 @pytest.mark.parametrize("width,offset", [(1, 0), (2, 3), (13, 1), (48, 0), (100, 7), (4096, 5)])
 def test_places_are_cleared_and_no_others(width, offset):
     """At any alignment and number of bytes a token; row pointers out of range touch nothing outside."""
