@@ -12,8 +12,9 @@ the current HIP stream of the current device, on which its tensors have to lie, 
 synchronised. Inputs are fp32 or bf16 tensors whose features are contiguous; tokens and heads may
 have any strides (tokens of ``decay_attention`` and ``gap_attention`` up to 2^22 values). Where an input of
 ``norm_rotate``, ``decay_attention`` or ``gap_attention`` requires a gradient, the result carries it, or the
-call raises where there is none for that input (``cos``, ``sin``, ``log_decay``). The other operators' results carry none. What a call
-writes to a caller's tensor counts as an in-place operation.
+call raises where there is none for that input (``cos``, ``sin``, ``log_decay``; tangents of forward-mode
+derivatives always). The other operators' results carry none. What a call writes to a caller's tensor counts as
+an in-place operation.
 """
 from __future__ import annotations
 
@@ -21,6 +22,7 @@ import ctypes
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from . import ALS_ERR_INVALID_ARG, ALS_OK, ALSError, lib
 
@@ -182,6 +184,15 @@ def _no_gradient(t, name):
         raise ValueError(f"{name} takes no gradient")
 
 
+def _no_tangents(*tensors):
+    """Forward-mode derivatives, which no operator gives, are refused rather than dropped."""
+    if getattr(forward_ad, "_current_level", 0) < 0:  # outside of any dual level no tensor has one
+        return
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError("an input has a tangent, and there are no forward-mode derivatives")
+
+
 def _writable(t, name):
     """Refuses a caller's tensor whose gradient a write by a kernel would lose unseen."""
     if t.requires_grad and torch.is_grad_enabled():
@@ -247,6 +258,7 @@ def norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps=1e-6, neighbo
     (``rotary_tables``); ``positions``: int32 [tokens], a row of the tables each (one outside them
     makes its token NaN). ``neighbours``: pair p is features 2 p and 2 p + 1 instead of p and
     p + pairs. Returns new (q, k). ``cos`` and ``sin`` take no gradient."""
+    _no_tangents(q, k, q_weight, k_weight, cos, sin)
     _no_gradient(cos, "cos")
     _no_gradient(sin, "sin")
     if torch.is_grad_enabled() and (
@@ -356,6 +368,7 @@ def decay_attention(q, k, v, log_decay, row_ptr, scale=None, initial_state=None,
     ``scale``: 1 / sqrt(key width) if None. ``initial_state``: fp32 [rows, heads, key width, value
     width], zero if None. Returns out [tokens, heads, value width], with ``return_state`` (out, the
     states after the rows' last tokens). ``log_decay`` takes no gradient."""
+    _no_tangents(q, k, v, log_decay, initial_state)
     _no_gradient(log_decay, "log_decay")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (q, k, v, initial_state)):
@@ -491,6 +504,7 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
     [buckets - 1] on the host, ascending from 1 or more, the first gap of each bucket but the first.
     ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``, and tokens that no
     row holds: as for ``decay_attention``. ``scale``: 1 / sqrt(width) if None. Returns out [tokens, heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
+    _no_tangents(q, k, v, bias)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or bias.requires_grad):
         out, *saved = _GapAttention.apply(q, k, v, bias, bounds, positions, row_ptr, scale)
     else:
