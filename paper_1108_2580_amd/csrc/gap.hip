@@ -3,7 +3,7 @@
 //   s_ij = scale q_i . k_j + bias[bucket(t_i - t_j)],  p_ij = exp(s_ij) / sum_j exp(s_ij),
 //   o_i = sum_j p_ij v_j.
 //
-// One pass over the keys: a block holds 64 or 128 queries of a head, reads keys and values in tiles through
+// One pass over the keys: a block holds 64 queries of a head, reads keys and values in tiles through
 // LDS, and keeps the largest score and the sum of the exponentials so far. Both products are on MFMA with
 // the queries as columns, so that the weights are operands of the second as they lie in registers. A block's
 // queries are neighbours in the packed order, of one row or of several: a token's row says which keys it
@@ -44,12 +44,10 @@ struct ReadArgs {
 };
 
 template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 32; }
-// Columns of 16 queries a wave. Two would halve what a score reads from LDS, at twice the registers: two blocks
-// of 128 queries a CU took 730 us for 134 219 bf16 tokens of 512 rows, 8 heads of 64, where four of 64 take 570
-// (one row of 62 496: 7.8 and 7.9 ms).
-template <typename T> constexpr int query_tiles() { return 1; }
 
-// One block: 64 queries of a head. RP: parts of a weight.
+// One block: 64 queries of a head, 16 a wave. RP: parts of a weight. Twice the queries would halve what a score reads
+// from LDS, at twice the registers: two blocks of 128 a CU took 730 us for 134 219 bf16 tokens of 512 rows, 8 heads
+// of 64, where four of 64 take 570 (one row of 62 496: 7.8 and 7.9 ms).
 //
 // What bounds it: vector instructions, of which a score takes 7 where a tile has one bucket (three for the two
 // parts of its weight) and about 7 more where it has several, and about 70 a tile and wave. Measured, 8 heads of
@@ -61,7 +59,7 @@ template <typename T> constexpr int query_tiles() { return 1; }
 // bias itself, 30 KB, leaves two.
 template <typename T, int D, bool VEC, typename Entry, int RP>
 __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 : 4) void k_gap_read(ReadArgs A) {
-  constexpr int KN = tile_keys<T>(), QT = query_tiles<T>(), BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+  constexpr int KN = tile_keys<T>(), LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, KT = KN / 16, KS = KN / 32, DF = D / 32, DT = D / 16;
   using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
@@ -76,58 +74,35 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
   const int head = (int)(blockIdx.x % (unsigned)G.heads);
   // a row's last tokens have the most keys: they go first
   const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
-  const int64_t t0 = tile * BQ;
+  const int64_t t0 = tile * 64;
 
   lb.start(G, head, tid);
   if (tid == 0) lbad = -1;
   // the block's keys: from its first row's first token to its last token that has a row
-  int span_first[QT], block_first = kNoRow, block_last = -1, rows_first = 0;
-#pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    const int64_t t = t0 + n * 64 + lane;
-    span_first[n] = span_of(G, A.spans, t).first;
-    block_first = min(block_first, span_first[n]);
-    rows_first = max(rows_first, span_first[n]);  // the last row's
-    if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
-  }
-  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
-  block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
-  rows_first = __builtin_amdgcn_readfirstlane(wave_max(rows_first));
+  const int span_first = span_of(G, A.spans, t0 + lane).first;
+  const int block_first = __builtin_amdgcn_readfirstlane(wave_min(span_first));
+  const int block_last = __builtin_amdgcn_readfirstlane(wave_max(span_first != kNoRow ? (int)t0 + lane : -1));
+  const int rows_first = __builtin_amdgcn_readfirstlane(wave_max(span_first));  // the last row's
   if (block_last < 0) return;
 
-  // this wave's queries, one a lane and tile
-  const int i0 = (int)t0 + wave * 16 * QT;
-  int at[QT], first[QT], pos[QT];
-  unsigned before[QT];
-  int first_min = kNoRow, first_max = 0, last = -1, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
-  Frag<NP> qf[QT][DF];
+  // this wave's queries, one a lane
+  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
+  const bool real = first != kNoRow;
+  const unsigned before = real ? (unsigned)(at - first) : 0u;
+  const int64_t t = real ? at : block_last;
+  const int pos = G.positions[t];
+  Frag<NP> qf[DF];
+  load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_q,
+                 lane, qf);
+  if (G.scale < 0.f) {
 #pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    const int index = wave * 16 * QT + n * 16 + m;  // in the block
-    at[n] = (int)t0 + index;
-    first[n] = __shfl(span_first[0], index & 63);
-    if (QT > 1 && wave >= 2) first[n] = __shfl(span_first[QT - 1], index & 63);
-    const bool real = first[n] != kNoRow;
-    before[n] = real ? (unsigned)(at[n] - first[n]) : 0u;
-    first_min = min(first_min, first[n]);
-    first_max = max(first_max, first[n]);
-    if (real) last = max(last, at[n]);
-    const int64_t t = real ? at[n] : block_last;
-    pos[n] = G.positions[t];
-    pos_min = min(pos_min, pos[n]);
-    pos_max = max(pos_max, pos[n]);
-    load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_q,
-                   lane, qf[n]);
-    if (G.scale < 0.f) {
-#pragma unroll
-      for (int d = 0; d < DF; ++d) qf[n][d] = negated(qf[n][d]);
-    }
+    for (int d = 0; d < DF; ++d) qf[d] = negated(qf[d]);
   }
-  first_min = __builtin_amdgcn_readfirstlane(wave_min(first_min));
-  first_max = __builtin_amdgcn_readfirstlane(wave_max(first_max));
-  last = __builtin_amdgcn_readfirstlane(wave_max(last));
-  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
-  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  const int first_min = __builtin_amdgcn_readfirstlane(wave_min(first));
+  const int first_max = __builtin_amdgcn_readfirstlane(wave_max(first));
+  const int last = __builtin_amdgcn_readfirstlane(wave_max(real ? at : -1));
+  const int pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos));
+  const int pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos));
   const float scale = fabsf(G.scale) * kLog2e;
 
   const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
@@ -150,16 +125,11 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
   BucketLanes bl;
   bl.read(lb, G, lane);
 
-  f32x4 o[QT][DT];
+  f32x4 o[DT];
   int bad_lo = 0, bad_hi = 0;  // keys among which some values were left out
-  float top[QT], base[QT], sum[QT];
+  float top = -__builtin_inff(), base = 0.f, sum = 0.f;
 #pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    top[n] = -__builtin_inff();
-    base[n] = sum[n] = 0.f;
-#pragma unroll
-    for (int c = 0; c < DT; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int c = 0; c < DT; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
     // addresses are formed anew in each tile: held across tiles they would cost a block its place on the CU
@@ -191,20 +161,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
     __builtin_amdgcn_sched_barrier(0);
 
     const bool partial = k0 + KN - 1 > i0 || k0 < first_max;
-    f32x4 s[QT][KT];
+    f32x4 s[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      Acc<NP> qk[QT];
-#pragma unroll
-      for (int n = 0; n < QT; ++n) qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
+      Acc<NP> qk;
+      qk.start(f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
       for (int d = 0; d < DF; ++d) {
         const Frag<NP> kf = frag_row<NP>(lk + t * 16 * LD + d * 32, LD, PART, lane);
-#pragma unroll
-        for (int n = 0; n < QT; ++n) qk[n].add(kf, qf[n][d]);
+        qk.add(kf, qf[d]);
       }
-#pragma unroll
-      for (int n = 0; n < QT; ++n) s[n][t] = qk[n].value();
+      s[t] = qk.value();
     }
 
     // one bucket for the tile's gaps, or one for each
@@ -214,139 +181,107 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
 
     // The largest score so far is followed only where it has grown by 8: exponentials up to 2^8 keep
     // their precision, and most tiles leave the sums as they are.
-    const auto follow = [&](float *most) {
-      bool grown = false;
+    const auto follow = [&](float most) {
+      most = column_max(most);
+      if (__any(most > top + 8.f)) {
+        const bool none = top == -__builtin_inff();  // so far: there is nothing to scale
+        top = fmaxf(top, most);
+        const float next = top == -__builtin_inff() ? 0.f : top;
+        const float factor = none ? 0.f : exp2_fast(base - next);
+        base = next;
+        sum *= factor;
 #pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        most[n] = column_max(most[n]);
-        grown = grown || most[n] > top[n] + 8.f;
-      }
-      if (__any(grown)) {
-#pragma unroll
-        for (int n = 0; n < QT; ++n) {
-          const bool none = top[n] == -__builtin_inff();  // so far: there is nothing to scale
-          top[n] = fmaxf(top[n], most[n]);
-          const float next = top[n] == -__builtin_inff() ? 0.f : top[n];
-          const float factor = none ? 0.f : exp2_fast(base[n] - next);
-          base[n] = next;
-          sum[n] *= factor;
-#pragma unroll
-          for (int c = 0; c < DT; ++c) o[n][c] *= factor;
-        }
+        for (int c = 0; c < DT; ++c) o[c] *= factor;
       }
     };
     // s -> 2^(by s + shift), of 32 keys, as operands
-    const auto weigh = [&](int w, float by, const float *shift, Frag<RP> *pf) {
+    const auto weigh = [&](int w, float by, float shift) {
 #pragma unroll
-      for (int n = 0; n < QT; ++n) {
+      for (int t = 2 * w; t < 2 * w + 2; ++t)
 #pragma unroll
-        for (int t = 2 * w; t < 2 * w + 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = exp2_fast(fmaf(s[n][t][e], by, shift[n]));
-            s[n][t][e] = x;
-            sum[n] += x;
-          }
-        asm("" : "+v"(sum[n]));  // now: put off, the sums would hold the weights' registers
-        pf[n] = as_frag<RP>(s[n][2 * w], s[n][2 * w + 1]);
-      }
+        for (int e = 0; e < 4; ++e) {
+          const float x = exp2_fast(fmaf(s[t][e], by, shift));
+          s[t][e] = x;
+          sum += x;
+        }
+      asm("" : "+v"(sum));  // now: put off, the sums would hold the weights' registers
+      return as_frag<RP>(s[2 * w], s[2 * w + 1]);
     };
-    const auto add_values = [&](int w, bool bad, const Frag<RP> *pf) {
+    const auto add_values = [&](int w, bool bad, const Frag<RP> &pf) {
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
         Frag<NP> vf = frag_col<NP, 4>(lv + w * 32 * LD + c * 16, LD, PART, lane);
         if (bad) vf = cleaned(vf);
-#pragma unroll
-        for (int n = 0; n < QT; ++n) o[n][c] = mma(vf, pf[n], o[n][c]);
+        o[c] = mma(vf, pf, o[c]);
       }
     };
-    float most[QT], shift[QT];
     if (plain) {
+      float most = s[0][0];
 #pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        most[n] = s[n][0][0];
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) most[n] = fmaxf(most[n], s[n][t][e]);
-        most[n] = fmaf(most[n], scale, b);
-      }
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, s[t][e]);
+      most = fmaf(most, scale, b);
       follow(most);
-#pragma unroll
-      for (int n = 0; n < QT; ++n) shift[n] = b - base[n];
+      const float shift = b - base;
 #pragma unroll
       for (int w = 0; w < KS; ++w) {
-        Frag<RP> pf[QT];
-        weigh(w, scale, shift, pf);
-        add_values(w, false, pf);
+        add_values(w, false, weigh(w, scale, shift));
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-#pragma unroll
-      for (int n = 0; n < QT; ++n) most[n] = -__builtin_inff();
+      float most = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
         const i32x4 kpos = *(const i32x4 *)(lpos + t * 16 + g * 4);
-        f32x4 add[QT];
+        f32x4 add;
 #pragma unroll
-        for (int n = 0; n < QT; ++n)
+        for (int e = 0; e < 4; ++e) add[e] = lb.bias_of(G, gap_of(pos, kpos[e]));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) add[n][e] = lb.bias_of(G, gap_of(pos[n], kpos[e]));
-#pragma unroll
-        for (int n = 0; n < QT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool kept = (unsigned)(k0 + t * 16 + g * 4 + e - first[n]) <= before[n];
-            const float x = kept ? fmaf(s[n][t][e], scale, add[n][e]) : -__builtin_inff();
-            s[n][t][e] = x;
-            most[n] = fmaxf(most[n], x);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const bool kept = (unsigned)(k0 + t * 16 + g * 4 + e - first) <= before;
+          const float x = kept ? fmaf(s[t][e], scale, add[e]) : -__builtin_inff();
+          s[t][e] = x;
+          most = fmaxf(most, x);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       follow(most);
 #pragma unroll
-      for (int n = 0; n < QT; ++n) shift[n] = -base[n];
-#pragma unroll
       for (int w = 0; w < KS; ++w) {
-        Frag<RP> pf[QT];
-        weigh(w, 1.f, shift, pf);
-        add_values(w, bad, pf);
+        add_values(w, bad, weigh(w, 1.f, -base));
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
 
+  const float total = column_sum(sum);
+  if (first == kNoRow) return;
+  if (bad_hi)
+    mark_read<T, DT>((const T *)v, A.v.token_stride, G.width, bad_lo, bad_hi, lane,
+                     [&](int j) { return (unsigned)(j - first) <= before; }, o);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const int64_t row = ((int64_t)at * G.heads + head) * G.width;
 #pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    const float total = column_sum(sum[n]);
-    if (first[n] == kNoRow) continue;
-    if (bad_hi)
-      mark_read<T, DT>((const T *)v, A.v.token_stride, G.width, bad_lo, bad_hi, lane,
-                       [&](int j) { return (unsigned)(j - first[n]) <= before[n]; }, o[n]);
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
-#pragma unroll
-    for (int c = 0; c < DT; ++c) {
-      const int d = c * 16 + g * 4;
-      if (d >= G.width) continue;
-      const f32x4 x = o[n][c] * inv;
-      store4((T *)A.out + row + d, x, G.width - d);
-      if constexpr (sizeof(T) == 2) {
-        if (A.rest) store_rest(A.rest + row + d, x, G.width - d);
-      }
+  for (int c = 0; c < DT; ++c) {
+    const int d = c * 16 + g * 4;
+    if (d >= G.width) continue;
+    const f32x4 x = o[c] * inv;
+    store4((T *)A.out + row + d, x, G.width - d);
+    if constexpr (sizeof(T) == 2) {
+      if (A.rest) store_rest(A.rest + row + d, x, G.width - d);
     }
-    if (A.stats && g == 0) {
-      float *to = A.stats + (int64_t)head * G.n_tokens + at[n];
-      to[0] = base[n];
-      to[(int64_t)G.heads * G.n_tokens] = inv;
-    }
+  }
+  if (A.stats && g == 0) {
+    float *to = A.stats + (int64_t)head * G.n_tokens + at;
+    to[0] = base;
+    to[(int64_t)G.heads * G.n_tokens] = inv;
   }
 }
 
 template <typename T, int D> hipError_t launch_read(ReadArgs A, bool vec, hipStream_t s) {
-  constexpr int BQ = 64 * query_tiles<T>();
   using Entry = uint8_t;
-  A.n_tiles = (A.G.n_tokens + BQ - 1) / BQ;
+  A.n_tiles = (A.G.n_tokens + 63) / 64;
   const int64_t per = max_blocks(256) / A.G.heads;
   for (A.tile0 = 0; A.tile0 < A.n_tiles; A.tile0 += per) {
     const int64_t n = A.n_tiles - A.tile0 < per ? A.n_tiles - A.tile0 : per;

@@ -79,7 +79,7 @@ template <int COLUMNS> struct BucketSums {
 // 25 003 tokens of 100 rows, 670 us.
 template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
-  constexpr int KN = tile_tokens<T>(), QT = 1, BQ = 64 * QT, LD = D + 16, PART = KN * LD;
+  constexpr int KN = tile_tokens<T>(), LD = D + 16, PART = KN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, KS = KN / 32, DF = D / 32, DT = D / 16;
   using Tiles = Staged<T, KN, D, VEC>;
   __shared__ __align__(16) bf16 lk[NP * PART];
@@ -94,102 +94,78 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = (int)(blockIdx.x % (unsigned)G.heads);
   const int64_t tile = A.n_tiles - 1 - (A.tile0 + blockIdx.x / (unsigned)G.heads);
-  const int64_t t0 = tile * BQ;
+  const int64_t t0 = tile * 64;
 
   lb.start(G, head, tid);
   if (tid == 0) lbad = -1;
   for (int n = tid; n < 4 * G.buckets * COLUMNS; n += 256) lsums[n] = 0.f;
-  int span_first[QT], block_first = kNoRow, block_last = -1, rows_first = 0;
-#pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    const int64_t t = t0 + n * 64 + lane;
-    span_first[n] = span_of(G, A.spans, t).first;
-    block_first = min(block_first, span_first[n]);
-    rows_first = max(rows_first, span_first[n]);
-    if (span_first[n] != kNoRow) block_last = max(block_last, (int)t);
-  }
-  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
-  block_last = __builtin_amdgcn_readfirstlane(wave_max(block_last));
-  rows_first = __builtin_amdgcn_readfirstlane(wave_max(rows_first));
+  const int span_first = span_of(G, A.spans, t0 + lane).first;
+  const int block_first = __builtin_amdgcn_readfirstlane(wave_min(span_first));
+  const int block_last = __builtin_amdgcn_readfirstlane(wave_max(span_first != kNoRow ? (int)t0 + lane : -1));
+  const int rows_first = __builtin_amdgcn_readfirstlane(wave_max(span_first));
   float *parts = A.dbias_parts + (int64_t)head * G.buckets * A.n_tiles + tile;
   if (block_last < 0) {
     if (tid < G.buckets) parts[tid * A.n_tiles] = 0.f;
     return;
   }
 
-  const int i0 = (int)t0 + wave * 16 * QT;
-  int at[QT], first[QT], pos[QT];
-  unsigned before[QT];
-  float top[QT], inv[QT], delta[QT];
-  int first_min = kNoRow, first_max = 0, last = -1, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
+  // this wave's queries, one a lane
+  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
+  const bool real = first != kNoRow;
+  const unsigned before = real ? (unsigned)(at - first) : 0u;
+  const int64_t t = real ? at : block_last;
+  const int pos = G.positions[t];
   // The matrix cores round down (not to nearest), which leaves all do . v a little short. That is nothing to
   // one of them, but dbias sums them over all tokens, where their own signs nearly cancel (1 075 431 tokens: off
   // by 3e-6 of its norm). So every other query's do is negated, and what comes of it once more at the end.
   const float sign = m & 1 ? -1.f : 1.f;
-  Frag<NP> qf[QT][DF], of[QT][DF];
+  Frag<NP> qf[DF], of[DF];
+  load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_rows,
+                 lane, qf);
+  const float *stats = A.stats + (int64_t)head * G.n_tokens + t;
+  float top = stats[0], inv = stats[(int64_t)G.heads * G.n_tokens];
+  // delta, and do as operands
+  float x = 0.f;
+  const int64_t row = (t * G.heads + head) * G.width;
 #pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    const int index = wave * 16 * QT + n * 16 + m;
-    at[n] = (int)t0 + index;
-    first[n] = __shfl(span_first[0], index & 63);
-    if (QT > 1 && wave >= 2) first[n] = __shfl(span_first[QT - 1], index & 63);
-    const bool real = first[n] != kNoRow;
-    before[n] = real ? (unsigned)(at[n] - first[n]) : 0u;
-    first_min = min(first_min, first[n]);
-    first_max = max(first_max, first[n]);
-    if (real) last = max(last, at[n]);
-    const int64_t t = real ? at[n] : block_last;
-    pos[n] = G.positions[t];
-    pos_min = min(pos_min, pos[n]);
-    pos_max = max(pos_max, pos[n]);
-    load_row<T, D>((const T *)A.q.data + t * A.q.token_stride + head * A.q.head_stride, G.width, A.vec_rows,
-                   lane, qf[n]);
-    const float *stats = A.stats + (int64_t)head * G.n_tokens + t;
-    top[n] = stats[0];
-    inv[n] = stats[(int64_t)G.heads * G.n_tokens];
-    // delta, and do as operands
-    float x = 0.f;
-    const int64_t row = (t * G.heads + head) * G.width;
+  for (int d = 0; d < DF; ++d) {
+    const int c = d * 32 + g * 8;
+    const Raw8<T> y = load8((const T *)A.d_out.data + t * A.d_out.token_stride + head * A.d_out.head_stride,
+                            c, G.width, A.vec_rows);
+    const Raw8<T> z = load8((const T *)A.out + row, c, G.width, A.vec_out);
+    f32x4 o[2] = {low4(z), high4(z)};
+    if constexpr (sizeof(T) == 2) {
+      if (A.rest) {
+        const Raw8<int16_t> r = load8(A.rest + row, c, G.width, A.vec_out);
 #pragma unroll
-    for (int d = 0; d < DF; ++d) {
-      const int c = d * 32 + g * 8;
-      const Raw8<T> y = load8((const T *)A.d_out.data + t * A.d_out.token_stride + head * A.d_out.head_stride,
-                              c, G.width, A.vec_rows);
-      const Raw8<T> z = load8((const T *)A.out + row, c, G.width, A.vec_out);
-      f32x4 o[2] = {low4(z), high4(z)};
-      if constexpr (sizeof(T) == 2) {
-        if (A.rest) {
-          const Raw8<int16_t> r = load8(A.rest + row, c, G.width, A.vec_out);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            o[0][e] = with_rest(z.v[e], r.v[e]);
-            o[1][e] = with_rest(z.v[4 + e], r.v[4 + e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          o[0][e] = with_rest(z.v[e], r.v[e]);
+          o[1][e] = with_rest(z.v[4 + e], r.v[4 + e]);
         }
       }
-      const f32x4 lo = low4(y), hi = high4(y);
+    }
+    const f32x4 lo = low4(y), hi = high4(y);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x = fmaf(lo[e], o[0][e], fmaf(hi[e], o[1][e], x));
-      of[n][d] = operand(y);
-      if (m & 1) of[n][d] = negated(of[n][d]);
-      if (G.scale < 0.f) qf[n][d] = negated(qf[n][d]);
-    }
-    delta[n] = column_sum(x);
-    if (g == 0 && real) A.delta[(int64_t)head * G.n_tokens + t] = delta[n];
-    // A sum that is no number would make a masked pair's zero one as well, on its way to dbias: the weights are
-    // formed as NaN instead, before the mask.
-    if (!(fabsf(inv[n]) <= kLargest)) {
-      top[n] = __builtin_nanf("");
-      inv[n] = 1.f;
-    }
-    delta[n] *= sign;
-    inv[n] *= sign;  // with the factor of a query's sums
+    for (int e = 0; e < 4; ++e) x = fmaf(lo[e], o[0][e], fmaf(hi[e], o[1][e], x));
+    of[d] = operand(y);
+    if (m & 1) of[d] = negated(of[d]);
+    if (G.scale < 0.f) qf[d] = negated(qf[d]);
   }
-  first_min = __builtin_amdgcn_readfirstlane(wave_min(first_min));
-  first_max = __builtin_amdgcn_readfirstlane(wave_max(first_max));
-  last = __builtin_amdgcn_readfirstlane(wave_max(last));
-  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
-  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  float delta = column_sum(x);
+  if (g == 0 && real) A.delta[(int64_t)head * G.n_tokens + t] = delta;
+  // A sum that is no number would make a masked pair's zero one as well, on its way to dbias: the weights are
+  // formed as NaN instead, before the mask.
+  if (!(fabsf(inv) <= kLargest)) {
+    top = __builtin_nanf("");
+    inv = 1.f;
+  }
+  delta *= sign;
+  inv *= sign;  // with the factor of a query's sums
+  const int first_min = __builtin_amdgcn_readfirstlane(wave_min(first));
+  const int first_max = __builtin_amdgcn_readfirstlane(wave_max(first));
+  const int last = __builtin_amdgcn_readfirstlane(wave_max(real ? at : -1));
+  const int pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos));
+  const int pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos));
   const float scale = fabsf(G.scale) * kLog2e;
 
   const char *k = (const char *)((const T *)A.k.data + head / G.group * A.k.head_stride);
@@ -212,26 +188,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
   BucketLanes bl;
   bl.read(lb, G, lane);
 
-  f32x4 dq[QT][DT];
+  f32x4 dq[DT];
 #pragma unroll
-  for (int n = 0; n < QT; ++n)
-#pragma unroll
-    for (int c = 0; c < DT; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < DT; ++c) dq[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   const BucketSums<COLUMNS> sums{lsums + wave * G.buckets * COLUMNS + (lane & (COLUMNS - 1)), lane};
-  // of the tiles so far whose gaps were all in bucket run_kind, before the queries' own factors
-  float run[QT];
-#pragma unroll
-  for (int n = 0; n < QT; ++n) run[n] = 0.f;
+  // of the tiles so far whose gaps were all in bucket run_kind, before the query's own factor
+  float run = 0.f;
   int run_kind = 0;
   int bad_lo = 0, bad_hi = 0;  // keys among which some values were left out
   const auto end_run = [&]() {
-    float sum = 0.f;
-#pragma unroll
-    for (int n = 0; n < QT; ++n) {
-      sum = fmaf(run[n], inv[n], sum);
-      run[n] = 0.f;
-    }
-    sums.add(run_kind, sum);
+    sums.add(run_kind, fmaf(run, inv, 0.f));  // one rounding before the sum's own
+    run = 0.f;
   };
 
   for (int k0 = block_first; k0 <= block_last; k0 += KN) {
@@ -273,100 +240,75 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
 #pragma unroll 1
     for (int w = 0; w < KS; ++w) {  // 32 keys at a time
       const bf16 *wk = lk + w * 32 * LD, *wv = lv + w * 32 * LD;
-      f32x4 s[QT][2], dp[QT][2];  // do . v - delta
+      f32x4 s[2], dp[2];  // do . v - delta
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        Acc<NP> qk[QT], ov[QT];
-#pragma unroll
-        for (int n = 0; n < QT; ++n) {
-          qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
-          ov[n].start(f32x4{0.f, 0.f, 0.f, 0.f} - delta[n]);
-        }
+        Acc<NP> qk, ov;
+        qk.start(f32x4{0.f, 0.f, 0.f, 0.f});
+        ov.start(f32x4{0.f, 0.f, 0.f, 0.f} - delta);
 #pragma unroll
         for (int d = 0; d < DF; ++d) {
           const Frag<NP> kf = frag_row<NP>(wk + t * 16 * LD + d * 32, LD, PART, lane);
           const Frag<NP> vf = frag_row<NP>(wv + t * 16 * LD + d * 32, LD, PART, lane);
-#pragma unroll
-          for (int n = 0; n < QT; ++n) {
-            qk[n].add(kf, qf[n][d]);
-            ov[n].add(vf, of[n][d]);
-          }
+          qk.add(kf, qf[d]);
+          ov.add(vf, of[d]);
         }
-#pragma unroll
-        for (int n = 0; n < QT; ++n) {
-          s[n][t] = qk[n].value();
-          dp[n][t] = ov[n].value();
-        }
+        s[t] = qk.value();
+        dp[t] = ov.value();
       }
       if (plain) {
+        const float shift = b - top;
 #pragma unroll
-        for (int n = 0; n < QT; ++n) {
-          const float shift = b - top[n];
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = exp2_fast(fmaf(s[n][t][e], scale, shift));
-              s[n][t][e] = p * dp[n][t][e];
-              run[n] += s[n][t][e];
-            }
-        }
+          for (int e = 0; e < 4; ++e) {
+            const float p = exp2_fast(fmaf(s[t][e], scale, shift));
+            s[t][e] = p * dp[t][e];
+            run += s[t][e];
+          }
       } else {
-        i32x4 kind[QT][2];
-        f32x4 add[QT][2];
+        i32x4 kind[2];
+        f32x4 add[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const i32x4 kpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
 #pragma unroll
-          for (int n = 0; n < QT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) kind[n][t][e] = lb.kind4(G, gap_of(pos[n], kpos[e]));
+          for (int e = 0; e < 4; ++e) kind[t][e] = lb.kind4(G, gap_of(pos, kpos[e]));
         }
 #pragma unroll
-        for (int n = 0; n < QT; ++n)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
+          for (int e = 0; e < 4; ++e) add[t][e] = lb.bias4(kind[t][e]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add[n][t][e] = lb.bias4(kind[n][t][e]);
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int n = 0; n < QT; ++n)
+          for (int e = 0; e < 4; ++e) {
+            const float p = exp2_fast(fmaf(s[t][e], scale, add[t][e]) - top);
+            const bool kept = (unsigned)(k0 + w * 32 + t * 16 + g * 4 + e - first) <= before;
+            s[t][e] = kept ? p * dp[t][e] : 0.f;
+          }
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = exp2_fast(fmaf(s[n][t][e], scale, add[n][t][e]) - top[n]);
-              const bool kept = (unsigned)(k0 + w * 32 + t * 16 + g * 4 + e - first[n]) <= before[n];
-              s[n][t][e] = kept ? p * dp[n][t][e] : 0.f;
-            }
-#pragma unroll
-        for (int n = 0; n < QT; ++n)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) sums.add(kind[n][t], s[n][t] * inv[n]);
+        for (int t = 0; t < 2; ++t) sums.add(kind[t], s[t] * inv);
       }
-      Frag<RP> df[QT];
-#pragma unroll
-      for (int n = 0; n < QT; ++n) df[n] = as_frag<RP>(s[n][0], s[n][1]);
+      const Frag<RP> df = as_frag<RP>(s[0], s[1]);
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
         Frag<NP> kf = frag_col<NP, 4>(wk + c * 16, LD, PART, lane);
         if (bad) kf = cleaned(kf);
-#pragma unroll
-        for (int n = 0; n < QT; ++n) dq[n][c] = mma(kf, df[n], dq[n][c]);
+        dq[c] = mma(kf, df, dq[c]);
       }
     }
   }
 
-#pragma unroll
-  for (int n = 0; n < QT; ++n) {
-    if (first[n] == kNoRow) continue;
+  if (real) {
     if (bad_hi)
       mark_read<T, DT>((const T *)k, A.k.token_stride, G.width, bad_lo, bad_hi, lane,
-                       [&](int j) { return (unsigned)(j - first[n]) <= before[n]; }, dq[n]);
-    const int64_t row = ((int64_t)at[n] * G.heads + head) * G.width;
+                       [&](int j) { return (unsigned)(j - first) <= before; }, dq);
+    T *to = (T *)A.dq + ((int64_t)at * G.heads + head) * G.width;
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
       const int d = c * 16 + g * 4;
-      if (d < G.width) store4((T *)A.dq + row + d, dq[n][c] * (G.scale * inv[n]), G.width - d);
+      if (d < G.width) store4(to + d, dq[c] * (G.scale * inv), G.width - d);
     }
   }
   end_run();
@@ -407,7 +349,7 @@ __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ par
 // tokens of 100 rows, 8 heads to 2, 720 us (MFMA 40 %, issue 41 %; 16 registers spilled).
 template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
-  constexpr int QN = tile_tokens<T>(), CT = 1, BK = 64 * CT, LD = D + 16, PART = QN * LD;
+  constexpr int QN = tile_tokens<T>(), BK = 64, LD = D + 16, PART = QN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
   // A query's factor of the weights goes into the exponent: good for 2^-21, which bf16 does not see, and a
   // product less a weight.
@@ -431,60 +373,36 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   const int64_t t0 = (A.tile0 + blockIdx.x / (unsigned)owners) * BK;
 
   // the block's queries: from its first token that has a row to its last row's end
-  int span_end[CT], block_first = kNoRow, block_end = 0, rows_end = kNoRow;
-#pragma unroll
-  for (int n = 0; n < CT; ++n) {
-    const int64_t t = t0 + n * 64 + lane;
-    span_end[n] = span_of(G, A.spans, t).end;
-    if (span_end[n] > 0) block_first = min(block_first, (int)t);
-    block_end = max(block_end, span_end[n]);
-    rows_end = min(rows_end, span_end[n]);  // the first row's
-  }
-  block_first = __builtin_amdgcn_readfirstlane(wave_min(block_first));
-  block_end = __builtin_amdgcn_readfirstlane(wave_max(block_end));
-  rows_end = __builtin_amdgcn_readfirstlane(wave_min(rows_end));
+  const int span_end = span_of(G, A.spans, t0 + lane).end;
+  const int block_first = __builtin_amdgcn_readfirstlane(wave_min(span_end > 0 ? (int)t0 + lane : kNoRow));
+  const int block_end = __builtin_amdgcn_readfirstlane(wave_max(span_end));
+  const int rows_end = __builtin_amdgcn_readfirstlane(wave_min(span_end));  // the first row's
   if (block_end == 0) return;
 
-  // this wave's keys, one a lane and tile
-  const int j0 = (int)t0 + wave * 16 * CT;
-  int at[CT], pos[CT];
-  unsigned after[CT];  // queries from the key on
-  int end_min = kNoRow, end_max = 0, pos_min = 0x7fffffff, pos_max = -0x7fffffff - 1;
-  Frag<NP> kf[CT][DF], vf[CT][DF];
+  // this wave's keys, one a lane
+  const int j0 = (int)t0 + wave * 16, at = j0 + m, end = __shfl(span_end, wave * 16 + m);
+  const unsigned after = end > 0 ? (unsigned)(end - at) : 0u;  // queries from the key on
+  const int64_t t = end > 0 ? at : block_first;
+  const int pos = G.positions[t];
+  Frag<NP> kf[DF], vf[DF];
+  load_row<T, D>((const T *)A.k.data + t * A.k.token_stride + k_head * A.k.head_stride, G.width, A.vec_rows,
+                 lane, kf);
+  load_row<T, D>((const T *)A.v.data + t * A.v.token_stride + k_head * A.v.head_stride, G.width, A.vec_rows,
+                 lane, vf);
+  if (G.scale < 0.f) {
 #pragma unroll
-  for (int n = 0; n < CT; ++n) {
-    const int index = wave * 16 * CT + n * 16 + m;
-    at[n] = (int)t0 + index;
-    int end = __shfl(span_end[0], index & 63);
-    if (CT > 1 && wave >= 2) end = __shfl(span_end[CT - 1], index & 63);
-    after[n] = end > 0 ? (unsigned)(end - at[n]) : 0u;
-    end_min = min(end_min, end);
-    end_max = max(end_max, end);
-    const int64_t t = end > 0 ? at[n] : block_first;
-    pos[n] = G.positions[t];
-    pos_min = min(pos_min, pos[n]);
-    pos_max = max(pos_max, pos[n]);
-    load_row<T, D>((const T *)A.k.data + t * A.k.token_stride + k_head * A.k.head_stride, G.width, A.vec_rows,
-                   lane, kf[n]);
-    load_row<T, D>((const T *)A.v.data + t * A.v.token_stride + k_head * A.v.head_stride, G.width, A.vec_rows,
-                   lane, vf[n]);
-    if (G.scale < 0.f) {
-#pragma unroll
-      for (int d = 0; d < DF; ++d) kf[n][d] = negated(kf[n][d]);
-    }
+    for (int d = 0; d < DF; ++d) kf[d] = negated(kf[d]);
   }
-  end_min = __builtin_amdgcn_readfirstlane(wave_min(end_min));
-  end_max = __builtin_amdgcn_readfirstlane(wave_max(end_max));
-  pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos_min));
-  pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos_max));
+  const int end_min = __builtin_amdgcn_readfirstlane(wave_min(end));
+  const int end_max = __builtin_amdgcn_readfirstlane(wave_max(end));
+  const int pos_min = __builtin_amdgcn_readfirstlane(wave_min(pos));
+  const int pos_max = __builtin_amdgcn_readfirstlane(wave_max(pos));
   const float scale = fabsf(G.scale) * kLog2e;
   const int64_t q_row = A.q.token_stride * (int)sizeof(T), o_row = A.d_out.token_stride * (int)sizeof(T);
 
-  f32x4 dk[CT][DT], dv[CT][DT];
+  f32x4 dk[DT], dv[DT];
 #pragma unroll
-  for (int n = 0; n < CT; ++n)
-#pragma unroll
-    for (int c = 0; c < DT; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < DT; ++c) dk[c] = dv[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   for (int head = head0; head < head1; ++head) {
     __syncthreads();
@@ -547,37 +465,28 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
       if (q0 + QN < block_end) fetch(q0 + QN);
       if (q0 + QN <= j0 || q0 >= end_max) continue;
 
-      const bool partial = q0 < j0 + 16 * CT - 1 || q0 + QN > end_min;
+      const bool partial = q0 < j0 + 15 || q0 + QN > end_min;
       const int one = bl.kind(gap_of(lrange[0], pos_max), gap_of(lrange[1], pos_min));
       const float b = bl.bias_of(one);
       const bool plain = bl.is_plain(one) && !partial;
 #pragma unroll 1
       for (int w = 0; w < QS; ++w) {  // 32 queries at a time
         const bf16 *wq = lq + w * 32 * LD, *wo = lo + w * 32 * LD;
-        f32x4 s[CT][2], dp[CT][2];  // do . v - delta
+        f32x4 s[2], dp[2];  // do . v - delta
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          Acc<NP> qk[CT], ov[CT];
-#pragma unroll
-          for (int n = 0; n < CT; ++n) {
-            qk[n].start(f32x4{0.f, 0.f, 0.f, 0.f});
-            ov[n].start(*(const f32x4 *)(ldelta + w * 32 + t * 16 + g * 4));  // -delta
-          }
+          Acc<NP> qk, ov;
+          qk.start(f32x4{0.f, 0.f, 0.f, 0.f});
+          ov.start(*(const f32x4 *)(ldelta + w * 32 + t * 16 + g * 4));  // -delta
 #pragma unroll
           for (int d = 0; d < DF; ++d) {
             const Frag<NP> qf = frag_row<NP>(wq + t * 16 * LD + d * 32, LD, PART, lane);
             const Frag<NP> of = frag_row<NP>(wo + t * 16 * LD + d * 32, LD, PART, lane);
-#pragma unroll
-            for (int n = 0; n < CT; ++n) {
-              qk[n].add(qf, kf[n][d]);
-              ov[n].add(of, vf[n][d]);
-            }
+            qk.add(qf, kf[d]);
+            ov.add(of, vf[d]);
           }
-#pragma unroll
-          for (int n = 0; n < CT; ++n) {
-            s[n][t] = qk[n].value();
-            dp[n][t] = ov[n].value();
-          }
+          s[t] = qk.value();
+          dp[t] = ov.value();
         }
         // s, dp -> p, ds
         if (plain) {
@@ -587,46 +496,35 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
             const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r);
             const f32x4 shift = LOG ? b - top + inv : b - top;
 #pragma unroll
-            for (int n = 0; n < CT; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float x = exp2_fast(fmaf(s[n][t][e], scale, shift[e])), p = LOG ? x : x * inv[e];
-                s[n][t][e] = p;
-                dp[n][t][e] = p * dp[n][t][e];
-              }
+            for (int e = 0; e < 4; ++e) {
+              const float x = exp2_fast(fmaf(s[t][e], scale, shift[e])), p = LOG ? x : x * inv[e];
+              s[t][e] = p;
+              dp[t][e] = p * dp[t][e];
+            }
           }
         } else {
-          f32x4 add[CT][2];
+          f32x4 add[2];
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const i32x4 qpos = *(const i32x4 *)(lpos + w * 32 + t * 16 + g * 4);
 #pragma unroll
-            for (int n = 0; n < CT; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) add[n][t][e] = lb.bias_of(G, gap_of(qpos[e], pos[n]));
+            for (int e = 0; e < 4; ++e) add[t][e] = lb.bias_of(G, gap_of(qpos[e], pos));
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int r = w * 32 + t * 16 + g * 4;
             const f32x4 top = *(const f32x4 *)(ltop + r), inv = *(const f32x4 *)(linv + r);
 #pragma unroll
-            for (int n = 0; n < CT; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float x = fmaf(s[n][t][e], scale, add[n][t][e]) - top[e];
-                const float p = LOG ? exp2_fast(x + inv[e]) : exp2_fast(x) * inv[e];
-                const bool kept = (unsigned)(q0 + r + e - at[n]) < after[n];
-                s[n][t][e] = kept ? p : 0.f;
-                dp[n][t][e] = kept ? p * dp[n][t][e] : 0.f;
-              }
+            for (int e = 0; e < 4; ++e) {
+              const float x = fmaf(s[t][e], scale, add[t][e]) - top[e];
+              const float p = LOG ? exp2_fast(x + inv[e]) : exp2_fast(x) * inv[e];
+              const bool kept = (unsigned)(q0 + r + e - at) < after;
+              s[t][e] = kept ? p : 0.f;
+              dp[t][e] = kept ? p * dp[t][e] : 0.f;
+            }
           }
         }
-        Frag<RP> pf[CT], df[CT];
-#pragma unroll
-        for (int n = 0; n < CT; ++n) {
-          pf[n] = as_frag<RP>(s[n][0], s[n][1]);
-          df[n] = as_frag<RP>(dp[n][0], dp[n][1]);
-        }
+        const Frag<RP> pf = as_frag<RP>(s[0], s[1]), df = as_frag<RP>(dp[0], dp[1]);
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
           Frag<NP> of = frag_col<NP, 4>(wo + c * 16, LD, PART, lane);
@@ -635,39 +533,30 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
             of = cleaned(of);
             qf = cleaned(qf);
           }
-#pragma unroll
-          for (int n = 0; n < CT; ++n) {
-            dv[n][c] = mma(of, pf[n], dv[n][c]);
-            dk[n][c] = mma(qf, df[n], dk[n][c]);
-          }
+          dv[c] = mma(of, pf, dv[c]);
+          dk[c] = mma(qf, df, dk[c]);
         }
       }
     }
     if (bad_hi) {
-#pragma unroll
-      for (int n = 0; n < CT; ++n) {
-        const auto ok = [&](int i) { return (unsigned)(i - at[n]) < after[n]; };
-        mark_read<T, DT>((const T *)o, A.d_out.token_stride, G.width, bad_lo, bad_hi, lane, ok, dv[n]);
-        mark_read<T, DT>((const T *)q, A.q.token_stride, G.width, bad_lo, bad_hi, lane, ok, dk[n]);
-      }
+      const auto ok = [&](int i) { return (unsigned)(i - at) < after; };
+      mark_read<T, DT>((const T *)o, A.d_out.token_stride, G.width, bad_lo, bad_hi, lane, ok, dv);
+      mark_read<T, DT>((const T *)q, A.q.token_stride, G.width, bad_lo, bad_hi, lane, ok, dk);
     }
   }
 
+  if (after == 0) return;
+  const int64_t row = ((int64_t)at * owners + owner) * G.width;
 #pragma unroll
-  for (int n = 0; n < CT; ++n) {
-    if (after[n] == 0) continue;
-    const int64_t row = ((int64_t)at[n] * owners + owner) * G.width;
-#pragma unroll
-    for (int c = 0; c < DT; ++c) {
-      const int d = c * 16 + g * 4;
-      if (d >= G.width) continue;
-      if (A.dk_parts) {
-        store4(A.dk_parts + row + d, dk[n][c] * G.scale, G.width - d);
-        store4(A.dv_parts + row + d, dv[n][c], G.width - d);
-      } else {
-        store4((T *)A.dk + row + d, dk[n][c] * G.scale, G.width - d);
-        store4((T *)A.dv + row + d, dv[n][c], G.width - d);
-      }
+  for (int c = 0; c < DT; ++c) {
+    const int d = c * 16 + g * 4;
+    if (d >= G.width) continue;
+    if (A.dk_parts) {
+      store4(A.dk_parts + row + d, dk[c] * G.scale, G.width - d);
+      store4(A.dv_parts + row + d, dv[c], G.width - d);
+    } else {
+      store4((T *)A.dk + row + d, dk[c] * G.scale, G.width - d);
+      store4((T *)A.dv + row + d, dv[c], G.width - d);
     }
   }
 }
