@@ -557,8 +557,8 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
  *   positions      device int32[n_tokens], any values; a gap below 0 is in bucket 0, one that does not fit 32
  *                  bits counts as the largest that does.
  *   buckets        1 .. 64; bounds: host int32[buckets - 1], >= 1 and ascending, the first gap of each bucket but
- *                  the first. They are read within the call. (Up to 8191 a table in LDS holds the gaps' buckets;
- *                  larger ones are searched, which takes longer.)
+ *                  the first. They are read within the call. (Up to 7679 a table in LDS holds the gaps' buckets;
+ *                  larger ones are searched, which takes up to 1.5 times as long.)
  *   bias           device fp32[q_heads, buckets]; -inf masks a bucket.
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
  *                  head h of k and v. width 1 .. 128.
@@ -567,7 +567,8 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
  *                  device int16 like out (bf16 only), what out's rounding left out.
  * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
  * NaN. Scores, weights and sums are fp32; weights of bf16 values enter their product as two bf16 values (off by
- * 2^-16 at most).
+ * 2^-16 at most) or, where stats are asked for, three, so that a bf16 output may differ in its last bit between a
+ * call with stats and one without.
  */
 typedef struct {
   int64_t n_tokens;

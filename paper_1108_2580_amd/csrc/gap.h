@@ -47,8 +47,10 @@ __device__ __forceinline__ int32_t gap_of(int32_t a, int32_t b) { return __built
 
 // ---- buckets --------------------------------------------------------------------------------------
 // The bucket of a gap is the number of bounds at it or below. Where the last bound is below kTableGaps a table
-// in LDS holds for each gap the bias itself (Entry float: one read a score) or the bucket (uint8_t, times four: a quarter of
-// the LDS, and a second read for the bias, whose 64 places are 64 banks); larger bounds are searched (Entry void).
+// in LDS holds for each gap the bias itself (Entry float: one read a score) or the bucket (uint8_t, times four: a
+// quarter of the LDS, and a second read for the bias, whose 64 places are 64 banks); larger bounds are searched
+// (Entry void), and such calls stage rows of any alignment. With a last bound of 7679 and of 7680, which no gap
+// reached, us a call: reading 134 219 tokens of 512 rows, 590 and 880; training on 1 075 431, 19 300 and 25 600.
 constexpr int kTableGaps = 7680;
 constexpr float kLargest = 3.402823466e38f;
 

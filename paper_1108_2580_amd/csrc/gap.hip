@@ -54,9 +54,11 @@ template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 3
 // 64 in bf16: one row of 62 496 tokens 7.9 ms, 500 TFLOP/s of a large product's 1235 (issue 85 %, MFMA 34 %, four
 // blocks a CU, with which the waves' MFMAs and exponentials overlap: three took 8.5); 134 219 tokens of 512 rows
 // 570 us (q, k, v and o at 1 TB/s of a copy's 5.1). fp32 at 128 wide, 25 003 tokens of 100 rows, 8 heads to 2:
-// 500 us (MFMA 31 %, issue 49 %, two blocks, which LDS and registers allow). 2000 rows of 25 at 50 wide: 111 us,
-// the latency of two or three tiles. A byte a gap in LDS (two reads a score) leaves four blocks a CU where the
-// bias itself, 30 KB, leaves two.
+// 500 us (MFMA 31 %, issue 49 %, two blocks, which LDS and registers allow). A block goes through its keys one tile
+// after the other, so a batch takes at least the time of its longest row's last block: of 2000 fp32 rows of 25 on
+// average at 50 wide, 111 us, the row of 1060 alone takes 95 (34 tiles; a block has 4.2 on average); of 8 bf16 rows,
+// 36 us, the row of 827 takes 33; of the 100 above, the row of 3013 takes 315. A byte a gap in LDS (two reads a
+// score) leaves four blocks a CU where the bias itself, 30 KB, leaves two.
 template <typename T, int D, bool VEC, typename Entry, int RP>
 __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 : 4) void k_gap_read(ReadArgs A) {
   constexpr int KN = tile_keys<T>(), LD = D + 16, PART = KN * LD;

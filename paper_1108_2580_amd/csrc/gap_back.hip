@@ -75,8 +75,9 @@ template <int COLUMNS> struct BucketSums {
 // What bounds it: vector instructions (about 20 a score where a tile has several buckets, 9 where it has one) and
 // waits, at two barriers a tile and at the reads before each write of dbias's sums, with the three blocks a CU (two
 // at 128 wide) that registers and LDS allow. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.1 ms
-// (issue 56 %, MFMA 16 %; 128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64 buckets 1.8 ms; fp32 at 128 wide,
-// 25 003 tokens of 100 rows, 670 us.
+// (issue 56 %, MFMA 16 %; 128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64
+// buckets 1.8 ms; fp32 at 128 wide, 25 003 tokens of 100 rows, 670 us, of which its longest row, 3013 tokens, takes
+// 405 alone (gap.hip: a block goes through its keys one tile after the other).
 template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
   constexpr int KN = tile_tokens<T>(), LD = D + 16, PART = KN * LD;
@@ -351,8 +352,8 @@ template <typename T, int D, bool VEC, typename Entry>
 __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   constexpr int QN = tile_tokens<T>(), BK = 64, LD = D + 16, PART = QN * LD;
   constexpr int NP = kParts<T>, RP = kReadParts<T>, QS = QN / 32, DF = D / 32, DT = D / 16;
-  // A query's factor of the weights goes into the exponent: good for 2^-21, which bf16 does not see, and a
-  // product less a weight.
+  // A query's factor of the weights goes into the exponent, a product less a weight: off by 2^-24 of the exponent's
+  // parts, the largest score (as the score is itself) and the logarithm of the sum, which bf16 does not see.
   constexpr bool LOG = sizeof(T) == 2;
   using Tiles = Staged<T, QN, D, VEC>;
   __shared__ __align__(16) bf16 lq[NP * PART];
