@@ -490,12 +490,14 @@ als_status als_norm_rotate_backward(const als_rotation *shape, als_dtype dtype, 
  *   q, k, v        token strides at most 2^22 values (d_out too; any where n_tokens is 1).
  *   row_ptr        device int64[n_rows + 1], non-decreasing from 0 to n_tokens (rows may be empty);
  *                  values out of [0, n_tokens] are taken as the nearest bound. What out and the gradients
- *                  hold for a token of no row stays as it is.
+ *                  hold for a token of no row stays as it is, but for clear_unheld.
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
  *                  head h of k and v. k_width, v_width 1 .. 128.
  *   log_decay      device fp32[q_heads], <= 0 (-inf forgets at once); a head above 0 or NaN gives NaN.
  *   initial_state, final_state  device fp32 [n_rows, q_heads, k_width, v_width], nullable.
  *   out            device [n_tokens, q_heads, v_width], packed.
+ *   clear_unheld   0, or 1: out and the gradients are zero at the tokens before the first row and behind the last,
+ *                  as what sums over all tokens needs them (one launch more).
  * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
  * NaN. bf16 inputs: products of bf16 with fp32 sums; the products of q and k with their decay, and the
  * state as q reads it, enter as two bf16 values each (off by 2^-16 at most). The state is kept in fp32.
@@ -510,6 +512,7 @@ typedef struct {
   int32_t k_width;
   int32_t v_width;
   float scale;
+  int32_t clear_unheld;
 } als_attention;
 
 int64_t als_decay_attention_workspace(const als_attention *shape);
@@ -531,7 +534,7 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
                                         void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /*
- * One token of each of n_rows rows (n_tokens and row_ptr of shape are not read; q, k and v may have any
+ * One token of each of n_rows rows (n_tokens, row_ptr and clear_unheld of shape are not read; q, k and v may have any
  * strides):
  *   state_out = exp(log_decay) state[source] + k v^T,   out = scale state_out^T q.
  *   state        device fp32 [n_sources, q_heads, k_width, v_width].
@@ -563,6 +566,7 @@ als_status als_decay_attention_step(const als_attention *shape, als_dtype dtype,
  *   q_heads        1 .. 1024, a multiple of k_heads: query heads h * q_heads / k_heads onwards share
  *                  head h of k and v. width 1 .. 128.
  *   out            device [n_tokens, q_heads, width], packed.
+ *   clear_unheld   0, or 1: out and the gradients are zero at tokens of no row.
  *   stats, rest    what the gradients read, both nullable: stats device fp32 [2, q_heads, n_tokens], rest
  *                  device int16 like out (bf16 only), what out's rounding left out.
  * Infinities and NaN reach no earlier token and no other row; what an infinity makes infinite may be
@@ -582,6 +586,7 @@ typedef struct {
   int32_t width;
   int32_t buckets;
   float scale;
+  int32_t clear_unheld;
 } als_gaps;
 
 int64_t als_gap_attention_workspace(const als_gaps *shape);
@@ -629,16 +634,6 @@ int64_t als_gap_attention_step_workspace(const als_gaps *shape, const als_gap_pa
 als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *path, als_dtype dtype, als_heads q,
                                   als_heads k, als_heads v, void *out, void *workspace,
                                   int64_t workspace_bytes, void *hip_stream);
-
-/*
- * Zeros in n (1 .. 4) packed device tensors at the tokens that no row holds, those before row_ptr[0] and from
- * row_ptr[n_rows] on, whose places als_decay_attention, als_gap_attention and their gradients leave as they are:
- * for results that go on into sums over all tokens. Token t of tensors[i] is the token_bytes[i] (1 .. 2^20)
- * bytes from t * token_bytes[i] on; tensors and token_bytes lie on the host and are read within the call.
- * n_tokens 0 .. 2^31 - 1; n_rows 0 .. 2^30; row_ptr as for als_decay_attention.
- */
-als_status als_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, int32_t n,
-                            void *const *tensors, const int64_t *token_bytes, void *hip_stream);
 
 /*
  * Beam search's selection. Each of n_lists lists has `beams` beams; beam w extended by item v scores

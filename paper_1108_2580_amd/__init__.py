@@ -42,7 +42,7 @@ EXPORTS = ("als_create", "als_half_sweep", "als_last_rmse_in", "als_rmse", "als_
            "als_decay_attention_backward_workspace", "als_decay_attention_step",
            "als_gap_attention", "als_gap_attention_workspace", "als_gap_attention_backward",
            "als_gap_attention_backward_workspace", "als_gap_attention_step",
-           "als_gap_attention_step_workspace", "als_clear_unheld",
+           "als_gap_attention_step_workspace",
            "als_beam_select", "als_beam_select_workspace", "als_reorder_states",
            "als_destroy", "als_status_str", "als_last_error")
 

@@ -42,6 +42,14 @@ __device__ __forceinline__ Span2 span_of(const GapShape &G, const Span2 *spans, 
   return span_from(G.row_ptr, G.n_rows, G.n_tokens, row, t);
 }
 
+// Zeros at token t, if there is one, of `rows` packed rows of a width: row `row` of each token.
+template <typename T>
+__device__ __forceinline__ void clear_row(const GapShape &G, void *out, int64_t t, int rows, int row, int c0) {
+  if (!G.clear_unheld || t >= G.n_tokens) return;
+  T *to = (T *)out + (t * rows + row) * G.width;
+  for (int c = c0; c < G.width; c += 4) to[c] = (T)0.f;
+}
+
 // a - b, at the ends of the range where it does not fit
 __device__ __forceinline__ int32_t gap_of(int32_t a, int32_t b) { return __builtin_elementwise_sub_sat(a, b); }
 

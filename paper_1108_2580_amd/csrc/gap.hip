@@ -85,10 +85,11 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : D == 64 && sizeof(T) == 4 ? 3 :
   const int block_first = __builtin_amdgcn_readfirstlane(wave_min(span_first));
   const int block_last = __builtin_amdgcn_readfirstlane(wave_max(span_first != kNoRow ? (int)t0 + lane : -1));
   const int rows_first = __builtin_amdgcn_readfirstlane(wave_max(span_first));  // the last row's
+  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
+  if (first == kNoRow) clear_row<T>(G, A.out, at, G.heads, head, g);
   if (block_last < 0) return;
 
   // this wave's queries, one a lane
-  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
   const bool real = first != kNoRow;
   const unsigned before = real ? (unsigned)(at - first) : 0u;
   const int64_t t = real ? at : block_last;

@@ -105,13 +105,14 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void k_gap_dq(BackArgs A) {
   const int block_last = __builtin_amdgcn_readfirstlane(wave_max(span_first != kNoRow ? (int)t0 + lane : -1));
   const int rows_first = __builtin_amdgcn_readfirstlane(wave_max(span_first));
   float *parts = A.dbias_parts + (int64_t)head * G.buckets * A.n_tiles + tile;
+  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
+  if (first == kNoRow) clear_row<T>(G, A.dq, at, G.heads, head, g);
   if (block_last < 0) {
     if (tid < G.buckets) parts[tid * A.n_tiles] = 0.f;
     return;
   }
 
   // this wave's queries, one a lane
-  const int i0 = (int)t0 + wave * 16, at = i0 + m, first = __shfl(span_first, wave * 16 + m);
   const bool real = first != kNoRow;
   const unsigned before = real ? (unsigned)(at - first) : 0u;
   const int64_t t = real ? at : block_last;
@@ -378,10 +379,14 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   const int block_first = __builtin_amdgcn_readfirstlane(wave_min(span_end > 0 ? (int)t0 + lane : kNoRow));
   const int block_end = __builtin_amdgcn_readfirstlane(wave_max(span_end));
   const int rows_end = __builtin_amdgcn_readfirstlane(wave_min(span_end));  // the first row's
+  const int j0 = (int)t0 + wave * 16, at = j0 + m, end = __shfl(span_end, wave * 16 + m);
+  if (end == 0 && !A.dk_parts) {
+    clear_row<T>(G, A.dk, at, owners, owner, g);
+    clear_row<T>(G, A.dv, at, owners, owner, g);
+  }
   if (block_end == 0) return;
 
   // this wave's keys, one a lane
-  const int j0 = (int)t0 + wave * 16, at = j0 + m, end = __shfl(span_end, wave * 16 + m);
   const unsigned after = end > 0 ? (unsigned)(end - at) : 0u;  // queries from the key on
   const int64_t t = end > 0 ? at : block_first;
   const int pos = G.positions[t];
@@ -562,7 +567,8 @@ __global__ __launch_bounds__(256, 2) void k_gap_dkv(BackArgs A) {
   }
 }
 
-// dk and dv of key heads from their query heads' parts, in their order, for the tokens that rows hold. Bound by
+// dk and dv of key heads from their query heads' parts, in their order, for the tokens that rows hold (and zeros for
+// the others, where they are asked for). Bound by
 // HBM: 76 us for 25 003 tokens of 8 heads of 128 to 2, 5.4 TB/s.
 template <typename T> __global__ __launch_bounds__(256) void k_gap_sum_heads(BackArgs A) {
   const GapShape &G = A.G;
@@ -571,10 +577,11 @@ template <typename T> __global__ __launch_bounds__(256) void k_gap_sum_heads(Bac
   for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < G.n_tokens * values; x += (int64_t)gridDim.x * 256) {
     const int64_t t = x / values;
     const int k_head = (int)(x % values) / pieces, c = (int)(x % values) % pieces * 4;
-    if (span_of(G, A.spans, t).end == 0) continue;
+    const bool held = span_of(G, A.spans, t).end != 0;
+    if (!held && !G.clear_unheld) continue;
     const int64_t from = (t * G.heads + k_head * G.group) * G.width + c;
     f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = k;
-    for (int h = 0; h < G.group; ++h)
+    for (int h = 0; h < (held ? G.group : 0); ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (c + e < G.width) {

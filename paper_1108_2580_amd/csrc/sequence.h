@@ -95,6 +95,7 @@ struct GapShape {
   int32_t heads, group;    // heads of q, and how many of them share one head of k and v
   int32_t width, buckets;
   float scale;
+  bool clear_unheld;       // whether tokens of no row get zeros
   int32_t last_bound;      // bounds[buckets - 2], 0 where there is one bucket
   int32_t bounds[63];
 };
@@ -137,8 +138,8 @@ hipError_t launch_gap_step(als_dtype dtype, const GapShape &g, const GapPath &p,
 // Packed tensors to clear at the tokens that no row holds (unheld.hip).
 struct Unheld {
   int32_t n;
-  char *data[4];
-  int64_t token_bytes[4];
+  char *data[3];
+  int64_t token_bytes[3];
 };
 hipError_t launch_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, const Unheld &u,
                                hipStream_t s);

@@ -163,6 +163,7 @@ als_status check_attention(const als_attention *s, als_dtype dtype, bool step) {
           (long long)s->n_tokens);
   REQUIRE(s->row_ptr, "row_ptr is NULL");
   REQUIRE(s->n_rows > 0 || s->n_tokens == 0, "tokens without rows");
+  REQUIRE(s->clear_unheld == 0 || s->clear_unheld == 1, "clear_unheld %d is not 0 or 1", s->clear_unheld);
   return ALS_OK;
 }
 
@@ -255,6 +256,7 @@ als_status check_gaps(const als_gaps *s, als_dtype dtype) {
   REQUIRE(s->row_ptr, "row_ptr is NULL");
   REQUIRE(s->n_tokens == 0 || s->positions, "positions is NULL");
   REQUIRE(s->n_rows > 0 || s->n_tokens == 0, "tokens without rows");
+  REQUIRE(s->clear_unheld == 0 || s->clear_unheld == 1, "clear_unheld %d is not 0 or 1", s->clear_unheld);
   return ALS_OK;
 }
 
@@ -270,6 +272,7 @@ als::GapShape gap_shape(const als_gaps *s) {
   g.width = s->width;
   g.buckets = s->buckets;
   g.scale = s->scale;
+  g.clear_unheld = s->clear_unheld != 0;
   for (int b = 0; b + 1 < s->buckets; ++b) g.last_bound = g.bounds[b] = s->bounds[b];
   return g;
 }
@@ -391,6 +394,10 @@ als_status als_decay_attention(const als_attention *shape, als_dtype dtype, als_
   p.out = out;
   hipError_t e = als::launch_places(dtype, p, (hipStream_t)hip_stream);
   if (e == hipSuccess) e = als::launch_attention(dtype, &p, 1, (hipStream_t)hip_stream);
+  if (e == hipSuccess && s->clear_unheld) {
+    const als::Unheld u{1, {(char *)out}, {(int64_t)s->q_heads * s->v_width * size}};
+    e = als::launch_clear_unheld(s->n_tokens, s->n_rows, s->row_ptr, u, (hipStream_t)hip_stream);
+  }
   return launched(e, "als_decay_attention");
 }
 
@@ -488,6 +495,13 @@ als_status als_decay_attention_backward(const als_attention *shape, als_dtype dt
   if (e == hipSuccess && shared_k)
     e = als::launch_sum_groups(dtype, shared_k, shared_v, n, s->q_heads, group, s->k_width, s->v_width,
                                dk, dv, stream);
+  if (e == hipSuccess && s->clear_unheld) {
+    const als::Unheld u{3,
+                        {(char *)dq, (char *)dk, (char *)dv},
+                        {(int64_t)s->q_heads * s->k_width * size, (int64_t)s->k_heads * s->k_width * size,
+                         (int64_t)s->k_heads * s->v_width * size}};
+    e = als::launch_clear_unheld(n, s->n_rows, s->row_ptr, u, stream);
+  }
   return launched(e, "als_decay_attention_backward");
 }
 
@@ -701,29 +715,6 @@ als_status als_gap_attention_step(const als_gaps *shape, const als_gap_path *pat
   return launched(als::launch_gap_step(dtype, gap_shape(s), g, q, k, v, out, workspace,
                                        (hipStream_t)hip_stream),
                   "als_gap_attention_step");
-}
-
-als_status als_clear_unheld(int64_t n_tokens, int64_t n_rows, const int64_t *row_ptr, int32_t n,
-                            void *const *tensors, const int64_t *token_bytes, void *hip_stream) {
-  REQUIRE(n_tokens >= 0 && n_tokens <= kMax31, "n_tokens %lld out of range", (long long)n_tokens);
-  REQUIRE(n_rows >= 0 && n_rows <= kMaxRows, "n_rows %lld out of range", (long long)n_rows);
-  REQUIRE(row_ptr, "row_ptr is NULL");
-  REQUIRE((uintptr_t)row_ptr % 8 == 0, "row_ptr is not aligned to its type");
-  REQUIRE(n >= 1 && n <= 4, "%d tensors outside [1, 4]", n);
-  REQUIRE(tensors && token_bytes, "tensors or token_bytes is NULL");
-  als::Unheld u{};
-  u.n = n;
-  const Span ptr = span(row_ptr, 8 * (n_rows + 1));
-  for (int i = 0; i < n; ++i) {
-    REQUIRE(token_bytes[i] >= 1 && token_bytes[i] <= 1LL << 20, "token_bytes[%d] = %lld outside [1, 2^20]", i,
-            (long long)token_bytes[i]);
-    REQUIRE(n_tokens == 0 || tensors[i], "tensors[%d] is NULL", i);
-    REQUIRE(!overlap(span(tensors[i], n_tokens * token_bytes[i]), ptr), "tensors[%d] overlaps row_ptr", i);
-    u.data[i] = (char *)tensors[i];
-    u.token_bytes[i] = token_bytes[i];
-  }
-  return launched(als::launch_clear_unheld(n_tokens, n_rows, row_ptr, u, (hipStream_t)hip_stream),
-                  "als_clear_unheld");
 }
 
 int64_t als_beam_select_workspace(const als_beams *shape) {

@@ -1,5 +1,5 @@
-// Zeros at the tokens that no row holds: those before the first row and behind the last. The attentions work on
-// rows and leave such places as they are; where their results go on into sums over all tokens (the gradient of a
+// Zeros at the tokens that no row holds: those before the first row and behind the last. The decayed attention works
+// on rows and leaves such places as they are; where its results go on into sums over all tokens (the gradient of a
 // projection), they have to count as nothing.
 //
 // Bound by the launch where there are no such tokens: each block reads the two ends of the rows.

@@ -46,13 +46,13 @@ class _Rotation(ctypes.Structure):
 class _Attention(ctypes.Structure):
     _fields_ = [("n_tokens", _i64), ("n_rows", _i64), ("row_ptr", _P), ("log_decay", _P),
                 ("q_heads", _i32), ("k_heads", _i32), ("k_width", _i32), ("v_width", _i32),
-                ("scale", _f32)]
+                ("scale", _f32), ("clear_unheld", _i32)]
 
 
 class _Gaps(ctypes.Structure):
     _fields_ = [("n_tokens", _i64), ("n_rows", _i64), ("row_ptr", _P), ("positions", _P), ("bias", _P),
                 ("bounds", _P), ("q_heads", _i32), ("k_heads", _i32), ("width", _i32), ("buckets", _i32),
-                ("scale", _f32)]
+                ("scale", _f32), ("clear_unheld", _i32)]
 
 
 class _GapPath(ctypes.Structure):
@@ -80,7 +80,6 @@ def _declare():
             ("als_gap_attention_backward",
              [G, st, H, H, H, H, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_gap_attention_step", [G, GP, st, H, H, H, _P, _P, _i64, _P]),
-            ("als_clear_unheld", [_i64, _i64, _P, _i32, ctypes.POINTER(_P), ctypes.POINTER(_i64), _P]),
             ("als_beam_select", [B, st, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P]),
             ("als_reorder_states", [_i64, _i32, _i32, _i64, _P, _P, _P, _P])):
         f = getattr(lib, name)
@@ -167,16 +166,6 @@ def _workspace(size, device):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-def _clear_unheld(row_ptr, *tensors):
-    """Zeros new packed tensors [tokens, ...] at the tokens that no row holds, which the attentions' calls leave
-    unset: what autograd goes on with is summed over all tokens."""
-    n = len(tensors)
-    sizes = (t.element_size() * math.prod(t.shape[1:]) for t in tensors)
-    _check(lib.als_clear_unheld(tensors[0].shape[0], row_ptr.numel() - 1, row_ptr.data_ptr(), n,
-                                (_P * n)(*(t.data_ptr() for t in tensors)), (_i64 * n)(*sizes),
-                                _stream(tensors[0].get_device())))
 
 
 def _no_gradient(t, name):
@@ -342,8 +331,9 @@ def _new_state(shape, device):
     return torch.empty((shape.n_rows, shape.q_heads, shape.k_width, shape.v_width), device=device)
 
 
-def _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state):
+def _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state, recorded=False):
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    shape.clear_unheld = recorded
     first = _state_ptr(initial_state, "initial_state", shape, dev)
     out = q.new_empty((q.shape[0], shape.q_heads, shape.v_width))
     state = _new_state(shape, q.device) if return_state else None
@@ -384,14 +374,20 @@ def decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale=None, ini
     """Gradients (dq, dk, dv, d_initial_state) of ``decay_attention`` from that of its output and,
     if given, of its returned state (``dstate``). The last is None unless there is an
     ``initial_state`` or ``d_initial`` is true. Those of tokens that no row holds are left unset."""
+    wanted = initial_state is not None if d_initial is None else d_initial
+    return _decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale, initial_state, dstate, wanted)
+
+
+def _decay_attention_backward(d_out, q, k, v, log_decay, row_ptr, scale, initial_state, dstate, d_initial,
+                              recorded=False):
     dev, code, shape, hq, hk, hv = _attention(q, k, v, log_decay, row_ptr, scale)
+    shape.clear_unheld = recorded
     hdo = _heads(d_out, "d_out", q.dtype, dev)
     _shaped(d_out, "d_out", (q.shape[0], shape.q_heads, shape.v_width))
     first = _state_ptr(initial_state, "initial_state", shape, dev)
     last = _state_ptr(dstate, "dstate", shape, dev)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
-    wanted = initial_state is not None if d_initial is None else d_initial
-    dfirst = _new_state(shape, q.device) if wanted else None
+    dfirst = _new_state(shape, q.device) if d_initial else None
     size = lib.als_decay_attention_backward_workspace(shape)
     work = _workspace(size, q.device)
     _check(lib.als_decay_attention_backward(shape, code, hdo, hq, hk, hv, first, last, dq.data_ptr(),
@@ -406,9 +402,7 @@ class _DecayAttention(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, log_decay, row_ptr, initial_state)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
-        out, state = _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state)
-        _clear_unheld(row_ptr, out)
-        return out, state
+        return _decay_attention(q, k, v, log_decay, row_ptr, scale, initial_state, return_state, True)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -417,10 +411,9 @@ class _DecayAttention(torch.autograd.Function):
         if d_out is None:
             d_out = torch.zeros((q.shape[0], q.shape[1], v.shape[2]), dtype=q.dtype, device=q.device)
         dstate = None if dstate is None else dstate.contiguous()
-        dq, dk, dv, d_initial = decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale,
-                                                         initial_state, dstate, d_initial=ctx.needs_input_grad[3])
-        _clear_unheld(row_ptr, dq, dk, dv)
-        return dq, dk, dv, d_initial, None, None, None, None
+        grads = _decay_attention_backward(_dense(d_out), q, k, v, log_decay, row_ptr, ctx.scale, initial_state,
+                                          dstate, ctx.needs_input_grad[3], True)
+        return (*grads, None, None, None, None)
 
 
 def decay_attention_step(q, k, v, log_decay, state, scale=None, source=None, state_out=None):
@@ -481,6 +474,7 @@ def _gaps(q, k, v, bias, bounds, positions, row_ptr, scale):
 def _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, save):
     dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
     _shaped(q, "q", (shape.n_tokens, shape.q_heads, shape.width))
+    shape.clear_unheld = 1
     out = q.new_empty(q.shape)
     stats = rest = None
     if save:
@@ -502,8 +496,10 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
     heads / key heads query heads; widths up to 128. ``bias``: fp32 [heads, buckets], up to 64 buckets;
     -inf masks a bucket, and a token left without a key has the output zero. ``bounds``: int32
     [buckets - 1] on the host, ascending from 1 or more, the first gap of each bucket but the first.
-    ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``, and tokens that no
-    row holds: as for ``decay_attention``. ``scale``: 1 / sqrt(width) if None. Returns out [tokens, heads, width], with ``return_saved`` (out, what ``gap_attention_backward`` needs)."""
+    ``positions``: int32 [tokens], any values (a gap below 0 is in bucket 0). ``row_ptr``: as for
+    ``decay_attention``, but the output and the gradients of a token that no row holds are always zero. ``scale``:
+    1 / sqrt(width) if None. Returns out [tokens, heads, width], with ``return_saved`` (out, what
+    ``gap_attention_backward`` needs)."""
     _no_tangents(q, k, v, bias)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or bias.requires_grad):
         out, *saved = _GapAttention.apply(q, k, v, bias, bounds, positions, row_ptr, scale)
@@ -514,7 +510,7 @@ def gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale=None, return_
 
 def gap_attention_backward(d_out, out, saved, q, k, v, bias, bounds, positions, row_ptr, scale=None):
     """Gradients (dq, dk, dv, dbias) of ``gap_attention`` from that of its output, its output (contiguous)
-    and what it saved. Those of tokens that no row holds are left unset."""
+    and what it saved."""
     dev, code, shape, hq, hk, hv = _gaps(q, k, v, bias, bounds, positions, row_ptr, scale)
     shaped = (shape.n_tokens, shape.q_heads, shape.width)
     _shaped(q, "q", shaped)
@@ -524,6 +520,7 @@ def gap_attention_backward(d_out, out, saved, q, k, v, bias, bounds, positions, 
     op = _array(out, "out", q.dtype, shaped, dev)
     sp = _array(stats, "saved[0]", torch.float32, (2, shape.q_heads, shape.n_tokens), dev)
     rp = None if rest is None else _array(rest, "saved[1]", torch.int16, shaped, dev)
+    shape.clear_unheld = 1
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     dbias = torch.empty_like(bias)
     size = lib.als_gap_attention_backward_workspace(shape)
@@ -538,7 +535,6 @@ class _GapAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, bias, bounds, positions, row_ptr, scale):
         out, stats, rest = _gap_attention(q, k, v, bias, bounds, positions, row_ptr, scale, True)
-        _clear_unheld(row_ptr, out)
         # the host's bounds are kept as they are now
         ctx.save_for_backward(out, stats, rest, q, k, v, bias, bounds.clone(), positions, row_ptr)
         ctx.scale = scale
@@ -552,9 +548,8 @@ class _GapAttention(torch.autograd.Function):
         if d_out is None:
             return (None,) * 8
         out, stats, rest, *args = ctx.saved_tensors
-        dq, dk, dv, dbias = gap_attention_backward(_dense(d_out), out, (stats, rest), *args, ctx.scale)
-        _clear_unheld(args[-1], dq, dk, dv)
-        return dq, dk, dv, dbias, None, None, None, None
+        return (*gap_attention_backward(_dense(d_out), out, (stats, rest), *args, ctx.scale), None, None, None,
+                None)
 
 
 def gap_attention_step(q, k, v, bias, bounds, q_positions, positions, row_ptr, k_path=None, v_path=None,

@@ -1,7 +1,6 @@
 """Tokens that no row holds (padding before the first row and behind the last) count as nothing where autograd
 records the attentions: their outputs and gradients are zero, whatever the new tensors held before, so that what
 sums over all tokens is what the rows alone give."""
-import ctypes
 import math
 
 import pytest
@@ -104,21 +103,59 @@ def test_projections_around_decay_attention(before, lens, after, dtype, poisoned
     same_sum(grads[1], plain.float().flatten(1), d_y, held)
 
 
-@pytest.mark.parametrize("width,offset", [(1, 0), (2, 3), (13, 1), (48, 0), (100, 7), (4096, 5)])
-def test_places_are_cleared_and_no_others(width, offset):
-    """At any alignment and number of bytes a token; row pointers out of range touch nothing outside."""
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,V,offset", [(1, 1, 0), (5, 3, 1), (24, 50, 3), (64, 128, 0)])
+@pytest.mark.parametrize("rows", ["few", "many"])
+def test_decay_attention_clears_its_places_and_no_others(rows, K, V, offset, dtype):
+    """At any alignment of the type; row pointers out of range touch nothing outside. Without clear_unheld all such
+    places stay as they are."""
     from paper_1108_2580_amd import lib, sequence as s
 
-    N = 300
-    for ptr, first, end in (([0, 300], 0, 300), ([3, 290], 3, 290), ([0, 0], 0, 0), ([17], 17, 17), ([300, 300], 300, 300),
-                            ([-4, 5, 1 << 40], 0, 300), ([7, 2], 7, 7), ([400, 400], 300, 300)):
+    N, H, size = 300, 2, 4 if dtype == "f32" else 2
+    q = dev(torch.ones(N, H, K, dtype=DTYPES[dtype]))
+    v, decay = dev(torch.ones(N, H, V, dtype=DTYPES[dtype])), dev(-torch.ones(H))
+    between = [] if rows == "few" else [40 + i // 2 for i in range(90)]
+    for a, b in ((0, 300), (30, 290), (39, 131), (-4, 1 << 40), (400, 400), (7, 7)):
+        ptr = [a] + (between if a < 40 and b > 85 else []) + [b]
         t = dev(torch.tensor(ptr))
-        whole = [torch.full((offset + N * w + 64,), 7, dtype=torch.uint8, device="cuda:0") for w in (width, 2 * width)]
-        at = (ctypes.c_void_p * 2)(*(x.data_ptr() + offset for x in whole))
-        s._check(lib.als_clear_unheld(N, len(ptr) - 1, t.data_ptr(), 2, at, (ctypes.c_int64 * 2)(width, 2 * width),
-                                      s._stream(0)))
-        for x, w in zip(whole, (width, 2 * width)):
-            want = torch.full_like(x, 7)
-            want[offset:offset + N * w].view(N, w)[:first] = 0
-            want[offset:offset + N * w].view(N, w)[end:] = 0
-            assert torch.equal(x, want), (ptr, w)
+        first, end = min(max(a, 0), N), min(max(b, 0), N)
+        for clear in (0, 1):
+            dev_, code, shape, hq, hk, hv = s._attention(q, q, v, decay, t, 1.0)
+            shape.clear_unheld = clear
+            need = lib.als_decay_attention_workspace(shape)
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda:0")
+            whole = torch.full((512 + size * (offset + N * H * V),), 0xA5, dtype=torch.uint8, device="cuda:0")
+            at = 256 + size * offset
+            s._check(lib.als_decay_attention(shape, code, hq, hk, hv, None, whole.data_ptr() + at, None, work.data_ptr(),
+                                             need, s._stream(dev_)))
+            out = whole[at:at + N * H * V * size].view(N, -1)
+            empty = 0 if clear else 0xA5
+            assert (out[:first] == empty).all() and (out[end:] == empty).all(), (ptr, clear)
+            assert (whole[:at] == 0xA5).all() and (whole[at + N * H * V * size:] == 0xA5).all()
+            if 0 <= a < b <= N:
+                assert (out[first:end].contiguous().view(DTYPES[dtype]) > 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk,D", [(2, 2, 7), (4, 1, 50), (2, 1, 128)])
+@pytest.mark.parametrize("before,lens,after", [(3, [30, 0, 41], 200), (130, [64], 1), (5, [2] * 80, 9), (70, [0], 3)])
+def test_gap_attention_gives_zeros(before, lens, after, H, Hk, D, dtype, poisoned):
+    """Also where nothing is recorded; padding of NaN reaches nothing."""
+    import paper_1108_2580_amd as p
+
+    log(f"{before} tokens, rows {lens[:4]}, {after} tokens, {H}/{Hk} heads, width {D}, {dtype}")
+    g, N, ptr, held, _ = batch(before, lens, after, 1, 3)
+    q, do = (dev(torch.randn(N, H, D, generator=g).to(DTYPES[dtype])) for _ in range(2))
+    k, v = (dev(torch.randn(N, Hk, D, generator=g).to(DTYPES[dtype])) for _ in range(2))
+    for t in (q, k, v, do):
+        t[~held] = math.nan
+    bias, bounds = dev(torch.randn(H, 3, generator=g)), torch.tensor([1, 50], dtype=torch.int32)
+    pos = dev(torch.randint(0, 300, (N,), generator=g).int())
+    args = (q, k, v, bias, bounds, pos, ptr, 0.3)
+    out, saved = p.gap_attention(*args, return_saved=True)
+    grads = p.gap_attention_backward(do, out, saved, *args)
+    for t in (out, *grads[:3]):
+        assert not t[~held].any() and torch.isfinite(t).all()
+    assert torch.isfinite(grads[3]).all()
+    if sum(lens):
+        assert out[held].any() and all(t[held].any() for t in grads[:3])
