@@ -51,7 +51,7 @@ template <typename T> constexpr int tile_keys() { return sizeof(T) == 2 ? 64 : 3
 //
 // What bounds it: vector instructions, of which a score takes 7 where a tile has one bucket (three for the two
 // parts of its weight) and about 7 more where it has several, and about 70 a tile and wave. Measured, 8 heads of
-// 64 in bf16: one row of 62 496 tokens 7.9 ms, 500 TFLOP/s of a large product's 1235 (issue 82 %, MFMA 34 %, four
+// 64 in bf16: one row of 62 496 tokens 7.9 ms, 500 TFLOP/s of a large product's 1235 (issue 83 %, MFMA 35 %, four
 // blocks a CU, with which the waves' MFMAs and exponentials overlap: three took 8.5); 134 219 tokens of 512 rows
 // 570 us (q, k, v and o at 1 TB/s of a copy's 5.1). fp32 at 128 wide, 25 003 tokens of 100 rows, 8 heads to 2:
 // 500 us (MFMA 31 %, issue 50 %, two blocks, which LDS and registers allow). A block goes through its keys one tile

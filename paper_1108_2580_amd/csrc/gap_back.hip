@@ -75,7 +75,7 @@ template <int COLUMNS> struct BucketSums {
 // What bounds it: vector instructions (about 20 a score where a tile has several buckets, 9 where it has one) and
 // waits, at two barriers a tile and at the reads before each write of dbias's sums, with the three blocks a CU (two
 // at 128 wide) that registers and LDS allow. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.1 ms
-// (issue 55 %, MFMA 16 %; 128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64
+// (issue 56 %, MFMA 16 %; 128 queries a block, two blocks a CU, took 7.5); four rows of 8000 at 128 wide with 64
 // buckets 1.8 ms; fp32 at 128 wide, 25 003 tokens of 100 rows, 670 us, of which its longest row, 3013 tokens, takes
 // 405 alone (gap.hip: a block goes through its keys one tile after the other).
 template <typename T, int D, bool VEC, typename Entry, int COLUMNS>
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(256) void k_gap_dbias(const float *__restrict__ par
 // One block: 64 keys of a key head, or of one of its query heads.
 //
 // What bounds it: vector instructions (13 a score where a tile has one bucket) with four products on MFMA, two of
-// them of two parts. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.0 ms (issue 62 %, MFMA 26 %,
+// them of two parts. Measured: 1 075 431 bf16 tokens of 4096 rows, 8 heads of 64, 7.0 ms (issue 63 %, MFMA 26 %,
 // three blocks a CU; 128 keys a block took 8.6); four rows of 8000 at 128 wide 2.0 ms; fp32 at 128 wide, 25 003
 // tokens of 100 rows, 8 heads to 2, 720 us (MFMA 40 %, issue 41 %; 16 registers spilled).
 template <typename T, int D, bool VEC, typename Entry>
