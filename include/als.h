@@ -597,7 +597,8 @@ als_status als_gap_attention(const als_gaps *shape, als_dtype dtype, als_heads q
 /*
  * Gradients of als_gap_attention: dq [n_tokens, q_heads, width], dk and dv [n_tokens, k_heads, width], packed,
  * and dbias fp32 [q_heads, buckets], from that of its output (d_out), its outputs (packed) and what it left in
- * stats and rest. Without rest (nullable) the gradients take in out's rounding.
+ * stats and rest. Without rest (nullable) the gradients take in out's rounding. dbias takes nothing from pairs of
+ * tokens that do not read each other, whatever their values.
  */
 int64_t als_gap_attention_backward_workspace(const als_gaps *shape);
 als_status als_gap_attention_backward(const als_gaps *shape, als_dtype dtype, als_heads d_out, als_heads q,

@@ -38,10 +38,11 @@ def pointers(n, few):
         yield [0] + [n + 5, -5] * 60 + [n]
 
 
+@pytest.mark.parametrize("clear", [0, 1])
 @pytest.mark.parametrize("few", [True, False])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,H,Hk,D", [(200, 2, 1, 32), (333, 4, 4, 50), (130, 2, 2, 128)])
-def test_reading_and_gradients(N, H, Hk, D, dtype, few):
+def test_reading_and_gradients(N, H, Hk, D, dtype, few, clear):
     from paper_1108_2580_amd import lib, sequence as s
 
     q, k, v, bias, bounds, pos, _, do = inputs([N], H, Hk, D, 8, dtype, 91)
@@ -53,6 +54,7 @@ def test_reading_and_gradients(N, H, Hk, D, dtype, few):
         held = (q, k, v, bias, pos, ptr, do)
         before = [raw(t) for t in held]
         dev_, code, shape, hq, hk, hv = s._gaps(q, k, v, bias, bounds, pos, ptr, 0.2)
+        shape.clear_unheld = clear
         st, hdo = s._stream(dev_), s._heads(do, "d_out", do.dtype, dev_)
         out, stats, rest = Buffer(N * H * D * size), Buffer(8 * N * H), Buffer(N * H * D * 2)
         need = lib.als_gap_attention_workspace(shape)
